@@ -488,6 +488,66 @@ int zoact_mix_rms_strided(zoact_ctx* ctx, const void* q, const void* k, const vo
                           int64_t rows, int32_t n, int32_t n_rep, int32_t head_dim, int64_t ld_q,
                           int64_t ld_kv, float eps, void* Y);
 
+/* ---- the two ends of a language model around the adapted stack ----
+ * The synthetic stacks begin at hidden states and end in a mean-square loss.  Fine-tuning on tokens (Section 5: every
+ * linear is adapted except embeddings and heads) begins at a table's rows and ends in the cross entropy of a head over
+ * the vocabulary; what lies there can be trained first-order, so these calls come with their gradients.
+ *
+ * Token ids and targets: idtype ZOACT_ID_INT32 / INT64.  A negative one is no token: its embedding row is zero, it adds
+ * nothing to a gradient, its loss is 0 and it is not counted in a mean.  One that is not below `vocab` is treated the
+ * same way and sets ZOACT_ERR_INVALID_ARG in the device status word.                                              */
+#define ZOACT_ID_INT32 0
+#define ZOACT_ID_INT64 1
+
+/* zoact_embed: Y [n_tok, d] = scale * E[ids[t]], E [vocab, d], both of dtype (the product rounded once).
+ * zoact_embed_grad: the gradient by E for dY [n_tok, d] of dtype,
+ *       dE[v] = scale * sum over t with ids[t] = v of dY[t]   (+ dE[v] with accumulate != 0),
+ *   dE [vocab, d] of edtype (dtype or FP32).  The sum is taken in fp32 over the tokens in an order that depends on the
+ *   ids alone (the same on every run) and rounded once.  accumulate == 0 writes every row, zero where no token has it;
+ *   accumulate != 0 touches only the rows of tokens that occur (a tied head's gradient lies there already).  Context
+ *   scratch: 8 bytes a token and the sums of pieces of rows (at most 12 d bytes for every 32 tokens).               */
+int zoact_embed(zoact_ctx* ctx, const void* E, int dtype, int64_t vocab, int32_t d, const void* ids, int idtype,
+                int64_t n_tok, float scale, void* Y);
+int zoact_embed_grad(zoact_ctx* ctx, const void* dY, int dtype, int64_t n_tok, int32_t d, const void* ids, int idtype,
+                     int64_t vocab, float scale, void* dE, int edtype, int accumulate);
+
+/* zoact_layer_norm: Y [rows, n] = (x - m) s gain + bias with m = mean(x), s = 1 / sqrt(mean((x - m)^2) + eps) of each
+ *   row of X (ld_x >= n elements apart; Y contiguous), X and Y of dtype, gain and bias [n] of pdtype (dtype or FP32) or
+ *   NULL (1 and 0).  mean and rstd [rows] fp32 receive m and s (NULL: not kept).
+ * zoact_layer_norm_grad: with u = dY gain and xh = (x - mean) rstd (the statistics that the forward call kept),
+ *       dX = rstd (u - mean(u) - xh mean(u xh)),  dgain = sum over rows of dY xh,  dbias = sum over rows of dY,
+ *   dX [rows, n] of dtype, dgain and dbias [n] fp32; any of the three may be NULL.  dY rows are ld_dy elements apart.
+ *   Sums in fp32 in a fixed order.  rows == 0 gives zero dgain and dbias.                                            */
+int zoact_layer_norm(zoact_ctx* ctx, const void* X, int dtype, int64_t rows, int32_t n, int64_t ld_x, const void* gain,
+                     const void* bias, int pdtype, float eps, void* Y, float* mean, float* rstd);
+int zoact_layer_norm_grad(zoact_ctx* ctx, const void* dY, int64_t ld_dy, const void* X, int dtype, int64_t rows,
+                          int32_t n, int64_t ld_x, const void* gain, int pdtype, const float* mean, const float* rstd,
+                          void* dX, float* dgain, float* dbias);
+
+/* Cross entropy of hidden states H [n_blocks T, d] against a head W [vocab, d] (both of dtype), z = H W^T:
+ *     lse = log sum_v exp(z_v),   loss = lse - z_target,   L_b = sum over block b's counted rows / N,
+ * row b T + t with target targets[t] (the evaluation blocks of a ZO step see the same targets; N counted rows in each,
+ * L_b = 0 where N = 0).  The logits are not kept: z exists in registers, a tile at a time.
+ * zoact_ce_loss: loss and lse [n_blocks T] fp32 and mean [n_blocks] fp64 = L_b; any but all three may be NULL.
+ * zoact_ce_pair: out[4] = {L+, L-, D, a} as zoact_loss_pair writes them: D = L+ - L- as the mean of the rows' loss
+ *   differences, a = D / (2 eps); H [2T, d].
+ * zoact_ce_multi: out[2 n_blocks - 1] = {L_0 .. L_q, a_1 .. a_q} as zoact_loss_multi, a_j = (L_j - L_0) / mu.
+ * zoact_ce_grad: the same losses for one block, and the gradient of grad_scale * L: dH [T, d] of dtype and
+ *   dW [vocab, d] of wgdtype (dtype or FP32); either may be NULL.  accumulate != 0 adds to dW, which must then be FP32
+ *   (ZOACT_ERR_UNSUPPORTED otherwise).  Context scratch: the gradient by the logits for a chunk of rows (at most 2 GiB or
+ *   256 rows), and 4 bytes a weight where several chunks add to a 16-bit dW.
+ * A mean or estimate that is not finite sets ZOACT_ERR_NONFINITE.  d % 8 == 0 (16-bit) or d % 4 == 0 (FP32); H, W, dH
+ * and dW 16-byte aligned.                                                                                         */
+int zoact_ce_loss(zoact_ctx* ctx, const void* H, int dtype, int64_t T, int32_t n_blocks, int32_t d, const void* W,
+                  int64_t vocab, const void* targets, int idtype, float* loss, float* lse, double* mean);
+int zoact_ce_pair(zoact_ctx* ctx, const void* H, int dtype, int64_t T, int32_t d, const void* W, int64_t vocab,
+                  const void* targets, int idtype, float eps, double* out);
+int zoact_ce_multi(zoact_ctx* ctx, const void* H, int dtype, int64_t T, int32_t n_blocks, int32_t d, const void* W,
+                   int64_t vocab, const void* targets, int idtype, float mu, double* out);
+int zoact_ce_grad(zoact_ctx* ctx, const void* H, int dtype, int64_t T, int32_t d, const void* W, int64_t vocab,
+                  const void* targets, int idtype, float grad_scale, float* loss, float* lse, double* mean, void* dH,
+                  void* dW, int wgdtype, int accumulate);
+
 /* ---- data-parallel replicas ----
  * A data-parallel ZO step shares everything but the tokens: every rank holds
  * the same W, U, C, m, v and seed, runs its token shard, and the ranks

@@ -18,5 +18,7 @@ from ._lib import (  # noqa: F401
     zoact_pair_forward_rs, zoact_pair_forward_gated_rs, zoact_rms_scale, rowscale_parts,
     zoact_multi_forward_rs, zoact_multi_forward_gated_rs, zoact_pair_forward_group_rs, zoact_multi_forward_group_rs,
     MAX_GROUP,
+    zoact_embed, zoact_embed_grad, zoact_layer_norm, zoact_layer_norm_grad,
+    zoact_ce_loss, zoact_ce_pair, zoact_ce_multi, zoact_ce_grad, ID_INT32, ID_INT64,
     DT_FP32, DT_BF16, DT_FP16, DT_INT4_G128, ACT_NONE, ACT_RELU, ACT_GELU, EXPORTS, LIB_PATH, TORCH_DT,
 )

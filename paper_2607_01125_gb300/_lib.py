@@ -31,6 +31,8 @@ MAX_GROUP = 4
 DT_FP32, DT_BF16, DT_FP16, DT_INT4_G128 = 0, 1, 2, 3
 ACT_NONE, ACT_RELU, ACT_GELU = 0, 1, 2
 
+ID_INT32, ID_INT64 = 0, 1
+
 TORCH_DT = {torch.float32: DT_FP32, torch.bfloat16: DT_BF16, torch.float16: DT_FP16}
 
 # every entry point include/zoact.h declares
@@ -45,6 +47,8 @@ EXPORTS = [
     "zoact_arena_hash", "zoact_pair_forward_rs", "zoact_pair_forward_gated_rs", "zoact_rms_scale",
     "zoact_multi_forward_rs", "zoact_multi_forward_gated_rs", "zoact_pair_forward_group_rs",
     "zoact_multi_forward_group_rs", "zoact_mix_rms_strided",
+    "zoact_embed", "zoact_embed_grad", "zoact_layer_norm", "zoact_layer_norm_grad",
+    "zoact_ce_loss", "zoact_ce_pair", "zoact_ce_multi", "zoact_ce_grad",
 ]
 
 
@@ -158,6 +162,14 @@ def load():
                                          ctypes.POINTER(zoact_eval_blocks), U64, I32, P, I32,
                                          ctypes.POINTER(zoact_rowscale)],
         "zoact_mix_rms_strided": [P, P, P, P, I32, I64, I32, I32, I32, I64, I64, F32, P],
+        "zoact_embed": [P, P, I32, I64, I32, P, I32, I64, F32, P],
+        "zoact_embed_grad": [P, P, I32, I64, I32, P, I32, I64, F32, P, I32, I32],
+        "zoact_layer_norm": [P, P, I32, I64, I32, I64, P, P, I32, F32, P, P, P],
+        "zoact_layer_norm_grad": [P, P, I64, P, I32, I64, I32, I64, P, I32, P, P, P, P, P],
+        "zoact_ce_loss": [P, P, I32, I64, I32, I32, P, I64, P, I32, P, P, P],
+        "zoact_ce_pair": [P, P, I32, I64, I32, P, I64, P, I32, F32, P],
+        "zoact_ce_multi": [P, P, I32, I64, I32, I32, P, I64, P, I32, F32, P],
+        "zoact_ce_grad": [P, P, I32, I64, I32, P, I64, P, I32, F32, P, P, P, P, P, I32, I32],
     }
     for name, argtypes in sig.items():
         fn = getattr(lib, name)
@@ -552,3 +564,128 @@ def zoact_multi_forward_gated_rs(ctx, gate, up, X, T, input_shared, points, seed
     _check("zoact_multi_forward_gated_rs", load().zoact_multi_forward_gated_rs(
         ctx.handle, ctypes.byref(gate), ctypes.byref(up), _ptr(X), _dt(X), int(T), int(input_shared), _ptr(P_gate),
         _ptr(P_up), ctypes.byref(b), int(seed), _ptr(H), _dt(H), ctypes.byref(rs)))
+
+
+# ---- the two ends of a language model: embedding, layer norm, cross entropy over the vocabulary ----
+_ID_DT = {torch.int32: ID_INT32, torch.int64: ID_INT64}
+
+
+def _rows(t):
+    """Device address and row stride of a matrix whose rows are contiguous (unit column stride)."""
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+        raise ValueError("libzoact takes matrices with unit column stride")
+    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else t.shape[1])
+
+
+def _out(t, shape, dtype, name):
+    """Address of an output (or None) whose shape and type the call fixes."""
+    if t is None:
+        return None
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
+        raise ValueError(f"{name}: expected {tuple(shape)} of {dtype}, got {tuple(t.shape)} of {t.dtype}")
+    return _ptr(t)
+
+
+def _id_args(ids):
+    if ids.dim() != 1 or ids.dtype not in _ID_DT:
+        raise ValueError("token ids and targets are vectors of int32 or int64")
+    return _ptr(ids), _ID_DT[ids.dtype]
+
+
+def zoact_embed(ctx, E, ids, Y, scale=1.0):
+    """Y [n_tok, d] = scale * E[ids]; rows of negative ids are zero."""
+    vocab, d = E.shape
+    pid, idt = _id_args(ids)
+    _check("zoact_embed", load().zoact_embed(ctx.handle, _ptr(E), _dt(E), vocab, d, pid, idt, ids.shape[0], float(scale),
+                                             _out(Y, (ids.shape[0], d), E.dtype, "Y")))
+
+
+def zoact_embed_grad(ctx, dY, ids, dE, scale=1.0, accumulate=False):
+    """dE [vocab, d] (dY's type or fp32) = scale * the sum of each id's rows of dY [n_tok, d], added to dE with
+    accumulate (rows without a token are then left alone)."""
+    vocab, d = dE.shape
+    pid, idt = _id_args(ids)
+    if tuple(dY.shape) != (ids.shape[0], d):
+        raise ValueError(f"dY: expected {(ids.shape[0], d)}, got {tuple(dY.shape)}")
+    _check("zoact_embed_grad", load().zoact_embed_grad(ctx.handle, _ptr(dY), _dt(dY), ids.shape[0], d, pid, idt, vocab,
+                                                       float(scale), _ptr(dE), _dt(dE), int(accumulate)))
+
+
+def _params(gain, bias, n, dtype):
+    """The type of gain and bias (one type where both are given; fp32 where neither is)."""
+    for t, name in ((gain, "gain"), (bias, "bias")):
+        if t is not None and (tuple(t.shape) != (n,) or t.dtype != (gain if gain is not None else bias).dtype):
+            raise ValueError(f"{name}: gain and bias are vectors of {n} of one type")
+    t = gain if gain is not None else bias
+    return DT_FP32 if t is None else _dt(t)
+
+
+def zoact_layer_norm(ctx, X, gain, bias, Y, eps=1e-5, mean=None, rstd=None):
+    """Layer norm of X's rows (a matrix with unit column stride); gain, bias: fp32 or X's type, or None."""
+    rows, n = X.shape
+    px, ld = _rows(X)
+    _check("zoact_layer_norm", load().zoact_layer_norm(
+        ctx.handle, px, _dt(X), rows, n, ld, _ptr(gain), _ptr(bias), _params(gain, bias, n, X.dtype), float(eps),
+        _out(Y, (rows, n), X.dtype, "Y"), _out(mean, (rows,), torch.float32, "mean"),
+        _out(rstd, (rows,), torch.float32, "rstd")))
+
+
+def zoact_layer_norm_grad(ctx, dY, X, gain, mean, rstd, dX=None, dgain=None, dbias=None):
+    """The gradient of zoact_layer_norm for dY (rows of unit column stride), from the statistics it kept."""
+    rows, n = X.shape
+    px, ld = _rows(X)
+    py, ldy = _rows(dY)
+    if tuple(dY.shape) != (rows, n) or dY.dtype != X.dtype:
+        raise ValueError("dY has X's shape and type")
+    _check("zoact_layer_norm_grad", load().zoact_layer_norm_grad(
+        ctx.handle, py, ldy, px, _dt(X), rows, n, ld, _ptr(gain), _params(gain, None, n, X.dtype),
+        _out(mean, (rows,), torch.float32, "mean"), _out(rstd, (rows,), torch.float32, "rstd"),
+        _out(dX, (rows, n), X.dtype, "dX"), _out(dgain, (n,), torch.float32, "dgain"),
+        _out(dbias, (n,), torch.float32, "dbias")))
+
+
+def _ce_args(H, W, targets, n_blocks):
+    rows, d = H.shape
+    T = targets.shape[0]
+    if rows != n_blocks * T or W.dim() != 2 or W.shape[1] != d or W.dtype != H.dtype:
+        raise ValueError("H [n_blocks T, d] and W [vocab, d] of one type, targets [T]")
+    pt, idt = _id_args(targets)
+    return rows, T, d, pt, idt
+
+
+def zoact_ce_loss(ctx, H, W, targets, n_blocks=1, loss=None, lse=None, mean=None):
+    """Cross entropy of H [n_blocks T, d] against the head W [vocab, d]: the rows' losses and log-sum-exps (fp32) and
+    each block's mean over the rows with targets[t] >= 0 (fp64)."""
+    rows, T, d, pt, idt = _ce_args(H, W, targets, n_blocks)
+    _check("zoact_ce_loss", load().zoact_ce_loss(
+        ctx.handle, _ptr(H), _dt(H), T, int(n_blocks), d, _ptr(W), W.shape[0], pt, idt,
+        _out(loss, (rows,), torch.float32, "loss"), _out(lse, (rows,), torch.float32, "lse"),
+        _out(mean, (int(n_blocks),), torch.float64, "mean")))
+
+
+def zoact_ce_pair(ctx, H, W, targets, eps, out):
+    """zoact_loss_pair with the cross entropy: H [2T, d] stacked, out (device fp64 [4]) = [L+, L-, D, a]."""
+    _, T, d, pt, idt = _ce_args(H, W, targets, 2)
+    _check("zoact_ce_pair", load().zoact_ce_pair(ctx.handle, _ptr(H), _dt(H), T, d, _ptr(W), W.shape[0], pt, idt,
+                                                 float(eps), _out(out, (4,), torch.float64, "out")))
+
+
+def zoact_ce_multi(ctx, H, W, targets, n_blocks, mu, out):
+    """zoact_loss_multi with the cross entropy: out (device fp64 [2 n_blocks - 1]) = [L_0 .. L_q, a_1 .. a_q]."""
+    _, T, d, pt, idt = _ce_args(H, W, targets, n_blocks)
+    _check("zoact_ce_multi", load().zoact_ce_multi(
+        ctx.handle, _ptr(H), _dt(H), T, int(n_blocks), d, _ptr(W), W.shape[0], pt, idt, float(mu),
+        _out(out, (2 * int(n_blocks) - 1,), torch.float64, "out")))
+
+
+def zoact_ce_grad(ctx, H, W, targets, dH=None, dW=None, loss=None, lse=None, mean=None, grad_scale=1.0, accumulate=False):
+    """The losses of zoact_ce_loss (one block) and the gradient of grad_scale * mean: dH like H, dW like W or fp32 (added
+    to with accumulate, fp32 only)."""
+    rows, _, d, pt, idt = _ce_args(H, W, targets, 1)
+    if dW is not None and tuple(dW.shape) != tuple(W.shape):
+        raise ValueError("dW has W's shape")
+    _check("zoact_ce_grad", load().zoact_ce_grad(
+        ctx.handle, _ptr(H), _dt(H), rows, d, _ptr(W), W.shape[0], pt, idt, float(grad_scale),
+        _out(loss, (rows,), torch.float32, "loss"), _out(lse, (rows,), torch.float32, "lse"),
+        _out(mean, (1,), torch.float64, "mean"), _out(dH, (rows, d), H.dtype, "dH"), _ptr(dW),
+        _dt(dW) if dW is not None else _dt(H), int(accumulate)))

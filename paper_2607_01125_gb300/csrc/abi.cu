@@ -757,6 +757,126 @@ int zoact_mix_rms_strided(zoact_ctx* ctx, const void* q, const void* k, const vo
   return launch_mix_rms(ctx, q, k, v, dtype, rows, n, n_rep, head_dim, eps, Y, ld_q, ld_kv);
 }
 
+static bool valid_id_type(int t) { return t == ZOACT_ID_INT32 || t == ZOACT_ID_INT64; }
+static bool aligned_ids(const void* p, int t) { return ((uintptr_t)p & (t == ZOACT_ID_INT64 ? 7u : 3u)) == 0; }
+static bool aligned_to(const void* p, int dtype) { return ((uintptr_t)p & (dtype_size(dtype) - 1)) == 0; }
+
+int zoact_embed(zoact_ctx* ctx, const void* E, int dtype, int64_t vocab, int32_t d, const void* ids, int idtype,
+                int64_t n_tok, float scale, void* Y) {
+  ZOACT_ENTER(ctx);
+  if (vocab <= 0 || d <= 0 || n_tok < 0 || !valid_act_dtype(dtype) || !valid_id_type(idtype)) return ZOACT_ERR_INVALID_ARG;
+  if (!E || !aligned_to(E, dtype)) return ZOACT_ERR_INVALID_ARG;
+  if (n_tok > 0 && (!ids || !Y || !aligned_ids(ids, idtype) || !aligned_to(Y, dtype))) return ZOACT_ERR_INVALID_ARG;
+  if (n_tok > 0x7fffffff || vocab > 0x7fffffff) return ZOACT_ERR_UNSUPPORTED;
+  return launch_embed(ctx, E, dtype, vocab, d, ids, idtype == ZOACT_ID_INT64, n_tok, scale, Y);
+}
+
+int zoact_embed_grad(zoact_ctx* ctx, const void* dY, int dtype, int64_t n_tok, int32_t d, const void* ids, int idtype,
+                     int64_t vocab, float scale, void* dE, int edtype, int accumulate) {
+  ZOACT_ENTER(ctx);
+  if (vocab <= 0 || d <= 0 || n_tok < 0 || !valid_act_dtype(dtype) || !valid_id_type(idtype)) return ZOACT_ERR_INVALID_ARG;
+  if (!dE || (edtype != dtype && edtype != ZOACT_DT_FP32) || !aligned_to(dE, edtype)) return ZOACT_ERR_INVALID_ARG;
+  if (n_tok > 0 && (!ids || !dY || !aligned_ids(ids, idtype) || !aligned_to(dY, dtype))) return ZOACT_ERR_INVALID_ARG;
+  if (n_tok > 0x7fffffff || vocab > 0x7fffffff) return ZOACT_ERR_UNSUPPORTED;
+  return launch_embed_grad(ctx, dY, dtype, n_tok, d, ids, idtype == ZOACT_ID_INT64, vocab, scale, dE, edtype, accumulate);
+}
+
+static bool valid_params(const void* gain, const void* bias, int pdtype, int dtype) {
+  return (pdtype == dtype || pdtype == ZOACT_DT_FP32) && aligned_to(gain, pdtype) && aligned_to(bias, pdtype);
+}
+
+int zoact_layer_norm(zoact_ctx* ctx, const void* X, int dtype, int64_t rows, int32_t n, int64_t ld_x, const void* gain,
+                     const void* bias, int pdtype, float eps, void* Y, float* mean, float* rstd) {
+  ZOACT_ENTER(ctx);
+  if (rows < 0 || n <= 0 || ld_x < n || !valid_act_dtype(dtype) || !(eps >= 0.f)) return ZOACT_ERR_INVALID_ARG;
+  if (!valid_params(gain, bias, pdtype, dtype)) return ZOACT_ERR_INVALID_ARG;
+  if (rows > 0 && (!X || !Y || !aligned_to(X, dtype) || !aligned_to(Y, dtype))) return ZOACT_ERR_INVALID_ARG;
+  if (rows > 0x7fffffff) return ZOACT_ERR_UNSUPPORTED;
+  return launch_layer_norm(ctx, X, dtype, rows, n, ld_x, gain, bias, pdtype, eps, Y, mean, rstd);
+}
+
+int zoact_layer_norm_grad(zoact_ctx* ctx, const void* dY, int64_t ld_dy, const void* X, int dtype, int64_t rows,
+                          int32_t n, int64_t ld_x, const void* gain, int pdtype, const float* mean, const float* rstd,
+                          void* dX, float* dgain, float* dbias) {
+  ZOACT_ENTER(ctx);
+  if (rows < 0 || n <= 0 || ld_x < n || ld_dy < n || !valid_act_dtype(dtype)) return ZOACT_ERR_INVALID_ARG;
+  if (!valid_params(gain, nullptr, pdtype, dtype)) return ZOACT_ERR_INVALID_ARG;
+  if (!dX && !dgain && !dbias) return ZOACT_ERR_INVALID_ARG;
+  if (rows > 0 && (!X || !dY || !mean || !rstd || !aligned_to(X, dtype) || !aligned_to(dY, dtype) ||
+                   !aligned_to(dX, dtype)))
+    return ZOACT_ERR_INVALID_ARG;
+  if (rows > 0x7fffffff) return ZOACT_ERR_UNSUPPORTED;
+  return launch_layer_norm_grad(ctx, dY, ld_dy, X, dtype, rows, n, ld_x, gain, pdtype, mean, rstd, dX, dgain, dbias);
+}
+
+// The arguments that every cross-entropy call has.
+static int check_ce(const CeArgs& c, int idtype) {
+  if (!valid_act_dtype(c.dtype) || !valid_id_type(idtype)) return ZOACT_ERR_INVALID_ARG;
+  if (c.T < 0 || c.nb < 1 || c.nb > ZOACT_MAX_EVAL_BLOCKS || c.d <= 0 || c.vocab <= 0) return ZOACT_ERR_INVALID_ARG;
+  if (c.d % (c.dtype == ZOACT_DT_FP32 ? 4 : 8) != 0) return ZOACT_ERR_INVALID_ARG;
+  if (!c.W || !aligned16(c.W)) return ZOACT_ERR_INVALID_ARG;
+  if (c.T > 0 && (!c.H || !c.targets || !aligned16(c.H) || !aligned_ids(c.targets, idtype))) return ZOACT_ERR_INVALID_ARG;
+  if (c.T > (1 << 26) || c.vocab > (1 << 26)) return ZOACT_ERR_UNSUPPORTED;
+  return ZOACT_OK;
+}
+
+static CeArgs ce_args(const void* H, int dtype, int64_t T, int32_t nb, int32_t d, const void* W, int64_t vocab,
+                      const void* targets, int idtype) {
+  CeArgs c = {};
+  c.H = H; c.W = W; c.targets = targets; c.id64 = idtype == ZOACT_ID_INT64; c.dtype = dtype;
+  c.nb = nb; c.d = d; c.T = T; c.rows = nb * T; c.vocab = vocab;
+  return c;
+}
+
+int zoact_ce_loss(zoact_ctx* ctx, const void* H, int dtype, int64_t T, int32_t n_blocks, int32_t d, const void* W,
+                  int64_t vocab, const void* targets, int idtype, float* loss, float* lse, double* mean) {
+  ZOACT_ENTER(ctx);
+  CeArgs c = ce_args(H, dtype, T, n_blocks, d, W, vocab, targets, idtype);
+  const int st = check_ce(c, idtype);
+  if (st) return st;
+  if (!loss && !lse && !mean) return ZOACT_ERR_INVALID_ARG;
+  c.loss = loss; c.lse = lse; c.mean = mean;
+  return launch_ce(ctx, c);
+}
+
+int zoact_ce_pair(zoact_ctx* ctx, const void* H, int dtype, int64_t T, int32_t d, const void* W, int64_t vocab,
+                  const void* targets, int idtype, float eps, double* out) {
+  ZOACT_ENTER(ctx);
+  CeArgs c = ce_args(H, dtype, T, 2, d, W, vocab, targets, idtype);
+  const int st = check_ce(c, idtype);
+  if (st) return st;
+  if (!out || !(eps > 0.f)) return ZOACT_ERR_INVALID_ARG;
+  c.est = 1; c.step = eps; c.out = out;
+  return launch_ce(ctx, c);
+}
+
+int zoact_ce_multi(zoact_ctx* ctx, const void* H, int dtype, int64_t T, int32_t n_blocks, int32_t d, const void* W,
+                   int64_t vocab, const void* targets, int idtype, float mu, double* out) {
+  ZOACT_ENTER(ctx);
+  CeArgs c = ce_args(H, dtype, T, n_blocks, d, W, vocab, targets, idtype);
+  const int st = check_ce(c, idtype);
+  if (st) return st;
+  if (!out || n_blocks < 2 || !(mu > 0.f)) return ZOACT_ERR_INVALID_ARG;
+  c.est = 2; c.step = mu; c.out = out;
+  return launch_ce(ctx, c);
+}
+
+int zoact_ce_grad(zoact_ctx* ctx, const void* H, int dtype, int64_t T, int32_t d, const void* W, int64_t vocab,
+                  const void* targets, int idtype, float grad_scale, float* loss, float* lse, double* mean, void* dH,
+                  void* dW, int wgdtype, int accumulate) {
+  ZOACT_ENTER(ctx);
+  CeArgs c = ce_args(H, dtype, T, 1, d, W, vocab, targets, idtype);
+  const int st = check_ce(c, idtype);
+  if (st) return st;
+  if (!dH && !dW) return ZOACT_ERR_INVALID_ARG;
+  if ((dH && !aligned16(dH)) || (dW && !aligned16(dW))) return ZOACT_ERR_INVALID_ARG;
+  if (wgdtype != dtype && wgdtype != ZOACT_DT_FP32) return ZOACT_ERR_INVALID_ARG;
+  if (accumulate && wgdtype != ZOACT_DT_FP32) return ZOACT_ERR_UNSUPPORTED;   // sums over calls are held in fp32
+  c.loss = loss; c.lse = lse; c.mean = mean;
+  c.dH = dH; c.dW = dW; c.wgdtype = wgdtype; c.accumulate = accumulate; c.grad_scale = grad_scale;
+  return launch_ce(ctx, c);
+}
+
 }  // extern "C"
 
 int zoact_mean_over_ranks(zoact_ctx* ctx, double* v, int64_t n, int32_t world) {

@@ -37,6 +37,9 @@ enum ScratchSlot {
   SLOT_STACKED_X,    // a shared input and its projection copied once per evaluation block (ranks above 32)
   SLOT_SK_PART,      // partial accumulators of the CTA-pair kernel's split tail
   SLOT_SK_TICKETS,   // its per-tile tickets (zero between launches)
+  SLOT_CE,           // cross entropy: count, target logits, row losses, the column tiles' maxima and sums
+  SLOT_CE_G,         // its gradient by the logits, for a chunk of rows
+  SLOT_CE_DW,        // fp32 sums of dW over several chunks of rows
   SLOT_COUNT
 };
 
@@ -157,6 +160,11 @@ __device__ __forceinline__ float silu_f(float x) { return x / (1.0f + expf(-x));
 
 inline size_t dtype_size(int dt) {
   return dt == ZOACT_DT_FP32 ? 4 : 2;
+}
+
+// Token id or target i of an array of int64 (id64) or int32.
+__device__ __forceinline__ int64_t load_id(const void* ids, int id64, int64_t i) {
+  return id64 ? __ldg(static_cast<const long long*>(ids) + i) : (int64_t)__ldg(static_cast<const int*>(ids) + i);
 }
 
 // ---- launchers (return ZOACT_* status) ----
@@ -296,6 +304,41 @@ int launch_adam(Ctx* ctx, float* C, float* m, float* v, const zoact_coeff_block*
 int launch_rms_norm(Ctx* ctx, const void* X, int dtype, int64_t rows, int n, float eps, void* Y);
 int launch_mix_rms(Ctx* ctx, const void* q, const void* k, const void* v, int dtype, int64_t rows,
                    int n, int n_rep, int head_dim, float eps, void* Y, int64_t ld_q, int64_t ld_kv);
+
+// Layer norm and its gradient (k_layernorm.cu): X rows ld apart, gain / bias of pdtype or nullptr.
+int launch_layer_norm(Ctx* ctx, const void* X, int dtype, int64_t rows, int n, int64_t ld, const void* gain,
+                      const void* bias, int pdtype, float eps, void* Y, float* mean, float* rstd);
+int launch_layer_norm_grad(Ctx* ctx, const void* dY, int64_t ld_dy, const void* X, int dtype, int64_t rows, int n,
+                           int64_t ld, const void* gain, int pdtype, const float* mean, const float* rstd, void* dX,
+                           float* dgain, float* dbias);
+
+// Embedding rows by token id and the table's gradient (k_embed.cu).
+int launch_embed(Ctx* ctx, const void* E, int dtype, int64_t vocab, int d, const void* ids, int id64, int64_t n,
+                 float scale, void* Y);
+int launch_embed_grad(Ctx* ctx, const void* dY, int dtype, int64_t n, int d, const void* ids, int id64, int64_t vocab,
+                      float scale, void* dE, int edtype, int accumulate);
+
+// Cross entropy over a vocabulary (k_ce.cu): rows = nb T, row b T + t has target t.
+struct CeArgs {
+  const void* H;        // [rows, d]
+  const void* W;        // [vocab, d]
+  const void* targets;  // [T], int64 (id64) or int32
+  int id64, dtype, nb, d;
+  int64_t rows, T, vocab;
+  float* loss;          // [rows] or nullptr
+  float* lse;           // [rows] or nullptr
+  double* mean;         // [nb] or nullptr
+  // estimator: 0 none, 1 the pair's {L+, L-, D, a} with eps = step, 2 {L_0 .. L_q, a_1 .. a_q} with mu = step
+  int est;
+  float step;
+  double* out;
+  // gradient of grad_scale * mean (nb = 1): [rows, d] of dtype and [vocab, d] of wgdtype, or nullptr
+  void* dH;
+  void* dW;
+  int wgdtype, accumulate;
+  float grad_scale;
+};
+int launch_ce(Ctx* ctx, const CeArgs& c);
 
 // Section 5.3 diagnostics (k_diag.cu): out[0] = ||Ua^T Ub||_F^2, out[2] = out[0] / ra;
 // energy: out[0] = ||U^T G||_F^2, out[1] = ||G||_F^2, out[2] = their ratio.  out: device fp64 [3].

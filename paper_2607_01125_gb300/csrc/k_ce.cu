@@ -1,0 +1,329 @@
+// Softmax cross entropy of hidden states H [rows, d] against a head W [vocab, d], without keeping the logits z = H W^T:
+//     lse_t = log sum_v exp z_tv,   loss_t = lse_t - z_t,target(t),   L_b = sum_t loss_t / N  (block b's counted rows)
+// and the gradient of s L by H and W.  With G = exp(z - lse) - onehot(target) on counted rows (0 on the others),
+//     dH = s/N G W,   dW = s/N G^T H.
+// A row whose target is negative has loss 0 and is not counted.
+#include "internal.h"
+
+namespace zoact {
+namespace {
+
+constexpr int TS = 64;              // tile of rows and of columns
+constexpr int TK = 16;
+constexpr int CE_THREADS = 256;     // 4 x 4 outputs a thread
+
+enum { MODE_CE = 0, MODE_G = 1, MODE_OUT = 2 };
+
+struct GemmArgs {
+  int64_t M, N, K;
+  int64_t sam, sak, sbn, sbk;       // element strides of A [M, K] and B [N, K]
+  // MODE_CE
+  float2* part;                     // [column tile][M]: maximum and sum of exp(z - maximum)
+  float* zt;                        // [M] the target's logit
+  const void* targets;
+  int id64;
+  int64_t T;
+  // MODE_G
+  const float2* stat;               // [M] the row's maximum and log sum exp(z - maximum)
+  float* G;
+  int64_t ldg;
+  // MODE_OUT
+  const double* count;              // counted rows (device)
+  float scale;
+  const float* add;                 // [M, N] or nullptr
+  void* out;                        // [M, N]
+};
+
+__device__ __forceinline__ int64_t target_of(const GemmArgs& a, int64_t row, int64_t vocab) {
+  const int64_t t = load_id(a.targets, a.id64, row % a.T);
+  return t >= 0 && t < vocab ? t : -1;
+}
+
+// D[m, n] = sum_k A[m, k] B[n, k] in fp32, 64 x 64 a block; sums of 1024 products are added up by themselves (one chain
+// over a vocabulary of 2^20 erred by 3e-4 of the terms' magnitudes).
+template <int MODE, typename TA, typename TB, typename TO>
+__global__ void __launch_bounds__(CE_THREADS)
+ce_gemm_kernel(const TA* __restrict__ A, const TB* __restrict__ B, const GemmArgs a) {
+  pdl_wait();
+  pdl_trigger();
+  __shared__ float sa[TK][TS + 1], sb[TK][TS + 1];
+  const int64_t m0 = (int64_t)blockIdx.y * TS, n0 = (int64_t)blockIdx.x * TS;
+  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+  float acc[4][4] = {}, sum[4][4] = {};
+  for (int64_t k0 = 0; k0 < a.K; k0 += TK) {
+    for (int e = threadIdx.x; e < TS * TK; e += CE_THREADS) {
+      const bool ak = a.sak == 1, bk = a.sbk == 1;       // the contiguous index varies fastest over the threads
+      const int am = ak ? e / TK : e % TS, ai = ak ? e % TK : e / TS;
+      const int bn = bk ? e / TK : e % TS, bi = bk ? e % TK : e / TS;
+      sa[ai][am] = m0 + am < a.M && k0 + ai < a.K ? to_f32<TA>(A[(m0 + am) * a.sam + (k0 + ai) * a.sak]) : 0.f;
+      sb[bi][bn] = n0 + bn < a.N && k0 + bi < a.K ? to_f32<TB>(B[(n0 + bn) * a.sbn + (k0 + bi) * a.sbk]) : 0.f;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < TK; ++k) {
+      float x[4], y[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) { x[i] = sa[k][ty * 4 + i]; y[i] = sb[k][tx * 4 + i]; }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(x[i], y[j], acc[i][j]);
+    }
+    __syncthreads();
+    if (k0 / TK % 64 == 63 || k0 + TK >= a.K) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) { sum[i][j] += acc[i][j]; acc[i][j] = 0.f; }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int64_t m = m0 + ty * 4 + i;
+    const bool mok = m < a.M;
+    if (MODE == MODE_CE) {
+      float mx = -INFINITY, s = 0.f;
+      const int64_t t = mok ? target_of(a, m, a.N) : -1;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int64_t n = n0 + tx * 4 + j;
+        if (n >= a.N) continue;
+        mx = fmaxf(mx, sum[i][j]);
+        if (n == t) a.zt[m] = sum[i][j];
+      }
+#pragma unroll
+      for (int o = 8; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (n0 + tx * 4 + j < a.N) s += expf(sum[i][j] - mx);
+#pragma unroll
+      for (int o = 8; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+      if (mok && tx == 0) a.part[(int64_t)blockIdx.x * a.M + m] = make_float2(mx, s);
+    } else if (MODE == MODE_G) {
+      if (!mok) continue;
+      const int64_t t = target_of(a, m, a.N);
+      const float2 st = a.stat[m];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int64_t n = n0 + tx * 4 + j;
+        if (n < a.N) a.G[m * a.ldg + n] = t < 0 ? 0.f : n == t ? expm1f((sum[i][j] - st.x) - st.y) : expf((sum[i][j] - st.x) - st.y);
+      }
+    } else {
+      if (!mok) continue;
+      const float f = (float)((double)a.scale / fmax(*a.count, 1.0));
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int64_t n = n0 + tx * 4 + j;
+        if (n >= a.N) continue;
+        const float v = sum[i][j] * f + (a.add ? a.add[m * a.N + n] : 0.f);
+        reinterpret_cast<TO*>(a.out)[m * a.N + n] = from_f32<TO>(v);
+      }
+    }
+  }
+}
+
+// The tiles' maxima m_i and sums s_i of a row joined: m, log s with s = sum s_i exp(m_i - m) in fp64 (a row that the
+// model predicts well has s = 1 + many terms that fp32 would drop one by one), lse = m + log s and loss = lse - z_t.
+// The gradient takes z - lse as (z - m) - log s, exact where z = m.
+__global__ void __launch_bounds__(CE_THREADS)
+ce_join_kernel(const float2* __restrict__ part, int64_t tiles, int64_t rows, const float* __restrict__ zt,
+               const void* __restrict__ targets, int id64, int64_t T, int64_t vocab, float2* __restrict__ stat,
+               float* __restrict__ lse, float* __restrict__ loss, int* status) {
+  pdl_wait();
+  pdl_trigger();
+  const int64_t row = (int64_t)blockIdx.x * CE_THREADS + threadIdx.x;
+  if (row >= rows) return;
+  float m = -INFINITY;
+  for (int64_t i = 0; i < tiles; ++i) m = fmaxf(m, part[i * rows + row].x);
+  double s = 0.0;
+  for (int64_t i = 0; i < tiles; ++i) {
+    const float2 p = part[i * rows + row];
+    s += (double)(p.y * expf(p.x - m));
+  }
+  const double ls = log(s);
+  const float l = (float)((double)m + ls);
+  stat[row] = make_float2(m, (float)ls);
+  lse[row] = l;
+  const int64_t t = load_id(targets, id64, row % T);
+  if (t >= vocab) record_error(status, ZOACT_ERR_INVALID_ARG);
+  loss[row] = t >= 0 && t < vocab ? l - zt[row] : 0.f;
+}
+
+// Block b: L_b = sum / N and D_b = sum over t of (loss_b - loss_0) / N, in fp64 and in a fixed order.
+//   mean [nb] (or nullptr); est: 1 = the pair's {L+, L-, D, a}, 2 = {L_0 .. L_q, a_1 .. a_q}, 0 = none.
+__global__ void __launch_bounds__(1024)
+ce_finish_kernel(const float* __restrict__ loss, int64_t T, int nb, const void* __restrict__ targets, int id64,
+                 int64_t vocab, double* mean, double* count, int est, double step, double* out, int* status) {
+  pdl_wait();
+  pdl_trigger();
+  __shared__ double red[3][32];
+  const int b = blockIdx.x;
+  const int other = est == 1 ? 1 : 0;       // the pair's D is L+ - L-, the others' L_b - L_0
+  double s = 0.0, dd = 0.0, n = 0.0;
+  for (int64_t t = threadIdx.x; t < T; t += 1024) {
+    const int64_t id = load_id(targets, id64, t);
+    if (id < 0 || id >= vocab) continue;
+    const double l = loss[b * T + t];
+    n += 1.0;
+    s += l;
+    if (est) dd += l - (double)loss[other * T + t];
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    s += __shfl_xor_sync(0xffffffffu, s, o);
+    dd += __shfl_xor_sync(0xffffffffu, dd, o);
+    n += __shfl_xor_sync(0xffffffffu, n, o);
+  }
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if (lane == 0) { red[0][warp] = s; red[1][warp] = dd; red[2][warp] = n; }
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  s = dd = n = 0.0;
+  for (int w = 0; w < 32; ++w) { s += red[0][w]; dd += red[1][w]; n += red[2][w]; }
+  const double den = n > 0.0 ? n : 1.0;
+  const double L = s / den, D = dd / den;
+  if (mean) mean[b] = L;
+  if (count && b == 0) *count = n;
+  bool fine = isfinite(L);
+  if (est == 1) {
+    out[b] = L;
+    if (b == 0) {
+      const double e = D / (2.0 * step);
+      out[2] = D;
+      out[3] = e;
+      fine = fine && isfinite(e);
+    }
+  } else if (est == 2) {
+    out[b] = L;
+    if (b > 0) {
+      const double e = D / step;
+      out[nb + b - 1] = e;
+      fine = fine && isfinite(e);
+    }
+  }
+  if (!fine) record_error(status, ZOACT_ERR_NONFINITE);
+}
+
+struct CeScratch {
+  double* count;
+  float *zt, *lse, *loss;
+  float2 *stat, *part;
+};
+
+bool ce_scratch(Ctx* ctx, int64_t rows, int64_t tiles, CeScratch& s) {
+  const size_t r = (size_t)((rows + 3) / 4 * 4);
+  char* p = (char*)scratch(ctx, SLOT_CE, 256 + r * 4 * 5 + (size_t)tiles * rows * sizeof(float2));
+  if (!p) return false;
+  s.count = (double*)p;
+  s.zt = (float*)(p + 256);
+  s.lse = s.zt + r;
+  s.loss = s.lse + r;
+  s.stat = (float2*)(s.loss + r);
+  s.part = s.stat + r;
+  return true;
+}
+
+template <int MODE, typename TA, typename TB, typename TO>
+int gemm(Ctx* ctx, const void* A, const void* B, const GemmArgs& a) {
+  const dim3 grid((unsigned)((a.N + TS - 1) / TS), (unsigned)((a.M + TS - 1) / TS));
+  ZOACT_CUDA_TRY(launch_pdl(ctx, ce_gemm_kernel<MODE, TA, TB, TO>, grid, dim3(CE_THREADS), 0, (const TA*)A, (const TB*)B, a));
+  ++ctx->n_launch;
+  return ZOACT_OK;
+}
+
+template <typename T>
+int run_forward(Ctx* ctx, const CeArgs& c, const CeScratch& s, int64_t tiles, float* lse, float* loss) {
+  GemmArgs a = {};
+  a.M = c.rows; a.N = c.vocab; a.K = c.d;
+  a.sam = c.d; a.sak = 1; a.sbn = c.d; a.sbk = 1;
+  a.part = s.part; a.zt = s.zt; a.targets = c.targets; a.id64 = c.id64; a.T = c.T;
+  const int st = gemm<MODE_CE, T, T, T>(ctx, c.H, c.W, a);
+  if (st) return st;
+  ZOACT_CUDA_TRY(launch_pdl(ctx, ce_join_kernel, dim3((unsigned)((c.rows + CE_THREADS - 1) / CE_THREADS)), dim3(CE_THREADS),
+                            0, (const float2*)s.part, tiles, c.rows, (const float*)s.zt, c.targets, c.id64, c.T, c.vocab,
+                            s.stat, lse, loss, ctx->d_status));
+  ++ctx->n_launch;
+  return ZOACT_OK;
+}
+
+template <typename T, typename TG>
+int run_backward(Ctx* ctx, const CeArgs& c, const CeScratch& s, float scale, void* dH, void* dW,
+                 int accumulate) {
+  const size_t most = (size_t)1 << 31;
+  int64_t chunk = (int64_t)(most / ((size_t)c.vocab * 4)) / TS * TS;
+  if (chunk < TS) chunk = TS;
+  if (chunk > c.rows) chunk = c.rows;
+  float* G = (float*)scratch(ctx, SLOT_CE_G, (size_t)chunk * c.vocab * 4);
+  if (!G) return ZOACT_ERR_NOMEM;
+  float* dWf = nullptr;             // fp32 sums of several chunks of rows
+  if (dW && sizeof(TG) != 4 && chunk < c.rows) {
+    dWf = (float*)scratch(ctx, SLOT_CE_DW, (size_t)c.vocab * c.d * 4);
+    if (!dWf) return ZOACT_ERR_NOMEM;
+  }
+  for (int64_t r0 = 0; r0 < c.rows; r0 += chunk) {
+    const int64_t n = c.rows - r0 < chunk ? c.rows - r0 : chunk;
+    const T* H = (const T*)c.H + r0 * c.d;
+    GemmArgs a = {};
+    a.M = n; a.N = c.vocab; a.K = c.d;
+    a.sam = c.d; a.sak = 1; a.sbn = c.d; a.sbk = 1;
+    a.targets = (const char*)c.targets + r0 * (c.id64 ? 8 : 4); a.id64 = c.id64; a.T = c.T;
+    a.stat = s.stat + r0; a.G = G; a.ldg = c.vocab;
+    int st = gemm<MODE_G, T, T, T>(ctx, H, c.W, a);
+    if (st) return st;
+    a.count = s.count; a.scale = scale;
+    if (dH) {
+      a.M = n; a.N = c.d; a.K = c.vocab;
+      a.sam = c.vocab; a.sak = 1; a.sbn = 1; a.sbk = c.d;
+      a.out = (T*)dH + r0 * c.d; a.add = nullptr;
+      st = gemm<MODE_OUT, float, T, T>(ctx, G, c.W, a);
+      if (st) return st;
+    }
+    if (dW) {
+      a.M = c.vocab; a.N = c.d; a.K = n;
+      a.sam = 1; a.sak = c.vocab; a.sbn = 1; a.sbk = c.d;
+      const bool last = r0 + n == c.rows;
+      if (dWf) {
+        a.add = r0 ? dWf : nullptr;
+        a.out = last ? dW : dWf;
+      } else {
+        a.out = dW;
+        a.add = r0 || accumulate ? (const float*)dW : nullptr;   // several chunks or accumulate: dW is fp32
+      }
+      st = dWf && !last ? gemm<MODE_OUT, float, T, float>(ctx, G, H, a) : gemm<MODE_OUT, float, T, TG>(ctx, G, H, a);
+      if (st) return st;
+    }
+  }
+  return ZOACT_OK;
+}
+
+template <typename T>
+int run(Ctx* ctx, const CeArgs& c) {
+  const int64_t tiles = (c.vocab + TS - 1) / TS;
+  CeScratch s;
+  if (!ce_scratch(ctx, c.rows, tiles, s)) return ZOACT_ERR_NOMEM;
+  float* lse = c.lse ? c.lse : s.lse;
+  float* loss = c.loss ? c.loss : s.loss;
+  int st = ZOACT_OK;
+  if (c.rows > 0) st = run_forward<T>(ctx, c, s, tiles, lse, loss);
+  if (st) return st;
+  ZOACT_CUDA_TRY(launch_pdl(ctx, ce_finish_kernel, dim3((unsigned)c.nb), dim3(1024), 0, (const float*)loss, c.T, c.nb,
+                            c.targets, c.id64, c.vocab, c.mean, s.count, c.est, (double)c.step, c.out, ctx->d_status));
+  ++ctx->n_launch;
+  if (c.dW && c.rows == 0 && !c.accumulate)
+    ZOACT_CUDA_TRY(cudaMemsetAsync(c.dW, 0, (size_t)c.vocab * c.d * dtype_size(c.wgdtype), ctx->stream));
+  if (c.rows == 0 || (!c.dH && !c.dW)) return ZOACT_OK;
+  return c.wgdtype == ZOACT_DT_FP32 ? run_backward<T, float>(ctx, c, s, c.grad_scale, c.dH, c.dW, c.accumulate)
+                                    : run_backward<T, T>(ctx, c, s, c.grad_scale, c.dH, c.dW, c.accumulate);
+}
+
+}  // namespace
+
+int launch_ce(Ctx* ctx, const CeArgs& c) {
+  switch (c.dtype) {
+    case ZOACT_DT_FP32: return run<float>(ctx, c);
+    case ZOACT_DT_BF16: return run<__nv_bfloat16>(ctx, c);
+    default: return run<__half>(ctx, c);
+  }
+}
+
+}  // namespace zoact
