@@ -1,0 +1,502 @@
+// The three products of the cross entropy over a vocabulary on CTA pairs (tcgen05 cta_group::2), with the vocabulary or
+// the width on the MMA's M side and the rows (tokens) on its N side:
+//
+//   logits   z^T = W H^T        M = vocab, N = rows,  K = d       epilogue: maximum and sum of exponentials per column
+//   by H     dH^T = W^T G^T     M = d,     N = rows,  K = vocab   epilogue: transposed store, or K pieces of the last tiles
+//   by W     dW = G^T H         M = vocab, N = d,     K = rows    epilogue: row-major store
+//
+// Rows on the N side make the padding of a ragged or small batch cheap (tiles of 32 to 256 rows in steps of 32), and the
+// logits' statistics reduce over the accumulator's lanes: a butterfly of shuffles leaves lane l with column l of 32.
+// Operands are read where they lie: K-major tiles as rows of 64 elements, and the transposed ones (W and G by columns, H by
+// columns) as M- or N-major tiles, 64 x 64 boxes whose descriptors step by boxes along M or N and by 8 K rows along K.
+// fp32 operands come as three bf16 parts each (24 bits); six products of parts run as six passes over K into one accumulator.
+//
+// The tensor core cuts its running fp32 sum off at every step of 16 products instead of rounding it: 4096 products of logits
+// came out 4e-6 low, five times what fp32 FMAs err by.  K is therefore taken in groups (Params::group_kb) whose sums the
+// epilogue adds up in registers, rounded; a group's sum is read while the next one runs into the other accumulator.
+//
+// Roles, barriers and bounded waits are those of the pair forward on CTA pairs: a TMA producer in each CTA, one MMA issuer
+// in the leader, eight epilogue warps in each (two warpgroups), two accumulators in TMEM.
+#pragma once
+#include "pair_tc2_kernel.cuh"
+
+namespace zoact {
+namespace ce {
+
+constexpr int BM = 128, BN = 256, BK = 64, STAGES = 6;    // BM: rows of a CTA, a pair has 2 BM
+constexpr int A_BYTES = BM * BK * 2;
+constexpr int STAGE_BYTES = 2 * A_BYTES;                  // A and up to BN / 2 rows of B
+constexpr int BOX_BYTES = 64 * BK * 2;                    // an M- or N-major box
+constexpr int EPI_THREADS = 256, EPI_BASE = 128, THREADS = EPI_BASE + EPI_THREADS;
+// Registers: 384 threads are launched with 168 each; the first warpgroup (producer, issuer) gives back what the epilogue's
+// two take for a tile's sums: 56 + 2 x 224 = 3 x 168.
+constexpr int REGS_ISSUE = 56, REGS_EPI = 224;
+constexpr int TMEM_COLS = 512;
+constexpr int STG_BYTES = 16384;                          // a warpgroup's staging buffer (128 rows x 128 bytes)
+constexpr int AUX_BYTES = 2 * STG_BYTES;
+constexpr int SMEM_BYTES = 1024 + STAGES * STAGE_BYTES + AUX_BYTES + 256;
+static_assert(SMEM_BYTES <= 232448, "dynamic shared memory above the 227 KB a CTA may use");
+
+enum Epi {
+  EPI_LSE = 0,   // column statistics
+  EPI_LOG,       // and the tile's maximum - z as 16-bit fixed point
+  EPI_Z,         // and z in fp32
+  EPI_COL,       // D^T scaled
+  EPI_ROW        // D scaled
+};
+
+struct Maps {
+  CUtensorMap a, b, out;
+};
+
+struct Params {
+  int num_m, num_n, num_kb, products, bn;
+  int group_kb;                     // K-blocks of one accumulation on the tensor core (EPI_ROW: all of a tile's)
+  int tail_first, tail_split;       // tiles from tail_first on run as tail_split pieces of K each
+  int64_t M, N;
+  int bf16;
+  int* status;
+  // logits: row n's target is targets[n % T]
+  float2* part;                     // [ceil(M / 128)][part_ld]: maximum and sum of exp(z - maximum)
+  int64_t part_ld;
+  float* zt;
+  const void* targets;
+  int id64;
+  int64_t T;
+  void* G;                          // EPI_LOG, EPI_Z: [N, ldg]
+  int64_t ldg;
+  // products by H and W: out = scale / max(count, 1) times D
+  const double* count;
+  float scale;
+  void* out;                        // EPI_COL: [N, M]
+  float* tail_part;                 // pieces of the tail's tiles: [piece][tile][bn][256]
+  int add;                          // EPI_ROW: add to out (fp32)
+};
+
+struct Shared {
+  uint64_t full[STAGES], empty[STAGES], tmem_full[2], tmem_empty[2], drain;
+  uint32_t tmem_base;
+  int abort_flag, epi_ok;
+};
+static_assert(sizeof(Shared) <= 256, "barrier block outgrew its shared-memory slot");
+
+struct Unit {
+  int m, n, kb0, kb1, slot;         // slot: index of a piece, or -1 for a whole tile
+};
+
+__device__ __forceinline__ bool unit_at(const Params& p, int u, Unit& w) {
+  const int tiles = p.num_m * p.num_n, tail = tiles - p.tail_first, K = p.num_kb * p.products;
+  int t = u;
+  w.kb0 = 0; w.kb1 = K; w.slot = -1;
+  if (u >= p.tail_first) {
+    const int s = u - p.tail_first;
+    if (s >= tail * p.tail_split) return false;
+    const int j = s / tail;         // pieces of one K range run together: they share their operands' lines in L2
+    t = p.tail_first + (s - j * tail);
+    if (p.tail_split > 1) {
+      w.kb0 = (int)((int64_t)j * K / p.tail_split);
+      w.kb1 = (int)((int64_t)(j + 1) * K / p.tail_split);
+      w.slot = s;
+    }
+  }
+  w.m = t / p.num_n;
+  w.n = t - w.m * p.num_n;
+  return true;
+}
+
+__device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const CUtensorMap* map, int32_t x, int32_t y, int32_t z,
+                                                 uint32_t bar_cluster) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], "
+      "[%5];" ::"r"(dst),
+      "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar_cluster)
+      : "memory");
+}
+// Add the box in shared memory to the tensor's elements (fp32), each once.
+__device__ __forceinline__ void tma_add_2d(const CUtensorMap* map, int32_t x, int32_t y, uint32_t src) {
+  asm volatile("cp.reduce.async.bulk.tensor.2d.global.shared::cta.add.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x),
+               "r"(y), "r"(src)
+               : "memory");
+}
+
+// M- or N-major operand tile with 128-byte swizzling: boxes of 64 elements x BK rows of K, BOX_BYTES apart along M or N,
+// 1024 bytes for 8 rows of K.
+__device__ __forceinline__ uint64_t sdesc_mn_sw128(uint32_t start) {
+  uint64_t d = 0;
+  d |= (uint64_t)((start & 0x3FFFFu) >> 4);
+  d |= (uint64_t)(BOX_BYTES >> 4) << 16;         // leading byte offset: the next 64 of M or N
+  d |= (uint64_t)(1024u >> 4) << 32;             // stride byte offset: the next 8 of K
+  d |= (uint64_t)1 << 46;
+  d |= (uint64_t)2 << 61;
+  return d;
+}
+template <bool MN>
+__device__ __forceinline__ uint64_t sdesc(uint32_t tile, int k) {
+  return MN ? sdesc_mn_sw128(tile + (uint32_t)k * 2048u) : tc::sdesc_k_sw128(tile + (uint32_t)k * 32u);
+}
+
+// Reduce 32 columns over the warp's 32 lanes: lane l returns column l's maximum (sum).  x is overwritten.
+template <bool MAX>
+__device__ __forceinline__ float columns_over_lanes(float* x, int lane) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    const bool up = lane & o;
+#pragma unroll
+    for (int i = 0; i < o; ++i) {
+      const float send = up ? x[i] : x[i + o], keep = up ? x[i + o] : x[i];
+      const float got = __shfl_xor_sync(0xffffffffu, send, o);
+      x[i] = MAX ? fmaxf(keep, got) : keep + got;
+    }
+  }
+  return x[0];
+}
+
+// A warp's part of an accumulator tile: 32 lanes, and of the tile's 32-column chunks those of its warpgroup (half, half + 2, ...).
+constexpr int CHUNKS = BN / 64;
+struct Part {
+  float x[CHUNKS][32];
+};
+
+// The sums over a unit's K groups, each read from its TMEM buffer as soon as it is complete.  False: the wait gave up.
+__device__ __forceinline__ bool sum_groups(const Params& p, Shared* ss, const Unit& w, int etid, int half, uint32_t t_quad,
+                                           uint32_t empty0, uint32_t empty1, volatile int* abort_flag, int& local, Part& a) {
+  const int nch = p.bn / 32;
+#pragma unroll 1
+  for (int kb = w.kb0; kb < w.kb1; kb += p.group_kb, ++local) {
+    const int buf = local & 1;
+    if (!pairtc::epi_wait_full(ss, buf, (uint32_t)(local >> 1) & 1u, abort_flag, p.status, etid)) return false;
+    const uint32_t t = t_quad + (uint32_t)(buf * BN);
+    const bool first = kb == w.kb0;
+#pragma unroll
+    for (int i = 0; i < CHUNKS; ++i) {
+      const int c = half + 2 * i;
+      if (c < nch) {
+        float y[32];
+        tc::tmem_ld32(t + (uint32_t)(c * 32), y);
+#pragma unroll
+        for (int j = 0; j < 32; ++j) a.x[i][j] = first ? y[j] : a.x[i][j] + y[j];
+      }
+    }
+    tc::tc_fence_before();
+    tc::named_bar_sync(3, EPI_THREADS);            // every epilogue thread of this CTA has read the buffer
+    if (etid == 0) pairtc::tc2::arrive_cluster(buf ? empty1 : empty0);
+  }
+  return true;
+}
+
+// Exchange area of the logits' epilogue, per warpgroup: [quad][column of its chunks], and each warp's copy of the columns'
+// maxima for broadcast reads.
+struct Exchange {
+  float mx[2][4][128], sum[2][4][128], all[8][128];
+};
+static_assert(sizeof(Exchange) <= AUX_BYTES, "exchange area");
+
+// Fixed point of the tile's maximum - z: 1 / LOG_STEPS, up to 16 (below exp(-16) of the tile's largest: 65535, no value).
+constexpr float LOG_STEPS = 4096.f;
+
+// One tile of logits: this CTA's 128 vocabulary entries from m0 and the tile's rows from n0; warp `quad` takes 32 entries.
+template <int EPI>
+__device__ __forceinline__ void epi_logits(const Params& p, Exchange* ex, Part& a, int half, int quad, int lane, int64_t m0,
+                                           int64_t n0) {
+  const int nch = p.bn / 32;
+  const int64_t v = m0 + quad * 32 + lane, vb = m0 + quad * 32;
+  const bool vok = v < p.M;
+#pragma unroll
+  for (int i = 0; i < CHUNKS; ++i) {
+    const int c = half + 2 * i;
+    if (c >= nch) continue;
+    // the target's logit, where one of these rows has its target among this warp's entries (seldom)
+    const int64_t n = n0 + c * 32 + lane;
+    const int64_t t = n < p.N ? load_id(p.targets, p.id64, n % p.T) : -1;
+    unsigned hits = __ballot_sync(0xffffffffu, t >= vb && t < vb + 32 && t < p.M);
+    while (hits) {
+      const int l = __ffs(hits) - 1;
+      hits &= hits - 1;
+      const int src = (int)(__shfl_sync(0xffffffffu, t, l) - vb);
+      float z = 0.f;
+#pragma unroll
+      for (int j = 0; j < 32; ++j) z = j == l ? a.x[i][j] : z;
+      if (lane == src) p.zt[n0 + c * 32 + l] = z;
+    }
+    float y[32];
+#pragma unroll
+    for (int j = 0; j < 32; ++j) y[j] = vok ? a.x[i][j] : -INFINITY;
+    ex->mx[half][quad][i * 32 + lane] = columns_over_lanes<true>(y, lane);
+  }
+  tc::named_bar_sync(4 + half, 128);
+  float* all = ex->all[half * 4 + quad];
+#pragma unroll
+  for (int i = 0; i < CHUNKS; ++i) {
+    const int k = i * 32 + lane;
+    if (half + 2 * i < nch)
+      all[k] = fmaxf(fmaxf(ex->mx[half][0][k], ex->mx[half][1][k]), fmaxf(ex->mx[half][2][k], ex->mx[half][3][k]));
+  }
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < CHUNKS; ++i) {
+    const int c = half + 2 * i;
+    if (c >= nch) continue;
+    const int64_t n = n0 + c * 32;
+    const int nv = (int)(p.N - n < 32 ? p.N - n : 32);
+    if (EPI == EPI_Z && vok) {
+      float* g = reinterpret_cast<float*>(p.G) + n * p.ldg + v;
+#pragma unroll
+      for (int j = 0; j < 32; ++j)
+        if (j < nv) g[j * p.ldg] = a.x[i][j];
+    }
+#pragma unroll
+    for (int j = 0; j < 32; j += 4) {
+      const float4 m = *reinterpret_cast<const float4*>(all + i * 32 + j);
+      a.x[i][j] -= m.x;
+      a.x[i][j + 1] -= m.y;
+      a.x[i][j + 2] -= m.z;
+      a.x[i][j + 3] -= m.w;
+    }
+    if (EPI == EPI_LOG && vok) {
+      uint16_t* g = reinterpret_cast<uint16_t*>(p.G) + n * p.ldg + v;
+#pragma unroll
+      for (int j = 0; j < 32; ++j)         // rounded in the low bits of a sum with 2^23
+        if (j < nv)
+          g[j * p.ldg] = (uint16_t)__float_as_uint(fminf(a.x[i][j] * -LOG_STEPS, 65535.f) + 8388608.f);
+    }
+#pragma unroll
+    for (int j = 0; j < 32; ++j) a.x[i][j] = vok ? __expf(a.x[i][j]) : 0.f;
+    ex->sum[half][quad][i * 32 + lane] = columns_over_lanes<false>(a.x[i], lane);
+  }
+  tc::named_bar_sync(4 + half, 128);
+  // chunk i's statistics by warp i of the warpgroup
+  const int c = half + 2 * quad, k = quad * 32 + lane;
+  const int64_t n = n0 + c * 32 + lane;
+  if (c < nch && n < p.N && m0 < p.M)
+    p.part[m0 / BM * p.part_ld + n] =
+        make_float2(all[k], (ex->sum[half][0][k] + ex->sum[half][1][k]) + (ex->sum[half][2][k] + ex->sum[half][3][k]));
+}
+
+// D^T scaled (or a K piece of it, unscaled fp32): a warp stores 32 consecutive elements of each row.
+template <typename TO>
+__device__ __forceinline__ void epi_col(const Params& p, const Part& a, int half, int row_in_cta, uint32_t rank, int64_t m0,
+                                        int64_t n0, int slot, float f) {
+  const int64_t m = m0 + row_in_cta;
+  const bool mok = m < p.M;
+#pragma unroll
+  for (int i = 0; i < CHUNKS; ++i) {
+    const int c = half + 2 * i;
+    if (c >= p.bn / 32) continue;
+    const int64_t n = n0 + c * 32;
+    if (slot >= 0) {
+      float* d = p.tail_part + ((size_t)slot * p.bn + c * 32) * (2 * BM) + rank * BM + row_in_cta;
+#pragma unroll
+      for (int j = 0; j < 32; ++j) d[j * (2 * BM)] = a.x[i][j];
+    } else if (mok) {
+      const int nv = (int)(p.N - n < 32 ? p.N - n : 32);
+      TO* d = reinterpret_cast<TO*>(p.out) + n * p.M + m;
+#pragma unroll
+      for (int j = 0; j < 32; ++j) {
+        if (j < nv) *d = from_f32<TO>(a.x[i][j] * f);
+        d += p.M;
+        asm volatile("" : "+l"(d));        // one address at a time: 32 of them do not fit beside the sums
+      }
+    }
+  }
+}
+
+// D scaled, through the warpgroup's staging buffer in 128-byte columns; one thread stores each box.
+template <typename TO>
+__device__ __forceinline__ void epi_row(const Params& p, const Maps& tm, uint8_t* stg, int etid, int half, int row_in_cta,
+                                        int64_t m0, int64_t n0, float f, uint32_t t_row, bool& pending) {
+  constexpr int CC = 128 / (int)sizeof(TO);
+  const int wcols = p.bn / 2, cb = half * wcols;
+  const bool issuer = (etid & 127) == 0;
+  const uint32_t sbuf = tc::smem_u32(stg + half * STG_BYTES);
+  for (int c = 0; c < wcols; c += CC) {
+    const int64_t n = n0 + cb + c;
+    if (n >= p.N || m0 >= p.M) break;               // uniform over the warpgroup
+    if (issuer && pending) tc::bulk_wait_read0();   // the buffer's previous store has read it
+    tc::named_bar_sync(4 + half, 128);
+#pragma unroll 1
+    for (int q = 0; q < CC; q += 32) {
+      float x[32];
+      tc::tmem_ld32(t_row + (uint32_t)(cb + c + q), x);
+#pragma unroll
+      for (int j = 0; j < 32; ++j) x[j] *= f;
+      pairtc::stage_granules<TO, 32>(sbuf, row_in_cta, q, x, true);
+    }
+    tc::fence_proxy_async_smem();
+    tc::named_bar_sync(4 + half, 128);
+    if (issuer) {
+      if (sizeof(TO) == 4 && p.add) tma_add_2d(&tm.out, (int32_t)n, (int32_t)m0, sbuf);
+      else tc::tma_store_2d(&tm.out, (int32_t)n, (int32_t)m0, sbuf);
+      tc::bulk_commit();
+      pending = true;
+    }
+  }
+}
+
+template <int EPI, bool A_MN, bool B_MN, typename TO>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
+ce_tc_kernel(const __grid_constant__ Maps tm, const Params p) {
+  namespace tc2 = pairtc::tc2;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  uint8_t* aux = smem + STAGES * STAGE_BYTES;
+  Shared* ss = reinterpret_cast<Shared*>(aux + AUX_BYTES);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = tc2::cluster_rank();
+  const bool leader = rank == 0;
+  volatile int* abort_flag = &ss->abort_flag;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < STAGES; ++s) {
+      tc::mbar_init(tc::smem_u32(&ss->full[s]), 2);    // one producer arrival from each CTA (the leader's copy is used)
+      tc::mbar_init(tc::smem_u32(&ss->empty[s]), 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      tc::mbar_init(tc::smem_u32(&ss->tmem_full[b]), 1);
+      tc::mbar_init(tc::smem_u32(&ss->tmem_empty[b]), 2);
+    }
+    tc::mbar_init(tc::smem_u32(&ss->drain), 1);
+    ss->abort_flag = 0;
+    tc::fence_mbar_init();
+    tc::prefetch_tmap(&tm.a);
+    tc::prefetch_tmap(&tm.b);
+    if (EPI == EPI_ROW) tc::prefetch_tmap(&tm.out);
+  }
+  if (warp == 1) {
+    tc2::tmem_alloc2(tc::smem_u32(&ss->tmem_base), TMEM_COLS);
+    tc2::tmem_relinquish2();
+  }
+  tc::tc_fence_before();
+  __syncthreads();
+  tc2::cluster_sync();                    // both CTAs' barriers exist before any remote arrival
+  tc::tc_fence_after();
+  const uint32_t tmem_base = ss->tmem_base;
+  pdl_wait();
+  pdl_trigger();
+
+  const int cluster_id = blockIdx.x >> 1, n_clusters = gridDim.x >> 1;
+  const int bh = p.bn / 2;
+  Unit w;
+
+  if (warp < EPI_BASE / 32) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_ISSUE));
+    if (warp == 0) {
+      // ---------------- TMA producer (both CTAs) ----------------
+      if (lane == 0) {
+        const uint32_t stage_tx = (uint32_t)(A_BYTES + bh * BK * 2);
+        int stage = 0;
+        uint32_t phase = 0;
+        bool ok = true;
+        for (int u = cluster_id; ok && unit_at(p, u, w); u += n_clusters) {
+          const int m0 = w.m * 2 * BM + (int)rank * BM, n0 = w.n * p.bn + (int)rank * bh;
+          for (int kb = w.kb0; kb < w.kb1; ++kb) {
+            if (!tc::mbar_wait(tc::smem_u32(&ss->empty[stage]), phase ^ 1u, abort_flag, p.status)) { ok = false; break; }
+            const uint32_t full_leader = tc2::map_to(tc::smem_u32(&ss->full[stage]), 0);
+            tc2::arrive_expect_tx_cluster(full_leader, stage_tx);
+            const uint32_t sa = tc::smem_u32(smem + stage * STAGE_BYTES), sb = sa + A_BYTES;
+            // products of parts (a, b): (0,0) (0,1) (1,0) (0,2) (1,1) (2,0)
+            const int pr = kb / p.num_kb, k = (kb - pr * p.num_kb) * BK;
+            const int pa = (0x210100 >> (4 * pr)) & 15, pb = (0x012010 >> (4 * pr)) & 15;
+            if (A_MN) {
+              tma_load_3d_pair(sa, &tm.a, m0, k, pa, full_leader);
+              tma_load_3d_pair(sa + BOX_BYTES, &tm.a, m0 + 64, k, pa, full_leader);
+            } else {
+              tma_load_3d_pair(sa, &tm.a, k, m0, pa, full_leader);
+            }
+            if (B_MN) {
+              for (int j = 0; j < bh / 64; ++j)
+                tma_load_3d_pair(sb + j * BOX_BYTES, &tm.b, n0 + 64 * j, k, pb, full_leader);
+            } else {
+              tma_load_3d_pair(sb, &tm.b, k, n0, pb, full_leader);
+            }
+            if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+          }
+        }
+        if (!ok) {
+          // our copies complete on the leader's barriers; give them time to land before the CTA winds down
+          const uint64_t t0 = tc::global_timer_ns();
+          while (tc::global_timer_ns() - t0 < 2000000ull) {
+          }
+        }
+      }
+    } else if (warp == 1) {
+      // ---------------- MMA issuer (leader CTA) ----------------
+      if (lane == 0 && leader) {
+        const uint32_t idesc = tc::idesc_f16(2 * BM, p.bn, p.bf16) | (A_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u);
+        int stage = 0, local = 0;
+        uint32_t phase = 0;
+        bool ok = true, issued_any = false;
+        for (int u = cluster_id; ok && unit_at(p, u, w); u += n_clusters) {
+          for (int g0 = w.kb0; ok && g0 < w.kb1; g0 += p.group_kb, ++local) {
+            const int buf = local & 1, g1 = min(g0 + p.group_kb, w.kb1);
+            if (!tc::mbar_wait(tc::smem_u32(&ss->tmem_empty[buf]), ((uint32_t)(local >> 1) & 1u) ^ 1u, abort_flag, p.status)) {
+              ok = false;
+              break;
+            }
+            tc::tc_fence_after();
+            const uint32_t d_tmem = tmem_base + (uint32_t)(buf * BN);
+            for (int kb = g0; kb < g1; ++kb) {
+              if (!tc::mbar_wait(tc::smem_u32(&ss->full[stage]), phase, abort_flag, p.status)) { ok = false; break; }
+              tc::tc_fence_after();
+              const uint32_t sa = tc::smem_u32(smem + stage * STAGE_BYTES), sb = sa + A_BYTES;
+#pragma unroll
+              for (int k = 0; k < BK / 16; ++k)
+                tc2::mma2_f16(d_tmem, sdesc<A_MN>(sa, k), sdesc<B_MN>(sb, k), idesc, (kb != g0 || k != 0) ? 1u : 0u);
+              tc2::commit2_both(tc::smem_u32(&ss->empty[stage]));
+              issued_any = true;
+              if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+            }
+            if (ok) tc2::commit2_both(tc::smem_u32(&ss->tmem_full[buf]));
+          }
+        }
+        if (issued_any) {
+          tc2::commit2_own(tc::smem_u32(&ss->drain));
+          tc::mbar_wait_drain(tc::smem_u32(&ss->drain), 0, 100000000ull);
+        }
+      }
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_EPI));
+    // ---------------- epilogue (warps 4..11, both CTAs) ----------------
+    const int etid = threadIdx.x - EPI_BASE, half = etid >> 7, quad = warp & 3;
+    const int row_in_cta = quad * 32 + lane;
+    const uint32_t empty0 = tc2::map_to(tc::smem_u32(&ss->tmem_empty[0]), 0);
+    const uint32_t empty1 = tc2::map_to(tc::smem_u32(&ss->tmem_empty[1]), 0);
+    float f = 0.f;
+    if (EPI == EPI_COL || EPI == EPI_ROW) f = (float)((double)p.scale / fmax(__ldcg(p.count), 1.0));
+    int local = 0;
+    bool pending = false;
+    const uint32_t t_quad = tmem_base + ((uint32_t)(quad * 32) << 16);
+    for (int u = cluster_id; unit_at(p, u, w); u += n_clusters) {
+      const int64_t m0 = (int64_t)w.m * 2 * BM + (int64_t)rank * BM, n0 = (int64_t)w.n * p.bn;
+      if constexpr (EPI == EPI_ROW) {
+        const int buf = local & 1;
+        if (!pairtc::epi_wait_full(ss, buf, (uint32_t)(local >> 1) & 1u, abort_flag, p.status, etid)) break;
+        epi_row<TO>(p, tm, aux, etid, half, row_in_cta, m0, n0, f, t_quad + (uint32_t)(buf * BN), pending);
+        tc::tc_fence_before();
+        tc::named_bar_sync(3, EPI_THREADS);        // every epilogue thread of this CTA has read the tile
+        if (etid == 0) tc2::arrive_cluster(buf ? empty1 : empty0);
+        ++local;
+      } else {
+        Part a;
+        if (!sum_groups(p, ss, w, etid, half, t_quad, empty0, empty1, abort_flag, local, a)) break;
+        if constexpr (EPI == EPI_COL)
+          epi_col<TO>(p, a, half, row_in_cta, rank, m0, n0, w.slot, f);
+        else
+          epi_logits<EPI>(p, reinterpret_cast<Exchange*>(aux), a, half, quad, lane, m0, n0);
+      }
+    }
+    if (pending) tc::bulk_wait0();
+  }
+
+  tc::tc_fence_before();
+  __syncthreads();
+  tc2::cluster_sync();                    // the peer's MMAs and copies are done before TMEM and smem go away
+  if (warp == 1) {
+    __syncwarp();
+    tc::tc_fence_after();
+    tc2::tmem_dealloc2(tmem_base, TMEM_COLS);
+  }
+}
+
+}  // namespace ce
+}  // namespace zoact

@@ -39,6 +39,7 @@ enum ScratchSlot {
   SLOT_SK_TICKETS,   // its per-tile tickets (zero between launches)
   SLOT_CE,           // cross entropy: count, target logits, row losses, the column tiles' maxima and sums
   SLOT_CE_G,         // its gradient by the logits, for a chunk of rows
+  SLOT_CE_TAIL,      // K pieces of the last tiles of its product by H
   SLOT_CE_DW,        // fp32 sums of dW over several chunks of rows
   SLOT_COUNT
 };

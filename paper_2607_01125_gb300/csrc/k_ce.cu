@@ -3,7 +3,7 @@
 // and the gradient of s L by H and W.  With G = exp(z - lse) - onehot(target) on counted rows (0 on the others),
 //     dH = s/N G W,   dW = s/N G^T H.
 // A row whose target is negative has loss 0 and is not counted.
-#include "internal.h"
+#include "ce_tc.h"
 
 namespace zoact {
 namespace {
@@ -125,21 +125,39 @@ ce_gemm_kernel(const TA* __restrict__ A, const TB* __restrict__ B, const GemmArg
 // The tiles' maxima m_i and sums s_i of a row joined: m, log s with s = sum s_i exp(m_i - m) in fp64 (a row that the
 // model predicts well has s = 1 + many terms that fp32 would drop one by one), lse = m + log s and loss = lse - z_t.
 // The gradient takes z - lse as (z - m) - log s, exact where z = m.
-__global__ void __launch_bounds__(CE_THREADS)
-ce_join_kernel(const float2* __restrict__ part, int64_t tiles, int64_t rows, const float* __restrict__ zt,
+// 32 rows a block, 32 groups of tiles each, joined in group order.
+__global__ void __launch_bounds__(1024)
+ce_join_kernel(const float2* __restrict__ part, int64_t tiles, int64_t part_ld, int64_t rows, const float* __restrict__ zt,
                const void* __restrict__ targets, int id64, int64_t T, int64_t vocab, float2* __restrict__ stat,
                float* __restrict__ lse, float* __restrict__ loss, int* status) {
   pdl_wait();
   pdl_trigger();
-  const int64_t row = (int64_t)blockIdx.x * CE_THREADS + threadIdx.x;
-  if (row >= rows) return;
+  __shared__ float mx[32][33];
+  __shared__ double sum[32][33];
+  const int lane = threadIdx.x & 31, group = threadIdx.x >> 5;
+  const int64_t row = (int64_t)blockIdx.x * 32 + lane;
   float m = -INFINITY;
-  for (int64_t i = 0; i < tiles; ++i) m = fmaxf(m, part[i * rows + row].x);
-  double s = 0.0;
-  for (int64_t i = 0; i < tiles; ++i) {
-    const float2 p = part[i * rows + row];
-    s += (double)(p.y * expf(p.x - m));
+  if (row < rows) {
+#pragma unroll 4
+    for (int64_t i = group; i < tiles; i += 32) m = fmaxf(m, part[i * part_ld + row].x);
   }
+  mx[group][lane] = m;
+  __syncthreads();
+#pragma unroll
+  for (int g = 0; g < 32; ++g) m = fmaxf(m, mx[g][lane]);
+  double s = 0.0;
+  if (row < rows) {
+#pragma unroll 4
+    for (int64_t i = group; i < tiles; i += 32) {
+      const float2 p = part[i * part_ld + row];
+      s += (double)(p.y * expf(p.x - m));
+    }
+  }
+  sum[group][lane] = s;
+  __syncthreads();
+  if (group != 0 || row >= rows) return;
+#pragma unroll
+  for (int g = 1; g < 32; ++g) s += sum[g][lane];
   const double ls = log(s);
   const float l = (float)((double)m + ls);
   stat[row] = make_float2(m, (float)ls);
@@ -149,11 +167,72 @@ ce_join_kernel(const float2* __restrict__ part, int64_t tiles, int64_t rows, con
   loss[row] = t >= 0 && t < vocab ? l - zt[row] : 0.f;
 }
 
+// The number of counted rows.
+__global__ void __launch_bounds__(1024)
+ce_count_kernel(const void* __restrict__ targets, int id64, int64_t T, int64_t vocab, double* count) {
+  pdl_wait();
+  pdl_trigger();
+  __shared__ int red[32];
+  int n = 0;
+  for (int64_t t = threadIdx.x; t < T; t += 1024) {
+    const int64_t id = load_id(targets, id64, t);
+    n += id >= 0 && id < vocab;
+  }
+  n = __reduce_add_sync(0xffffffffu, n);
+  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = n;
+  __syncthreads();
+  if (threadIdx.x < 32) {
+    n = __reduce_add_sync(0xffffffffu, red[threadIdx.x]);
+    if (threadIdx.x == 0) *count = n;
+  }
+}
+
+// What a chunk of rows kept of its logits, 4096 (m_tile - z) in 16 bits, to G = exp(z - lse) - onehot in the operands' type,
+// in place.  The fixed point errs by 1.2e-4 of the exponential at most, a third of fp16's rounding (exp(z - m_tile) in fp16
+// would have rounded twice; beyond 16 below the tile's largest nothing is kept).  fp16's G is scaled by 2^15 (undone in
+// the products' scale): 1 / vocab would lie among its subnormals.  The target's element is expm1(z_t - lse): p - 1 from a
+// rounded p would lose what is left of it where the model is nearly right.
+constexpr float G_SCALE_FP16 = 32768.f;
+
+template <typename T>
+__global__ void __launch_bounds__(CE_THREADS)
+ce_scale_kernel(void* __restrict__ G, int64_t ldg, const float2* __restrict__ part, int64_t part_ld,
+                const float2* __restrict__ stat, const float* __restrict__ zt, const void* __restrict__ targets, int id64,
+                int64_t vocab) {
+  pdl_wait();
+  pdl_trigger();
+  constexpr float scale = sizeof(T) == 2 && __is_same(T, __half) ? G_SCALE_FP16 : 1.f;
+  const int64_t row = blockIdx.y, v0 = ((int64_t)blockIdx.x * CE_THREADS + threadIdx.x) * 8;
+  if (v0 >= vocab) return;
+  uint4* g = reinterpret_cast<uint4*>(reinterpret_cast<__half*>(G) + row * ldg + v0);
+  const int64_t t = load_id(targets, id64, row);
+  const bool counted = t >= 0 && t < vocab;
+  uint4 q = make_uint4(0, 0, 0, 0);
+  if (counted) {
+    q = *g;
+    const float2 st = stat[row];
+    const float c = (part[v0 / ce::V_TILE * part_ld + row].x - st.x) - st.y;
+    const float none = c == c ? 0.f : c;   // a row that is not finite stays so
+    uint32_t* w = reinterpret_cast<uint32_t*>(&q);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t lo = w[i] & 0xffffu, hi = w[i] >> 16;
+      const float a = lo == 65535u ? none : __expf(fmaf((float)lo, -1.f / 4096.f, c)) * scale;
+      const float b = hi == 65535u ? none : __expf(fmaf((float)hi, -1.f / 4096.f, c)) * scale;
+      T o[2] = {from_f32<T>(a), from_f32<T>(b)};
+      w[i] = *reinterpret_cast<const uint32_t*>(o);
+    }
+    if (t >= v0 && t < v0 + 8)
+      reinterpret_cast<T*>(&q)[t - v0] = from_f32<T>(expm1f((zt[row] - st.x) - st.y) * scale);
+  }
+  *g = q;
+}
+
 // Block b: L_b = sum / N and D_b = sum over t of (loss_b - loss_0) / N, in fp64 and in a fixed order.
 //   mean [nb] (or nullptr); est: 1 = the pair's {L+, L-, D, a}, 2 = {L_0 .. L_q, a_1 .. a_q}, 0 = none.
 __global__ void __launch_bounds__(1024)
 ce_finish_kernel(const float* __restrict__ loss, int64_t T, int nb, const void* __restrict__ targets, int id64,
-                 int64_t vocab, double* mean, double* count, int est, double step, double* out, int* status) {
+                 int64_t vocab, double* mean, int est, double step, double* out, int* status) {
   pdl_wait();
   pdl_trigger();
   __shared__ double red[3][32];
@@ -183,7 +262,6 @@ ce_finish_kernel(const float* __restrict__ loss, int64_t T, int nb, const void* 
   const double den = n > 0.0 ? n : 1.0;
   const double L = s / den, D = dd / den;
   if (mean) mean[b] = L;
-  if (count && b == 0) *count = n;
   bool fine = isfinite(L);
   if (est == 1) {
     out[b] = L;
@@ -208,11 +286,13 @@ struct CeScratch {
   double* count;
   float *zt, *lse, *loss;
   float2 *stat, *part;
+  int64_t part_ld;
 };
 
-bool ce_scratch(Ctx* ctx, int64_t rows, int64_t tiles, CeScratch& s) {
+// part_rows: rows whose statistics are held at a time.
+bool ce_scratch(Ctx* ctx, int64_t rows, int64_t part_rows, int64_t tiles, CeScratch& s) {
   const size_t r = (size_t)((rows + 3) / 4 * 4);
-  char* p = (char*)scratch(ctx, SLOT_CE, 256 + r * 4 * 5 + (size_t)tiles * rows * sizeof(float2));
+  char* p = (char*)scratch(ctx, SLOT_CE, 256 + r * 4 * 5 + (size_t)tiles * part_rows * sizeof(float2));
   if (!p) return false;
   s.count = (double*)p;
   s.zt = (float*)(p + 256);
@@ -220,6 +300,7 @@ bool ce_scratch(Ctx* ctx, int64_t rows, int64_t tiles, CeScratch& s) {
   s.loss = s.lse + r;
   s.stat = (float2*)(s.loss + r);
   s.part = s.stat + r;
+  s.part_ld = part_rows;
   return true;
 }
 
@@ -227,6 +308,23 @@ template <int MODE, typename TA, typename TB, typename TO>
 int gemm(Ctx* ctx, const void* A, const void* B, const GemmArgs& a) {
   const dim3 grid((unsigned)((a.N + TS - 1) / TS), (unsigned)((a.M + TS - 1) / TS));
   ZOACT_CUDA_TRY(launch_pdl(ctx, ce_gemm_kernel<MODE, TA, TB, TO>, grid, dim3(CE_THREADS), 0, (const TA*)A, (const TB*)B, a));
+  ++ctx->n_launch;
+  return ZOACT_OK;
+}
+
+// Join rows [r0, r0 + n), whose statistics lie at the beginning of s.part.
+int join(Ctx* ctx, const CeArgs& c, const CeScratch& s, int64_t tiles, int64_t r0, int64_t n, float* lse, float* loss) {
+  // with several blocks the rows are all there; a chunk of rows (one block) takes its own targets
+  const void* targets = (const char*)c.targets + r0 * (c.id64 ? 8 : 4);
+  ZOACT_CUDA_TRY(launch_pdl(ctx, ce_join_kernel, dim3((unsigned)((n + 31) / 32)), dim3(1024), 0, (const float2*)s.part, tiles,
+                            s.part_ld, n, (const float*)s.zt + r0, targets, c.id64, c.T, c.vocab, s.stat + r0, lse + r0,
+                            loss + r0, ctx->d_status));
+  ++ctx->n_launch;
+  return ZOACT_OK;
+}
+
+int count_rows(Ctx* ctx, const CeArgs& c, const CeScratch& s) {
+  ZOACT_CUDA_TRY(launch_pdl(ctx, ce_count_kernel, dim3(1), dim3(1024), 0, c.targets, c.id64, c.T, c.vocab, s.count));
   ++ctx->n_launch;
   return ZOACT_OK;
 }
@@ -239,11 +337,7 @@ int run_forward(Ctx* ctx, const CeArgs& c, const CeScratch& s, int64_t tiles, fl
   a.part = s.part; a.zt = s.zt; a.targets = c.targets; a.id64 = c.id64; a.T = c.T;
   const int st = gemm<MODE_CE, T, T, T>(ctx, c.H, c.W, a);
   if (st) return st;
-  ZOACT_CUDA_TRY(launch_pdl(ctx, ce_join_kernel, dim3((unsigned)((c.rows + CE_THREADS - 1) / CE_THREADS)), dim3(CE_THREADS),
-                            0, (const float2*)s.part, tiles, c.rows, (const float*)s.zt, c.targets, c.id64, c.T, c.vocab,
-                            s.stat, lse, loss, ctx->d_status));
-  ++ctx->n_launch;
-  return ZOACT_OK;
+  return join(ctx, c, s, tiles, 0, c.rows, lse, loss);
 }
 
 template <typename T, typename TG>
@@ -296,33 +390,122 @@ int run_backward(Ctx* ctx, const CeArgs& c, const CeScratch& s, float scale, voi
   return ZOACT_OK;
 }
 
+// The losses' means and estimates.
+int finish(Ctx* ctx, const CeArgs& c, const float* loss) {
+  if (!c.mean && !c.est) return ZOACT_OK;
+  ZOACT_CUDA_TRY(launch_pdl(ctx, ce_finish_kernel, dim3((unsigned)c.nb), dim3(1024), 0, loss, c.T, c.nb, c.targets, c.id64,
+                            c.vocab, c.mean, c.est, (double)c.step, c.out, ctx->d_status));
+  ++ctx->n_launch;
+  return ZOACT_OK;
+}
+
 template <typename T>
-int run(Ctx* ctx, const CeArgs& c) {
-  const int64_t tiles = (c.vocab + TS - 1) / TS;
+__global__ void __launch_bounds__(CE_THREADS) ce_round_kernel(const float4* __restrict__ x, int64_t n4, T* __restrict__ y) {
+  pdl_wait();
+  pdl_trigger();
+  for (int64_t i = (int64_t)blockIdx.x * CE_THREADS + threadIdx.x; i < n4; i += (int64_t)gridDim.x * CE_THREADS) {
+    const float4 v = x[i];
+    T o[4] = {from_f32<T>(v.x), from_f32<T>(v.y), from_f32<T>(v.z), from_f32<T>(v.w)};
+    *reinterpret_cast<uint2*>(y + 4 * i) = *reinterpret_cast<const uint2*>(o);
+  }
+}
+
+// 16-bit operands: the products on the tensor cores.  Where the gradient is asked for, chunk by chunk of rows: logits, whose
+// exponentials are kept in 16 bits, the rows' sums, G in place, and its two products.
+template <typename T>
+int run_tc(Ctx* ctx, const CeArgs& c) {
+  using ce::Operand;
+  const int64_t tiles = (c.vocab + ce::V_TILE - 1) / ce::V_TILE, ldg = (c.vocab + 63) / 64 * 64;
+  const bool grad = c.dH || c.dW;
+  int64_t chunk = c.rows;
+  if (grad) {
+    chunk = (int64_t)(((size_t)1 << 31) / ((size_t)ldg * 2)) / 256 * 256;
+    if (chunk < 256) chunk = 256;
+    if (chunk > c.rows) chunk = c.rows;
+  }
   CeScratch s;
-  if (!ce_scratch(ctx, c.rows, tiles, s)) return ZOACT_ERR_NOMEM;
+  if (!ce_scratch(ctx, c.rows, chunk, tiles, s)) return ZOACT_ERR_NOMEM;
   float* lse = c.lse ? c.lse : s.lse;
   float* loss = c.loss ? c.loss : s.loss;
-  int st = ZOACT_OK;
-  if (c.rows > 0) st = run_forward<T>(ctx, c, s, tiles, lse, loss);
+  const Operand W = {c.W, c.dtype, c.vocab, c.d, c.d, 1, c.vocab * c.d};
+  int st;
+  if (!grad) {
+    const Operand H = {c.H, c.dtype, c.rows, c.d, c.d, 1, c.rows * c.d};
+    st = ce::launch_logits(ctx, W, H, s.part, s.part_ld, s.zt, c.targets, c.id64, c.T, ce::KEEP_NONE, nullptr, 0);
+    if (!st) st = join(ctx, c, s, tiles, 0, c.rows, lse, loss);
+    return st ? st : finish(ctx, c, loss);
+  }
+  void* G = scratch(ctx, SLOT_CE_G, (size_t)chunk * ldg * 2);
+  if (!G) return ZOACT_ERR_NOMEM;
+  // several chunks add to dW in fp32: a 16-bit dW is rounded from the whole sum
+  const bool parts = chunk < c.rows;
+  float* dWf = nullptr;
+  if (c.dW && parts && c.wgdtype != ZOACT_DT_FP32) {
+    dWf = (float*)scratch(ctx, SLOT_CE_DW, (size_t)c.vocab * c.d * 4);
+    if (!dWf) return ZOACT_ERR_NOMEM;
+  }
+  st = count_rows(ctx, c, s);
   if (st) return st;
-  ZOACT_CUDA_TRY(launch_pdl(ctx, ce_finish_kernel, dim3((unsigned)c.nb), dim3(1024), 0, (const float*)loss, c.T, c.nb,
-                            c.targets, c.id64, c.vocab, c.mean, s.count, c.est, (double)c.step, c.out, ctx->d_status));
-  ++ctx->n_launch;
-  if (c.dW && c.rows == 0 && !c.accumulate)
-    ZOACT_CUDA_TRY(cudaMemsetAsync(c.dW, 0, (size_t)c.vocab * c.d * dtype_size(c.wgdtype), ctx->stream));
-  if (c.rows == 0 || (!c.dH && !c.dW)) return ZOACT_OK;
-  return c.wgdtype == ZOACT_DT_FP32 ? run_backward<T, float>(ctx, c, s, c.grad_scale, c.dH, c.dW, c.accumulate)
-                                    : run_backward<T, T>(ctx, c, s, c.grad_scale, c.dH, c.dW, c.accumulate);
+  const float scale = c.dtype == ZOACT_DT_FP16 ? c.grad_scale / G_SCALE_FP16 : c.grad_scale;
+  for (int64_t r0 = 0; r0 < c.rows; r0 += chunk) {
+    const int64_t n = c.rows - r0 < chunk ? c.rows - r0 : chunk;
+    const Operand H = {(const T*)c.H + r0 * c.d, c.dtype, n, c.d, c.d, 1, n * c.d};
+    const Operand Gm = {G, c.dtype, n, c.vocab, ldg, 1, n * ldg};
+    const void* targets = (const char*)c.targets + r0 * (c.id64 ? 8 : 4);
+    st = ce::launch_logits(ctx, W, H, s.part, s.part_ld, s.zt + r0, targets, c.id64, c.T, ce::KEEP_LOG, G, ldg);
+    if (!st) st = join(ctx, c, s, tiles, r0, n, lse, loss);
+    if (st) return st;
+    const int64_t cols = (c.vocab + 8 * CE_THREADS - 1) / (8 * CE_THREADS);
+    for (int64_t y = 0; y < n; y += 65535) {
+      const int64_t ny = n - y < 65535 ? n - y : 65535;
+      ZOACT_CUDA_TRY(launch_pdl(ctx, ce_scale_kernel<T>, dim3((unsigned)cols, (unsigned)ny), dim3(CE_THREADS), 0,
+                                (void*)((__half*)G + y * ldg), ldg, (const float2*)s.part + y, s.part_ld,
+                                (const float2*)s.stat + r0 + y, (const float*)s.zt + r0 + y,
+                                (const void*)((const char*)targets + y * (c.id64 ? 8 : 4)), c.id64, c.vocab));
+      ++ctx->n_launch;
+    }
+    if (c.dH) st = ce::launch_by_h(ctx, W, Gm, s.count, scale, (T*)c.dH + r0 * c.d, c.dtype);
+    if (!st && c.dW)
+      st = ce::launch_by_w(ctx, Gm, H, s.count, scale, dWf ? (void*)dWf : c.dW, dWf ? ZOACT_DT_FP32 : c.wgdtype,
+                           r0 > 0 || c.accumulate);
+    if (st) return st;
+  }
+  if (dWf) {
+    const int64_t total = c.vocab * c.d / 4;        // d is a multiple of 8
+    const int64_t blocks = (total + CE_THREADS - 1) / CE_THREADS;
+    ZOACT_CUDA_TRY(launch_pdl(ctx, ce_round_kernel<T>, dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(CE_THREADS), 0,
+                              (const float4*)dWf, total, (T*)c.dW));
+    ++ctx->n_launch;
+  }
+  return finish(ctx, c, loss);
+}
+
+// fp32 operands.
+int run_fp32(Ctx* ctx, const CeArgs& c) {
+  const int64_t tiles = (c.vocab + TS - 1) / TS;
+  CeScratch s;
+  if (!ce_scratch(ctx, c.rows, c.rows, tiles, s)) return ZOACT_ERR_NOMEM;
+  float* lse = c.lse ? c.lse : s.lse;
+  float* loss = c.loss ? c.loss : s.loss;
+  int st = run_forward<float>(ctx, c, s, tiles, lse, loss);
+  if (!st) st = finish(ctx, c, loss);
+  if (st || (!c.dH && !c.dW)) return st;
+  st = count_rows(ctx, c, s);
+  return st ? st : run_backward<float, float>(ctx, c, s, c.grad_scale, c.dH, c.dW, c.accumulate);
 }
 
 }  // namespace
 
 int launch_ce(Ctx* ctx, const CeArgs& c) {
+  if (c.rows == 0) {                       // no token: losses of 0, no gradient
+    if (c.dW && !c.accumulate)
+      ZOACT_CUDA_TRY(cudaMemsetAsync(c.dW, 0, (size_t)c.vocab * c.d * dtype_size(c.wgdtype), ctx->stream));
+    return finish(ctx, c, nullptr);
+  }
   switch (c.dtype) {
-    case ZOACT_DT_FP32: return run<float>(ctx, c);
-    case ZOACT_DT_BF16: return run<__nv_bfloat16>(ctx, c);
-    default: return run<__half>(ctx, c);
+    case ZOACT_DT_FP32: return run_fp32(ctx, c);
+    case ZOACT_DT_BF16: return run_tc<__nv_bfloat16>(ctx, c);
+    default: return run_tc<__half>(ctx, c);
   }
 }
 

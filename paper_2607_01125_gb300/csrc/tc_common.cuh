@@ -353,6 +353,10 @@ __device__ __forceinline__ void st_shared_v4(uint32_t addr, uint4 v) {
 // elements, box = box_rows x 64 columns, 128-byte swizzle, zero fill outside).
 int encode_tmap_2d_16bit(CUtensorMap* map, const void* base, int dtype, int64_t rows, int64_t cols,
                          int box_rows);
+// Host: the same for `parts` slabs (part_stride elements apart) of [rows, cols] with rows ld elements apart (both strides
+// multiples of 8); a box lies in one slab and is zero-filled at the slab's own edges.
+int encode_tmap_3d_16bit(CUtensorMap* map, const void* base, int dtype, int64_t parts, int64_t rows, int64_t cols,
+                         int64_t ld, int64_t part_stride, int box_rows);
 // Host: unswizzled boxes of 8- or 16-bit integers (INT4 packed weights, fp16 scales read as raw bits).
 int encode_tmap_2d_int(CUtensorMap* map, const void* base, int elem_bytes, int64_t rows, int64_t cols, int box_cols,
                        int box_rows);
