@@ -14,17 +14,28 @@ struct Operand {
   int64_t part_stride;
 };
 
-constexpr int V_TILE = 128;          // vocabulary entries of one pair of column statistics
+constexpr int V_TILE = 128;          // vocabulary entries of one pair of a row's statistics
 enum { KEEP_NONE = 0, KEEP_LOG = 1, KEEP_Z = 2 };
 
-// z^T = W H^T: per column n the maximum and the sum of exp(z - maximum) of each V_TILE entries (part, rows part_ld apart)
-// and the target's logit (zt); keep: min(65535, round(4096 (maximum - z))) as 16-bit integers, or z in fp32, to G [H.rows, ldg].
+// What the logits leave for the gradient and what it becomes, in blocks of 64 vocabulary entries: [parts][blocks][rows][64]
+// of 16 bits (KEEP_Z: fp32, one part), zero from the vocabulary's end to its last block's.
+struct Blocks {
+  void* p;
+  int dtype;
+  int64_t rows, vocab;
+  int parts;
+  int64_t blocks() const { return (vocab + 63) / 64; }
+};
+
+// Logits z = H W^T: of each row the maximum and the sum of exp(z - maximum) over every V_TILE entries (part, [tile][part_ld])
+// and the target's logit (zt; row r has targets[r % T]); keep: min(65535, round(4096 (maximum - z))) as 16-bit integers, or z
+// in fp32, to G.
 int launch_logits(Ctx* ctx, const Operand& W, const Operand& H, float2* part, int64_t part_ld, float* zt, const void* targets,
-                  int id64, int64_t T, int keep, void* G, int64_t ldg);
-// out [G.rows, W.cols] of dtype = scale / max(count, 1) G W.
-int launch_by_h(Ctx* ctx, const Operand& W, const Operand& G, const double* count, float scale, void* out, int dtype);
-// out [G.cols, H.cols] of dtype = scale / max(count, 1) G^T H, added to out (fp32) with add.
-int launch_by_w(Ctx* ctx, const Operand& G, const Operand& H, const double* count, float scale, void* out, int dtype, int add);
+                  int id64, int64_t T, int keep, const Blocks& G);
+// out [G.rows, W.cols] of dtype = alpha G W.
+int launch_by_h(Ctx* ctx, const Operand& W, const Blocks& G, const float* alpha, void* out, int dtype);
+// out [G.vocab, H.cols] of dtype = alpha G^T H, added to out (fp32) with add.
+int launch_by_w(Ctx* ctx, const Blocks& G, const Operand& H, const float* alpha, void* out, int dtype, int add);
 
 }  // namespace ce
 }  // namespace zoact

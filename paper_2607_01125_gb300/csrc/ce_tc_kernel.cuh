@@ -1,14 +1,16 @@
-// The three products of the cross entropy over a vocabulary on CTA pairs (tcgen05 cta_group::2), with the vocabulary or
-// the width on the MMA's M side and the rows (tokens) on its N side:
+// The three products of the cross entropy over a vocabulary on CTA pairs (tcgen05 cta_group::2):
 //
-//   logits   z^T = W H^T        M = vocab, N = rows,  K = d       epilogue: maximum and sum of exponentials per column
-//   by H     dH^T = W^T G^T     M = d,     N = rows,  K = vocab   epilogue: transposed store, or K pieces of the last tiles
-//   by W     dW = G^T H         M = vocab, N = d,     K = rows    epilogue: row-major store
+//   logits   z   = H W^T     M = rows,  N = vocab, K = d      epilogue: maximum and sum of exponentials per row, a thread a row
+//            z^T = W H^T     M = vocab, N = rows,  K = d      the same over the accumulator's lanes, for few or ragged rows
+//   by H     dH^T = W^T G^T  M = d,     N = rows,  K = vocab  epilogue: transposed store, or K pieces of the last tiles
+//   by W     dW = G^T H      M = vocab, N = d,     K = rows   epilogue: row-major store
 //
-// Rows on the N side make the padding of a ragged or small batch cheap (tiles of 32 to 256 rows in steps of 32), and the
-// logits' statistics reduce over the accumulator's lanes: a butterfly of shuffles leaves lane l with column l of 32.
-// Operands are read where they lie: K-major tiles as rows of 64 elements, and the transposed ones (W and G by columns, H by
-// columns) as M- or N-major tiles, 64 x 64 boxes whose descriptors step by boxes along M or N and by 8 K rows along K.
+// Rows on the N side make the padding of a ragged or small batch cheap (tiles of 32 to 256 rows in steps of 32); there the
+// logits' statistics reduce by a butterfly of shuffles that leaves lane l with column l of 32, which a thread that owns a
+// row does without: a tile's epilogue took 13 000 cycles with shuffles, more than two groups of the main loop.
+// W and H are read as they lie: K-major tiles as rows of 64 elements, and the transposed ones (W and H by columns) as M- or
+// N-major tiles, 64 x 64 boxes whose descriptors step by boxes along M or N and by 8 K rows along K.  G, which only these
+// kernels see, lies in blocks of 64 vocabulary entries, [block][row][64]: every box of it is contiguous.
 // fp32 operands come as three bf16 parts each (24 bits); six products of parts run as six passes over K into one accumulator.
 //
 // The tensor core cuts its running fp32 sum off at every step of 16 products instead of rounding it: 4096 products of logits
@@ -23,22 +25,26 @@
 namespace zoact {
 namespace ce {
 
-constexpr int BM = 128, BN = 256, BK = 64, STAGES = 6;    // BM: rows of a CTA, a pair has 2 BM
+constexpr int BM = 128, BN = 256, BK = 64;                // BM: rows of a CTA, a pair has 2 BM
 constexpr int A_BYTES = BM * BK * 2;
-constexpr int STAGE_BYTES = 2 * A_BYTES;                  // A and up to BN / 2 rows of B
+// The ring: stages of A and bn / 2 rows of B, as many as fit (6 at bn = 256, 10 at 32).
+constexpr int MAX_STAGES = 10;
+__host__ __device__ constexpr int stage_bytes(int bn) { return A_BYTES + bn / 2 * BK * 2; }
 constexpr int BOX_BYTES = 64 * BK * 2;                    // an M- or N-major box
 constexpr int EPI_THREADS = 256, EPI_BASE = 128, THREADS = EPI_BASE + EPI_THREADS;
 // Registers: 384 threads are launched with 168 each; the first warpgroup (producer, issuer) gives back what the epilogue's
 // two take for a tile's sums: 56 + 2 x 224 = 3 x 168.
 constexpr int REGS_ISSUE = 56, REGS_EPI = 224;
-constexpr int TMEM_COLS = 512;
-constexpr int STG_BYTES = 16384;                          // a warpgroup's staging buffer (128 rows x 128 bytes)
-constexpr int AUX_BYTES = 2 * STG_BYTES;
-constexpr int SMEM_BYTES = 1024 + STAGES * STAGE_BYTES + AUX_BYTES + 256;
+constexpr int TMEM_COLS = 512, MAX_BUF = 4;
+constexpr int STG_BYTES = 16384;                          // a staging buffer (128 rows x 128 bytes)
+// Epilogue area beside the ring: a staging buffer for each warpgroup, or two where all that the epilogue does is to store.
+__host__ __device__ constexpr int aux_bytes(int epi) { return epi == 4 ? 4 * STG_BYTES : 2 * STG_BYTES; }
+__host__ __device__ constexpr int ring_bytes(int epi) { return 229376 - aux_bytes(epi); }
+constexpr int SMEM_BYTES = 1024 + 229376 + 256;
 static_assert(SMEM_BYTES <= 232448, "dynamic shared memory above the 227 KB a CTA may use");
 
 enum Epi {
-  EPI_LSE = 0,   // column statistics
+  EPI_LSE = 0,   // the rows' statistics
   EPI_LOG,       // and the tile's maximum - z as 16-bit fixed point
   EPI_Z,         // and z in fp32
   EPI_COL,       // D^T scaled
@@ -51,30 +57,32 @@ struct Maps {
 
 struct Params {
   int num_m, num_n, num_kb, products, bn;
+  int n_first;                      // tile order: along N first (the operand of M streams, that of N stays in L2), or along M
   int group_kb;                     // K-blocks of one accumulation on the tensor core (EPI_ROW: all of a tile's)
   int tail_first, tail_split;       // tiles from tail_first on run as tail_split pieces of K each
   int64_t M, N;
+  int g_blocks;                     // blocks of 64 vocabulary entries of one part of G
   int bf16;
   int* status;
-  // logits: row n's target is targets[n % T]
-  float2* part;                     // [ceil(M / 128)][part_ld]: maximum and sum of exp(z - maximum)
+  int nbuf, stages;                 // accumulators in TMEM, stages of the ring
+  // logits: row r's target is targets[r % T]
+  float2* part;                     // [ceil(vocab / 128)][part_ld]: maximum and sum of exp(z - maximum)
   int64_t part_ld;
   float* zt;
   const void* targets;
   int id64;
-  int64_t T;
-  void* G;                          // EPI_LOG, EPI_Z: [N, ldg]
-  int64_t ldg;
-  // products by H and W: out = scale / max(count, 1) times D
-  const double* count;
-  float scale;
+  uint32_t T;
+  int64_t rows, vocab;
+  void* G;                          // EPI_LOG, EPI_Z: [ceil(vocab / 64)][rows][64]
+  // products by H and W: out = alpha D
+  const float* alpha;
   void* out;                        // EPI_COL: [N, M]
   float* tail_part;                 // pieces of the tail's tiles: [piece][tile][bn][256]
   int add;                          // EPI_ROW: add to out (fp32)
 };
 
 struct Shared {
-  uint64_t full[STAGES], empty[STAGES], tmem_full[2], tmem_empty[2], drain;
+  uint64_t full[MAX_STAGES], empty[MAX_STAGES], tmem_full[MAX_BUF], tmem_empty[MAX_BUF], drain;
   uint32_t tmem_base;
   int abort_flag, epi_ok;
 };
@@ -99,8 +107,13 @@ __device__ __forceinline__ bool unit_at(const Params& p, int u, Unit& w) {
       w.slot = s;
     }
   }
-  w.m = t / p.num_n;
-  w.n = t - w.m * p.num_n;
+  if (p.n_first) {
+    w.m = t / p.num_n;
+    w.n = t - w.m * p.num_n;
+  } else {
+    w.n = t / p.num_m;
+    w.m = t - w.n * p.num_m;
+  }
   return true;
 }
 
@@ -151,25 +164,48 @@ __device__ __forceinline__ float columns_over_lanes(float* x, int lane) {
   return x[0];
 }
 
-// A warp's part of an accumulator tile: 32 lanes, and of the tile's 32-column chunks those of its warpgroup (half, half + 2, ...).
+// The accumulators in turn.
+struct Ring {
+  int buf = 0;
+  uint32_t phase = 0;
+  __device__ __forceinline__ void next(int nbuf) {
+    if (++buf == nbuf) { buf = 0; phase ^= 1u; }
+  }
+};
+
+// Wait until accumulator r.buf is complete (pairtc::epi_wait_full), and give it back to the issuer once every epilogue
+// thread of this CTA has read it.
+__device__ __forceinline__ bool acc_wait(const Params& p, Shared* ss, const Ring& r, int etid, volatile int* abort_flag) {
+  return pairtc::epi_wait_full(ss, r.buf, r.phase, abort_flag, p.status, etid);
+}
+__device__ __forceinline__ void acc_free(Shared* ss, const Ring& r, int etid) {
+  tc::tc_fence_before();
+  tc::named_bar_sync(3, EPI_THREADS);
+  if (etid == 0) pairtc::tc2::arrive_cluster(pairtc::tc2::map_to(tc::smem_u32(&ss->tmem_empty[r.buf]), 0));
+}
+
+// A warp's part of an accumulator tile: 32 lanes, and its warpgroup's 32-column chunks: the half's own 128 columns
+// (ADJACENT), or chunks half, half + 2, ...
 constexpr int CHUNKS = BN / 64;
 struct Part {
   float x[CHUNKS][32];
 };
+template <bool ADJACENT>
+__device__ __forceinline__ int chunk_of(int half, int i) { return ADJACENT ? half * CHUNKS + i : half + 2 * i; }
 
-// The sums over a unit's K groups, each read from its TMEM buffer as soon as it is complete.  False: the wait gave up.
+// The sums over a unit's K groups, each read from its accumulator as soon as it is complete.  False: the wait gave up.
+template <bool ADJACENT>
 __device__ __forceinline__ bool sum_groups(const Params& p, Shared* ss, const Unit& w, int etid, int half, uint32_t t_quad,
-                                           uint32_t empty0, uint32_t empty1, volatile int* abort_flag, int& local, Part& a) {
+                                           volatile int* abort_flag, Ring& r, Part& a) {
   const int nch = p.bn / 32;
 #pragma unroll 1
-  for (int kb = w.kb0; kb < w.kb1; kb += p.group_kb, ++local) {
-    const int buf = local & 1;
-    if (!pairtc::epi_wait_full(ss, buf, (uint32_t)(local >> 1) & 1u, abort_flag, p.status, etid)) return false;
-    const uint32_t t = t_quad + (uint32_t)(buf * BN);
+  for (int kb = w.kb0; kb < w.kb1; kb += p.group_kb) {
+    if (!acc_wait(p, ss, r, etid, abort_flag)) return false;
+    const uint32_t t = t_quad + (uint32_t)(r.buf * p.bn);
     const bool first = kb == w.kb0;
 #pragma unroll
     for (int i = 0; i < CHUNKS; ++i) {
-      const int c = half + 2 * i;
+      const int c = chunk_of<ADJACENT>(half, i);
       if (c < nch) {
         float y[32];
         tc::tmem_ld32(t + (uint32_t)(c * 32), y);
@@ -177,38 +213,115 @@ __device__ __forceinline__ bool sum_groups(const Params& p, Shared* ss, const Un
         for (int j = 0; j < 32; ++j) a.x[i][j] = first ? y[j] : a.x[i][j] + y[j];
       }
     }
-    tc::tc_fence_before();
-    tc::named_bar_sync(3, EPI_THREADS);            // every epilogue thread of this CTA has read the buffer
-    if (etid == 0) pairtc::tc2::arrive_cluster(buf ? empty1 : empty0);
+    acc_free(ss, r, etid);
+    r.next(p.nbuf);
   }
   return true;
 }
 
-// Exchange area of the logits' epilogue, per warpgroup: [quad][column of its chunks], and each warp's copy of the columns'
+// Fixed point of the tile's maximum - z: 1 / LOG_STEPS, up to 16 (below exp(-16) of the tile's largest: 65535, no value);
+// rounded in the low bits of a sum with 2^23.  x = z - maximum.
+constexpr float LOG_STEPS = 4096.f;
+__device__ __forceinline__ uint32_t log_fixed(float x) {
+  return __float_as_uint(fminf(x * -LOG_STEPS, 65535.f) + 8388608.f) & 0xffffu;
+}
+__device__ __forceinline__ float exp_of(float x) { return pairtc::exp2_sfu(x * 1.44269504f); }
+
+// One tile of logits, M = rows: a thread has a row and the 128 vocabulary entries of its warpgroup from v0.
+template <int EPI>
+__device__ __forceinline__ void epi_rows(const Params& p, const Maps& tm, uint8_t* stg, Part& a, int etid, int half, int row_in_cta,
+                                         int64_t m0, int64_t v0, bool& pending) {
+  const int64_t row = m0 + row_in_cta;
+  const bool ok = row < p.rows;
+  const int64_t left = p.vocab - v0;
+  const int nv = left >= 128 ? 128 : left > 0 ? (int)left : 0;          // uniform
+  if (nv < 128) {
+#pragma unroll
+    for (int i = 0; i < CHUNKS; ++i)
+#pragma unroll
+      for (int j = 0; j < 32; ++j)
+        if (i * 32 + j >= nv) a.x[i][j] = -INFINITY;
+  }
+  const int64_t t = ok ? load_id(p.targets, p.id64, (uint32_t)row % p.T) - v0 : -1;
+  if (t >= 0 && t < nv) {                                               // seldom
+    float z = 0.f;
+#pragma unroll
+    for (int i = 0; i < CHUNKS; ++i)
+#pragma unroll
+      for (int j = 0; j < 32; ++j) z = i * 32 + j == (int)t ? a.x[i][j] : z;
+    p.zt[row] = z;
+  }
+  if (EPI == EPI_Z && ok) {
+#pragma unroll
+    for (int i = 0; i < CHUNKS; ++i) {
+      if (i * 32 >= nv) continue;
+      float4* g = reinterpret_cast<float4*>(reinterpret_cast<float*>(p.G) + (((v0 / 64 + i / 2) * p.rows + row) * 64 + (i & 1) * 32));
+#pragma unroll
+      for (int j = 0; j < 8; ++j) g[j] = make_float4(a.x[i][4 * j], a.x[i][4 * j + 1], a.x[i][4 * j + 2], a.x[i][4 * j + 3]);
+    }
+  }
+  float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+  for (int i = 0; i < CHUNKS; ++i)
+#pragma unroll
+    for (int j = 0; j < 32; ++j) mx[j & 3] = fmaxf(mx[j & 3], a.x[i][j]);
+  const float m = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+  float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < CHUNKS; ++i) {
+#pragma unroll
+    for (int j = 0; j < 32; ++j) a.x[i][j] -= m;
+    if (EPI == EPI_LOG && (i & 1) == 0) {           // a box of 64 entries: wait until the last one has been read
+      if ((etid & 127) == 0 && pending) tc::bulk_wait_read0();
+      tc::named_bar_sync(4 + half, 128);
+    }
+    if (EPI == EPI_LOG) {
+      const uint32_t sbuf = tc::smem_u32(stg + half * STG_BYTES);
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        uint32_t q[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) q[k] = log_fixed(a.x[i][8 * g + 2 * k]) | log_fixed(a.x[i][8 * g + 2 * k + 1]) << 16;
+        tc::st_shared_v4(sbuf + pairtc::sw128_off(row_in_cta, (i & 1) * 4 + g), make_uint4(q[0], q[1], q[2], q[3]));
+      }
+      if (i & 1) {
+        tc::fence_proxy_async_smem();
+        tc::named_bar_sync(4 + half, 128);
+        if ((etid & 127) == 0 && (i / 2) * 64 < nv && m0 < p.rows) {
+          tc::tma_store_3d(&tm.out, 0, (int32_t)m0, (int32_t)(v0 / 64 + i / 2), sbuf);
+          tc::bulk_commit();
+          pending = true;
+        }
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 32; ++j) s[j & 3] += exp_of(a.x[i][j]);
+  }
+  if (ok && nv > 0) p.part[v0 / BM * p.part_ld + row] = make_float2(m, (s[0] + s[1]) + (s[2] + s[3]));
+}
+
+// Exchange area of the epilogue below, per warpgroup: [quad][column of its chunks], and each warp's copy of the columns'
 // maxima for broadcast reads.
 struct Exchange {
   float mx[2][4][128], sum[2][4][128], all[8][128];
 };
-static_assert(sizeof(Exchange) <= AUX_BYTES, "exchange area");
+static_assert(sizeof(Exchange) <= aux_bytes(0), "exchange area");
 
-// Fixed point of the tile's maximum - z: 1 / LOG_STEPS, up to 16 (below exp(-16) of the tile's largest: 65535, no value).
-constexpr float LOG_STEPS = 4096.f;
-
-// One tile of logits: this CTA's 128 vocabulary entries from m0 and the tile's rows from n0; warp `quad` takes 32 entries.
+// One tile of logits, M = vocab: this CTA's 128 entries from m0 and the tile's rows from n0; warp `quad` takes 32 entries.
 template <int EPI>
-__device__ __forceinline__ void epi_logits(const Params& p, Exchange* ex, Part& a, int half, int quad, int lane, int64_t m0,
-                                           int64_t n0) {
+__device__ __forceinline__ void epi_lanes(const Params& p, Exchange* ex, Part& a, int half, int quad, int lane, int64_t m0,
+                                          int64_t n0) {
   const int nch = p.bn / 32;
   const int64_t v = m0 + quad * 32 + lane, vb = m0 + quad * 32;
-  const bool vok = v < p.M;
+  const bool vok = v < p.vocab;
 #pragma unroll
   for (int i = 0; i < CHUNKS; ++i) {
-    const int c = half + 2 * i;
+    const int c = chunk_of<false>(half, i);
     if (c >= nch) continue;
     // the target's logit, where one of these rows has its target among this warp's entries (seldom)
     const int64_t n = n0 + c * 32 + lane;
-    const int64_t t = n < p.N ? load_id(p.targets, p.id64, n % p.T) : -1;
-    unsigned hits = __ballot_sync(0xffffffffu, t >= vb && t < vb + 32 && t < p.M);
+    const int64_t t = n < p.rows ? load_id(p.targets, p.id64, (uint32_t)n % p.T) : -1;
+    unsigned hits = __ballot_sync(0xffffffffu, t >= vb && t < vb + 32 && t < p.vocab);
     while (hits) {
       const int l = __ffs(hits) - 1;
       hits &= hits - 1;
@@ -228,21 +341,22 @@ __device__ __forceinline__ void epi_logits(const Params& p, Exchange* ex, Part& 
 #pragma unroll
   for (int i = 0; i < CHUNKS; ++i) {
     const int k = i * 32 + lane;
-    if (half + 2 * i < nch)
+    if (chunk_of<false>(half, i) < nch)
       all[k] = fmaxf(fmaxf(ex->mx[half][0][k], ex->mx[half][1][k]), fmaxf(ex->mx[half][2][k], ex->mx[half][3][k]));
   }
   __syncwarp();
 #pragma unroll
   for (int i = 0; i < CHUNKS; ++i) {
-    const int c = half + 2 * i;
+    const int c = chunk_of<false>(half, i);
     if (c >= nch) continue;
     const int64_t n = n0 + c * 32;
-    const int nv = (int)(p.N - n < 32 ? p.N - n : 32);
+    const int nv = (int)(p.rows - n < 32 ? p.rows - n : 32);
+    const int64_t at = ((v >> 6) * p.rows + n) * 64 + (v & 63);       // a row is 64 elements from the next
     if (EPI == EPI_Z && vok) {
-      float* g = reinterpret_cast<float*>(p.G) + n * p.ldg + v;
+      float* g = reinterpret_cast<float*>(p.G) + at;
 #pragma unroll
       for (int j = 0; j < 32; ++j)
-        if (j < nv) g[j * p.ldg] = a.x[i][j];
+        if (j < nv) g[j * 64] = a.x[i][j];
     }
 #pragma unroll
     for (int j = 0; j < 32; j += 4) {
@@ -253,21 +367,20 @@ __device__ __forceinline__ void epi_logits(const Params& p, Exchange* ex, Part& 
       a.x[i][j + 3] -= m.w;
     }
     if (EPI == EPI_LOG && vok) {
-      uint16_t* g = reinterpret_cast<uint16_t*>(p.G) + n * p.ldg + v;
+      uint16_t* g = reinterpret_cast<uint16_t*>(p.G) + at;
 #pragma unroll
-      for (int j = 0; j < 32; ++j)         // rounded in the low bits of a sum with 2^23
-        if (j < nv)
-          g[j * p.ldg] = (uint16_t)__float_as_uint(fminf(a.x[i][j] * -LOG_STEPS, 65535.f) + 8388608.f);
+      for (int j = 0; j < 32; ++j)
+        if (j < nv) g[j * 64] = (uint16_t)log_fixed(a.x[i][j]);
     }
 #pragma unroll
-    for (int j = 0; j < 32; ++j) a.x[i][j] = vok ? __expf(a.x[i][j]) : 0.f;
+    for (int j = 0; j < 32; ++j) a.x[i][j] = vok ? exp_of(a.x[i][j]) : 0.f;
     ex->sum[half][quad][i * 32 + lane] = columns_over_lanes<false>(a.x[i], lane);
   }
   tc::named_bar_sync(4 + half, 128);
   // chunk i's statistics by warp i of the warpgroup
-  const int c = half + 2 * quad, k = quad * 32 + lane;
+  const int c = chunk_of<false>(half, quad), k = quad * 32 + lane;
   const int64_t n = n0 + c * 32 + lane;
-  if (c < nch && n < p.N && m0 < p.M)
+  if (c < nch && n < p.rows && m0 < p.vocab)
     p.part[m0 / BM * p.part_ld + n] =
         make_float2(all[k], (ex->sum[half][0][k] + ex->sum[half][1][k]) + (ex->sum[half][2][k] + ex->sum[half][3][k]));
 }
@@ -280,7 +393,7 @@ __device__ __forceinline__ void epi_col(const Params& p, const Part& a, int half
   const bool mok = m < p.M;
 #pragma unroll
   for (int i = 0; i < CHUNKS; ++i) {
-    const int c = half + 2 * i;
+    const int c = chunk_of<false>(half, i);
     if (c >= p.bn / 32) continue;
     const int64_t n = n0 + c * 32;
     if (slot >= 0) {
@@ -300,57 +413,64 @@ __device__ __forceinline__ void epi_col(const Params& p, const Part& a, int half
   }
 }
 
-// D scaled, through the warpgroup's staging buffer in 128-byte columns; one thread stores each box.
+// D scaled, through the warpgroup's two staging buffers in boxes of 128 bytes; one thread stores each pair of boxes (a tile
+// of 16-bit outputs is one pair: its only wait is for the tile before it).
 template <typename TO>
 __device__ __forceinline__ void epi_row(const Params& p, const Maps& tm, uint8_t* stg, int etid, int half, int row_in_cta,
                                         int64_t m0, int64_t n0, float f, uint32_t t_row, bool& pending) {
   constexpr int CC = 128 / (int)sizeof(TO);
   const int wcols = p.bn / 2, cb = half * wcols;
   const bool issuer = (etid & 127) == 0;
-  const uint32_t sbuf = tc::smem_u32(stg + half * STG_BYTES);
-  for (int c = 0; c < wcols; c += CC) {
+  const uint32_t sbuf = tc::smem_u32(stg + half * 2 * STG_BYTES);
+  for (int c = 0; c < wcols; c += 2 * CC) {
     const int64_t n = n0 + cb + c;
     if (n >= p.N || m0 >= p.M) break;               // uniform over the warpgroup
-    if (issuer && pending) tc::bulk_wait_read0();   // the buffer's previous store has read it
+    if (issuer && pending) tc::bulk_wait_read0();   // the buffers' previous stores have read them
     tc::named_bar_sync(4 + half, 128);
 #pragma unroll 1
-    for (int q = 0; q < CC; q += 32) {
+    for (int q = 0; q < 2 * CC && c + q < wcols; q += 32) {
       float x[32];
       tc::tmem_ld32(t_row + (uint32_t)(cb + c + q), x);
 #pragma unroll
       for (int j = 0; j < 32; ++j) x[j] *= f;
-      pairtc::stage_granules<TO, 32>(sbuf, row_in_cta, q, x, true);
+      pairtc::stage_granules<TO, 32>(sbuf + (uint32_t)(q / CC * STG_BYTES), row_in_cta, q % CC, x, true);
     }
     tc::fence_proxy_async_smem();
     tc::named_bar_sync(4 + half, 128);
     if (issuer) {
-      if (sizeof(TO) == 4 && p.add) tma_add_2d(&tm.out, (int32_t)n, (int32_t)m0, sbuf);
-      else tc::tma_store_2d(&tm.out, (int32_t)n, (int32_t)m0, sbuf);
+      for (int b = 0; b < 2 && c + b * CC < wcols && n + b * CC < p.N; ++b) {
+        if (sizeof(TO) == 4 && p.add) tma_add_2d(&tm.out, (int32_t)(n + b * CC), (int32_t)m0, sbuf + b * STG_BYTES);
+        else tc::tma_store_2d(&tm.out, (int32_t)(n + b * CC), (int32_t)m0, sbuf + b * STG_BYTES);
+      }
       tc::bulk_commit();
       pending = true;
     }
   }
 }
 
-template <int EPI, bool A_MN, bool B_MN, typename TO>
+// ROWS_M: the logits' form with rows on the M side.
+template <int EPI, bool ROWS_M, typename TO>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
 ce_tc_kernel(const __grid_constant__ Maps tm, const Params p) {
   namespace tc2 = pairtc::tc2;
+  // by H: A = W by columns, B = G by rows; by W: A = G by columns, B = H by columns
+  constexpr bool A_MN = EPI == EPI_COL || EPI == EPI_ROW, B_MN = EPI == EPI_ROW;
+  constexpr bool A_BLOCKS = EPI == EPI_ROW, B_BLOCKS = EPI == EPI_COL;      // G
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  uint8_t* aux = smem + STAGES * STAGE_BYTES;
-  Shared* ss = reinterpret_cast<Shared*>(aux + AUX_BYTES);
+  uint8_t* aux = smem + ring_bytes(EPI);
+  Shared* ss = reinterpret_cast<Shared*>(aux + aux_bytes(EPI));
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = tc2::cluster_rank();
   const bool leader = rank == 0;
   volatile int* abort_flag = &ss->abort_flag;
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < STAGES; ++s) {
+    for (int s = 0; s < MAX_STAGES; ++s) {
       tc::mbar_init(tc::smem_u32(&ss->full[s]), 2);    // one producer arrival from each CTA (the leader's copy is used)
       tc::mbar_init(tc::smem_u32(&ss->empty[s]), 1);
     }
-    for (int b = 0; b < 2; ++b) {
+    for (int b = 0; b < MAX_BUF; ++b) {
       tc::mbar_init(tc::smem_u32(&ss->tmem_full[b]), 1);
       tc::mbar_init(tc::smem_u32(&ss->tmem_empty[b]), 2);
     }
@@ -359,7 +479,7 @@ ce_tc_kernel(const __grid_constant__ Maps tm, const Params p) {
     tc::fence_mbar_init();
     tc::prefetch_tmap(&tm.a);
     tc::prefetch_tmap(&tm.b);
-    if (EPI == EPI_ROW) tc::prefetch_tmap(&tm.out);
+    if (EPI == EPI_ROW || (EPI == EPI_LOG && ROWS_M)) tc::prefetch_tmap(&tm.out);
   }
   if (warp == 1) {
     tc2::tmem_alloc2(tc::smem_u32(&ss->tmem_base), TMEM_COLS);
@@ -374,84 +494,85 @@ ce_tc_kernel(const __grid_constant__ Maps tm, const Params p) {
   pdl_trigger();
 
   const int cluster_id = blockIdx.x >> 1, n_clusters = gridDim.x >> 1;
-  const int bh = p.bn / 2;
+  const int bh = p.bn / 2, sbytes = stage_bytes(p.bn);
   Unit w;
 
   if (warp < EPI_BASE / 32) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_ISSUE));
-    if (warp == 0) {
+    if (warp == 0 && lane == 0) {
       // ---------------- TMA producer (both CTAs) ----------------
-      if (lane == 0) {
-        const uint32_t stage_tx = (uint32_t)(A_BYTES + bh * BK * 2);
-        int stage = 0;
-        uint32_t phase = 0;
-        bool ok = true;
-        for (int u = cluster_id; ok && unit_at(p, u, w); u += n_clusters) {
-          const int m0 = w.m * 2 * BM + (int)rank * BM, n0 = w.n * p.bn + (int)rank * bh;
-          for (int kb = w.kb0; kb < w.kb1; ++kb) {
-            if (!tc::mbar_wait(tc::smem_u32(&ss->empty[stage]), phase ^ 1u, abort_flag, p.status)) { ok = false; break; }
-            const uint32_t full_leader = tc2::map_to(tc::smem_u32(&ss->full[stage]), 0);
-            tc2::arrive_expect_tx_cluster(full_leader, stage_tx);
-            const uint32_t sa = tc::smem_u32(smem + stage * STAGE_BYTES), sb = sa + A_BYTES;
-            // products of parts (a, b): (0,0) (0,1) (1,0) (0,2) (1,1) (2,0)
-            const int pr = kb / p.num_kb, k = (kb - pr * p.num_kb) * BK;
-            const int pa = (0x210100 >> (4 * pr)) & 15, pb = (0x012010 >> (4 * pr)) & 15;
-            if (A_MN) {
-              tma_load_3d_pair(sa, &tm.a, m0, k, pa, full_leader);
-              tma_load_3d_pair(sa + BOX_BYTES, &tm.a, m0 + 64, k, pa, full_leader);
-            } else {
-              tma_load_3d_pair(sa, &tm.a, k, m0, pa, full_leader);
-            }
-            if (B_MN) {
-              for (int j = 0; j < bh / 64; ++j)
-                tma_load_3d_pair(sb + j * BOX_BYTES, &tm.b, n0 + 64 * j, k, pb, full_leader);
-            } else {
-              tma_load_3d_pair(sb, &tm.b, k, n0, pb, full_leader);
-            }
-            if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+      const uint32_t stage_tx = (uint32_t)(A_BYTES + bh * BK * 2);
+      int stage = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      for (int u = cluster_id; ok && unit_at(p, u, w); u += n_clusters) {
+        const int m0 = w.m * 2 * BM + (int)rank * BM, n0 = w.n * p.bn + (int)rank * bh;
+        for (int kb = w.kb0; kb < w.kb1; ++kb) {
+          if (!tc::mbar_wait(tc::smem_u32(&ss->empty[stage]), phase ^ 1u, abort_flag, p.status)) { ok = false; break; }
+          const uint32_t full_leader = tc2::map_to(tc::smem_u32(&ss->full[stage]), 0);
+          tc2::arrive_expect_tx_cluster(full_leader, stage_tx);
+          const uint32_t sa = tc::smem_u32(smem + stage * sbytes), sb = sa + A_BYTES;
+          // products of parts (a, b): (0,0) (0,1) (1,0) (0,2) (1,1) (2,0)
+          const int pr = kb / p.num_kb, kblk = kb - pr * p.num_kb, k = kblk * BK;
+          const int pa = (0x210100 >> (4 * pr)) & 15, pb = (0x012010 >> (4 * pr)) & 15;
+          if (A_BLOCKS) {
+            tma_load_3d_pair(sa, &tm.a, 0, k, m0 / 64 + pa * p.g_blocks, full_leader);
+            tma_load_3d_pair(sa + BOX_BYTES, &tm.a, 0, k, m0 / 64 + 1 + pa * p.g_blocks, full_leader);
+          } else if (A_MN) {
+            tma_load_3d_pair(sa, &tm.a, m0, k, pa, full_leader);
+            tma_load_3d_pair(sa + BOX_BYTES, &tm.a, m0 + 64, k, pa, full_leader);
+          } else {
+            tma_load_3d_pair(sa, &tm.a, k, m0, pa, full_leader);
           }
-        }
-        if (!ok) {
-          // our copies complete on the leader's barriers; give them time to land before the CTA winds down
-          const uint64_t t0 = tc::global_timer_ns();
-          while (tc::global_timer_ns() - t0 < 2000000ull) {
+          if (B_BLOCKS) {
+            tma_load_3d_pair(sb, &tm.b, 0, n0, kblk + pb * p.g_blocks, full_leader);
+          } else if (B_MN) {
+            for (int j = 0; j < bh / 64; ++j)
+              tma_load_3d_pair(sb + j * BOX_BYTES, &tm.b, n0 + 64 * j, k, pb, full_leader);
+          } else {
+            tma_load_3d_pair(sb, &tm.b, k, n0, pb, full_leader);
           }
+          if (++stage == p.stages) { stage = 0; phase ^= 1u; }
         }
       }
-    } else if (warp == 1) {
+      if (!ok) {
+        // our copies complete on the leader's barriers; give them time to land before the CTA winds down
+        const uint64_t t0 = tc::global_timer_ns();
+        while (tc::global_timer_ns() - t0 < 2000000ull) {
+        }
+      }
+    } else if (warp == 1 && lane == 0 && leader) {
       // ---------------- MMA issuer (leader CTA) ----------------
-      if (lane == 0 && leader) {
-        const uint32_t idesc = tc::idesc_f16(2 * BM, p.bn, p.bf16) | (A_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u);
-        int stage = 0, local = 0;
-        uint32_t phase = 0;
-        bool ok = true, issued_any = false;
-        for (int u = cluster_id; ok && unit_at(p, u, w); u += n_clusters) {
-          for (int g0 = w.kb0; ok && g0 < w.kb1; g0 += p.group_kb, ++local) {
-            const int buf = local & 1, g1 = min(g0 + p.group_kb, w.kb1);
-            if (!tc::mbar_wait(tc::smem_u32(&ss->tmem_empty[buf]), ((uint32_t)(local >> 1) & 1u) ^ 1u, abort_flag, p.status)) {
-              ok = false;
-              break;
-            }
+      const uint32_t idesc = tc::idesc_f16(2 * BM, p.bn, p.bf16) | (A_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u);
+      int stage = 0;
+      uint32_t phase = 0;
+      bool ok = true, issued_any = false;
+      Ring r;
+      for (int u = cluster_id; ok && unit_at(p, u, w); u += n_clusters) {
+        for (int g0 = w.kb0; ok && g0 < w.kb1; g0 += p.group_kb) {
+          const int g1 = min(g0 + p.group_kb, w.kb1);
+          if (!tc::mbar_wait(tc::smem_u32(&ss->tmem_empty[r.buf]), r.phase ^ 1u, abort_flag, p.status)) { ok = false; break; }
+          tc::tc_fence_after();
+          const uint32_t d_tmem = tmem_base + (uint32_t)(r.buf * p.bn);
+          for (int kb = g0; kb < g1; ++kb) {
+            if (!tc::mbar_wait(tc::smem_u32(&ss->full[stage]), phase, abort_flag, p.status)) { ok = false; break; }
             tc::tc_fence_after();
-            const uint32_t d_tmem = tmem_base + (uint32_t)(buf * BN);
-            for (int kb = g0; kb < g1; ++kb) {
-              if (!tc::mbar_wait(tc::smem_u32(&ss->full[stage]), phase, abort_flag, p.status)) { ok = false; break; }
-              tc::tc_fence_after();
-              const uint32_t sa = tc::smem_u32(smem + stage * STAGE_BYTES), sb = sa + A_BYTES;
+            const uint32_t sa = tc::smem_u32(smem + stage * sbytes), sb = sa + A_BYTES;
 #pragma unroll
-              for (int k = 0; k < BK / 16; ++k)
-                tc2::mma2_f16(d_tmem, sdesc<A_MN>(sa, k), sdesc<B_MN>(sb, k), idesc, (kb != g0 || k != 0) ? 1u : 0u);
-              tc2::commit2_both(tc::smem_u32(&ss->empty[stage]));
-              issued_any = true;
-              if (++stage == STAGES) { stage = 0; phase ^= 1u; }
-            }
-            if (ok) tc2::commit2_both(tc::smem_u32(&ss->tmem_full[buf]));
+            for (int k = 0; k < BK / 16; ++k)
+              tc2::mma2_f16(d_tmem, sdesc<A_MN>(sa, k), sdesc<B_MN>(sb, k), idesc, (kb != g0 || k != 0) ? 1u : 0u);
+            tc2::commit2_both(tc::smem_u32(&ss->empty[stage]));
+            issued_any = true;
+            if (++stage == p.stages) { stage = 0; phase ^= 1u; }
           }
+          if (!ok) break;
+          tc2::commit2_both(tc::smem_u32(&ss->tmem_full[r.buf]));
+          r.next(p.nbuf);
         }
-        if (issued_any) {
-          tc2::commit2_own(tc::smem_u32(&ss->drain));
-          tc::mbar_wait_drain(tc::smem_u32(&ss->drain), 0, 100000000ull);
-        }
+      }
+      if (issued_any) {
+        tc2::commit2_own(tc::smem_u32(&ss->drain));
+        tc::mbar_wait_drain(tc::smem_u32(&ss->drain), 0, 100000000ull);
       }
     }
   } else {
@@ -459,30 +580,27 @@ ce_tc_kernel(const __grid_constant__ Maps tm, const Params p) {
     // ---------------- epilogue (warps 4..11, both CTAs) ----------------
     const int etid = threadIdx.x - EPI_BASE, half = etid >> 7, quad = warp & 3;
     const int row_in_cta = quad * 32 + lane;
-    const uint32_t empty0 = tc2::map_to(tc::smem_u32(&ss->tmem_empty[0]), 0);
-    const uint32_t empty1 = tc2::map_to(tc::smem_u32(&ss->tmem_empty[1]), 0);
     float f = 0.f;
-    if (EPI == EPI_COL || EPI == EPI_ROW) f = (float)((double)p.scale / fmax(__ldcg(p.count), 1.0));
-    int local = 0;
+    if (EPI == EPI_COL || EPI == EPI_ROW) f = __ldcg(p.alpha);
+    Ring r;
     bool pending = false;
     const uint32_t t_quad = tmem_base + ((uint32_t)(quad * 32) << 16);
     for (int u = cluster_id; unit_at(p, u, w); u += n_clusters) {
       const int64_t m0 = (int64_t)w.m * 2 * BM + (int64_t)rank * BM, n0 = (int64_t)w.n * p.bn;
       if constexpr (EPI == EPI_ROW) {
-        const int buf = local & 1;
-        if (!pairtc::epi_wait_full(ss, buf, (uint32_t)(local >> 1) & 1u, abort_flag, p.status, etid)) break;
-        epi_row<TO>(p, tm, aux, etid, half, row_in_cta, m0, n0, f, t_quad + (uint32_t)(buf * BN), pending);
-        tc::tc_fence_before();
-        tc::named_bar_sync(3, EPI_THREADS);        // every epilogue thread of this CTA has read the tile
-        if (etid == 0) tc2::arrive_cluster(buf ? empty1 : empty0);
-        ++local;
+        if (!acc_wait(p, ss, r, etid, abort_flag)) break;
+        epi_row<TO>(p, tm, aux, etid, half, row_in_cta, m0, n0, f, t_quad + (uint32_t)(r.buf * p.bn), pending);
+        acc_free(ss, r, etid);
+        r.next(p.nbuf);
       } else {
         Part a;
-        if (!sum_groups(p, ss, w, etid, half, t_quad, empty0, empty1, abort_flag, local, a)) break;
+        if (!sum_groups<ROWS_M>(p, ss, w, etid, half, t_quad, abort_flag, r, a)) break;
         if constexpr (EPI == EPI_COL)
           epi_col<TO>(p, a, half, row_in_cta, rank, m0, n0, w.slot, f);
+        else if constexpr (ROWS_M)
+          epi_rows<EPI>(p, tm, aux, a, etid, half, row_in_cta, m0, n0 + half * 128, pending);
         else
-          epi_logits<EPI>(p, reinterpret_cast<Exchange*>(aux), a, half, quad, lane, m0, n0);
+          epi_lanes<EPI>(p, reinterpret_cast<Exchange*>(aux), a, half, quad, lane, m0, n0);
       }
     }
     if (pending) tc::bulk_wait0();

@@ -3,6 +3,8 @@
 // and the gradient of s L by H and W.  With G = exp(z - lse) - onehot(target) on counted rows (0 on the others),
 //     dH = s/N G W,   dW = s/N G^T H.
 // A row whose target is negative has loss 0 and is not counted.
+#include <type_traits>
+
 #include "ce_tc.h"
 
 namespace zoact {
@@ -28,8 +30,7 @@ struct GemmArgs {
   float* G;
   int64_t ldg;
   // MODE_OUT
-  const double* count;              // counted rows (device)
-  float scale;
+  const float* alpha;               // device
   const float* add;                 // [M, N] or nullptr
   void* out;                        // [M, N]
 };
@@ -110,7 +111,7 @@ ce_gemm_kernel(const TA* __restrict__ A, const TB* __restrict__ B, const GemmArg
       }
     } else {
       if (!mok) continue;
-      const float f = (float)((double)a.scale / fmax(*a.count, 1.0));
+      const float f = *a.alpha;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int64_t n = n0 + tx * 4 + j;
@@ -122,54 +123,76 @@ ce_gemm_kernel(const TA* __restrict__ A, const TB* __restrict__ B, const GemmArg
   }
 }
 
-// The tiles' maxima m_i and sums s_i of a row joined: m, log s with s = sum s_i exp(m_i - m) in fp64 (a row that the
-// model predicts well has s = 1 + many terms that fp32 would drop one by one), lse = m + log s and loss = lse - z_t.
+// The tiles' maxima m_i and sums s_i of a row joined: m, log s with s = sum s_i exp(m_i - m) (a row that the model predicts
+// well has s = 1 + many terms that fp32 alone would drop one by one), lse = m + log s and loss = lse - z_t.
 // The gradient takes z - lse as (z - m) - log s, exact where z = m.
-// 32 rows a block, 32 groups of tiles each, joined in group order.
+// All of it in fp32 with what the additions round off beside the sum (fp64 FMAs run at 1/64 of the rate: with them this kernel
+// took 24 us for 2048 rows of 1002 tiles).  A block has ROWS rows; 1024 / ROWS groups of threads take their tiles in turn,
+// and a warp a row joins the groups.
+struct MaxSum {
+  float m, hi, lo;                         // sum of exp(z - m): hi + lo
+};
+__device__ __forceinline__ MaxSum join_sums(const MaxSum& a, const MaxSum& b) {
+  MaxSum c;
+  c.m = fmaxf(a.m, b.m);
+  const float fa = a.m == c.m ? 1.f : expf(a.m - c.m), fb = b.m == c.m ? 1.f : expf(b.m - c.m);
+  const float x = a.hi * fa, y = b.hi * fb;
+  c.hi = x + y;
+  c.lo = a.lo * fa + b.lo * fb + (x >= y ? (x - c.hi) + y : (y - c.hi) + x);      // what hi rounded off
+  return c;
+}
+
+template <int ROWS>
 __global__ void __launch_bounds__(1024)
 ce_join_kernel(const float2* __restrict__ part, int64_t tiles, int64_t part_ld, int64_t rows, const float* __restrict__ zt,
                const void* __restrict__ targets, int id64, int64_t T, int64_t vocab, float2* __restrict__ stat,
                float* __restrict__ lse, float* __restrict__ loss, int* status) {
   pdl_wait();
   pdl_trigger();
-  __shared__ float mx[32][33];
-  __shared__ double sum[32][33];
-  const int lane = threadIdx.x & 31, group = threadIdx.x >> 5;
-  const int64_t row = (int64_t)blockIdx.x * 32 + lane;
-  float m = -INFINITY;
-  if (row < rows) {
-#pragma unroll 4
-    for (int64_t i = group; i < tiles; i += 32) m = fmaxf(m, part[i * part_ld + row].x);
-  }
-  mx[group][lane] = m;
-  __syncthreads();
-#pragma unroll
-  for (int g = 0; g < 32; ++g) m = fmaxf(m, mx[g][lane]);
-  double s = 0.0;
-  if (row < rows) {
-#pragma unroll 4
-    for (int64_t i = group; i < tiles; i += 32) {
-      const float2 p = part[i * part_ld + row];
-      s += (double)(p.y * expf(p.x - m));
+  constexpr int GROUPS = 1024 / ROWS;
+  static_assert(GROUPS % 32 == 0 && ROWS <= 32, "a warp joins a row's groups");
+  __shared__ float mx[ROWS][GROUPS + 1], hi[ROWS][GROUPS + 1], lo[ROWS][GROUPS + 1];
+  {
+    const int r = threadIdx.x % ROWS, group = threadIdx.x / ROWS;
+    const int64_t row = (int64_t)blockIdx.x * ROWS + r;
+    MaxSum a = {-INFINITY, 0.f, 0.f};
+    if (row < rows) {
+#pragma unroll 8
+      for (int64_t i = group; i < tiles; i += GROUPS) {
+        const float2 p = part[i * part_ld + row];
+        a = join_sums(a, MaxSum{p.x, p.y, 0.f});
+      }
     }
+    mx[r][group] = a.m;
+    hi[r][group] = a.hi;
+    lo[r][group] = a.lo;
   }
-  sum[group][lane] = s;
   __syncthreads();
-  if (group != 0 || row >= rows) return;
+  const int r = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int64_t row = (int64_t)blockIdx.x * ROWS + r;
+  if (r >= ROWS || row >= rows) return;
+  MaxSum a = {mx[r][lane], hi[r][lane], lo[r][lane]};
 #pragma unroll
-  for (int g = 1; g < 32; ++g) s += sum[g][lane];
-  const double ls = log(s);
-  const float l = (float)((double)m + ls);
-  stat[row] = make_float2(m, (float)ls);
+  for (int g = 32; g < GROUPS; g += 32) a = join_sums(a, MaxSum{mx[r][lane + g], hi[r][lane + g], lo[r][lane + g]});
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const MaxSum b = {__shfl_xor_sync(0xffffffffu, a.m, o), __shfl_xor_sync(0xffffffffu, a.hi, o),
+                      __shfl_xor_sync(0xffffffffu, a.lo, o)};
+    a = (lane & o) ? join_sums(b, a) : join_sums(a, b);              // one order for both
+  }
+  if (lane != 0) return;
+  const float ls = logf(a.hi) + a.lo / a.hi;
+  const float l = a.m + ls;
+  stat[row] = make_float2(a.m, ls);
   lse[row] = l;
   const int64_t t = load_id(targets, id64, row % T);
   if (t >= vocab) record_error(status, ZOACT_ERR_INVALID_ARG);
   loss[row] = t >= 0 && t < vocab ? l - zt[row] : 0.f;
 }
 
-// The number of counted rows.
+// alpha = scale / N, N the number of counted rows (at least 1): the factor of the gradient's products.
 __global__ void __launch_bounds__(1024)
-ce_count_kernel(const void* __restrict__ targets, int id64, int64_t T, int64_t vocab, double* count) {
+ce_alpha_kernel(const void* __restrict__ targets, int id64, int64_t T, int64_t vocab, float scale, float* alpha) {
   pdl_wait();
   pdl_trigger();
   __shared__ int red[32];
@@ -183,7 +206,7 @@ ce_count_kernel(const void* __restrict__ targets, int id64, int64_t T, int64_t v
   __syncthreads();
   if (threadIdx.x < 32) {
     n = __reduce_add_sync(0xffffffffu, red[threadIdx.x]);
-    if (threadIdx.x == 0) *count = n;
+    if (threadIdx.x == 0) *alpha = (float)((double)scale / (double)(n > 1 ? n : 1));
   }
 }
 
@@ -194,38 +217,78 @@ ce_count_kernel(const void* __restrict__ targets, int id64, int64_t T, int64_t v
 // rounded p would lose what is left of it where the model is nearly right.
 constexpr float G_SCALE_FP16 = 32768.f;
 
+__device__ __forceinline__ float exp2_ftz(float x) {
+  float e;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(x));
+  return e;
+}
+
+// Thread: 8 entries of SCALE_ROWS rows, loaded together; block: 32 SCALE_ROWS rows of one block of 64 entries (blockIdx.x
+// their group, blockIdx.y the block).
+constexpr int SCALE_ROWS = 4;
+
 template <typename T>
 __global__ void __launch_bounds__(CE_THREADS)
-ce_scale_kernel(void* __restrict__ G, int64_t ldg, const float2* __restrict__ part, int64_t part_ld,
+ce_scale_kernel(void* __restrict__ G, int64_t blk0, int64_t rows, const float2* __restrict__ part, int64_t part_ld,
                 const float2* __restrict__ stat, const float* __restrict__ zt, const void* __restrict__ targets, int id64,
                 int64_t vocab) {
   pdl_wait();
   pdl_trigger();
-  constexpr float scale = sizeof(T) == 2 && __is_same(T, __half) ? G_SCALE_FP16 : 1.f;
-  const int64_t row = blockIdx.y, v0 = ((int64_t)blockIdx.x * CE_THREADS + threadIdx.x) * 8;
-  if (v0 >= vocab) return;
-  uint4* g = reinterpret_cast<uint4*>(reinterpret_cast<__half*>(G) + row * ldg + v0);
-  const int64_t t = load_id(targets, id64, row);
-  const bool counted = t >= 0 && t < vocab;
-  uint4 q = make_uint4(0, 0, 0, 0);
-  if (counted) {
-    q = *g;
-    const float2 st = stat[row];
-    const float c = (part[v0 / ce::V_TILE * part_ld + row].x - st.x) - st.y;
-    const float none = c == c ? 0.f : c;   // a row that is not finite stays so
-    uint32_t* w = reinterpret_cast<uint32_t*>(&q);
+  constexpr float scale = std::is_same<T, __half>::value ? G_SCALE_FP16 : 1.f;
+  const int64_t blk = blk0 + blockIdx.y, v0 = blk * 64 + threadIdx.x % 8 * 8;
+  const int64_t row0 = (int64_t)blockIdx.x * (32 * SCALE_ROWS) + threadIdx.x / 8;
+  uint4* g = reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(G) + (blk * rows + row0) * 64 + threadIdx.x % 8 * 8);
+  constexpr int STEP = 32 * 64 / 8;        // from a row to the thread's next one, in vectors
+  uint4 q[SCALE_ROWS];
+  int64_t t[SCALE_ROWS];
+  float c[SCALE_ROWS];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint32_t lo = w[i] & 0xffffu, hi = w[i] >> 16;
-      const float a = lo == 65535u ? none : __expf(fmaf((float)lo, -1.f / 4096.f, c)) * scale;
-      const float b = hi == 65535u ? none : __expf(fmaf((float)hi, -1.f / 4096.f, c)) * scale;
-      T o[2] = {from_f32<T>(a), from_f32<T>(b)};
-      w[i] = *reinterpret_cast<const uint32_t*>(o);
+  for (int k = 0; k < SCALE_ROWS; ++k) {
+    const int64_t row = row0 + 32 * k;
+    t[k] = -1;
+    if (row < rows) {
+      t[k] = load_id(targets, id64, row);
+      q[k] = g[k * STEP];
+      const float2 st = __ldg(stat + row);
+      c[k] = (__ldg(&part[blk / (ce::V_TILE / 64) * part_ld + row].x) - st.x) - st.y;
     }
-    if (t >= v0 && t < v0 + 8)
-      reinterpret_cast<T*>(&q)[t - v0] = from_f32<T>(expm1f((zt[row] - st.x) - st.y) * scale);
   }
-  *g = q;
+#pragma unroll
+  for (int k = 0; k < SCALE_ROWS; ++k) {
+    const int64_t row = row0 + 32 * k;
+    if (row >= rows) return;
+    if (t[k] >= 0 && t[k] < vocab) {
+      uint32_t* w = reinterpret_cast<uint32_t*>(&q[k]);
+      const float none = c[k] == c[k] ? 0.f : c[k];      // a row that is not finite stays so
+      const float c2 = c[k] * 1.44269504f;
+      float e[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        // 2^23 + the fixed point, by its bytes: the conversion instruction shares the exponential's unit
+        const uint32_t bits = __byte_perm(w[i / 2], 0x4b000000u, i & 1 ? 0x7632 : 0x7610);
+        const float x = __uint_as_float(bits) - 8388608.f;
+        e[i] = bits == 0x4b00ffffu ? none : exp2_ftz(fmaf(x, -1.44269504f / 4096.f, c2)) * scale;
+      }
+      if (t[k] >= v0 && t[k] < v0 + 8) {
+        const float2 st = stat[row];
+        const float g_t = expm1f((zt[row] - st.x) - st.y) * scale;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e[i] = t[k] == v0 + i ? g_t : e[i];
+      }
+      if (v0 + 8 > vocab) {                              // the last block's rest
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e[i] = v0 + i < vocab ? e[i] : 0.f;
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        T o[2] = {from_f32<T>(e[2 * i]), from_f32<T>(e[2 * i + 1])};
+        w[i] = *reinterpret_cast<const uint32_t*>(o);
+      }
+    } else {
+      q[k] = make_uint4(0, 0, 0, 0);
+    }
+    g[k * STEP] = q[k];
+  }
 }
 
 // Block b: L_b = sum / N and D_b = sum over t of (loss_b - loss_0) / N, in fp64 and in a fixed order.
@@ -283,7 +346,7 @@ ce_finish_kernel(const float* __restrict__ loss, int64_t T, int nb, const void* 
 }
 
 struct CeScratch {
-  double* count;
+  float* alpha;
   float *zt, *lse, *loss;
   float2 *stat, *part;
   int64_t part_ld;
@@ -294,7 +357,7 @@ bool ce_scratch(Ctx* ctx, int64_t rows, int64_t part_rows, int64_t tiles, CeScra
   const size_t r = (size_t)((rows + 3) / 4 * 4);
   char* p = (char*)scratch(ctx, SLOT_CE, 256 + r * 4 * 5 + (size_t)tiles * part_rows * sizeof(float2));
   if (!p) return false;
-  s.count = (double*)p;
+  s.alpha = (float*)p;
   s.zt = (float*)(p + 256);
   s.lse = s.zt + r;
   s.loss = s.lse + r;
@@ -316,15 +379,16 @@ int gemm(Ctx* ctx, const void* A, const void* B, const GemmArgs& a) {
 int join(Ctx* ctx, const CeArgs& c, const CeScratch& s, int64_t tiles, int64_t r0, int64_t n, float* lse, float* loss) {
   // with several blocks the rows are all there; a chunk of rows (one block) takes its own targets
   const void* targets = (const char*)c.targets + r0 * (c.id64 ? 8 : 4);
-  ZOACT_CUDA_TRY(launch_pdl(ctx, ce_join_kernel, dim3((unsigned)((n + 31) / 32)), dim3(1024), 0, (const float2*)s.part, tiles,
-                            s.part_ld, n, (const float*)s.zt + r0, targets, c.id64, c.T, c.vocab, s.stat + r0, lse + r0,
+  constexpr int ROWS = 8;
+  ZOACT_CUDA_TRY(launch_pdl(ctx, ce_join_kernel<ROWS>, dim3((unsigned)((n + ROWS - 1) / ROWS)), dim3(1024), 0,
+                            (const float2*)s.part, tiles, s.part_ld, n, (const float*)s.zt + r0, targets, c.id64, c.T, c.vocab, s.stat + r0, lse + r0,
                             loss + r0, ctx->d_status));
   ++ctx->n_launch;
   return ZOACT_OK;
 }
 
-int count_rows(Ctx* ctx, const CeArgs& c, const CeScratch& s) {
-  ZOACT_CUDA_TRY(launch_pdl(ctx, ce_count_kernel, dim3(1), dim3(1024), 0, c.targets, c.id64, c.T, c.vocab, s.count));
+int make_alpha(Ctx* ctx, const CeArgs& c, const CeScratch& s, float scale) {
+  ZOACT_CUDA_TRY(launch_pdl(ctx, ce_alpha_kernel, dim3(1), dim3(1024), 0, c.targets, c.id64, c.T, c.vocab, scale, s.alpha));
   ++ctx->n_launch;
   return ZOACT_OK;
 }
@@ -341,7 +405,7 @@ int run_forward(Ctx* ctx, const CeArgs& c, const CeScratch& s, int64_t tiles, fl
 }
 
 template <typename T, typename TG>
-int run_backward(Ctx* ctx, const CeArgs& c, const CeScratch& s, float scale, void* dH, void* dW,
+int run_backward(Ctx* ctx, const CeArgs& c, const CeScratch& s, void* dH, void* dW,
                  int accumulate) {
   const size_t most = (size_t)1 << 31;
   int64_t chunk = (int64_t)(most / ((size_t)c.vocab * 4)) / TS * TS;
@@ -364,7 +428,7 @@ int run_backward(Ctx* ctx, const CeArgs& c, const CeScratch& s, float scale, voi
     a.stat = s.stat + r0; a.G = G; a.ldg = c.vocab;
     int st = gemm<MODE_G, T, T, T>(ctx, H, c.W, a);
     if (st) return st;
-    a.count = s.count; a.scale = scale;
+    a.alpha = s.alpha;
     if (dH) {
       a.M = n; a.N = c.d; a.K = c.vocab;
       a.sam = c.vocab; a.sak = 1; a.sbn = 1; a.sbk = c.d;
@@ -415,11 +479,11 @@ __global__ void __launch_bounds__(CE_THREADS) ce_round_kernel(const float4* __re
 template <typename T>
 int run_tc(Ctx* ctx, const CeArgs& c) {
   using ce::Operand;
-  const int64_t tiles = (c.vocab + ce::V_TILE - 1) / ce::V_TILE, ldg = (c.vocab + 63) / 64 * 64;
+  const int64_t tiles = (c.vocab + ce::V_TILE - 1) / ce::V_TILE, blocks = (c.vocab + 63) / 64;
   const bool grad = c.dH || c.dW;
   int64_t chunk = c.rows;
   if (grad) {
-    chunk = (int64_t)(((size_t)1 << 31) / ((size_t)ldg * 2)) / 256 * 256;
+    chunk = (int64_t)(((size_t)1 << 31) / ((size_t)blocks * 128)) / 256 * 256;
     if (chunk < 256) chunk = 256;
     if (chunk > c.rows) chunk = c.rows;
   }
@@ -431,11 +495,11 @@ int run_tc(Ctx* ctx, const CeArgs& c) {
   int st;
   if (!grad) {
     const Operand H = {c.H, c.dtype, c.rows, c.d, c.d, 1, c.rows * c.d};
-    st = ce::launch_logits(ctx, W, H, s.part, s.part_ld, s.zt, c.targets, c.id64, c.T, ce::KEEP_NONE, nullptr, 0);
+    st = ce::launch_logits(ctx, W, H, s.part, s.part_ld, s.zt, c.targets, c.id64, c.T, ce::KEEP_NONE, ce::Blocks{});
     if (!st) st = join(ctx, c, s, tiles, 0, c.rows, lse, loss);
     return st ? st : finish(ctx, c, loss);
   }
-  void* G = scratch(ctx, SLOT_CE_G, (size_t)chunk * ldg * 2);
+  void* G = scratch(ctx, SLOT_CE_G, (size_t)chunk * blocks * 128);
   if (!G) return ZOACT_ERR_NOMEM;
   // several chunks add to dW in fp32: a 16-bit dW is rounded from the whole sum
   const bool parts = chunk < c.rows;
@@ -444,29 +508,27 @@ int run_tc(Ctx* ctx, const CeArgs& c) {
     dWf = (float*)scratch(ctx, SLOT_CE_DW, (size_t)c.vocab * c.d * 4);
     if (!dWf) return ZOACT_ERR_NOMEM;
   }
-  st = count_rows(ctx, c, s);
+  st = make_alpha(ctx, c, s, c.dtype == ZOACT_DT_FP16 ? c.grad_scale / G_SCALE_FP16 : c.grad_scale);
   if (st) return st;
-  const float scale = c.dtype == ZOACT_DT_FP16 ? c.grad_scale / G_SCALE_FP16 : c.grad_scale;
   for (int64_t r0 = 0; r0 < c.rows; r0 += chunk) {
     const int64_t n = c.rows - r0 < chunk ? c.rows - r0 : chunk;
     const Operand H = {(const T*)c.H + r0 * c.d, c.dtype, n, c.d, c.d, 1, n * c.d};
-    const Operand Gm = {G, c.dtype, n, c.vocab, ldg, 1, n * ldg};
+    const ce::Blocks Gm = {G, c.dtype, n, c.vocab, 1};
     const void* targets = (const char*)c.targets + r0 * (c.id64 ? 8 : 4);
-    st = ce::launch_logits(ctx, W, H, s.part, s.part_ld, s.zt + r0, targets, c.id64, c.T, ce::KEEP_LOG, G, ldg);
+    st = ce::launch_logits(ctx, W, H, s.part, s.part_ld, s.zt + r0, targets, c.id64, c.T, ce::KEEP_LOG, Gm);
     if (!st) st = join(ctx, c, s, tiles, r0, n, lse, loss);
     if (st) return st;
-    const int64_t cols = (c.vocab + 8 * CE_THREADS - 1) / (8 * CE_THREADS);
-    for (int64_t y = 0; y < n; y += 65535) {
-      const int64_t ny = n - y < 65535 ? n - y : 65535;
-      ZOACT_CUDA_TRY(launch_pdl(ctx, ce_scale_kernel<T>, dim3((unsigned)cols, (unsigned)ny), dim3(CE_THREADS), 0,
-                                (void*)((__half*)G + y * ldg), ldg, (const float2*)s.part + y, s.part_ld,
-                                (const float2*)s.stat + r0 + y, (const float*)s.zt + r0 + y,
-                                (const void*)((const char*)targets + y * (c.id64 ? 8 : 4)), c.id64, c.vocab));
+    const int64_t row_groups = (n + 32 * SCALE_ROWS - 1) / (32 * SCALE_ROWS);
+    for (int64_t b = 0; b < blocks; b += 65535) {
+      const int64_t nb = blocks - b < 65535 ? blocks - b : 65535;
+      ZOACT_CUDA_TRY(launch_pdl(ctx, ce_scale_kernel<T>, dim3((unsigned)row_groups, (unsigned)nb), dim3(CE_THREADS), 0, G, b, n,
+                                (const float2*)s.part, s.part_ld, (const float2*)s.stat + r0, (const float*)s.zt + r0, targets,
+                                c.id64, c.vocab));
       ++ctx->n_launch;
     }
-    if (c.dH) st = ce::launch_by_h(ctx, W, Gm, s.count, scale, (T*)c.dH + r0 * c.d, c.dtype);
+    if (c.dH) st = ce::launch_by_h(ctx, W, Gm, s.alpha, (T*)c.dH + r0 * c.d, c.dtype);
     if (!st && c.dW)
-      st = ce::launch_by_w(ctx, Gm, H, s.count, scale, dWf ? (void*)dWf : c.dW, dWf ? ZOACT_DT_FP32 : c.wgdtype,
+      st = ce::launch_by_w(ctx, Gm, H, s.alpha, dWf ? (void*)dWf : c.dW, dWf ? ZOACT_DT_FP32 : c.wgdtype,
                            r0 > 0 || c.accumulate);
     if (st) return st;
   }
@@ -490,8 +552,8 @@ int run_fp32(Ctx* ctx, const CeArgs& c) {
   int st = run_forward<float>(ctx, c, s, tiles, lse, loss);
   if (!st) st = finish(ctx, c, loss);
   if (st || (!c.dH && !c.dW)) return st;
-  st = count_rows(ctx, c, s);
-  return st ? st : run_backward<float, float>(ctx, c, s, c.grad_scale, c.dH, c.dW, c.accumulate);
+  st = make_alpha(ctx, c, s, c.grad_scale);
+  return st ? st : run_backward<float, float>(ctx, c, s, c.dH, c.dW, c.accumulate);
 }
 
 }  // namespace
