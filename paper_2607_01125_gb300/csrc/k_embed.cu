@@ -1,75 +1,383 @@
-// The embedding at the input of a language model: scaled rows of a table by
-// token id, and the table's gradient.  A negative id is a token without a row
-// (padding): its output is zero and it adds nothing to the gradient.
+// The embedding at the input of a language model: scaled rows of a table by token id, and the table's gradient.  A negative id
+// is a token without a row (padding): its output is zero and it adds nothing to the gradient.
+//
+// Both are bound by memory.  The gradient sums the tokens of each id in token order, whatever their number: the tokens are
+// sorted by id (stable), a block takes 32 sorted tokens and a slice of the columns, writes the rows whose tokens it has all
+// of, and leaves its sums of the first and the last id where these go on in other blocks to a second kernel.  The sort runs
+// in one cluster of eight CTAs, which exchange their digit counts through shared memory; in its launch all other SMs write
+// the zeros of a dense gradient, which takes longer.
 #include "internal.h"
+#include "tc_common.cuh"
 
 namespace zoact {
 namespace {
 
 constexpr int EMB_THREADS = 256;
 
-template <typename T>
+template <int E, typename T>
+__device__ __forceinline__ void emb_load(const T* p, float* v) {
+  if constexpr (E == 1) {
+    v[0] = to_f32<T>(*p);
+  } else {
+    constexpr int N = 16 / (int)sizeof(T);
+#pragma unroll
+    for (int q = 0; q < E / N; ++q) {
+      const uint4 u = *reinterpret_cast<const uint4*>(p + q * N);
+      const T* e = reinterpret_cast<const T*>(&u);
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[q * N + i] = to_f32<T>(e[i]);
+    }
+  }
+}
+template <int E, typename T>
+__device__ __forceinline__ void emb_store(T* p, const float* v) {
+  if constexpr (E == 1) {
+    *p = from_f32<T>(v[0]);
+  } else {
+    constexpr int N = 16 / (int)sizeof(T);
+#pragma unroll
+    for (int q = 0; q < E / N; ++q) {
+      uint4 u;
+      T* e = reinterpret_cast<T*>(&u);
+#pragma unroll
+      for (int i = 0; i < N; ++i) e[i] = from_f32<T>(v[q * N + i]);
+      *reinterpret_cast<uint4*>(p + q * N) = u;
+    }
+  }
+}
+
+// A block a token, VPT vectors of a thread in flight together.
+template <typename T, int E>
 __global__ void __launch_bounds__(EMB_THREADS)
-embed_kernel(const T* __restrict__ E, const void* __restrict__ ids, int id64, int64_t vocab, int d, float scale,
+embed_kernel(const T* __restrict__ tab, const void* __restrict__ ids, int id64, int64_t vocab, int d, float scale,
              T* __restrict__ Y, int* status) {
+  constexpr int VPT = 4;
   pdl_wait();                              // ids and table as earlier kernels left them
   pdl_trigger();
   const int64_t t = blockIdx.x;
   const int64_t id = load_id(ids, id64, t);
   const bool ok = id >= 0 && id < vocab;
   if (id >= vocab && threadIdx.x == 0) record_error(status, ZOACT_ERR_INVALID_ARG);
-  const T* e = E + (ok ? id : 0) * d;
-  for (int i = threadIdx.x; i < d; i += EMB_THREADS)
-    Y[t * d + i] = from_f32<T>(ok ? to_f32<T>(e[i]) * scale : 0.f);
-}
-
-// One block per table row: the ids are searched in token order, so the sum's order is fixed.
-template <typename T, typename TE>
-__global__ void __launch_bounds__(EMB_THREADS)
-embed_grad_kernel(const T* __restrict__ dY, int64_t n_tok, int d, const void* __restrict__ ids, int id64, int64_t vocab,
-                  float scale, TE* __restrict__ dE, int accumulate, int* status) {
-  pdl_wait();
-  pdl_trigger();
-  __shared__ int hit[EMB_THREADS];
-  const int64_t v = blockIdx.x;
-  bool any = false;
-  for (int c0 = 0; c0 < d; c0 += EMB_THREADS) {
-    const int c = c0 + threadIdx.x;
-    float sum = 0.f;
-    for (int64_t t0 = 0; t0 < n_tok; t0 += EMB_THREADS) {
-      const int64_t t = t0 + threadIdx.x;
-      const int64_t id = t < n_tok ? load_id(ids, id64, t) : -1;
-      if (id >= vocab && v == 0) record_error(status, ZOACT_ERR_INVALID_ARG);
-      hit[threadIdx.x] = id == v;
-      if (__syncthreads_or(id == v)) {
-        any = true;
-        for (int k = 0; k < EMB_THREADS; ++k)
-          if (hit[k] && c < d) sum += to_f32<T>(dY[(t0 + k) * d + c]);
-      }
-      __syncthreads();
+  const T* e = tab + (ok ? id : 0) * d;
+  T* y = Y + t * d;
+  const int nv = d / E;
+  for (int i0 = threadIdx.x; i0 < nv; i0 += VPT * blockDim.x) {
+    float v[VPT][E];
+#pragma unroll
+    for (int k = 0; k < VPT; ++k) {
+#pragma unroll
+      for (int j = 0; j < E; ++j) v[k][j] = 0.f;
+      const int i = i0 + k * blockDim.x;
+      if (ok && i < nv) emb_load<E, T>(e + (int64_t)i * E, v[k]);
     }
-    if (c < d && (any || !accumulate)) {
-      const float old = accumulate ? to_f32<TE>(dE[v * d + c]) : 0.f;
-      dE[v * d + c] = from_f32<TE>(fmaf(scale, sum, old));
+#pragma unroll
+    for (int k = 0; k < VPT; ++k) {
+      const int i = i0 + k * blockDim.x;
+#pragma unroll
+      for (int j = 0; j < E; ++j) v[k][j] *= scale;
+      if (i < nv) emb_store<E, T>(y + (int64_t)i * E, v[k]);
     }
   }
 }
 
-template <typename T>
-int run_embed(Ctx* ctx, const void* E, int64_t vocab, int d, const void* ids, int id64, int64_t n, float scale, void* Y) {
-  ZOACT_CUDA_TRY(launch_pdl(ctx, embed_kernel<T>, dim3((unsigned)n), dim3(EMB_THREADS), 0, (const T*)E, ids, id64, vocab,
-                            d, scale, (T*)Y, ctx->d_status));
+// ---- tokens sorted by id ----
+constexpr int SORT_CTAS = 8, SORT_THREADS = 1024, SORT_WARPS = SORT_THREADS / 32;
+constexpr int DIGIT_BITS = 9, DIGITS = 1 << DIGIT_BITS;
+
+__device__ __forceinline__ void cluster_barrier() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t cluster_peer_u32(const uint32_t* p, uint32_t rank) {
+  uint32_t a, v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(tc::smem_u32(p)), "r"(rank));
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+  return v;
+}
+
+struct SortShared {
+  uint32_t hist[SORT_WARPS][DIGITS];       // a warp's count of each digit, then where its next item of that digit goes
+  uint32_t total[DIGITS], base[DIGITS];
+  uint32_t warp_sum[DIGITS / 32];
+};
+
+// Stable sort of the tokens by id, least significant digits first; ids that are no token's become `vocab` and end up last.
+// A warp has a contiguous range of items in each pass and keeps its items' order within a digit by its lanes' order.
+// Items are (id, token); the first pass reads the ids and writes b, the next reads b and writes a, and so on.
+__device__ __forceinline__ void sort_tokens(SortShared& sh, const void* __restrict__ ids, int id64, int64_t n, uint32_t vocab,
+                                            int passes, uint2* a, uint2* b, int* status) {
+  uint32_t rank;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const uint32_t below = (1u << lane) - 1u;
+  const int64_t per = ((n + SORT_CTAS * SORT_WARPS - 1) / (SORT_CTAS * SORT_WARPS) + 31) / 32 * 32;
+  const int64_t i0 = ((int64_t)rank * SORT_WARPS + warp) * per, i1 = i0 + per < n ? i0 + per : n;
+  for (int p = 0; p < passes; ++p) {
+    const int shift = p * DIGIT_BITS;
+    auto item = [&](int64_t i) {
+      if (p > 0) return __ldcg(a + i);
+      const int64_t id = load_id(ids, id64, i);
+      const bool ok = id >= 0 && id < (int64_t)vocab;
+      return make_uint2(ok ? (uint32_t)id : vocab, (uint32_t)i);
+    };
+    for (int d = threadIdx.x; d < SORT_WARPS * DIGITS; d += SORT_THREADS) (&sh.hist[0][0])[d] = 0u;
+    __syncthreads();
+    for (int64_t i = i0 + lane; i - lane < i1; i += 32) {
+      const bool in = i < i1;
+      uint32_t d = DIGITS;                 // lanes past the range match each other only
+      if (in) {
+        const uint2 it = item(i);
+        if (p == 0 && it.x == vocab && load_id(ids, id64, i) >= (int64_t)vocab) record_error(status, ZOACT_ERR_INVALID_ARG);
+        d = (it.x >> shift) & (DIGITS - 1);
+      }
+      const uint32_t same = __match_any_sync(0xffffffffu, d);
+      if (in && (same & below) == 0) sh.hist[warp][d] += __popc(same);
+      __syncwarp();
+    }
+    __syncthreads();
+    // a digit's items: warps in order within the CTA ...
+    uint32_t mine = 0;
+    if (threadIdx.x < DIGITS) {
+      for (int w = 0; w < SORT_WARPS; ++w) {
+        const uint32_t c = sh.hist[w][threadIdx.x];
+        sh.hist[w][threadIdx.x] = mine;
+        mine += c;
+      }
+      sh.total[threadIdx.x] = mine;
+    }
+    cluster_barrier();
+    // ... CTAs in order within the cluster, and digits in order
+    uint32_t before = 0, all = 0;
+    if (threadIdx.x < DIGITS) {
+#pragma unroll
+      for (uint32_t r = 0; r < SORT_CTAS; ++r) {
+        const uint32_t c = cluster_peer_u32(&sh.total[threadIdx.x], r);
+        before += r < rank ? c : 0u;
+        all += c;
+      }
+      uint32_t incl = all;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t v = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += v;
+      }
+      if (lane == 31) sh.warp_sum[warp] = incl;
+      sh.base[threadIdx.x] = incl - all + before;
+    }
+    __syncthreads();
+    if (threadIdx.x < DIGITS) {
+      uint32_t s = 0;
+      for (int w = 0; w < warp; ++w) s += sh.warp_sum[w];
+      sh.base[threadIdx.x] += s;
+    }
+    __syncthreads();
+    for (int64_t i = i0 + lane; i - lane < i1; i += 32) {
+      const bool in = i < i1;
+      uint2 it = make_uint2(0u, 0u);
+      uint32_t d = DIGITS;
+      if (in) {
+        it = item(i);
+        d = (it.x >> shift) & (DIGITS - 1);
+      }
+      const uint32_t same = __match_any_sync(0xffffffffu, d);
+      uint32_t at = 0;
+      if (in) at = sh.hist[warp][d];
+      __syncwarp();
+      if (in) {
+        if ((same & below) == 0) sh.hist[warp][d] = at + __popc(same);
+        __stcg(b + sh.base[d] + at + __popc(same & below), it);
+      }
+      __syncwarp();
+    }
+    cluster_barrier();                     // the items are in place, and the counts may be overwritten
+    uint2* t = a;
+    a = b;
+    b = t;
+  }
+}
+
+// Zeros to [p, p + bytes) by the launch's other CTAs.
+__device__ __forceinline__ void zero_bytes(uint8_t* p, int64_t bytes, int64_t worker, int64_t workers) {
+  const int64_t head = (16 - ((uintptr_t)p & 15)) & 15;
+  uint4* v = reinterpret_cast<uint4*>(p + head);
+  const int64_t nv = bytes > head ? (bytes - head) / 16 : 0;
+  for (int64_t i = worker; i < nv; i += workers) v[i] = make_uint4(0u, 0u, 0u, 0u);
+  if (worker < head && worker < bytes) p[worker] = 0;
+  const int64_t tail = head + nv * 16;
+  if (tail + worker < bytes && worker < 16) p[tail + worker] = 0;
+}
+
+__global__ void __cluster_dims__(SORT_CTAS, 1, 1) __launch_bounds__(SORT_THREADS)
+embed_sort_kernel(const void* __restrict__ ids, int id64, int64_t n, int64_t vocab, int passes, uint2* a, uint2* b,
+                  uint8_t* zero, int64_t zero_len, int* status) {
+  extern __shared__ __align__(16) uint8_t sort_smem[];
+  SortShared& sh = *reinterpret_cast<SortShared*>(sort_smem);
+  pdl_wait();
+  pdl_trigger();
+  if (blockIdx.x < SORT_CTAS)              // the first cluster
+    sort_tokens(sh, ids, id64, n, (uint32_t)vocab, passes, a, b, status);
+  else
+    zero_bytes(zero, zero_len, (int64_t)(blockIdx.x - SORT_CTAS) * SORT_THREADS + threadIdx.x,
+               (int64_t)(gridDim.x - SORT_CTAS) * SORT_THREADS);
+}
+
+// ---- sums of sorted tokens ----
+constexpr int PIECE = 32;                  // sorted tokens of a block
+
+// One block: tokens [32 blockIdx.x, ...) of the sorted list, columns of slice blockIdx.y.  part [pieces][2][d] fp32: the sum of
+// the piece's first id where earlier pieces have it too, and of its last id where only later ones do.
+template <typename T, typename TE, int E>
+__global__ void __launch_bounds__(EMB_THREADS)
+embed_sum_kernel(const T* __restrict__ dY, int64_t n, int d, const uint2* __restrict__ sorted, uint32_t vocab, float scale,
+                 TE* __restrict__ dE, int accumulate, float* __restrict__ part) {
+  pdl_wait();
+  pdl_trigger();
+  __shared__ uint2 item[PIECE + 2];        // with the tokens before and after
+  const int64_t p0 = (int64_t)blockIdx.x * PIECE;
+  if (threadIdx.x < PIECE + 2) {
+    const int64_t i = p0 + (int)threadIdx.x - 1;
+    item[threadIdx.x] = i >= 0 && i < n ? __ldcg(sorted + i) : make_uint2(0xffffffffu, 0u);
+  }
+  __syncthreads();
+  const int64_t c = ((int64_t)blockIdx.y * EMB_THREADS + threadIdx.x) * E;
+  if (c >= d) return;
+  const int cnt = n - p0 < PIECE ? (int)(n - p0) : PIECE;
+  float sum[E];
+#pragma unroll
+  for (int j = 0; j < E; ++j) sum[j] = 0.f;
+  bool first = item[1].x == item[0].x;     // the current id's tokens began before this piece
+  constexpr int AHEAD = 8;                 // rows in flight
+  float v[AHEAD][E];
+#pragma unroll 1
+  for (int i0 = 0; i0 < cnt; i0 += AHEAD) {
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k)
+      if (i0 + k < cnt && item[i0 + k + 1].x < vocab) emb_load<E, T>(dY + (int64_t)item[i0 + k + 1].y * d + c, v[k]);
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+      const int i = i0 + k;
+      if (i >= cnt) break;
+      const uint32_t id = item[i + 1].x, next = item[i + 2].x;
+      if (id >= vocab) break;              // the rest are no tokens
+#pragma unroll
+      for (int j = 0; j < E; ++j) sum[j] += v[k][j];
+      if (next == id && i + 1 < cnt) continue;
+      const bool goes_on = next == id;     // in the next piece
+      if (first || goes_on) {
+        float* o = part + ((int64_t)blockIdx.x * 2 + (first ? 0 : 1)) * d + c;
+        emb_store<E, float>(o, sum);
+      } else {
+        TE* o = dE + (int64_t)id * d + c;
+        float old[E];
+        if (accumulate) emb_load<E, TE>(o, old);
+#pragma unroll
+        for (int j = 0; j < E; ++j) sum[j] = accumulate ? fmaf(scale, sum[j], old[j]) : scale * sum[j];
+        emb_store<E, TE>(o, sum);
+      }
+#pragma unroll
+      for (int j = 0; j < E; ++j) sum[j] = 0.f;
+      first = false;
+    }
+  }
+}
+
+// The ids that several pieces have: the block of the piece where one begins adds the pieces' sums in order.
+template <typename TE, int E>
+__global__ void __launch_bounds__(EMB_THREADS)
+embed_join_kernel(int64_t n, int d, const uint2* __restrict__ sorted, uint32_t vocab, float scale, TE* __restrict__ dE,
+                  int accumulate, const float* __restrict__ part) {
+  pdl_wait();
+  pdl_trigger();
+  const int64_t p = blockIdx.x, end = (p + 1) * PIECE;
+  if (end >= n) return;
+  const uint32_t id = __ldcg(sorted + end - 1).x;
+  if (id >= vocab || __ldcg(sorted + end).x != id) return;                                      // ends here
+  const bool whole = __ldcg(sorted + p * PIECE).x == id;
+  if (whole && p > 0 && __ldcg(sorted + p * PIECE - 1).x == id) return;                         // began earlier
+  const int64_t c = ((int64_t)blockIdx.y * EMB_THREADS + threadIdx.x) * E;
+  if (c >= d) return;
+  float sum[E];
+  emb_load<E, float>(part + (p * 2 + 1) * d + c, sum);
+  constexpr int AHEAD = 4;
+  for (int64_t q = p + 1;; q += AHEAD) {
+    float v[AHEAD][E];
+    bool has[AHEAD];
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+      has[k] = (q + k) * PIECE < n && __ldcg(sorted + (q + k) * PIECE).x == id;
+      if (has[k]) emb_load<E, float>(part + (q + k) * 2 * d + c, v[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k)
+      if (has[k]) {
+#pragma unroll
+        for (int j = 0; j < E; ++j) sum[j] += v[k][j];
+      }
+    if (!has[AHEAD - 1]) break;            // sorted: no later piece has it either
+  }
+  TE* o = dE + (int64_t)id * d + c;
+  float old[E];
+  if (accumulate) emb_load<E, TE>(o, old);
+#pragma unroll
+  for (int j = 0; j < E; ++j) sum[j] = accumulate ? fmaf(scale, sum[j], old[j]) : scale * sum[j];
+  emb_store<E, TE>(o, sum);
+}
+
+bool on16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
+
+template <typename T, int E>
+int go_embed(Ctx* ctx, const void* tab, int64_t vocab, int d, const void* ids, int id64, int64_t n, float scale, void* Y) {
+  const int threads = (d / E + 127) / 128 * 32;      // four vectors a thread
+  ZOACT_CUDA_TRY(launch_pdl(ctx, embed_kernel<T, E>, dim3((unsigned)n), dim3(threads < EMB_THREADS ? threads : EMB_THREADS), 0,
+                            (const T*)tab, ids, id64, vocab, d, scale, (T*)Y, ctx->d_status));
   ++ctx->n_launch;
+  return ZOACT_OK;
+}
+
+template <typename T>
+int run_embed(Ctx* ctx, const void* tab, int64_t vocab, int d, const void* ids, int id64, int64_t n, float scale, void* Y) {
+  constexpr int E = 16 / (int)sizeof(T);
+  return d % E == 0 && on16(tab) && on16(Y) ? go_embed<T, E>(ctx, tab, vocab, d, ids, id64, n, scale, Y)
+                                            : go_embed<T, 1>(ctx, tab, vocab, d, ids, id64, n, scale, Y);
+}
+
+template <typename T, typename TE, int E>
+int go_sums(Ctx* ctx, const void* dY, int64_t n, int d, const uint2* sorted, int64_t vocab, float scale, void* dE, int accumulate,
+            float* part) {
+  const dim3 grid((unsigned)((n + PIECE - 1) / PIECE), (unsigned)((d / E + EMB_THREADS - 1) / EMB_THREADS));
+  ZOACT_CUDA_TRY(launch_pdl(ctx, embed_sum_kernel<T, TE, E>, grid, dim3(EMB_THREADS), 0, (const T*)dY, n, d, sorted,
+                            (uint32_t)vocab, scale, (TE*)dE, accumulate, part));
+  ++ctx->n_launch;
+  if (grid.x > 1) {
+    ZOACT_CUDA_TRY(launch_pdl(ctx, embed_join_kernel<TE, E>, grid, dim3(EMB_THREADS), 0, n, d, sorted, (uint32_t)vocab, scale,
+                              (TE*)dE, accumulate, (const float*)part));
+    ++ctx->n_launch;
+  }
   return ZOACT_OK;
 }
 
 template <typename T, typename TE>
 int run_embed_grad(Ctx* ctx, const void* dY, int64_t n, int d, const void* ids, int id64, int64_t vocab, float scale,
                    void* dE, int accumulate) {
-  ZOACT_CUDA_TRY(launch_pdl(ctx, embed_grad_kernel<T, TE>, dim3((unsigned)vocab), dim3(EMB_THREADS), 0, (const T*)dY, n, d,
-                            ids, id64, vocab, scale, (TE*)dE, accumulate, ctx->d_status));
+  constexpr int E = 16 / (int)sizeof(T);
+  const int64_t pieces = (n + PIECE - 1) / PIECE;
+  const size_t list = ((size_t)n * sizeof(uint2) + 255) / 256 * 256;
+  char* s = (char*)scratch(ctx, SLOT_EMBED, 2 * list + (size_t)pieces * 2 * d * 4);
+  if (!s) return ZOACT_ERR_NOMEM;
+  uint2* a = (uint2*)s;
+  uint2* b = (uint2*)(s + list);
+  float* part = (float*)(s + 2 * list);
+  int passes = 1;
+  while (passes * DIGIT_BITS < 32 && (vocab >> (passes * DIGIT_BITS)) != 0) ++passes;
+  const unsigned ctas = accumulate ? SORT_CTAS : (unsigned)(ctx->sm_count / SORT_CTAS * SORT_CTAS);
+  ZOACT_CUDA_TRY(cudaFuncSetAttribute(embed_sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(SortShared)));
+  ZOACT_CUDA_TRY(launch_pdl(ctx, embed_sort_kernel, dim3(ctas > 2 * SORT_CTAS || accumulate ? ctas : 2 * SORT_CTAS),
+                            dim3(SORT_THREADS), sizeof(SortShared), ids, id64, n, vocab, passes, a, b, (uint8_t*)dE,
+                            accumulate ? (int64_t)0 : vocab * d * (int64_t)sizeof(TE), ctx->d_status));
   ++ctx->n_launch;
-  return ZOACT_OK;
+  if (n == 0) return ZOACT_OK;
+  const uint2* sorted = passes % 2 ? b : a;
+  return d % E == 0 && on16(dY) && on16(dE) ? go_sums<T, TE, E>(ctx, dY, n, d, sorted, vocab, scale, dE, accumulate, part)
+                                            : go_sums<T, TE, 1>(ctx, dY, n, d, sorted, vocab, scale, dE, accumulate, part);
 }
 
 }  // namespace
