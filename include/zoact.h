@@ -505,7 +505,7 @@ int zoact_mix_rms_strided(zoact_ctx* ctx, const void* q, const void* k, const vo
  *   dE [vocab, d] of edtype (dtype or FP32).  The sum is taken in fp32 over the tokens in an order that depends on the
  *   ids alone (the same on every run) and rounded once.  accumulate == 0 writes every row, zero where no token has it;
  *   accumulate != 0 touches only the rows of tokens that occur (a tied head's gradient lies there already).  Context
- *   scratch: 16 bytes a token, and 8 d bytes for every 32 tokens.                                                   */
+ *   scratch: 16 bytes a token, and 8 d bytes for every 16 tokens.                                                   */
 int zoact_embed(zoact_ctx* ctx, const void* E, int dtype, int64_t vocab, int32_t d, const void* ids, int idtype,
                 int64_t n_tok, float scale, void* Y);
 int zoact_embed_grad(zoact_ctx* ctx, const void* dY, int dtype, int64_t n_tok, int32_t d, const void* ids, int idtype,

@@ -2,7 +2,7 @@
 // is a token without a row (padding): its output is zero and it adds nothing to the gradient.
 //
 // Both are bound by memory.  The gradient sums the tokens of each id in token order, whatever their number: the tokens are
-// sorted by id (stable), a block takes 32 sorted tokens and a slice of the columns, writes the rows whose tokens it has all
+// sorted by id (stable), a block takes 16 sorted tokens and a slice of the columns, writes the rows whose tokens it has all
 // of, and leaves its sums of the first and the last id where these go on in other blocks to a second kernel.  The sort runs
 // in one cluster of eight CTAs, which exchange their digit counts through shared memory; in its launch all other SMs write
 // the zeros of a dense gradient, which takes longer.
@@ -94,7 +94,7 @@ __device__ __forceinline__ uint32_t cluster_peer_u32(const uint32_t* p, uint32_t
   return v;
 }
 
-struct SortShared {
+struct __align__(16) SortShared {
   uint32_t hist[SORT_WARPS][DIGITS];       // a warp's count of each digit, then where its next item of that digit goes
   uint32_t total[DIGITS], base[DIGITS];
   uint32_t warp_sum[DIGITS / 32];
@@ -119,7 +119,8 @@ __device__ __forceinline__ void sort_tokens(SortShared& sh, const void* __restri
       const bool ok = id >= 0 && id < (int64_t)vocab;
       return make_uint2(ok ? (uint32_t)id : vocab, (uint32_t)i);
     };
-    for (int d = threadIdx.x; d < SORT_WARPS * DIGITS; d += SORT_THREADS) (&sh.hist[0][0])[d] = 0u;
+    for (int d = threadIdx.x; d < SORT_WARPS * DIGITS / 4; d += SORT_THREADS)
+      reinterpret_cast<uint4*>(sh.hist)[d] = make_uint4(0u, 0u, 0u, 0u);
     __syncthreads();
     for (int64_t i = i0 + lane; i - lane < i1; i += 32) {
       const bool in = i < i1;
@@ -137,10 +138,13 @@ __device__ __forceinline__ void sort_tokens(SortShared& sh, const void* __restri
     // a digit's items: warps in order within the CTA ...
     uint32_t mine = 0;
     if (threadIdx.x < DIGITS) {
+      uint32_t c[SORT_WARPS];
+#pragma unroll
+      for (int w = 0; w < SORT_WARPS; ++w) c[w] = sh.hist[w][threadIdx.x];
+#pragma unroll
       for (int w = 0; w < SORT_WARPS; ++w) {
-        const uint32_t c = sh.hist[w][threadIdx.x];
         sh.hist[w][threadIdx.x] = mine;
-        mine += c;
+        mine += c[w];
       }
       sh.total[threadIdx.x] = mine;
     }
@@ -195,15 +199,24 @@ __device__ __forceinline__ void sort_tokens(SortShared& sh, const void* __restri
   }
 }
 
-// Zeros to [p, p + bytes) by the launch's other CTAs.
-__device__ __forceinline__ void zero_bytes(uint8_t* p, int64_t bytes, int64_t worker, int64_t workers) {
+// Zeros to [p, p + bytes) by the launch's other CTAs, ZERO_VECTORS 16-byte stores a thread and no loop: a CTA for each 64 KB in
+// address order writes 7.3 TB/s where a loop over the SMs' CTAs wrote 6.4 (and 4.6 in clusters, which do not fill every SM).
+constexpr int ZERO_VECTORS = 4;
+constexpr int64_t ZERO_BYTES = (int64_t)SORT_THREADS * ZERO_VECTORS * 16;     // of a CTA
+
+__device__ __forceinline__ void zero_bytes(uint8_t* p, int64_t bytes, int64_t cta) {
   const int64_t head = (16 - ((uintptr_t)p & 15)) & 15;
-  uint4* v = reinterpret_cast<uint4*>(p + head);
   const int64_t nv = bytes > head ? (bytes - head) / 16 : 0;
-  for (int64_t i = worker; i < nv; i += workers) v[i] = make_uint4(0u, 0u, 0u, 0u);
-  if (worker < head && worker < bytes) p[worker] = 0;
-  const int64_t tail = head + nv * 16;
-  if (tail + worker < bytes && worker < 16) p[tail + worker] = 0;
+  uint4* v = reinterpret_cast<uint4*>(p + head);
+  const int64_t i0 = cta * SORT_THREADS * ZERO_VECTORS + threadIdx.x;
+#pragma unroll
+  for (int k = 0; k < ZERO_VECTORS; ++k)
+    if (i0 + k * SORT_THREADS < nv) v[i0 + k * SORT_THREADS] = make_uint4(0u, 0u, 0u, 0u);
+  if (cta == 0 && threadIdx.x < 16) {              // the ends of an array that does not begin or end on 16 bytes
+    const int64_t tail = head + nv * 16;
+    if ((int64_t)threadIdx.x < head && (int64_t)threadIdx.x < bytes) p[threadIdx.x] = 0;
+    if (tail + (int64_t)threadIdx.x < bytes) p[tail + threadIdx.x] = 0;
+  }
 }
 
 __global__ void __cluster_dims__(SORT_CTAS, 1, 1) __launch_bounds__(SORT_THREADS)
@@ -216,19 +229,24 @@ embed_sort_kernel(const void* __restrict__ ids, int id64, int64_t n, int64_t voc
   if (blockIdx.x < SORT_CTAS)              // the first cluster
     sort_tokens(sh, ids, id64, n, (uint32_t)vocab, passes, a, b, status);
   else
-    zero_bytes(zero, zero_len, (int64_t)(blockIdx.x - SORT_CTAS) * SORT_THREADS + threadIdx.x,
-               (int64_t)(gridDim.x - SORT_CTAS) * SORT_THREADS);
+    zero_bytes(zero, zero_len, (int64_t)blockIdx.x - SORT_CTAS);
 }
 
 // ---- sums of sorted tokens ----
-constexpr int PIECE = 32;                  // sorted tokens of a block
+constexpr int PIECE = 16;                  // sorted tokens of a block, all in flight together
 
-// One block: tokens [32 blockIdx.x, ...) of the sorted list, columns of slice blockIdx.y.  part [pieces][2][d] fp32: the sum of
-// the piece's first id where earlier pieces have it too, and of its last id where only later ones do.
-template <typename T, typename TE, int E>
+// E elements that lie together, in one load.
+template <typename T, int E>
+struct alignas(E * sizeof(T)) Raw {
+  T e[E];
+};
+
+// One block: tokens [PIECE blockIdx.x, ...) of the sorted list, columns of slice blockIdx.y.  part [pieces][2][d] fp32: the sum
+// of the piece's first id where earlier pieces have it too, and of its last id where only later ones do.
+template <typename T, typename TE, int E, bool ADD>
 __global__ void __launch_bounds__(EMB_THREADS)
 embed_sum_kernel(const T* __restrict__ dY, int64_t n, int d, const uint2* __restrict__ sorted, uint32_t vocab, float scale,
-                 TE* __restrict__ dE, int accumulate, float* __restrict__ part) {
+                 TE* __restrict__ dE, float* __restrict__ part) {
   pdl_wait();
   pdl_trigger();
   __shared__ uint2 item[PIECE + 2];        // with the tokens before and after
@@ -238,88 +256,88 @@ embed_sum_kernel(const T* __restrict__ dY, int64_t n, int d, const uint2* __rest
     item[threadIdx.x] = i >= 0 && i < n ? __ldcg(sorted + i) : make_uint2(0xffffffffu, 0u);
   }
   __syncthreads();
-  const int64_t c = ((int64_t)blockIdx.y * EMB_THREADS + threadIdx.x) * E;
+  const int64_t c = ((int64_t)blockIdx.y * blockDim.x + threadIdx.x) * E;
   if (c >= d) return;
-  const int cnt = n - p0 < PIECE ? (int)(n - p0) : PIECE;
+  const uint32_t before = item[0].x;
+  Raw<T, E> v[PIECE];
+  Raw<TE, E> old[ADD ? PIECE : 1];
+#pragma unroll
+  for (int k = 0; k < PIECE; ++k) {
+    const uint32_t id = item[k + 1].x;     // past the list's end, and where it is no token's: not below vocab
+    if (id < vocab) {
+      v[k] = *reinterpret_cast<const Raw<T, E>*>(dY + (int64_t)item[k + 1].y * d + c);
+      if (ADD && id != before && item[k + 2].x != id) old[k] = *reinterpret_cast<const Raw<TE, E>*>(dE + (int64_t)id * d + c);
+    }
+  }
   float sum[E];
 #pragma unroll
   for (int j = 0; j < E; ++j) sum[j] = 0.f;
-  bool first = item[1].x == item[0].x;     // the current id's tokens began before this piece
-  constexpr int AHEAD = 8;                 // rows in flight
-  float v[AHEAD][E];
-#pragma unroll 1
-  for (int i0 = 0; i0 < cnt; i0 += AHEAD) {
 #pragma unroll
-    for (int k = 0; k < AHEAD; ++k)
-      if (i0 + k < cnt && item[i0 + k + 1].x < vocab) emb_load<E, T>(dY + (int64_t)item[i0 + k + 1].y * d + c, v[k]);
+  for (int k = 0; k < PIECE; ++k) {
+    const uint32_t id = item[k + 1].x, next = item[k + 2].x;
+    if (id >= vocab) continue;
 #pragma unroll
-    for (int k = 0; k < AHEAD; ++k) {
-      const int i = i0 + k;
-      if (i >= cnt) break;
-      const uint32_t id = item[i + 1].x, next = item[i + 2].x;
-      if (id >= vocab) break;              // the rest are no tokens
+    for (int j = 0; j < E; ++j) sum[j] += to_f32<T>(v[k].e[j]);
+    if (next == id && k + 1 < PIECE) continue;
+    if (id == before || next == id) {
+      Raw<float, E>* o = reinterpret_cast<Raw<float, E>*>(part + ((int64_t)blockIdx.x * 2 + (id == before ? 0 : 1)) * d + c);
+      Raw<float, E> r;
 #pragma unroll
-      for (int j = 0; j < E; ++j) sum[j] += v[k][j];
-      if (next == id && i + 1 < cnt) continue;
-      const bool goes_on = next == id;     // in the next piece
-      if (first || goes_on) {
-        float* o = part + ((int64_t)blockIdx.x * 2 + (first ? 0 : 1)) * d + c;
-        emb_store<E, float>(o, sum);
-      } else {
-        TE* o = dE + (int64_t)id * d + c;
-        float old[E];
-        if (accumulate) emb_load<E, TE>(o, old);
+      for (int j = 0; j < E; ++j) r.e[j] = sum[j];
+      *o = r;
+    } else {
+      Raw<TE, E> r;
 #pragma unroll
-        for (int j = 0; j < E; ++j) sum[j] = accumulate ? fmaf(scale, sum[j], old[j]) : scale * sum[j];
-        emb_store<E, TE>(o, sum);
-      }
-#pragma unroll
-      for (int j = 0; j < E; ++j) sum[j] = 0.f;
-      first = false;
+      for (int j = 0; j < E; ++j) r.e[j] = from_f32<TE>(ADD ? fmaf(scale, sum[j], to_f32<TE>(old[ADD ? k : 0].e[j])) : scale * sum[j]);
+      *reinterpret_cast<Raw<TE, E>*>(dE + (int64_t)id * d + c) = r;
     }
+#pragma unroll
+    for (int j = 0; j < E; ++j) sum[j] = 0.f;
   }
 }
 
 // The ids that several pieces have: the block of the piece where one begins adds the pieces' sums in order.
-template <typename TE, int E>
+template <typename TE, int E, bool ADD>
 __global__ void __launch_bounds__(EMB_THREADS)
 embed_join_kernel(int64_t n, int d, const uint2* __restrict__ sorted, uint32_t vocab, float scale, TE* __restrict__ dE,
-                  int accumulate, const float* __restrict__ part) {
+                  const float* __restrict__ part) {
   pdl_wait();
   pdl_trigger();
   const int64_t p = blockIdx.x, end = (p + 1) * PIECE;
   if (end >= n) return;
-  const uint32_t id = __ldcg(sorted + end - 1).x;
-  if (id >= vocab || __ldcg(sorted + end).x != id) return;                                      // ends here
-  const bool whole = __ldcg(sorted + p * PIECE).x == id;
-  if (whole && p > 0 && __ldcg(sorted + p * PIECE - 1).x == id) return;                         // began earlier
-  const int64_t c = ((int64_t)blockIdx.y * EMB_THREADS + threadIdx.x) * E;
+  const uint32_t id = __ldcg(sorted + end - 1).x, after = __ldcg(sorted + end).x;
+  const uint32_t before = p > 0 ? __ldcg(sorted + p * PIECE - 1).x : 0xffffffffu;
+  if (id >= vocab || after != id || before == id) return;            // it ends here, or began earlier
+  const int64_t c = ((int64_t)blockIdx.y * blockDim.x + threadIdx.x) * E;
   if (c >= d) return;
+  TE* o = dE + (int64_t)id * d + c;
+  Raw<TE, E> old;
+  if (ADD) old = *reinterpret_cast<const Raw<TE, E>*>(o);
+  const Raw<float, E> own = *reinterpret_cast<const Raw<float, E>*>(part + (p * 2 + 1) * d + c);
   float sum[E];
-  emb_load<E, float>(part + (p * 2 + 1) * d + c, sum);
-  constexpr int AHEAD = 4;
+#pragma unroll
+  for (int j = 0; j < E; ++j) sum[j] = own.e[j];
+  constexpr int AHEAD = 8;
   for (int64_t q = p + 1;; q += AHEAD) {
-    float v[AHEAD][E];
+    Raw<float, E> v[AHEAD];
     bool has[AHEAD];
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k) {
       has[k] = (q + k) * PIECE < n && __ldcg(sorted + (q + k) * PIECE).x == id;
-      if (has[k]) emb_load<E, float>(part + (q + k) * 2 * d + c, v[k]);
+      if (has[k]) v[k] = *reinterpret_cast<const Raw<float, E>*>(part + (q + k) * 2 * d + c);
     }
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k)
       if (has[k]) {
 #pragma unroll
-        for (int j = 0; j < E; ++j) sum[j] += v[k][j];
+        for (int j = 0; j < E; ++j) sum[j] += v[k].e[j];
       }
     if (!has[AHEAD - 1]) break;            // sorted: no later piece has it either
   }
-  TE* o = dE + (int64_t)id * d + c;
-  float old[E];
-  if (accumulate) emb_load<E, TE>(o, old);
+  Raw<TE, E> r;
 #pragma unroll
-  for (int j = 0; j < E; ++j) sum[j] = accumulate ? fmaf(scale, sum[j], old[j]) : scale * sum[j];
-  emb_store<E, TE>(o, sum);
+  for (int j = 0; j < E; ++j) r.e[j] = from_f32<TE>(ADD ? fmaf(scale, sum[j], to_f32<TE>(old.e[j])) : scale * sum[j]);
+  *reinterpret_cast<Raw<TE, E>*>(o) = r;
 }
 
 bool on16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
@@ -340,16 +358,16 @@ int run_embed(Ctx* ctx, const void* tab, int64_t vocab, int d, const void* ids, 
                                             : go_embed<T, 1>(ctx, tab, vocab, d, ids, id64, n, scale, Y);
 }
 
-template <typename T, typename TE, int E>
-int go_sums(Ctx* ctx, const void* dY, int64_t n, int d, const uint2* sorted, int64_t vocab, float scale, void* dE, int accumulate,
-            float* part) {
-  const dim3 grid((unsigned)((n + PIECE - 1) / PIECE), (unsigned)((d / E + EMB_THREADS - 1) / EMB_THREADS));
-  ZOACT_CUDA_TRY(launch_pdl(ctx, embed_sum_kernel<T, TE, E>, grid, dim3(EMB_THREADS), 0, (const T*)dY, n, d, sorted,
-                            (uint32_t)vocab, scale, (TE*)dE, accumulate, part));
+template <typename T, typename TE, int E, bool ADD>
+int go_sums(Ctx* ctx, const void* dY, int64_t n, int d, const uint2* sorted, int64_t vocab, float scale, void* dE, float* part) {
+  const int nv = d / E, slices = (nv + EMB_THREADS - 1) / EMB_THREADS, threads = ((nv + slices - 1) / slices + 31) / 32 * 32;
+  const dim3 grid((unsigned)((n + PIECE - 1) / PIECE), (unsigned)slices);
+  ZOACT_CUDA_TRY(launch_pdl(ctx, embed_sum_kernel<T, TE, E, ADD>, grid, dim3(threads), 0, (const T*)dY, n, d, sorted,
+                            (uint32_t)vocab, scale, (TE*)dE, part));
   ++ctx->n_launch;
   if (grid.x > 1) {
-    ZOACT_CUDA_TRY(launch_pdl(ctx, embed_join_kernel<TE, E>, grid, dim3(EMB_THREADS), 0, n, d, sorted, (uint32_t)vocab, scale,
-                              (TE*)dE, accumulate, (const float*)part));
+    ZOACT_CUDA_TRY(launch_pdl(ctx, embed_join_kernel<TE, E, ADD>, grid, dim3(threads), 0, n, d, sorted, (uint32_t)vocab, scale,
+                              (TE*)dE, (const float*)part));
     ++ctx->n_launch;
   }
   return ZOACT_OK;
@@ -358,7 +376,7 @@ int go_sums(Ctx* ctx, const void* dY, int64_t n, int d, const uint2* sorted, int
 template <typename T, typename TE>
 int run_embed_grad(Ctx* ctx, const void* dY, int64_t n, int d, const void* ids, int id64, int64_t vocab, float scale,
                    void* dE, int accumulate) {
-  constexpr int E = 16 / (int)sizeof(T);
+  constexpr int E = 16 / (int)(sizeof(T) > sizeof(TE) ? sizeof(T) : sizeof(TE));
   const int64_t pieces = (n + PIECE - 1) / PIECE;
   const size_t list = ((size_t)n * sizeof(uint2) + 255) / 256 * 256;
   char* s = (char*)scratch(ctx, SLOT_EMBED, 2 * list + (size_t)pieces * 2 * d * 4);
@@ -368,16 +386,20 @@ int run_embed_grad(Ctx* ctx, const void* dY, int64_t n, int d, const void* ids, 
   float* part = (float*)(s + 2 * list);
   int passes = 1;
   while (passes * DIGIT_BITS < 32 && (vocab >> (passes * DIGIT_BITS)) != 0) ++passes;
-  const unsigned ctas = accumulate ? SORT_CTAS : (unsigned)(ctx->sm_count / SORT_CTAS * SORT_CTAS);
+  const int64_t zero_len = accumulate ? 0 : vocab * d * (int64_t)sizeof(TE);
+  const int64_t ctas = SORT_CTAS + (zero_len + ZERO_BYTES - 1) / ZERO_BYTES;
   ZOACT_CUDA_TRY(cudaFuncSetAttribute(embed_sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(SortShared)));
-  ZOACT_CUDA_TRY(launch_pdl(ctx, embed_sort_kernel, dim3(ctas > 2 * SORT_CTAS || accumulate ? ctas : 2 * SORT_CTAS),
-                            dim3(SORT_THREADS), sizeof(SortShared), ids, id64, n, vocab, passes, a, b, (uint8_t*)dE,
-                            accumulate ? (int64_t)0 : vocab * d * (int64_t)sizeof(TE), ctx->d_status));
+  ZOACT_CUDA_TRY(launch_pdl(ctx, embed_sort_kernel, dim3((unsigned)((ctas + SORT_CTAS - 1) / SORT_CTAS * SORT_CTAS)),
+                            dim3(SORT_THREADS), sizeof(SortShared), ids, id64, n, vocab, passes, a, b, (uint8_t*)dE, zero_len,
+                            ctx->d_status));
   ++ctx->n_launch;
   if (n == 0) return ZOACT_OK;
   const uint2* sorted = passes % 2 ? b : a;
-  return d % E == 0 && on16(dY) && on16(dE) ? go_sums<T, TE, E>(ctx, dY, n, d, sorted, vocab, scale, dE, accumulate, part)
-                                            : go_sums<T, TE, 1>(ctx, dY, n, d, sorted, vocab, scale, dE, accumulate, part);
+  if (d % E == 0 && on16(dY) && on16(dE))
+    return accumulate ? go_sums<T, TE, E, true>(ctx, dY, n, d, sorted, vocab, scale, dE, part)
+                      : go_sums<T, TE, E, false>(ctx, dY, n, d, sorted, vocab, scale, dE, part);
+  return accumulate ? go_sums<T, TE, 1, true>(ctx, dY, n, d, sorted, vocab, scale, dE, part)
+                    : go_sums<T, TE, 1, false>(ctx, dY, n, d, sorted, vocab, scale, dE, part);
 }
 
 }  // namespace

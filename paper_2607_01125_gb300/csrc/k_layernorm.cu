@@ -17,6 +17,56 @@ namespace {
 
 constexpr int LN_THREADS = 256;
 
+// Pairs of fp32 in one instruction, each half rounded as by itself.
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(*reinterpret_cast<uint64_t*>(&a)), "l"(*reinterpret_cast<uint64_t*>(&b)));
+  return *reinterpret_cast<float2*>(&r);
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(*reinterpret_cast<uint64_t*>(&a)), "l"(*reinterpret_cast<uint64_t*>(&b)));
+  return *reinterpret_cast<float2*>(&r);
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;"
+      : "=l"(r)
+      : "l"(*reinterpret_cast<uint64_t*>(&a)), "l"(*reinterpret_cast<uint64_t*>(&b)), "l"(*reinterpret_cast<uint64_t*>(&c)));
+  return *reinterpret_cast<float2*>(&r);
+}
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+
+// A 16-byte vector's elements in pairs, and back.
+template <typename T>
+__device__ __forceinline__ void unpack(const uint4& u, float2* f) {
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+  if constexpr (sizeof(T) == 4) {
+    f[0] = make_float2(__uint_as_float(w[0]), __uint_as_float(w[1]));
+    f[1] = make_float2(__uint_as_float(w[2]), __uint_as_float(w[3]));
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const T* e = reinterpret_cast<const T*>(&w[i]);
+      f[i] = make_float2(to_f32<T>(e[0]), to_f32<T>(e[1]));
+    }
+  }
+}
+template <typename T>
+__device__ __forceinline__ uint4 pack(const float2* f) {
+  if constexpr (sizeof(T) == 4) {
+    return make_uint4(__float_as_uint(f[0].x), __float_as_uint(f[0].y), __float_as_uint(f[1].x), __float_as_uint(f[1].y));
+  } else {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      T o[2] = {from_f32<T>(f[i].x), from_f32<T>(f[i].y)};
+      w[i] = *reinterpret_cast<const uint32_t*>(o);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+}
+
 template <typename TP>
 __device__ __forceinline__ float param_at(const TP* p, int64_t i, float none) { return p ? to_f32<TP>(p[i]) : none; }
 
@@ -147,6 +197,79 @@ ln_rows_kernel(const T* __restrict__ X, int64_t ld, int64_t rows, int n, const T
   }
 }
 
+// A warp a row, the row's vectors packed in registers: no barrier, and with four rows a block ten times the bytes in flight
+// of a block a row (8192 x 5120 fp16: 49 us with ln_rows_kernel, 160 threads a row).  For many rows; few rows take
+// ln_rows_kernel, whose threads share a row's work.
+template <typename T, typename TP, int VPT>
+__global__ void __launch_bounds__(128)
+ln_warp_kernel(const T* __restrict__ X, int64_t ld, int64_t rows, int n, const TP* __restrict__ g, const TP* __restrict__ b,
+               float eps, T* __restrict__ Y, float* __restrict__ mean, float* __restrict__ rstd) {
+  constexpr int E = 16 / (int)sizeof(T), P = E / 2;
+  pdl_wait();
+  pdl_trigger();
+  const int lane = threadIdx.x & 31;
+  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
+  if (row >= rows) return;
+  const uint4* x = reinterpret_cast<const uint4*>(X + row * ld);
+  const int nv = n / E;
+  uint4 q[VPT];
+#pragma unroll
+  for (int j = 0; j < VPT; ++j) {
+    q[j] = make_uint4(0u, 0u, 0u, 0u);
+    if (lane + 32 * j < nv) q[j] = __ldcs(x + lane + 32 * j);
+  }
+  float2 s = make_float2(0.f, 0.f);
+#pragma unroll
+  for (int j = 0; j < VPT; ++j) {
+    float2 f[P];
+    unpack<T>(q[j], f);
+#pragma unroll
+    for (int i = 0; i < P; ++i) s = add2(s, f[i]);
+  }
+  float t = s.x + s.y;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
+  const float m = t / (float)n;
+  s = make_float2(0.f, 0.f);
+#pragma unroll
+  for (int j = 0; j < VPT; ++j) {
+    float2 f[P];
+    unpack<T>(q[j], f);
+    if (lane + 32 * j < nv) {
+#pragma unroll
+      for (int i = 0; i < P; ++i) {
+        const float2 c = add2(f[i], both(-m));
+        s = fma2(c, c, s);
+      }
+    }
+  }
+  t = s.x + s.y;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
+  const float r = 1.f / sqrtf(t / (float)n + eps);
+  uint4* y = reinterpret_cast<uint4*>(Y + row * n);
+#pragma unroll
+  for (int j = 0; j < VPT; ++j) {
+    const int v = lane + 32 * j;
+    if (v < nv) {
+      float2 f[P];
+      float gg[E], bb[E];
+      unpack<T>(q[j], f);
+      load_param<TP, E>(g, (int64_t)v * E, 1.f, gg);
+      load_param<TP, E>(b, (int64_t)v * E, 0.f, bb);
+#pragma unroll
+      for (int i = 0; i < P; ++i)
+        f[i] = fma2(mul2(add2(f[i], both(-m)), both(r)), make_float2(gg[2 * i], gg[2 * i + 1]),
+                    make_float2(bb[2 * i], bb[2 * i + 1]));
+      y[v] = pack<T>(f);
+    }
+  }
+  if (lane == 0) {
+    if (mean) mean[row] = m;
+    if (rstd) rstd[row] = r;
+  }
+}
+
 // dX alone, as ln_rows_kernel.
 template <typename T, typename TP, int E, int VPT>
 __global__ void __launch_bounds__(most_threads(E, true))
@@ -270,26 +393,29 @@ ln_grad_cols_kernel(const T* __restrict__ dY, int64_t ld_dy, const T* __restrict
   part[((int64_t)blockIdx.y * 2 + 1) * n + i] = sb;
 }
 
-// dg and db from part [parts][2][n], in part order within each of 8 groups.
-__global__ void __launch_bounds__(256)
+// dg and db from part [parts][2][n], in part order within each of 32 groups.
+__global__ void __launch_bounds__(1024)
 ln_join_kernel(const float* __restrict__ part, int parts, int n, float* __restrict__ dg, float* __restrict__ db) {
   pdl_wait();
   pdl_trigger();
-  __shared__ float red[8][33];
+  __shared__ float red[32][33];
   const int c = threadIdx.x & 31, group = threadIdx.x >> 5;
   const int64_t col = (int64_t)blockIdx.x * 32 + c;
   float s = 0.f;
   if (col < 2 * (int64_t)n) {
 #pragma unroll 8
-    for (int p = group; p < parts; p += 8) s += part[(int64_t)p * 2 * n + col];
+    for (int p = group; p < parts; p += 32) s += __ldcg(part + (int64_t)p * 2 * n + col);
   }
   red[group][c] = s;
   __syncthreads();
-  if (group != 0 || col >= 2 * (int64_t)n) return;
+  // warp w adds the groups of column w, pairwise by its lanes
+  s = red[c][group];
 #pragma unroll
-  for (int k = 1; k < 8; ++k) s += red[k][c];
-  float* out = col < n ? dg : db;
-  if (out) out[col < n ? col : col - n] = s;
+  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  const int64_t mine = (int64_t)blockIdx.x * 32 + group;
+  if (c != 0 || mine >= 2 * (int64_t)n) return;
+  float* out = mine < n ? dg : db;
+  if (out) out[mine < n ? mine : mine - n] = s;
 }
 
 // The whole gradient in one pass: block b takes rows b, b + gridDim.x, ...; thread t columns of vectors t, t + blockDim.x, ...
@@ -332,13 +458,18 @@ ln_grad_ring_kernel(const T* __restrict__ dY, int64_t ld_dy, const T* __restrict
   };
   if (threadIdx.x == 0)
     for (int64_t i = 0; i < mine && i < stages; ++i) fetch(i);
-  float gg[VPT][E], sg[VPT][E], sb[VPT][E];
+  constexpr int P = E / 2;
+  float2 gg[VPT][P], sg[VPT][P], sb[VPT][P];
 #pragma unroll
   for (int j = 0; j < VPT; ++j) {
     const int v = threadIdx.x + j * blockDim.x;
-    if (v < nv) load_param<TP, E>(g, (int64_t)v * E, 1.f, gg[j]);
+    float one[E];
+    if (v < nv) load_param<TP, E>(g, (int64_t)v * E, 1.f, one);
 #pragma unroll
-    for (int k = 0; k < E; ++k) sg[j][k] = sb[j][k] = 0.f;
+    for (int k = 0; k < P; ++k) {
+      gg[j][k] = make_float2(one[2 * k], one[2 * k + 1]);
+      sg[j][k] = sb[j][k] = make_float2(0.f, 0.f);
+    }
   }
   float m = mean[blockIdx.x], r = rstd[blockIdx.x];
   bool failed = false;
@@ -348,27 +479,28 @@ ln_grad_ring_kernel(const T* __restrict__ dY, int64_t ld_dy, const T* __restrict
     if (i + 1 < mine) { m1 = mean[row + gridDim.x]; r1 = rstd[row + gridDim.x]; }
     const int s = (int)(i % stages);
     const bool ok = tc::mbar_wait(tc::smem_u32(&bars[s]), (uint32_t)(i / stages) & 1u, &abort_flag, status);
-    const T* xs = reinterpret_cast<const T*>(ring + (size_t)s * 2 * row_bytes);
-    const T* ys = xs + n;
-    float u[VPT][E], xh[VPT][E];
-    float2 t = make_float2(0.f, 0.f);
+    const uint4* xs = reinterpret_cast<const uint4*>(ring + (size_t)s * 2 * row_bytes);
+    const uint4* ys = xs + nv;
+    float2 u[VPT][P], xh[VPT][P];
+    float2 ta = make_float2(0.f, 0.f), tb = make_float2(0.f, 0.f);
 #pragma unroll
     for (int j = 0; j < VPT; ++j) {
       const int v = threadIdx.x + j * blockDim.x;
       if (v < nv) {
-        load_e<T, E>(xs + v * E, xh[j]);
-        load_e<T, E>(ys + v * E, u[j]);
+        unpack<T>(xs[v], xh[j]);
+        unpack<T>(ys[v], u[j]);
 #pragma unroll
-        for (int k = 0; k < E; ++k) {
-          xh[j][k] = (xh[j][k] - m) * r;
-          sg[j][k] = fmaf(u[j][k], xh[j][k], sg[j][k]);
-          sb[j][k] += u[j][k];
-          u[j][k] *= gg[j][k];
-          t.x += u[j][k];
-          t.y = fmaf(u[j][k], xh[j][k], t.y);
+        for (int k = 0; k < P; ++k) {
+          xh[j][k] = mul2(add2(xh[j][k], both(-m)), both(r));
+          sg[j][k] = fma2(u[j][k], xh[j][k], sg[j][k]);
+          sb[j][k] = add2(sb[j][k], u[j][k]);
+          u[j][k] = mul2(u[j][k], gg[j][k]);
+          ta = add2(ta, u[j][k]);
+          tb = fma2(u[j][k], xh[j][k], tb);
         }
       }
     }
+    float2 t = make_float2(ta.x + ta.y, tb.x + tb.y);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
       t.x += __shfl_xor_sync(0xffffffffu, t.x, o);
@@ -384,14 +516,15 @@ ln_grad_ring_kernel(const T* __restrict__ dY, int64_t ld_dy, const T* __restrict
     t = make_float2(0.f, 0.f);
     for (int w = 0; w < (int)(blockDim.x >> 5); ++w) { t.x += rd[w].x; t.y += rd[w].y; }
     if (dX) {
-      const float c1 = t.x / (float)n, c2 = t.y / (float)n;
+      const float2 c1 = both(-t.x / (float)n), c2 = both(-t.y / (float)n);
+      uint4* out = reinterpret_cast<uint4*>(dX + row * n);
 #pragma unroll
       for (int j = 0; j < VPT; ++j) {
         const int v = threadIdx.x + j * blockDim.x;
         if (v < nv) {
 #pragma unroll
-          for (int k = 0; k < E; ++k) u[j][k] = (u[j][k] - c1 - xh[j][k] * c2) * r;
-          store_e<T, E>(dX + row * n + (int64_t)v * E, u[j]);
+          for (int k = 0; k < P; ++k) u[j][k] = mul2(fma2(xh[j][k], c2, add2(u[j][k], c1)), both(r));
+          out[v] = pack<T>(u[j]);
         }
       }
     }
@@ -414,10 +547,78 @@ ln_grad_ring_kernel(const T* __restrict__ dY, int64_t ld_dy, const T* __restrict
     if (v < nv) {
       float* p = part + (int64_t)blockIdx.x * 2 * n + (int64_t)v * E;
 #pragma unroll
-      for (int k = 0; k < E; k += 4) {
-        *reinterpret_cast<float4*>(p + k) = make_float4(sg[j][k], sg[j][k + 1], sg[j][k + 2], sg[j][k + 3]);
-        *reinterpret_cast<float4*>(p + n + k) = make_float4(sb[j][k], sb[j][k + 1], sb[j][k + 2], sb[j][k + 3]);
+      for (int k = 0; k < P; k += 2) {
+        *reinterpret_cast<float4*>(p + 2 * k) = make_float4(sg[j][k].x, sg[j][k].y, sg[j][k + 1].x, sg[j][k + 1].y);
+        *reinterpret_cast<float4*>(p + n + 2 * k) = make_float4(sb[j][k].x, sb[j][k].y, sb[j][k + 1].x, sb[j][k + 1].y);
       }
+    }
+  }
+}
+
+// The same for rows that no 16-byte copy can start at: elements t, t + blockDim.x, ... of a thread, the next row's loaded
+// before this one's reduction.
+constexpr int ONE_THREADS = 512;
+
+template <typename T, typename TP, int VPT>
+__global__ void __launch_bounds__(ONE_THREADS)
+ln_grad_one_kernel(const T* __restrict__ dY, int64_t ld_dy, const T* __restrict__ X, int64_t ld, int64_t rows, int n,
+                   const TP* __restrict__ g, const float* __restrict__ mean, const float* __restrict__ rstd,
+                   T* __restrict__ dX, float* __restrict__ part) {
+  __shared__ float2 red[2][16];
+  pdl_wait();
+  pdl_trigger();
+  float gg[VPT], sg[VPT], sb[VPT], x1[VPT], y1[VPT];
+  float m1 = 0.f, r1 = 0.f;
+  auto fetch = [&](int64_t row) {
+    m1 = mean[row];
+    r1 = rstd[row];
+#pragma unroll
+    for (int j = 0; j < VPT; ++j) {
+      const int i = threadIdx.x + j * blockDim.x;
+      x1[j] = i < n ? to_f32<T>(X[row * ld + i]) : 0.f;
+      y1[j] = i < n ? to_f32<T>(dY[row * ld_dy + i]) : 0.f;
+    }
+  };
+  fetch(blockIdx.x);
+#pragma unroll
+  for (int j = 0; j < VPT; ++j) {
+    const int i = threadIdx.x + j * blockDim.x;
+    gg[j] = i < n ? param_at(g, i, 1.f) : 0.f;
+    sg[j] = sb[j] = 0.f;
+  }
+  int turn = 0;
+  for (int64_t row = blockIdx.x; row < rows; row += gridDim.x, turn ^= 1) {
+    const float r = r1;
+    float u[VPT], xh[VPT];
+    float2 t = make_float2(0.f, 0.f);
+#pragma unroll
+    for (int j = 0; j < VPT; ++j) {        // elements past the row: dY and gain are 0
+      xh[j] = (x1[j] - m1) * r;
+      sg[j] = fmaf(y1[j], xh[j], sg[j]);
+      sb[j] += y1[j];
+      u[j] = y1[j] * gg[j];
+      t.x += u[j];
+      t.y = fmaf(u[j], xh[j], t.y);
+    }
+    if (row + gridDim.x < rows) fetch(row + gridDim.x);
+    t = row_sum(t, red[turn]);
+    if (dX) {
+      t.x /= (float)n;
+      t.y /= (float)n;
+#pragma unroll
+      for (int j = 0; j < VPT; ++j) {
+        const int i = threadIdx.x + j * blockDim.x;
+        if (i < n) dX[row * n + i] = from_f32<T>((u[j] - t.x - xh[j] * t.y) * r);
+      }
+    }
+  }
+  if (!part) return;
+#pragma unroll
+  for (int j = 0; j < VPT; ++j) {
+    const int i = threadIdx.x + j * blockDim.x;
+    if (i < n) {
+      part[(int64_t)blockIdx.x * 2 * n + i] = sg[j];
+      part[((int64_t)blockIdx.x * 2 + 1) * n + i] = sb[j];
     }
   }
 }
@@ -451,6 +652,15 @@ int go_rows(Ctx* ctx, const RowShape& s, const void* X, int64_t rows, int n, int
   return ZOACT_OK;
 }
 
+template <typename T, typename TP, int VPT>
+int go_warp(Ctx* ctx, const void* X, int64_t rows, int n, int64_t ld, const void* g, const void* b, float eps, void* Y,
+            float* mean, float* rstd) {
+  ZOACT_CUDA_TRY(launch_pdl(ctx, ln_warp_kernel<T, TP, VPT>, dim3((unsigned)((rows + 3) / 4)), dim3(128), 0, (const T*)X, ld, rows,
+                            n, (const TP*)g, (const TP*)b, eps, (T*)Y, mean, rstd));
+  ++ctx->n_launch;
+  return ZOACT_OK;
+}
+
 template <typename T, typename TP, int E, int VPT>
 int go_grad_rows(Ctx* ctx, const RowShape& s, const void* dY, int64_t ld_dy, const void* X, int64_t rows, int n, int64_t ld,
                  const void* g, const float* mean, const float* rstd, void* dX) {
@@ -467,6 +677,14 @@ int run_ln(Ctx* ctx, const void* X, int64_t rows, int n, int64_t ld, const void*
   constexpr int E = 16 / (int)sizeof(T);
   RowShape s;
   const bool vec = n % E == 0 && ld % E == 0 && vec16(X) && vec16(Y) && vec16(g) && vec16(b);
+  // a warp a row where there are enough rows for that and a row fits in a warp's registers
+  if (vec && n / E <= 32 * 20 && rows >= 4 * (int64_t)ctx->sm_count) {
+    const int vpt = (n / E + 31) / 32;
+    if (vpt <= 4) return go_warp<T, TP, 4>(ctx, X, rows, n, ld, g, b, eps, Y, mean, rstd);
+    if (vpt <= 8) return go_warp<T, TP, 8>(ctx, X, rows, n, ld, g, b, eps, Y, mean, rstd);
+    if (vpt <= 16) return go_warp<T, TP, 16>(ctx, X, rows, n, ld, g, b, eps, Y, mean, rstd);
+    return go_warp<T, TP, 20>(ctx, X, rows, n, ld, g, b, eps, Y, mean, rstd);
+  }
   if (vec && row_shape(n / E, VEC_VPT, 3, most_threads(E, false), s)) {
     switch (s.vpt) {
       case 1: return go_rows<T, TP, E, 1>(ctx, s, X, rows, n, ld, g, b, eps, Y, mean, rstd);
@@ -484,7 +702,7 @@ int run_ln(Ctx* ctx, const void* X, int64_t rows, int n, int64_t ld, const void*
 }
 
 int join_parts(Ctx* ctx, const float* part, int parts, int n, float* dg, float* db) {
-  ZOACT_CUDA_TRY(launch_pdl(ctx, ln_join_kernel, dim3((unsigned)((2 * (int64_t)n + 31) / 32)), dim3(256), 0, part, parts, n, dg, db));
+  ZOACT_CUDA_TRY(launch_pdl(ctx, ln_join_kernel, dim3((unsigned)((2 * (int64_t)n + 31) / 32)), dim3(1024), 0, part, parts, n, dg, db));
   ++ctx->n_launch;
   return ZOACT_OK;
 }
@@ -513,6 +731,22 @@ int go_ring(Ctx* ctx, int threads, const void* dY, int64_t ld_dy, const void* X,
   return part ? join_parts(ctx, part, blocks, n, dg, db) : ZOACT_OK;
 }
 
+template <typename T, typename TP, int VPT>
+int go_one(Ctx* ctx, int threads, const void* dY, int64_t ld_dy, const void* X, int64_t rows, int n, int64_t ld, const void* g,
+           const float* mean, const float* rstd, void* dX, float* dg, float* db) {
+  const int64_t most = (int64_t)ctx->sm_count * (threads <= 256 ? 4 : 2);
+  const int blocks = (int)(rows < most ? rows : most);
+  float* part = nullptr;
+  if (dg || db) {
+    part = (float*)scratch(ctx, SLOT_LN, (size_t)blocks * 2 * n * 4);
+    if (!part) return ZOACT_ERR_NOMEM;
+  }
+  ZOACT_CUDA_TRY(launch_pdl(ctx, ln_grad_one_kernel<T, TP, VPT>, dim3((unsigned)blocks), dim3(threads), 0, (const T*)dY, ld_dy,
+                            (const T*)X, ld, rows, n, (const TP*)g, mean, rstd, (T*)dX, part));
+  ++ctx->n_launch;
+  return part ? join_parts(ctx, part, blocks, n, dg, db) : ZOACT_OK;
+}
+
 template <typename T, typename TP>
 int run_ln_grad(Ctx* ctx, const void* dY, int64_t ld_dy, const void* X, int64_t rows, int n, int64_t ld, const void* g,
                 const float* mean, const float* rstd, void* dX, float* dg, float* db) {
@@ -528,17 +762,13 @@ int run_ln_grad(Ctx* ctx, const void* dY, int64_t ld_dy, const void* X, int64_t 
           return go_ring<T, TP, 4>(ctx, s.threads, dY, ld_dy, X, rows, n, ld, g, mean, rstd, dX, dg, db);
     }
   }
+  if (rows > 0 && !vec && row_shape(n, ONE_VPT, 2, ONE_THREADS, s))
+    return s.vpt == 4 ? go_one<T, TP, 4>(ctx, s.threads, dY, ld_dy, X, rows, n, ld, g, mean, rstd, dX, dg, db)
+                      : go_one<T, TP, 16>(ctx, s.threads, dY, ld_dy, X, rows, n, ld, g, mean, rstd, dX, dg, db);
   int st = ZOACT_OK;
   if (dX && rows > 0) {
-    if (vec && row_shape(n / E, VEC_VPT, 3, most_threads(E, true), s)) {
-      switch (s.vpt) {
-        case 1: st = go_grad_rows<T, TP, E, 1>(ctx, s, dY, ld_dy, X, rows, n, ld, g, mean, rstd, dX); break;
-        case 2: st = go_grad_rows<T, TP, E, 2>(ctx, s, dY, ld_dy, X, rows, n, ld, g, mean, rstd, dX); break;
-        default: st = go_grad_rows<T, TP, E, 4>(ctx, s, dY, ld_dy, X, rows, n, ld, g, mean, rstd, dX); break;
-      }
-    } else if (row_shape(n, ONE_VPT, 2, most_threads(1, true), s)) {
-      st = s.vpt == 4 ? go_grad_rows<T, TP, 1, 4>(ctx, s, dY, ld_dy, X, rows, n, ld, g, mean, rstd, dX)
-                      : go_grad_rows<T, TP, 1, 16>(ctx, s, dY, ld_dy, X, rows, n, ld, g, mean, rstd, dX);
+    if (vec && row_shape(n / E, VEC_VPT, 3, most_threads(E, true), s)) {       // longer than the ring kernel's rows
+      st = go_grad_rows<T, TP, E, 4>(ctx, s, dY, ld_dy, X, rows, n, ld, g, mean, rstd, dX);
     } else {
       ZOACT_CUDA_TRY(launch_pdl(ctx, ln_grad_long_kernel<T, TP>, dim3((unsigned)rows), dim3(LN_THREADS), 0, (const T*)dY, ld_dy,
                                 (const T*)X, ld, n, (const TP*)g, mean, rstd, (T*)dX));
