@@ -58,7 +58,7 @@ struct Maps {
 struct Params {
   int num_m, num_n, num_kb, products, bn;
   int n_first;                      // tile order: along N first (the operand of M streams, that of N stays in L2), or along M
-  int group_kb;                     // K-blocks of one accumulation on the tensor core (EPI_ROW: all of a tile's)
+  int group_kb;                     // K-blocks of one accumulation on the tensor core
   int tail_first, tail_split;       // tiles from tail_first on run as tail_split pieces of K each
   int64_t M, N;
   int g_blocks;                     // blocks of 64 vocabulary entries of one part of G
@@ -389,56 +389,58 @@ __device__ __forceinline__ void epi_lanes(const Params& p, Exchange* ex, Part& a
 template <typename TO>
 __device__ __forceinline__ void epi_col(const Params& p, const Part& a, int half, int row_in_cta, uint32_t rank, int64_t m0,
                                         int64_t n0, int slot, float f) {
-  const int64_t m = m0 + row_in_cta;
-  const bool mok = m < p.M;
+  const int nch = p.bn / 32;
+  if (slot >= 0) {
+    float* d = p.tail_part + ((size_t)slot * p.bn + half * 32) * (2 * BM) + rank * BM + row_in_cta;
+#pragma unroll
+    for (int i = 0; i < CHUNKS; ++i) {
+      if (chunk_of<false>(half, i) >= nch) break;
+#pragma unroll
+      for (int j = 0; j < 32; ++j) d[(i * 64 + j) * (2 * BM)] = a.x[i][j];
+    }
+    return;
+  }
+  if (m0 + row_in_cta >= p.M) return;
+  TO* d = reinterpret_cast<TO*>(p.out) + (n0 + half * 32) * p.M + m0 + row_in_cta;
+  int left = (int)(p.N - n0 < p.bn ? p.N - n0 : p.bn) - half * 32;      // rows from this warpgroup's first chunk on
 #pragma unroll
   for (int i = 0; i < CHUNKS; ++i) {
-    const int c = chunk_of<false>(half, i);
-    if (c >= p.bn / 32) continue;
-    const int64_t n = n0 + c * 32;
-    if (slot >= 0) {
-      float* d = p.tail_part + ((size_t)slot * p.bn + c * 32) * (2 * BM) + rank * BM + row_in_cta;
 #pragma unroll
-      for (int j = 0; j < 32; ++j) d[j * (2 * BM)] = a.x[i][j];
-    } else if (mok) {
-      const int nv = (int)(p.N - n < 32 ? p.N - n : 32);
-      TO* d = reinterpret_cast<TO*>(p.out) + n * p.M + m;
-#pragma unroll
-      for (int j = 0; j < 32; ++j) {
-        if (j < nv) *d = from_f32<TO>(a.x[i][j] * f);
-        d += p.M;
-        asm volatile("" : "+l"(d));        // one address at a time: 32 of them do not fit beside the sums
-      }
+    for (int j = 0; j < 32; ++j) {
+      if (j < left) *d = from_f32<TO>(a.x[i][j] * f);
+      d += p.M;
+      asm volatile("" : "+l"(d));          // one address at a time: 32 of them do not fit beside the sums
     }
+    d += 32 * p.M;
+    left -= 64;
   }
 }
 
-// D scaled, through the warpgroup's two staging buffers in boxes of 128 bytes; one thread stores each pair of boxes (a tile
-// of 16-bit outputs is one pair: its only wait is for the tile before it).
+// D scaled, from the warpgroup's 128 columns through its two staging buffers in boxes of 128 bytes; one thread stores each pair
+// of boxes (16-bit outputs are one pair: the only wait is for the tile before).
 template <typename TO>
-__device__ __forceinline__ void epi_row(const Params& p, const Maps& tm, uint8_t* stg, int etid, int half, int row_in_cta,
-                                        int64_t m0, int64_t n0, float f, uint32_t t_row, bool& pending) {
-  constexpr int CC = 128 / (int)sizeof(TO);
-  const int wcols = p.bn / 2, cb = half * wcols;
+__device__ __forceinline__ void epi_row(const Params& p, const Maps& tm, uint8_t* stg, Part& a, int etid, int half,
+                                        int row_in_cta, int64_t m0, int64_t n0, float f, bool& pending) {
+  constexpr int CC = 128 / (int)sizeof(TO), PAIRS = 128 / (2 * CC);
   const bool issuer = (etid & 127) == 0;
   const uint32_t sbuf = tc::smem_u32(stg + half * 2 * STG_BYTES);
-  for (int c = 0; c < wcols; c += 2 * CC) {
-    const int64_t n = n0 + cb + c;
-    if (n >= p.N || m0 >= p.M) break;               // uniform over the warpgroup
-    if (issuer && pending) tc::bulk_wait_read0();   // the buffers' previous stores have read them
-    tc::named_bar_sync(4 + half, 128);
-#pragma unroll 1
-    for (int q = 0; q < 2 * CC && c + q < wcols; q += 32) {
-      float x[32];
-      tc::tmem_ld32(t_row + (uint32_t)(cb + c + q), x);
 #pragma unroll
-      for (int j = 0; j < 32; ++j) x[j] *= f;
-      pairtc::stage_granules<TO, 32>(sbuf + (uint32_t)(q / CC * STG_BYTES), row_in_cta, q % CC, x, true);
+  for (int c = 0; c < PAIRS; ++c) {
+    const int64_t n = n0 + half * 128 + c * 2 * CC;
+    if (n >= p.N || m0 >= p.M || half * 128 >= p.bn) break;      // uniform over the warpgroup
+    if (issuer && pending) tc::bulk_wait_read0();               // the buffers' previous stores have read them
+    tc::named_bar_sync(4 + half, 128);
+#pragma unroll
+    for (int i = c * 2 * CC / 32; i < (c + 1) * 2 * CC / 32; ++i) {
+#pragma unroll
+      for (int j = 0; j < 32; ++j) a.x[i][j] *= f;
+      const int q = i * 32 - c * 2 * CC;
+      pairtc::stage_granules<TO, 32>(sbuf + (uint32_t)(q / CC * STG_BYTES), row_in_cta, q % CC, a.x[i], true);
     }
     tc::fence_proxy_async_smem();
     tc::named_bar_sync(4 + half, 128);
     if (issuer) {
-      for (int b = 0; b < 2 && c + b * CC < wcols && n + b * CC < p.N; ++b) {
+      for (int b = 0; b < 2 && n + b * CC < p.N; ++b) {
         if (sizeof(TO) == 4 && p.add) tma_add_2d(&tm.out, (int32_t)(n + b * CC), (int32_t)m0, sbuf + b * STG_BYTES);
         else tc::tma_store_2d(&tm.out, (int32_t)(n + b * CC), (int32_t)m0, sbuf + b * STG_BYTES);
       }
@@ -587,21 +589,16 @@ ce_tc_kernel(const __grid_constant__ Maps tm, const Params p) {
     const uint32_t t_quad = tmem_base + ((uint32_t)(quad * 32) << 16);
     for (int u = cluster_id; unit_at(p, u, w); u += n_clusters) {
       const int64_t m0 = (int64_t)w.m * 2 * BM + (int64_t)rank * BM, n0 = (int64_t)w.n * p.bn;
-      if constexpr (EPI == EPI_ROW) {
-        if (!acc_wait(p, ss, r, etid, abort_flag)) break;
-        epi_row<TO>(p, tm, aux, etid, half, row_in_cta, m0, n0, f, t_quad + (uint32_t)(r.buf * p.bn), pending);
-        acc_free(ss, r, etid);
-        r.next(p.nbuf);
-      } else {
-        Part a;
-        if (!sum_groups<ROWS_M>(p, ss, w, etid, half, t_quad, abort_flag, r, a)) break;
-        if constexpr (EPI == EPI_COL)
-          epi_col<TO>(p, a, half, row_in_cta, rank, m0, n0, w.slot, f);
-        else if constexpr (ROWS_M)
-          epi_rows<EPI>(p, tm, aux, a, etid, half, row_in_cta, m0, n0 + half * 128, pending);
-        else
-          epi_lanes<EPI>(p, reinterpret_cast<Exchange*>(aux), a, half, quad, lane, m0, n0);
-      }
+      Part a;
+      if (!sum_groups<ROWS_M || EPI == EPI_ROW>(p, ss, w, etid, half, t_quad, abort_flag, r, a)) break;
+      if constexpr (EPI == EPI_ROW)
+        epi_row<TO>(p, tm, aux, a, etid, half, row_in_cta, m0, n0, f, pending);
+      else if constexpr (EPI == EPI_COL)
+        epi_col<TO>(p, a, half, row_in_cta, rank, m0, n0, w.slot, f);
+      else if constexpr (ROWS_M)
+        epi_rows<EPI>(p, tm, aux, a, etid, half, row_in_cta, m0, n0 + half * 128, pending);
+      else
+        epi_lanes<EPI>(p, reinterpret_cast<Exchange*>(aux), a, half, quad, lane, m0, n0);
     }
     if (pending) tc::bulk_wait0();
   }

@@ -40,6 +40,7 @@ enum ScratchSlot {
   SLOT_CE,           // cross entropy: count, target logits, row losses, the column tiles' maxima and sums
   SLOT_EMBED,        // embedding gradient: sorted tokens, sums of pieces of rows
   SLOT_LN,           // layer norm: sums of the gain's and the bias's gradient by block
+  SLOT_CE_SPLIT,     // its fp32 operands in three bf16 parts
   SLOT_CE_G,         // its gradient by the logits, for a chunk of rows
   SLOT_CE_TAIL,      // K pieces of the last tiles of its product by H
   SLOT_CE_DW,        // fp32 sums of dW over several chunks of rows

@@ -10,118 +10,7 @@
 namespace zoact {
 namespace {
 
-constexpr int TS = 64;              // tile of rows and of columns
-constexpr int TK = 16;
-constexpr int CE_THREADS = 256;     // 4 x 4 outputs a thread
-
-enum { MODE_CE = 0, MODE_G = 1, MODE_OUT = 2 };
-
-struct GemmArgs {
-  int64_t M, N, K;
-  int64_t sam, sak, sbn, sbk;       // element strides of A [M, K] and B [N, K]
-  // MODE_CE
-  float2* part;                     // [column tile][M]: maximum and sum of exp(z - maximum)
-  float* zt;                        // [M] the target's logit
-  const void* targets;
-  int id64;
-  int64_t T;
-  // MODE_G
-  const float2* stat;               // [M] the row's maximum and log sum exp(z - maximum)
-  float* G;
-  int64_t ldg;
-  // MODE_OUT
-  const float* alpha;               // device
-  const float* add;                 // [M, N] or nullptr
-  void* out;                        // [M, N]
-};
-
-__device__ __forceinline__ int64_t target_of(const GemmArgs& a, int64_t row, int64_t vocab) {
-  const int64_t t = load_id(a.targets, a.id64, row % a.T);
-  return t >= 0 && t < vocab ? t : -1;
-}
-
-// D[m, n] = sum_k A[m, k] B[n, k] in fp32, 64 x 64 a block; sums of 1024 products are added up by themselves (one chain
-// over a vocabulary of 2^20 erred by 3e-4 of the terms' magnitudes).
-template <int MODE, typename TA, typename TB, typename TO>
-__global__ void __launch_bounds__(CE_THREADS)
-ce_gemm_kernel(const TA* __restrict__ A, const TB* __restrict__ B, const GemmArgs a) {
-  pdl_wait();
-  pdl_trigger();
-  __shared__ float sa[TK][TS + 1], sb[TK][TS + 1];
-  const int64_t m0 = (int64_t)blockIdx.y * TS, n0 = (int64_t)blockIdx.x * TS;
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  float acc[4][4] = {}, sum[4][4] = {};
-  for (int64_t k0 = 0; k0 < a.K; k0 += TK) {
-    for (int e = threadIdx.x; e < TS * TK; e += CE_THREADS) {
-      const bool ak = a.sak == 1, bk = a.sbk == 1;       // the contiguous index varies fastest over the threads
-      const int am = ak ? e / TK : e % TS, ai = ak ? e % TK : e / TS;
-      const int bn = bk ? e / TK : e % TS, bi = bk ? e % TK : e / TS;
-      sa[ai][am] = m0 + am < a.M && k0 + ai < a.K ? to_f32<TA>(A[(m0 + am) * a.sam + (k0 + ai) * a.sak]) : 0.f;
-      sb[bi][bn] = n0 + bn < a.N && k0 + bi < a.K ? to_f32<TB>(B[(n0 + bn) * a.sbn + (k0 + bi) * a.sbk]) : 0.f;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < TK; ++k) {
-      float x[4], y[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) { x[i] = sa[k][ty * 4 + i]; y[i] = sb[k][tx * 4 + i]; }
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(x[i], y[j], acc[i][j]);
-    }
-    __syncthreads();
-    if (k0 / TK % 64 == 63 || k0 + TK >= a.K) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) { sum[i][j] += acc[i][j]; acc[i][j] = 0.f; }
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int64_t m = m0 + ty * 4 + i;
-    const bool mok = m < a.M;
-    if (MODE == MODE_CE) {
-      float mx = -INFINITY, s = 0.f;
-      const int64_t t = mok ? target_of(a, m, a.N) : -1;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int64_t n = n0 + tx * 4 + j;
-        if (n >= a.N) continue;
-        mx = fmaxf(mx, sum[i][j]);
-        if (n == t) a.zt[m] = sum[i][j];
-      }
-#pragma unroll
-      for (int o = 8; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (n0 + tx * 4 + j < a.N) s += expf(sum[i][j] - mx);
-#pragma unroll
-      for (int o = 8; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-      if (mok && tx == 0) a.part[(int64_t)blockIdx.x * a.M + m] = make_float2(mx, s);
-    } else if (MODE == MODE_G) {
-      if (!mok) continue;
-      const int64_t t = target_of(a, m, a.N);
-      const float2 st = a.stat[m];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int64_t n = n0 + tx * 4 + j;
-        if (n < a.N) a.G[m * a.ldg + n] = t < 0 ? 0.f : n == t ? expm1f((sum[i][j] - st.x) - st.y) : expf((sum[i][j] - st.x) - st.y);
-      }
-    } else {
-      if (!mok) continue;
-      const float f = *a.alpha;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int64_t n = n0 + tx * 4 + j;
-        if (n >= a.N) continue;
-        const float v = sum[i][j] * f + (a.add ? a.add[m * a.N + n] : 0.f);
-        reinterpret_cast<TO*>(a.out)[m * a.N + n] = from_f32<TO>(v);
-      }
-    }
-  }
-}
+constexpr int CE_THREADS = 256;
 
 // The tiles' maxima m_i and sums s_i of a row joined: m, log s with s = sum s_i exp(m_i - m) (a row that the model predicts
 // well has s = 1 + many terms that fp32 alone would drop one by one), lse = m + log s and loss = lse - z_t.
@@ -367,14 +256,6 @@ bool ce_scratch(Ctx* ctx, int64_t rows, int64_t part_rows, int64_t tiles, CeScra
   return true;
 }
 
-template <int MODE, typename TA, typename TB, typename TO>
-int gemm(Ctx* ctx, const void* A, const void* B, const GemmArgs& a) {
-  const dim3 grid((unsigned)((a.N + TS - 1) / TS), (unsigned)((a.M + TS - 1) / TS));
-  ZOACT_CUDA_TRY(launch_pdl(ctx, ce_gemm_kernel<MODE, TA, TB, TO>, grid, dim3(CE_THREADS), 0, (const TA*)A, (const TB*)B, a));
-  ++ctx->n_launch;
-  return ZOACT_OK;
-}
-
 // Join rows [r0, r0 + n), whose statistics lie at the beginning of s.part.
 int join(Ctx* ctx, const CeArgs& c, const CeScratch& s, int64_t tiles, int64_t r0, int64_t n, float* lse, float* loss) {
   // with several blocks the rows are all there; a chunk of rows (one block) takes its own targets
@@ -390,67 +271,6 @@ int join(Ctx* ctx, const CeArgs& c, const CeScratch& s, int64_t tiles, int64_t r
 int make_alpha(Ctx* ctx, const CeArgs& c, const CeScratch& s, float scale) {
   ZOACT_CUDA_TRY(launch_pdl(ctx, ce_alpha_kernel, dim3(1), dim3(1024), 0, c.targets, c.id64, c.T, c.vocab, scale, s.alpha));
   ++ctx->n_launch;
-  return ZOACT_OK;
-}
-
-template <typename T>
-int run_forward(Ctx* ctx, const CeArgs& c, const CeScratch& s, int64_t tiles, float* lse, float* loss) {
-  GemmArgs a = {};
-  a.M = c.rows; a.N = c.vocab; a.K = c.d;
-  a.sam = c.d; a.sak = 1; a.sbn = c.d; a.sbk = 1;
-  a.part = s.part; a.zt = s.zt; a.targets = c.targets; a.id64 = c.id64; a.T = c.T;
-  const int st = gemm<MODE_CE, T, T, T>(ctx, c.H, c.W, a);
-  if (st) return st;
-  return join(ctx, c, s, tiles, 0, c.rows, lse, loss);
-}
-
-template <typename T, typename TG>
-int run_backward(Ctx* ctx, const CeArgs& c, const CeScratch& s, void* dH, void* dW,
-                 int accumulate) {
-  const size_t most = (size_t)1 << 31;
-  int64_t chunk = (int64_t)(most / ((size_t)c.vocab * 4)) / TS * TS;
-  if (chunk < TS) chunk = TS;
-  if (chunk > c.rows) chunk = c.rows;
-  float* G = (float*)scratch(ctx, SLOT_CE_G, (size_t)chunk * c.vocab * 4);
-  if (!G) return ZOACT_ERR_NOMEM;
-  float* dWf = nullptr;             // fp32 sums of several chunks of rows
-  if (dW && sizeof(TG) != 4 && chunk < c.rows) {
-    dWf = (float*)scratch(ctx, SLOT_CE_DW, (size_t)c.vocab * c.d * 4);
-    if (!dWf) return ZOACT_ERR_NOMEM;
-  }
-  for (int64_t r0 = 0; r0 < c.rows; r0 += chunk) {
-    const int64_t n = c.rows - r0 < chunk ? c.rows - r0 : chunk;
-    const T* H = (const T*)c.H + r0 * c.d;
-    GemmArgs a = {};
-    a.M = n; a.N = c.vocab; a.K = c.d;
-    a.sam = c.d; a.sak = 1; a.sbn = c.d; a.sbk = 1;
-    a.targets = (const char*)c.targets + r0 * (c.id64 ? 8 : 4); a.id64 = c.id64; a.T = c.T;
-    a.stat = s.stat + r0; a.G = G; a.ldg = c.vocab;
-    int st = gemm<MODE_G, T, T, T>(ctx, H, c.W, a);
-    if (st) return st;
-    a.alpha = s.alpha;
-    if (dH) {
-      a.M = n; a.N = c.d; a.K = c.vocab;
-      a.sam = c.vocab; a.sak = 1; a.sbn = 1; a.sbk = c.d;
-      a.out = (T*)dH + r0 * c.d; a.add = nullptr;
-      st = gemm<MODE_OUT, float, T, T>(ctx, G, c.W, a);
-      if (st) return st;
-    }
-    if (dW) {
-      a.M = c.vocab; a.N = c.d; a.K = n;
-      a.sam = 1; a.sak = c.vocab; a.sbn = 1; a.sbk = c.d;
-      const bool last = r0 + n == c.rows;
-      if (dWf) {
-        a.add = r0 ? dWf : nullptr;
-        a.out = last ? dW : dWf;
-      } else {
-        a.out = dW;
-        a.add = r0 || accumulate ? (const float*)dW : nullptr;   // several chunks or accumulate: dW is fp32
-      }
-      st = dWf && !last ? gemm<MODE_OUT, float, T, float>(ctx, G, H, a) : gemm<MODE_OUT, float, T, TG>(ctx, G, H, a);
-      if (st) return st;
-    }
-  }
   return ZOACT_OK;
 }
 
@@ -474,16 +294,94 @@ __global__ void __launch_bounds__(CE_THREADS) ce_round_kernel(const float4* __re
   }
 }
 
-// 16-bit operands: the products on the tensor cores.  Where the gradient is asked for, chunk by chunk of rows: logits, whose
-// exponentials are kept in 16 bits, the rows' sums, G in place, and its two products.
+// fp32 operands in three bf16 parts: rows of W and then of H [., d] to [3][rows][ld] each, ld = d rounded up to 8 (what lies
+// past d is not read).  blockIdx.y: row (its blocks stride over the rows); four elements a thread.
+__global__ void __launch_bounds__(CE_THREADS)
+ce_split_kernel(const float* __restrict__ W, int64_t w_rows, uint16_t* __restrict__ W3, const float* __restrict__ H,
+                int64_t h_rows, uint16_t* __restrict__ H3, int d, int ld) {
+  pdl_wait();
+  pdl_trigger();
+  const int c4 = d / 4;
+  const int64_t total = (w_rows + h_rows) * c4;
+  for (int64_t i = (int64_t)blockIdx.x * CE_THREADS + threadIdx.x; i < total; i += (int64_t)gridDim.x * CE_THREADS) {
+    int64_t row = i / c4;
+    const int c = (int)(i - row * c4) * 4;
+    const bool of_w = row < w_rows;
+    if (!of_w) row -= w_rows;
+    float4 v = *reinterpret_cast<const float4*>((of_w ? W : H) + row * d + c);
+    uint16_t* o = (of_w ? W3 : H3) + row * ld + c;
+    const int64_t part = (of_w ? w_rows : h_rows) * ld;
+#pragma unroll
+    for (int p = 0; p < 3; ++p) {
+      const uint32_t lo = next_part_bf16x2(v.x, v.y), hi = next_part_bf16x2(v.z, v.w);
+      *reinterpret_cast<uint2*>(o + p * part) = make_uint2(lo, hi);
+    }
+  }
+}
+
+// fp32: the kept logits of a chunk of rows, [blocks][rows][64], to G = exp(z - lse) - onehot in three bf16 parts of the same
+// layout.  Thread: 4 entries of a row.
+__global__ void __launch_bounds__(CE_THREADS)
+ce_split_g_kernel(const float* __restrict__ Z, uint16_t* __restrict__ G, int64_t blocks, int64_t rows,
+                  const float2* __restrict__ stat, const void* __restrict__ targets, int id64, int64_t vocab) {
+  pdl_wait();
+  pdl_trigger();
+  const int64_t n4 = blocks * rows * 16;
+  for (int64_t i = (int64_t)blockIdx.x * CE_THREADS + threadIdx.x; i < n4; i += (int64_t)gridDim.x * CE_THREADS) {
+    const int64_t line = i / 16, blk = line / rows, row = line - blk * rows, v0 = blk * 64 + (i - line * 16) * 4;
+    const int64_t t = load_id(targets, id64, row);
+    float e[4] = {0.f, 0.f, 0.f, 0.f};
+    if (t >= 0 && t < vocab && v0 < vocab) {
+      const float4 z = *reinterpret_cast<const float4*>(Z + i * 4);
+      const float2 st = stat[row];
+      const float x[4] = {z.x, z.y, z.z, z.w};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float y = (x[k] - st.x) - st.y;
+        e[k] = v0 + k >= vocab ? 0.f : v0 + k == t ? expm1f(y) : expf(y);
+      }
+    }
+#pragma unroll
+    for (int p = 0; p < 3; ++p) {
+      const uint32_t lo = next_part_bf16x2(e[0], e[1]), hi = next_part_bf16x2(e[2], e[3]);
+      *reinterpret_cast<uint2*>(G + (p * blocks * rows + line) * 64 + (i - line * 16) * 4) = make_uint2(lo, hi);
+    }
+  }
+}
+
+unsigned stride_blocks(const Ctx* ctx, int64_t items) {
+  const int64_t blocks = (items + CE_THREADS - 1) / CE_THREADS, most = (int64_t)ctx->sm_count * 32;
+  return (unsigned)(blocks < most ? blocks : most);
+}
+
+// What the rows [r0, r0 + n) of a 16-bit call keep of their logits, to G.
 template <typename T>
-int run_tc(Ctx* ctx, const CeArgs& c) {
+int make_g(Ctx* ctx, const CeArgs& c, const CeScratch& s, const ce::Blocks& G, int64_t r0, int64_t n, const void* targets) {
+  const int64_t row_groups = (n + 32 * SCALE_ROWS - 1) / (32 * SCALE_ROWS), blocks = G.blocks();
+  for (int64_t b = 0; b < blocks; b += 65535) {
+    const int64_t nb = blocks - b < 65535 ? blocks - b : 65535;
+    ZOACT_CUDA_TRY(launch_pdl(ctx, ce_scale_kernel<T>, dim3((unsigned)row_groups, (unsigned)nb), dim3(CE_THREADS), 0, G.p, b, n,
+                              (const float2*)s.part, s.part_ld, (const float2*)s.stat + r0, (const float*)s.zt + r0, targets,
+                              c.id64, c.vocab));
+    ++ctx->n_launch;
+  }
+  return ZOACT_OK;
+}
+
+// The products on the tensor cores; fp32 operands in three bf16 parts.  Where the gradient is asked for, chunk by chunk of
+// rows: logits, of which 16 bits (fp32: all) are kept, the rows' sums, G, and its two products.
+template <typename T>
+int run(Ctx* ctx, const CeArgs& c) {
   using ce::Operand;
+  constexpr bool F32 = sizeof(T) == 4;
+  constexpr int PARTS = F32 ? 3 : 1;
+  const int optype = F32 ? ZOACT_DT_BF16 : c.dtype;
   const int64_t tiles = (c.vocab + ce::V_TILE - 1) / ce::V_TILE, blocks = (c.vocab + 63) / 64;
   const bool grad = c.dH || c.dW;
+  const size_t row_bytes = (size_t)blocks * 64 * (F32 ? 10 : 2);       // of G (fp32: the logits and three parts)
   int64_t chunk = c.rows;
   if (grad) {
-    chunk = (int64_t)(((size_t)1 << 31) / ((size_t)blocks * 128)) / 256 * 256;
+    chunk = (int64_t)(((size_t)1 << 31) / row_bytes) / 256 * 256;
     if (chunk < 256) chunk = 256;
     if (chunk > c.rows) chunk = c.rows;
   }
@@ -491,20 +389,29 @@ int run_tc(Ctx* ctx, const CeArgs& c) {
   if (!ce_scratch(ctx, c.rows, chunk, tiles, s)) return ZOACT_ERR_NOMEM;
   float* lse = c.lse ? c.lse : s.lse;
   float* loss = c.loss ? c.loss : s.loss;
-  const Operand W = {c.W, c.dtype, c.vocab, c.d, c.d, 1, c.vocab * c.d};
+  Operand W = {c.W, optype, c.vocab, c.d, c.d, 1, c.vocab * c.d}, H = {c.H, optype, c.rows, c.d, c.d, 1, c.rows * c.d};
+  if constexpr (F32) {
+    const int64_t ld = (c.d + 7) / 8 * 8;
+    uint16_t* W3 = (uint16_t*)scratch(ctx, SLOT_CE_SPLIT, (size_t)(c.vocab + c.rows) * ld * 6);
+    if (!W3) return ZOACT_ERR_NOMEM;
+    uint16_t* H3 = W3 + 3 * c.vocab * ld;
+    ZOACT_CUDA_TRY(launch_pdl(ctx, ce_split_kernel, dim3(stride_blocks(ctx, (c.vocab + c.rows) * (c.d / 4))), dim3(CE_THREADS), 0,
+                              (const float*)c.W, c.vocab, W3, (const float*)c.H, c.rows, H3, c.d, (int)ld));
+    ++ctx->n_launch;
+    W = {W3, optype, c.vocab, c.d, ld, 3, c.vocab * ld};
+    H = {H3, optype, c.rows, c.d, ld, 3, c.rows * ld};
+  }
   int st;
   if (!grad) {
-    const Operand H = {c.H, c.dtype, c.rows, c.d, c.d, 1, c.rows * c.d};
     st = ce::launch_logits(ctx, W, H, s.part, s.part_ld, s.zt, c.targets, c.id64, c.T, ce::KEEP_NONE, ce::Blocks{});
     if (!st) st = join(ctx, c, s, tiles, 0, c.rows, lse, loss);
     return st ? st : finish(ctx, c, loss);
   }
-  void* G = scratch(ctx, SLOT_CE_G, (size_t)chunk * blocks * 128);
-  if (!G) return ZOACT_ERR_NOMEM;
+  char* kept = (char*)scratch(ctx, SLOT_CE_G, (size_t)chunk * row_bytes);
+  if (!kept) return ZOACT_ERR_NOMEM;
   // several chunks add to dW in fp32: a 16-bit dW is rounded from the whole sum
-  const bool parts = chunk < c.rows;
   float* dWf = nullptr;
-  if (c.dW && parts && c.wgdtype != ZOACT_DT_FP32) {
+  if (c.dW && chunk < c.rows && c.wgdtype != ZOACT_DT_FP32) {
     dWf = (float*)scratch(ctx, SLOT_CE_DW, (size_t)c.vocab * c.d * 4);
     if (!dWf) return ZOACT_ERR_NOMEM;
   }
@@ -512,48 +419,38 @@ int run_tc(Ctx* ctx, const CeArgs& c) {
   if (st) return st;
   for (int64_t r0 = 0; r0 < c.rows; r0 += chunk) {
     const int64_t n = c.rows - r0 < chunk ? c.rows - r0 : chunk;
-    const Operand H = {(const T*)c.H + r0 * c.d, c.dtype, n, c.d, c.d, 1, n * c.d};
-    const ce::Blocks Gm = {G, c.dtype, n, c.vocab, 1};
+    Operand Hc = H;
+    Hc.p = (const uint16_t*)H.p + r0 * H.ld;
+    Hc.rows = n;
+    ce::Blocks G = {kept, optype, n, c.vocab, PARTS};
     const void* targets = (const char*)c.targets + r0 * (c.id64 ? 8 : 4);
-    st = ce::launch_logits(ctx, W, H, s.part, s.part_ld, s.zt + r0, targets, c.id64, c.T, ce::KEEP_LOG, Gm);
+    st = ce::launch_logits(ctx, W, Hc, s.part, s.part_ld, s.zt + r0, targets, c.id64, c.T, F32 ? ce::KEEP_Z : ce::KEEP_LOG, G);
     if (!st) st = join(ctx, c, s, tiles, r0, n, lse, loss);
     if (st) return st;
-    const int64_t row_groups = (n + 32 * SCALE_ROWS - 1) / (32 * SCALE_ROWS);
-    for (int64_t b = 0; b < blocks; b += 65535) {
-      const int64_t nb = blocks - b < 65535 ? blocks - b : 65535;
-      ZOACT_CUDA_TRY(launch_pdl(ctx, ce_scale_kernel<T>, dim3((unsigned)row_groups, (unsigned)nb), dim3(CE_THREADS), 0, G, b, n,
-                                (const float2*)s.part, s.part_ld, (const float2*)s.stat + r0, (const float*)s.zt + r0, targets,
-                                c.id64, c.vocab));
+    if constexpr (F32) {
+      G.p = kept + (size_t)blocks * n * 64 * 4;
+      ZOACT_CUDA_TRY(launch_pdl(ctx, ce_split_g_kernel, dim3(stride_blocks(ctx, blocks * n * 16)), dim3(CE_THREADS), 0,
+                                (const float*)kept, (uint16_t*)G.p, blocks, n, (const float2*)s.stat + r0, targets, c.id64,
+                                c.vocab));
       ++ctx->n_launch;
+    } else {
+      st = make_g<T>(ctx, c, s, G, r0, n, targets);
     }
-    if (c.dH) st = ce::launch_by_h(ctx, W, Gm, s.alpha, (T*)c.dH + r0 * c.d, c.dtype);
+    if (!st && c.dH) st = ce::launch_by_h(ctx, W, G, s.alpha, (T*)c.dH + r0 * c.d, c.dtype);
     if (!st && c.dW)
-      st = ce::launch_by_w(ctx, Gm, H, s.alpha, dWf ? (void*)dWf : c.dW, dWf ? ZOACT_DT_FP32 : c.wgdtype,
+      st = ce::launch_by_w(ctx, G, Hc, s.alpha, dWf ? (void*)dWf : c.dW, dWf ? ZOACT_DT_FP32 : c.wgdtype,
                            r0 > 0 || c.accumulate);
     if (st) return st;
   }
-  if (dWf) {
-    const int64_t total = c.vocab * c.d / 4;        // d is a multiple of 8
-    const int64_t blocks = (total + CE_THREADS - 1) / CE_THREADS;
-    ZOACT_CUDA_TRY(launch_pdl(ctx, ce_round_kernel<T>, dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(CE_THREADS), 0,
-                              (const float4*)dWf, total, (T*)c.dW));
-    ++ctx->n_launch;
+  if constexpr (!F32) {
+    if (dWf) {
+      const int64_t total = c.vocab * c.d / 4;      // d is a multiple of 8
+      ZOACT_CUDA_TRY(launch_pdl(ctx, ce_round_kernel<T>, dim3(stride_blocks(ctx, total)), dim3(CE_THREADS), 0, (const float4*)dWf,
+                                total, (T*)c.dW));
+      ++ctx->n_launch;
+    }
   }
   return finish(ctx, c, loss);
-}
-
-// fp32 operands.
-int run_fp32(Ctx* ctx, const CeArgs& c) {
-  const int64_t tiles = (c.vocab + TS - 1) / TS;
-  CeScratch s;
-  if (!ce_scratch(ctx, c.rows, c.rows, tiles, s)) return ZOACT_ERR_NOMEM;
-  float* lse = c.lse ? c.lse : s.lse;
-  float* loss = c.loss ? c.loss : s.loss;
-  int st = run_forward<float>(ctx, c, s, tiles, lse, loss);
-  if (!st) st = finish(ctx, c, loss);
-  if (st || (!c.dH && !c.dW)) return st;
-  st = make_alpha(ctx, c, s, c.grad_scale);
-  return st ? st : run_backward<float, float>(ctx, c, s, c.dH, c.dW, c.accumulate);
 }
 
 }  // namespace
@@ -565,9 +462,9 @@ int launch_ce(Ctx* ctx, const CeArgs& c) {
     return finish(ctx, c, nullptr);
   }
   switch (c.dtype) {
-    case ZOACT_DT_FP32: return run_fp32(ctx, c);
-    case ZOACT_DT_BF16: return run_tc<__nv_bfloat16>(ctx, c);
-    default: return run_tc<__half>(ctx, c);
+    case ZOACT_DT_FP32: return run<float>(ctx, c);
+    case ZOACT_DT_BF16: return run<__nv_bfloat16>(ctx, c);
+    default: return run<__half>(ctx, c);
   }
 }
 

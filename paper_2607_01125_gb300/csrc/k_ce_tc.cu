@@ -7,9 +7,9 @@ namespace ce {
 namespace {
 
 // K-blocks of 64 that the tensor core sums by itself, at most: its cut-off costs about 1.6e-8 of the sum for each 16 products,
-// and reading a group's sum about 300 cycles of it.  Logits end in fp32 (12 blocks: 7e-7; 8 cost 2% more time); the product by
-// H ends in 16 bits (64: 4e-6).
-constexpr int LOGIT_GROUP = 12, BY_H_GROUP = 64;
+// and reading a group's sum about 300 cycles of it.  Logits end in fp32 (12 blocks: 7e-7; 8 cost 2% more time); products that
+// end in 16 bits take 64 (4e-6), and fp32 operands, whose six products are summed alike, 4 (3e-7).
+constexpr int LOGIT_GROUP = 12, GRAD_GROUP = 64, FP32_GROUP = 4;
 constexpr double ROWS_M_GAIN = 1.15;
 
 int even_groups(int kb, int most) {
@@ -140,7 +140,7 @@ int launch_logits(Ctx* ctx, const Operand& W, const Operand& H, float2* part, in
   p.num_n = (int)((p.N + p.bn - 1) / p.bn);
   p.num_kb = (int)((W.cols + BK - 1) / BK);
   p.products = W.parts == 3 ? 6 : 1;
-  p.group_kb = even_groups(p.num_kb * p.products, LOGIT_GROUP);
+  p.group_kb = even_groups(p.num_kb * p.products, p.products > 1 ? FP32_GROUP : LOGIT_GROUP);
   p.nbuf = buffers(p.bn);
   p.tail_first = p.num_m * p.num_n; p.tail_split = 1;
   p.bf16 = W.dtype == ZOACT_DT_BF16; p.status = ctx->d_status;
@@ -167,7 +167,7 @@ int launch_by_h(Ctx* ctx, const Operand& W, const Blocks& G, const float* alpha,
   p.num_kb = (int)G.blocks();
   p.g_blocks = p.num_kb;
   p.products = W.parts == 3 ? 6 : 1;
-  p.group_kb = even_groups(p.num_kb * p.products, BY_H_GROUP);
+  p.group_kb = even_groups(p.num_kb * p.products, p.products > 1 ? FP32_GROUP : GRAD_GROUP);
   // the tail is cut along K: only the rows' padding counts
   p.bn = tile_rows(ctx, 1 << 20, p.N, nullptr);
   p.nbuf = buffers(p.bn);
@@ -198,7 +198,7 @@ int launch_by_w(Ctx* ctx, const Blocks& G, const Operand& H, const float* alpha,
   p.num_kb = (int)((H.rows + BK - 1) / BK);
   p.g_blocks = (int)G.blocks();
   p.products = H.parts == 3 ? 6 : 1;
-  p.group_kb = p.num_kb * p.products;
+  p.group_kb = even_groups(p.num_kb * p.products, p.products > 1 ? FP32_GROUP : GRAD_GROUP);
   p.tail_first = p.num_m * p.num_n; p.tail_split = 1;
   p.bf16 = H.dtype == ZOACT_DT_BF16; p.status = ctx->d_status;
   p.alpha = alpha; p.out = out; p.add = add;
