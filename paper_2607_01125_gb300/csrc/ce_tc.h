@@ -34,8 +34,9 @@ int launch_logits(Ctx* ctx, const Operand& W, const Operand& H, float2* part, in
                   int id64, int64_t T, int keep, const Blocks& G);
 // out [G.rows, W.cols] of dtype = alpha G W.
 int launch_by_h(Ctx* ctx, const Operand& W, const Blocks& G, const float* alpha, void* out, int dtype);
-// out [G.vocab, H.cols] of dtype = alpha G^T H, added to out (fp32) with add.
-int launch_by_w(Ctx* ctx, const Blocks& G, const Operand& H, const float* alpha, void* out, int dtype, int add);
+// out [G.vocab, H.cols] of dtype = alpha G^T H, added to out (fp32) with add; rows without a target are not taken.
+int launch_by_w(Ctx* ctx, const Blocks& G, const Operand& H, const void* targets, int id64, const float* alpha, void* out,
+                int dtype, int add);
 
 }  // namespace ce
 }  // namespace zoact

@@ -8,9 +8,10 @@
 // Rows on the N side make the padding of a ragged or small batch cheap (tiles of 32 to 256 rows in steps of 32); there the
 // logits' statistics reduce by a butterfly of shuffles that leaves lane l with column l of 32, which a thread that owns a
 // row does without: a tile's epilogue took 13 000 cycles with shuffles, more than two groups of the main loop.
-// W and H are read as they lie: K-major tiles as rows of 64 elements, and the transposed ones (W and H by columns) as M- or
-// N-major tiles, 64 x 64 boxes whose descriptors step by boxes along M or N and by 8 K rows along K.  G, which only these
-// kernels see, lies in blocks of 64 vocabulary entries, [block][row][64]: every box of it is contiguous.
+// W is read as it lies: as rows of 64 elements, and by columns as M-major tiles, 64 x 64 boxes whose descriptors step by boxes
+// along M and by 8 K rows along K.  G, which only these kernels see, lies in blocks of 64 vocabulary entries,
+// [block][row][64]: every box of it is contiguous, and M-major for the product by W.  H is small and is transposed for that one
+// (read by columns as an N-major tile beside the M-major one, it ran at 1630 TFLOP/s).
 // fp32 operands come as three bf16 parts each (24 bits); six products of parts run as six passes over K into one accumulator.
 //
 // The tensor core cuts its running fp32 sum off at every step of 16 products instead of rounding it: 4096 products of logits
@@ -37,8 +38,8 @@ constexpr int EPI_THREADS = 256, EPI_BASE = 128, THREADS = EPI_BASE + EPI_THREAD
 constexpr int REGS_ISSUE = 56, REGS_EPI = 224;
 constexpr int TMEM_COLS = 512, MAX_BUF = 4;
 constexpr int STG_BYTES = 16384;                          // a staging buffer (128 rows x 128 bytes)
-// Epilogue area beside the ring: a staging buffer for each warpgroup, or two where all that the epilogue does is to store.
-__host__ __device__ constexpr int aux_bytes(int epi) { return epi == 4 ? 4 * STG_BYTES : 2 * STG_BYTES; }
+// Epilogue area beside the ring: a staging buffer for each warpgroup, or two.
+__host__ __device__ constexpr int aux_bytes(int epi) { return epi == 5 ? 4 * STG_BYTES : 2 * STG_BYTES; }
 __host__ __device__ constexpr int ring_bytes(int epi) { return 229376 - aux_bytes(epi); }
 constexpr int SMEM_BYTES = 1024 + 229376 + 256;
 static_assert(SMEM_BYTES <= 232448, "dynamic shared memory above the 227 KB a CTA may use");
@@ -48,7 +49,8 @@ enum Epi {
   EPI_LOG,       // and the tile's maximum - z as 16-bit fixed point
   EPI_Z,         // and z in fp32
   EPI_COL,       // D^T scaled
-  EPI_ROW        // D scaled
+  EPI_ROW,       // D scaled, from registers
+  EPI_ROW_STAGED // the same through shared memory
 };
 
 struct Maps {
@@ -78,7 +80,7 @@ struct Params {
   const float* alpha;
   void* out;                        // EPI_COL: [N, M]
   float* tail_part;                 // pieces of the tail's tiles: [piece][tile][bn][256]
-  int add;                          // EPI_ROW: add to out (fp32)
+  int add, out_32;                  // EPI_ROW: add to out (fp32); out and its rows lie on 32 bytes
 };
 
 struct Shared {
@@ -198,11 +200,14 @@ template <bool ADJACENT>
 __device__ __forceinline__ bool sum_groups(const Params& p, Shared* ss, const Unit& w, int etid, int half, uint32_t t_quad,
                                            volatile int* abort_flag, Ring& r, Part& a) {
   const int nch = p.bn / 32;
+#pragma unroll
+  for (int i = 0; i < CHUNKS; ++i)
+#pragma unroll
+    for (int j = 0; j < 32; ++j) a.x[i][j] = 0.f;
 #pragma unroll 1
   for (int kb = w.kb0; kb < w.kb1; kb += p.group_kb) {
     if (!acc_wait(p, ss, r, etid, abort_flag)) return false;
     const uint32_t t = t_quad + (uint32_t)(r.buf * p.bn);
-    const bool first = kb == w.kb0;
 #pragma unroll
     for (int i = 0; i < CHUNKS; ++i) {
       const int c = chunk_of<ADJACENT>(half, i);
@@ -210,7 +215,7 @@ __device__ __forceinline__ bool sum_groups(const Params& p, Shared* ss, const Un
         float y[32];
         tc::tmem_ld32(t + (uint32_t)(c * 32), y);
 #pragma unroll
-        for (int j = 0; j < 32; ++j) a.x[i][j] = first ? y[j] : a.x[i][j] + y[j];
+        for (int j = 0; j < 32; ++j) a.x[i][j] += y[j];
       }
     }
     acc_free(ss, r, etid);
@@ -416,10 +421,63 @@ __device__ __forceinline__ void epi_col(const Params& p, const Part& a, int half
   }
 }
 
-// D scaled, from the warpgroup's 128 columns through its two staging buffers in boxes of 128 bytes; one thread stores each pair
-// of boxes (16-bit outputs are one pair: the only wait is for the tile before).
+// 32 bytes of one thread, or two halves where a row does not lie on 32 bytes.
+__device__ __forceinline__ void store_32(void* p, const uint32_t* w, bool whole) {
+  if (whole) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]),
+                 "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+                 : "memory");
+  } else {
+    reinterpret_cast<uint4*>(p)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+    reinterpret_cast<uint4*>(p)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+  }
+}
+
+// D scaled, from registers: a thread has a row's 128 columns of its warpgroup and writes them in whole sectors.  Staged in
+// shared memory for bulk stores, a tile's 64 KB of writes and reads there add 2600 cycles to a main loop that is bound by the
+// same memory (the gradient for W alone, 4096 x 128256 in bf16: 768 rows 1202 us for 1136, 2048 rows 2873 for 2847).  Where K
+// is short the output's bytes are the bound, and boxes of 128 rows reach DRAM in better order (1 row: 359 us for 490, 256 rows
+// 500 for 576), so both stay: see STAGED_BELOW.
 template <typename TO>
-__device__ __forceinline__ void epi_row(const Params& p, const Maps& tm, uint8_t* stg, Part& a, int etid, int half,
+__device__ __forceinline__ void epi_row(const Params& p, const Part& a, int half, int row_in_cta, int64_t m0, int64_t n0, float f) {
+  const int64_t m = m0 + row_in_cta, n = n0 + half * 128;
+  if (m >= p.M) return;
+  TO* d = reinterpret_cast<TO*>(p.out) + m * p.N + n;
+  constexpr int PER = 32 / (int)sizeof(TO);          // elements of a store
+  const int left = (int)(p.N - n < 128 ? p.N - n : 128);
+  const bool whole = p.out_32 != 0;
+#pragma unroll
+  for (int i = 0; i < CHUNKS; ++i) {
+    if (half * 128 + i * 32 >= p.bn) break;
+#pragma unroll
+    for (int j = 0; j < 32; j += PER) {
+      const int c = i * 32 + j;
+      if (c >= left) break;
+      uint32_t w[8];
+      if constexpr (sizeof(TO) == 2) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) w[k] = pairtc::pack2(a.x[i][j + 2 * k] * f, a.x[i][j + 2 * k + 1] * f, (TO*)nullptr);
+      } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) w[k] = __float_as_uint(a.x[i][j + k] * f);
+        if (p.add) {
+#pragma unroll
+          for (int k = 0; k < 8; ++k)
+            if (c + k < left) w[k] = __float_as_uint(__uint_as_float(w[k]) + d[c + k]);
+        }
+      }
+      if (c + PER <= left)
+        store_32(d + c, w, whole);
+      else                                 // the last columns: 16 bytes
+        *reinterpret_cast<uint4*>(d + c) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+  }
+}
+
+// The same through the warpgroup's two staging buffers in boxes of 128 bytes; one thread stores each pair of boxes (16-bit
+// outputs are one pair: the only wait is for the tile before).
+template <typename TO>
+__device__ __forceinline__ void epi_row_staged(const Params& p, const Maps& tm, uint8_t* stg, Part& a, int etid, int half,
                                         int row_in_cta, int64_t m0, int64_t n0, float f, bool& pending) {
   constexpr int CC = 128 / (int)sizeof(TO), PAIRS = 128 / (2 * CC);
   const bool issuer = (etid & 127) == 0;
@@ -455,9 +513,9 @@ template <int EPI, bool ROWS_M, typename TO>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
 ce_tc_kernel(const __grid_constant__ Maps tm, const Params p) {
   namespace tc2 = pairtc::tc2;
-  // by H: A = W by columns, B = G by rows; by W: A = G by columns, B = H by columns
-  constexpr bool A_MN = EPI == EPI_COL || EPI == EPI_ROW, B_MN = EPI == EPI_ROW;
-  constexpr bool A_BLOCKS = EPI == EPI_ROW, B_BLOCKS = EPI == EPI_COL;      // G
+  // by H: A = W by columns, B = G by rows; by W: A = G by columns, B = H^T by rows
+  constexpr bool BY_W = EPI == EPI_ROW || EPI == EPI_ROW_STAGED, A_MN = EPI == EPI_COL || BY_W;
+  constexpr bool A_BLOCKS = BY_W, B_BLOCKS = EPI == EPI_COL;                // G
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   uint8_t* aux = smem + ring_bytes(EPI);
@@ -481,7 +539,7 @@ ce_tc_kernel(const __grid_constant__ Maps tm, const Params p) {
     tc::fence_mbar_init();
     tc::prefetch_tmap(&tm.a);
     tc::prefetch_tmap(&tm.b);
-    if (EPI == EPI_ROW || (EPI == EPI_LOG && ROWS_M)) tc::prefetch_tmap(&tm.out);
+    if ((EPI == EPI_LOG && ROWS_M) || EPI == EPI_ROW_STAGED) tc::prefetch_tmap(&tm.out);
   }
   if (warp == 1) {
     tc2::tmem_alloc2(tc::smem_u32(&ss->tmem_base), TMEM_COLS);
@@ -528,9 +586,6 @@ ce_tc_kernel(const __grid_constant__ Maps tm, const Params p) {
           }
           if (B_BLOCKS) {
             tma_load_3d_pair(sb, &tm.b, 0, n0, kblk + pb * p.g_blocks, full_leader);
-          } else if (B_MN) {
-            for (int j = 0; j < bh / 64; ++j)
-              tma_load_3d_pair(sb + j * BOX_BYTES, &tm.b, n0 + 64 * j, k, pb, full_leader);
           } else {
             tma_load_3d_pair(sb, &tm.b, k, n0, pb, full_leader);
           }
@@ -545,7 +600,7 @@ ce_tc_kernel(const __grid_constant__ Maps tm, const Params p) {
       }
     } else if (warp == 1 && lane == 0 && leader) {
       // ---------------- MMA issuer (leader CTA) ----------------
-      const uint32_t idesc = tc::idesc_f16(2 * BM, p.bn, p.bf16) | (A_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u);
+      const uint32_t idesc = tc::idesc_f16(2 * BM, p.bn, p.bf16) | (A_MN ? 1u << 15 : 0u);
       int stage = 0;
       uint32_t phase = 0;
       bool ok = true, issued_any = false;
@@ -562,7 +617,7 @@ ce_tc_kernel(const __grid_constant__ Maps tm, const Params p) {
             const uint32_t sa = tc::smem_u32(smem + stage * sbytes), sb = sa + A_BYTES;
 #pragma unroll
             for (int k = 0; k < BK / 16; ++k)
-              tc2::mma2_f16(d_tmem, sdesc<A_MN>(sa, k), sdesc<B_MN>(sb, k), idesc, (kb != g0 || k != 0) ? 1u : 0u);
+              tc2::mma2_f16(d_tmem, sdesc<A_MN>(sa, k), tc::sdesc_k_sw128(sb + (uint32_t)k * 32u), idesc, (kb != g0 || k != 0) ? 1u : 0u);
             tc2::commit2_both(tc::smem_u32(&ss->empty[stage]));
             issued_any = true;
             if (++stage == p.stages) { stage = 0; phase ^= 1u; }
@@ -583,16 +638,18 @@ ce_tc_kernel(const __grid_constant__ Maps tm, const Params p) {
     const int etid = threadIdx.x - EPI_BASE, half = etid >> 7, quad = warp & 3;
     const int row_in_cta = quad * 32 + lane;
     float f = 0.f;
-    if (EPI == EPI_COL || EPI == EPI_ROW) f = __ldcg(p.alpha);
+    if (EPI == EPI_COL || BY_W) f = __ldcg(p.alpha);
     Ring r;
     bool pending = false;
     const uint32_t t_quad = tmem_base + ((uint32_t)(quad * 32) << 16);
     for (int u = cluster_id; unit_at(p, u, w); u += n_clusters) {
       const int64_t m0 = (int64_t)w.m * 2 * BM + (int64_t)rank * BM, n0 = (int64_t)w.n * p.bn;
       Part a;
-      if (!sum_groups<ROWS_M || EPI == EPI_ROW>(p, ss, w, etid, half, t_quad, abort_flag, r, a)) break;
+      if (!sum_groups<ROWS_M || BY_W>(p, ss, w, etid, half, t_quad, abort_flag, r, a)) break;
       if constexpr (EPI == EPI_ROW)
-        epi_row<TO>(p, tm, aux, a, etid, half, row_in_cta, m0, n0, f, pending);
+        epi_row<TO>(p, a, half, row_in_cta, m0, n0, f);
+      else if constexpr (EPI == EPI_ROW_STAGED)
+        epi_row_staged<TO>(p, tm, aux, a, etid, half, row_in_cta, m0, n0, f, pending);
       else if constexpr (EPI == EPI_COL)
         epi_col<TO>(p, a, half, row_in_cta, rank, m0, n0, w.slot, f);
       else if constexpr (ROWS_M)

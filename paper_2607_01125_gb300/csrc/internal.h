@@ -42,6 +42,7 @@ enum ScratchSlot {
   SLOT_LN,           // layer norm: sums of the gain's and the bias's gradient by block
   SLOT_CE_SPLIT,     // its fp32 operands in three bf16 parts
   SLOT_CE_G,         // its gradient by the logits, for a chunk of rows
+  SLOT_CE_HT,        // H by columns, for its product by W
   SLOT_CE_TAIL,      // K pieces of the last tiles of its product by H
   SLOT_CE_DW,        // fp32 sums of dW over several chunks of rows
   SLOT_COUNT

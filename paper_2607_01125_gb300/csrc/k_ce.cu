@@ -438,8 +438,8 @@ int run(Ctx* ctx, const CeArgs& c) {
     }
     if (!st && c.dH) st = ce::launch_by_h(ctx, W, G, s.alpha, (T*)c.dH + r0 * c.d, c.dtype);
     if (!st && c.dW)
-      st = ce::launch_by_w(ctx, G, Hc, s.alpha, dWf ? (void*)dWf : c.dW, dWf ? ZOACT_DT_FP32 : c.wgdtype,
-                           r0 > 0 || c.accumulate);
+      st = ce::launch_by_w(ctx, G, Hc, targets, c.id64, s.alpha, dWf ? (void*)dWf : c.dW,
+                           dWf ? ZOACT_DT_FP32 : c.wgdtype, r0 > 0 || c.accumulate);
     if (st) return st;
   }
   if constexpr (!F32) {

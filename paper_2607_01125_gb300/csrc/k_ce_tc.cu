@@ -11,6 +11,8 @@ namespace {
 // end in 16 bits take 64 (4e-6), and fp32 operands, whose six products are summed alike, 4 (3e-7).
 constexpr int LOGIT_GROUP = 12, GRAD_GROUP = 64, FP32_GROUP = 4;
 constexpr double ROWS_M_GAIN = 1.15;
+// K-blocks below which the product by W stores through shared memory: 384 rows 718 us for 753, 512 rows 850 for 838 (epi_row).
+constexpr int STAGED_BELOW = 8;
 
 int even_groups(int kb, int most) {
   const int groups = (kb + most - 1) / most;
@@ -187,11 +189,60 @@ int launch_by_h(Ctx* ctx, const Operand& W, const Blocks& G, const float* alpha,
   }
 }
 
-int launch_by_w(Ctx* ctx, const Blocks& G, const Operand& H, const float* alpha, void* out, int dtype, int add) {
+// Rows of H to columns: [parts][rows][cols] (rows ld_in apart) to [parts][cols][ld_out], 64 x 64 a block.  Rows without a
+// target become zeros: G's zeros would not take a NaN or an infinity out of the sum over the rows.
+__global__ void __launch_bounds__(256)
+ce_transpose_kernel(const uint16_t* __restrict__ in, int64_t rows, int cols, int64_t ld_in, int64_t part_in,
+                    uint16_t* __restrict__ out, int64_t ld_out, const void* __restrict__ targets, int id64, int64_t vocab) {
+  pdl_wait();
+  pdl_trigger();
+  __shared__ uint16_t t[64][66];
+  __shared__ bool counted[64];
+  const int64_t r0 = (int64_t)blockIdx.x * 64, c0 = (int64_t)blockIdx.y * 64;
+  in += blockIdx.z * part_in;
+  out += (int64_t)blockIdx.z * cols * ld_out;
+  const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
+  uint32_t in_w[8];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const int64_t r = r0 + y + 8 * k, c = c0 + 2 * x;
+    in_w[k] = 0;
+    if (r < rows && c < cols) in_w[k] = *reinterpret_cast<const uint32_t*>(in + r * ld_in + c);      // cols is even
+  }
+  if (threadIdx.x < 64) {
+    const int64_t id = r0 + threadIdx.x < rows ? load_id(targets, id64, r0 + threadIdx.x) : -1;
+    counted[threadIdx.x] = id >= 0 && id < vocab;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const uint32_t w = counted[y + 8 * k] ? in_w[k] : 0;
+    t[y + 8 * k][2 * x] = (uint16_t)w;
+    t[y + 8 * k][2 * x + 1] = (uint16_t)(w >> 16);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const int64_t c = c0 + y + 8 * k, r = r0 + 2 * x;
+    if (c < cols && r < ld_out)            // ld_out is even; past `rows` zeros, which are not read
+      *reinterpret_cast<uint32_t*>(out + c * ld_out + r) = (uint32_t)t[2 * x][y + 8 * k] | (uint32_t)t[2 * x + 1][y + 8 * k] << 16;
+  }
+}
+
+int launch_by_w(Ctx* ctx, const Blocks& G, const Operand& H, const void* targets, int id64, const float* alpha, void* out,
+                int dtype, int add) {
+  const int64_t ld = (H.rows + 7) / 8 * 8;
+  uint16_t* T = (uint16_t*)scratch(ctx, SLOT_CE_HT, (size_t)H.parts * H.cols * ld * 2);
+  if (!T) return ZOACT_ERR_NOMEM;
+  ZOACT_CUDA_TRY(launch_pdl(ctx, ce_transpose_kernel, dim3((unsigned)((H.rows + 63) / 64), (unsigned)((H.cols + 63) / 64), H.parts),
+                            dim3(256), 0, (const uint16_t*)H.p, H.rows, (int)H.cols, H.ld, H.part_stride, T, ld,
+                            targets, id64, G.vocab));
+  ++ctx->n_launch;
+  const Operand HT = {T, H.dtype, H.cols, H.rows, ld, H.parts, H.cols * ld};
   Params p = {};
   p.M = G.vocab; p.N = H.cols;
   p.num_m = (int)((p.M + 2 * BM - 1) / (2 * BM));
-  p.bn = p.N > 128 ? 256 : 128;      // whole boxes of 64 for each CTA
+  p.bn = up32(p.N);
   p.nbuf = 2;
   p.num_n = (int)((p.N + p.bn - 1) / p.bn);
   p.n_first = 1;
@@ -202,15 +253,19 @@ int launch_by_w(Ctx* ctx, const Blocks& G, const Operand& H, const float* alpha,
   p.tail_first = p.num_m * p.num_n; p.tail_split = 1;
   p.bf16 = H.dtype == ZOACT_DT_BF16; p.status = ctx->d_status;
   p.alpha = alpha; p.out = out; p.add = add;
+  p.out_32 = ((uintptr_t)out & 31) == 0 && p.N * (int64_t)dtype_size(dtype) % 32 == 0;
+  const bool staged = p.num_kb * p.products < STAGED_BELOW;
   Maps tm;
   int st = encode(&tm.a, G, 64);
-  if (!st) st = encode(&tm.b, H, 64);
-  if (!st) st = encode_tmap_store(&tm.out, out, dtype, p.M, p.N, 128 / (int)dtype_size(dtype), BM, true);
+  if (!st) st = encode(&tm.b, HT, p.bn / 2);
+  if (!st && staged) st = encode_tmap_store(&tm.out, out, dtype, p.M, p.N, 128 / (int)dtype_size(dtype), BM, true);
   if (st) return st;
+  if (!staged) tm.out = tm.a;
   switch (dtype) {
-    case ZOACT_DT_FP32: return launch<EPI_ROW, false, float>(ctx, tm, p);
-    case ZOACT_DT_BF16: return launch<EPI_ROW, false, __nv_bfloat16>(ctx, tm, p);
-    default: return launch<EPI_ROW, false, __half>(ctx, tm, p);
+    case ZOACT_DT_FP32: return staged ? launch<EPI_ROW_STAGED, false, float>(ctx, tm, p) : launch<EPI_ROW, false, float>(ctx, tm, p);
+    case ZOACT_DT_BF16:
+      return staged ? launch<EPI_ROW_STAGED, false, __nv_bfloat16>(ctx, tm, p) : launch<EPI_ROW, false, __nv_bfloat16>(ctx, tm, p);
+    default: return staged ? launch<EPI_ROW_STAGED, false, __half>(ctx, tm, p) : launch<EPI_ROW, false, __half>(ctx, tm, p);
   }
 }
 

@@ -386,6 +386,29 @@ def test_cross_entropy_without_a_counted_row(ctx):
     assert (out == 0).all()
 
 
+@pytest.mark.parametrize("dt", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("T", [40, 700])
+def test_cross_entropy_of_ignored_rows_that_are_not_finite(ctx, dt, T):
+    """What lies in a row without a target reaches no output: the same bits as with zeros there."""
+    d, vocab = 128, 700
+    rng = np.random.default_rng(T)
+    t = _targets(rng, T, vocab, 0.3)
+    t[[0, T - 1]] = -1
+    H, W = rnd(1, T, d, dt=dt), rnd(2, vocab, d, std=0.2, dt=dt)
+    out = []
+    for fill in (0.0, float("nan"), float("inf"), torch.finfo(TYPES[dt]).min):
+        h = H.clone()
+        h[torch.as_tensor(t < 0, device=DEV)] = fill
+        dH, dW = torch.empty_like(h), torch.empty_like(W)
+        loss, mean = torch.empty(T, device=DEV), torch.empty(1, dtype=torch.float64, device=DEV)
+        zo.zoact_ce_grad(ctx, h, W, ints(t), dH=dH, dW=dW, loss=loss, mean=mean)
+        clean(ctx)
+        out.append((dH, dW, loss, mean))
+    assert all(torch.isfinite(x).all() for x in out[0])
+    for other in out[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(out[0], other))
+
+
 def test_cross_entropy_of_non_finite_rows(ctx):
     H, W, t = rnd(1, 40, 64, dt="bf16"), rnd(2, 500, 64, dt="bf16"), ints(np.arange(40))
     H[7, 3] = float("nan")
