@@ -21,6 +21,9 @@ writes out:
   activations), a hand-written cyclic Jacobi eigensolver used as its pin, and
   the randomised subspace iteration that reaches the same subspace.
 * ``graphs``  -- the synthetic model graphs that chain adapted linears.
+* ``ends``    -- the two ends of a language model around them: embedding rows by token id, layer norm and the cross entropy
+  of a head over the vocabulary, each with its gradient, from their formulas (Section 5 fine-tunes on tokens; embeddings
+  and heads are not adapted).
 
 Pinned: every function has at least one ``-m "not gpu"`` test in ``tests/``
 against a value or property fixed by the paper or by mathematics (known-answer

@@ -459,6 +459,102 @@ class ZOStep:
         return self.loss_out
 
 
+class TokenStep:
+    """A language model around an adapted stack: table rows of token ids, the stack, layer norm, and the cross entropy of a
+    head over the vocabulary (`head`, or the table itself where it is None: tied).
+
+    step() is a ZO step of the stack's coefficients (the ends are frozen).  ends_grad() gives the exact gradient by the ends'
+    own parameters, for a first-order optimiser beside it.  A stack has no backward pass, so behind one the table is left as
+    it is where it is the embedding, and a tied table's gradient is its part as the head; with stack=None the embedding feeds
+    the norm directly and the table's gradient is whole (the ends warmed up before a stack is put between them).
+
+    table [vocab, d] and head [vocab, d] of the activations' type; gain and bias [d] fp32 or that type, or None.
+    ids and targets [T] int32 or int64 on the device; a negative one is no token.
+    """
+
+    def __init__(self, stack, table, head=None, gain=None, bias=None, scale=1.0, norm_eps=1e-5, ctx=None):
+        if stack is None and ctx is None:
+            raise ValueError("TokenStep: a context is needed where there is no stack")
+        if stack is not None and stack.dtype != table.dtype:
+            raise ValueError(f"TokenStep: a table of {table.dtype} before a stack of {stack.dtype}")
+        if head is not None and (head.shape != table.shape or head.dtype != table.dtype):
+            raise ValueError("TokenStep: table and head have one shape and type")
+        self.stack = stack
+        self.ctx = stack.ctx if ctx is None else ctx
+        self.table, self.gain, self.bias = table, gain, bias
+        self.head = table if head is None else head
+        self.scale, self.norm_eps = float(scale), float(norm_eps)
+        self.n_blocks = 1 if stack is None else stack.nb
+        self.hidden = None                          # the stack's output of the latest forward()
+        self.normed = None                          # after the norm: the head's input
+        self.dtable = self.dhead = self.dgain = self.dbias = None
+        self._bufs = {}
+
+    def buf(self, key, shape, dtype=None):
+        t = self._bufs.get(key)
+        if t is None or tuple(t.shape) != tuple(shape):
+            t = torch.empty(shape, dtype=self.table.dtype if dtype is None else dtype, device=self.table.device)
+            self._bufs[key] = t
+        return t
+
+    def forward(self, ids, seed=0, query=0):
+        """The head's input [n_blocks T, d] for the step's evaluation blocks (without a stack: [T, d])."""
+        d = self.table.shape[1]
+        if self.stack is not None and ids.shape[0] != self.stack.T:
+            raise ValueError(f"TokenStep: {ids.shape[0]} ids, the stack takes {self.stack.T}")
+        x = self.buf("x", (ids.shape[0], d))
+        Z.zoact_embed(self.ctx, self.table, ids, x, scale=self.scale)
+        self.hidden = x if self.stack is None else self.stack.forward(x, seed, query)
+        rows = self.hidden.shape[0]
+        self.normed = self.buf("normed", (rows, d))
+        Z.zoact_layer_norm(self.ctx, self.hidden, self.gain, self.bias, self.normed, eps=self.norm_eps,
+                           mean=self.buf("mean", (rows,), torch.float32), rstd=self.buf("rstd", (rows,), torch.float32))
+        return self.normed
+
+    def loss(self, targets):
+        """The loss vector of the latest forward(): ZOStep.loss with the cross entropy in place of the mean square (the
+        stack's two vectors take turns); without a stack [L]."""
+        if self.stack is None:
+            out = self.buf("loss", (1,), torch.float64)
+            Z.zoact_ce_loss(self.ctx, self.normed, self.head, targets, mean=out)
+            return out
+        s = self.stack
+        s._loss_i ^= 1
+        if s.n_queries is None:
+            Z.zoact_ce_pair(self.ctx, self.normed, self.head, targets, s.eps, s.loss_out)
+        else:
+            Z.zoact_ce_multi(self.ctx, self.normed, self.head, targets, s.nb, s.eps, s.loss_out)
+        return s.loss_out
+
+    def step(self, ids, targets, step, seed, query, lr=None):
+        """One ZO step on tokens.  Returns the device loss vector."""
+        self.forward(ids, seed, query)
+        out = self.loss(targets)
+        self.stack.update(step, seed, query, lr)
+        return out
+
+    def ends_grad(self, ids, targets, grad_scale=1.0):
+        """The gradient of grad_scale times the loss of the latest forward()'s first block (one-sided: the unperturbed
+        point; two-sided: the + point) by the ends' parameters, in fp32: dhead, dgain, dbias and, without a stack, dtable
+        (tied: dtable is dhead, the sum of both uses).  Returns that block's mean loss (device, fp64 [1])."""
+        T, d = ids.shape[0], self.table.shape[1]
+        if self.dhead is None:
+            f32 = dict(dtype=torch.float32, device=self.table.device)
+            self.dhead = torch.empty(self.head.shape, **f32)
+            self.dgain, self.dbias = torch.empty(d, **f32), torch.empty(d, **f32)
+            tied = self.head is self.table
+            self.dtable = self.dhead if tied else torch.empty(self.table.shape, **f32) if self.stack is None else None
+        mean = self.buf("grad_loss", (1,), torch.float64)
+        dy = self.buf("dy", (T, d))
+        Z.zoact_ce_grad(self.ctx, self.normed[:T], self.head, targets, dH=dy, dW=self.dhead, mean=mean, grad_scale=grad_scale)
+        dx = self.buf("dx", (T, d)) if self.stack is None else None
+        Z.zoact_layer_norm_grad(self.ctx, dy, self.hidden[:T], self.gain, self._bufs["mean"][:T], self._bufs["rstd"][:T],
+                                dX=dx, dgain=self.dgain, dbias=self.dbias)
+        if self.stack is None:
+            Z.zoact_embed_grad(self.ctx, dx, ids, self.dtable, scale=self.scale, accumulate=self.head is self.table)
+        return mean
+
+
 class HostFeeder:
     """Runs ZO steps on batches of PINNED host tensors, overlapping each batch's host-to-device copy (on a
     side stream, into one of two device buffer sets) with the previous step's compute.
