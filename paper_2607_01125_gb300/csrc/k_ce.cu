@@ -13,7 +13,7 @@ namespace {
 constexpr int CE_THREADS = 256;
 
 // The tiles' maxima m_i and sums s_i of a row joined: m, log s with s = sum s_i exp(m_i - m) (a row that the model predicts
-// well has s = 1 + many terms that fp32 alone would drop one by one), lse = m + log s and loss = lse - z_t.
+// well has s = 1 + many terms that fp32 alone would drop one by one), lse = m + log s and loss = (m - z_t) + log s.
 // The gradient takes z - lse as (z - m) - log s, exact where z = m.
 // All of it in fp32 with what the additions round off beside the sum (fp64 FMAs run at 1/64 of the rate: with them this kernel
 // took 24 us for 2048 rows of 1002 tiles).  A block has ROWS rows; 1024 / ROWS groups of threads take their tiles in turn,
@@ -76,7 +76,7 @@ ce_join_kernel(const float2* __restrict__ part, int64_t tiles, int64_t part_ld, 
   lse[row] = l;
   const int64_t t = load_id(targets, id64, row % T);
   if (t >= vocab) record_error(status, ZOACT_ERR_INVALID_ARG);
-  loss[row] = t >= 0 && t < vocab ? l - zt[row] : 0.f;
+  loss[row] = t >= 0 && t < vocab ? (a.m - zt[row]) + ls : 0.f;      // not l - zt: l's rounding would stay in a small loss
 }
 
 // alpha = scale / N, N the number of counted rows (at least 1): the factor of the gradient's products.
