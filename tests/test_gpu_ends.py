@@ -121,6 +121,17 @@ def test_embed_grad_of_uneven_ids(ctx, kind, accumulate):
     _embed_grad_case(ctx, "bf16", "bf16", list(ids), 24, vocab, accumulate, idt)
 
 
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("n", [10239, 10240, 10241, 40000])
+def test_embed_grad_of_long_lists(ctx, n, accumulate):
+    """Both ways to order the tokens, with ids as frequent as 1 / rank (the first has a tenth of them) and unfrequent ones."""
+    rng = np.random.default_rng(n)
+    vocab = 50003
+    ids = np.exp(rng.random(n) * np.log(vocab)).astype(np.int64) * 7919 % vocab
+    ids[rng.random(n) < 0.1] = -1
+    _embed_grad_case(ctx, "fp16", "fp32", list(ids), 8, vocab, accumulate)
+
+
 def test_embed_of_no_tokens(ctx):
     E, none = rnd(1, 5, 8), ints([], torch.int64)
     zo.zoact_embed(ctx, E, none, torch.empty(0, 8, device=DEV))
