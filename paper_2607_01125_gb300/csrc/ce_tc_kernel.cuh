@@ -134,20 +134,25 @@ __device__ __forceinline__ void tma_add_2d(const CUtensorMap* map, int32_t x, in
                : "memory");
 }
 
-// M- or N-major operand tile with 128-byte swizzling: boxes of 64 elements x BK rows of K, BOX_BYTES apart along M or N,
-// 1024 bytes for 8 rows of K.
-__device__ __forceinline__ uint64_t sdesc_mn_sw128(uint32_t start) {
-  uint64_t d = 0;
-  d |= (uint64_t)((start & 0x3FFFFu) >> 4);
-  d |= (uint64_t)(BOX_BYTES >> 4) << 16;         // leading byte offset: the next 64 of M or N
-  d |= (uint64_t)(1024u >> 4) << 32;             // stride byte offset: the next 8 of K
-  d |= (uint64_t)1 << 46;
-  d |= (uint64_t)2 << 61;
-  return d;
+// Low words of the operands' descriptors at `tile` (both with 128-byte swizzling; the high words are constants), and what a
+// step of 16 in K adds.  K-major: rows of BK elements, 1024 bytes for 8 rows.  M-major: boxes of 64 elements x BK rows of K,
+// BOX_BYTES apart along M, 1024 bytes for 8 rows of K.
+constexpr uint32_t SDESC_HI = (1024u >> 4) | 1u << 14 | 2u << 29;
+__device__ __forceinline__ uint32_t sdesc_lo(uint32_t tile, bool mn) {
+  return tile >> 4 | (mn ? (uint32_t)(BOX_BYTES >> 4) << 16 : 1u << 16);
 }
-template <bool MN>
-__device__ __forceinline__ uint64_t sdesc(uint32_t tile, int k) {
-  return MN ? sdesc_mn_sw128(tile + (uint32_t)k * 2048u) : tc::sdesc_k_sw128(tile + (uint32_t)k * 32u);
+__device__ __forceinline__ uint64_t sdesc(uint32_t lo) { return (uint64_t)SDESC_HI << 32 | lo; }
+__host__ __device__ constexpr uint32_t sdesc_step(bool mn) { return mn ? 2048u >> 4 : 32u >> 4; }
+
+// One lane of a converged warp, the same one each time.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t is;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(is));
+  return is != 0;
+}
+// A wait of a whole warp (in every lane, with one answer).
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* status) {
+  return __all_sync(0xffffffffu, tc::mbar_wait(bar, parity, abort_flag, status));
 }
 
 // Reduce 32 columns over the warp's 32 lanes: lane l returns column l's maximum (sum).  x is overwritten.
@@ -520,8 +525,8 @@ ce_tc_kernel(const __grid_constant__ Maps tm, const Params p) {
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   uint8_t* aux = smem + ring_bytes(EPI);
   Shared* ss = reinterpret_cast<Shared*>(aux + aux_bytes(EPI));
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const uint32_t rank = tc2::cluster_rank();
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+  const uint32_t rank = __shfl_sync(0xffffffffu, tc2::cluster_rank(), 0);
   const bool leader = rank == 0;
   volatile int* abort_flag = &ss->abort_flag;
 
@@ -549,7 +554,7 @@ ce_tc_kernel(const __grid_constant__ Maps tm, const Params p) {
   __syncthreads();
   tc2::cluster_sync();                    // both CTAs' barriers exist before any remote arrival
   tc::tc_fence_after();
-  const uint32_t tmem_base = ss->tmem_base;
+  const uint32_t tmem_base = __shfl_sync(0xffffffffu, ss->tmem_base, 0);
   pdl_wait();
   pdl_trigger();
 
@@ -559,36 +564,45 @@ ce_tc_kernel(const __grid_constant__ Maps tm, const Params p) {
 
   if (warp < EPI_BASE / 32) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_ISSUE));
-    if (warp == 0 && lane == 0) {
+    // Both loops run in whole warps that elect a lane for each copy, MMA and arrival: what the compiler knows to be the
+    // warp's own is in the registers that these instructions take.  (One lane's loop took 333 ns a K-block, whatever its
+    // size, and a division for the K-block's product 26 of them.)
+    if (warp == 0) {
       // ---------------- TMA producer (both CTAs) ----------------
       const uint32_t stage_tx = (uint32_t)(A_BYTES + bh * BK * 2);
+      const uint32_t ring = tc::smem_u32(smem), empty = tc::smem_u32(&ss->empty[0]);
+      const uint32_t full = tc2::map_to(tc::smem_u32(&ss->full[0]), 0);       // the leader's
       int stage = 0;
       uint32_t phase = 0;
       bool ok = true;
       for (int u = cluster_id; ok && unit_at(p, u, w); u += n_clusters) {
         const int m0 = w.m * 2 * BM + (int)rank * BM, n0 = w.n * p.bn + (int)rank * bh;
+        // products of parts (a, b): (0,0) (0,1) (1,0) (0,2) (1,1) (2,0)
+        int pr = w.kb0 / p.num_kb, kblk = w.kb0 - pr * p.num_kb;
         for (int kb = w.kb0; kb < w.kb1; ++kb) {
-          if (!tc::mbar_wait(tc::smem_u32(&ss->empty[stage]), phase ^ 1u, abort_flag, p.status)) { ok = false; break; }
-          const uint32_t full_leader = tc2::map_to(tc::smem_u32(&ss->full[stage]), 0);
-          tc2::arrive_expect_tx_cluster(full_leader, stage_tx);
-          const uint32_t sa = tc::smem_u32(smem + stage * sbytes), sb = sa + A_BYTES;
-          // products of parts (a, b): (0,0) (0,1) (1,0) (0,2) (1,1) (2,0)
-          const int pr = kb / p.num_kb, kblk = kb - pr * p.num_kb, k = kblk * BK;
-          const int pa = (0x210100 >> (4 * pr)) & 15, pb = (0x012010 >> (4 * pr)) & 15;
-          if (A_BLOCKS) {
-            tma_load_3d_pair(sa, &tm.a, 0, k, m0 / 64 + pa * p.g_blocks, full_leader);
-            tma_load_3d_pair(sa + BOX_BYTES, &tm.a, 0, k, m0 / 64 + 1 + pa * p.g_blocks, full_leader);
-          } else if (A_MN) {
-            tma_load_3d_pair(sa, &tm.a, m0, k, pa, full_leader);
-            tma_load_3d_pair(sa + BOX_BYTES, &tm.a, m0 + 64, k, pa, full_leader);
-          } else {
-            tma_load_3d_pair(sa, &tm.a, k, m0, pa, full_leader);
+          if (!warp_wait(empty + (uint32_t)stage * 8u, phase ^ 1u, abort_flag, p.status)) { ok = false; break; }
+          const uint32_t bar = full + (uint32_t)stage * 8u;
+          const uint32_t sa = ring + (uint32_t)(stage * sbytes), sb = sa + A_BYTES;
+          const int k = kblk * BK, pa = (0x210100 >> (4 * pr)) & 15, pb = (0x012010 >> (4 * pr)) & 15;
+          if (elect_one()) {
+            tc2::arrive_expect_tx_cluster(bar, stage_tx);
+            if (A_BLOCKS) {
+              tma_load_3d_pair(sa, &tm.a, 0, k, m0 / 64 + pa * p.g_blocks, bar);
+              tma_load_3d_pair(sa + BOX_BYTES, &tm.a, 0, k, m0 / 64 + 1 + pa * p.g_blocks, bar);
+            } else if (A_MN) {
+              tma_load_3d_pair(sa, &tm.a, m0, k, pa, bar);
+              tma_load_3d_pair(sa + BOX_BYTES, &tm.a, m0 + 64, k, pa, bar);
+            } else {
+              tma_load_3d_pair(sa, &tm.a, k, m0, pa, bar);
+            }
+            if (B_BLOCKS) {
+              tma_load_3d_pair(sb, &tm.b, 0, n0, kblk + pb * p.g_blocks, bar);
+            } else {
+              tma_load_3d_pair(sb, &tm.b, k, n0, pb, bar);
+            }
           }
-          if (B_BLOCKS) {
-            tma_load_3d_pair(sb, &tm.b, 0, n0, kblk + pb * p.g_blocks, full_leader);
-          } else {
-            tma_load_3d_pair(sb, &tm.b, k, n0, pb, full_leader);
-          }
+          __syncwarp();
+          if (++kblk == p.num_kb) { kblk = 0; ++pr; }
           if (++stage == p.stages) { stage = 0; phase ^= 1u; }
         }
       }
@@ -598,9 +612,11 @@ ce_tc_kernel(const __grid_constant__ Maps tm, const Params p) {
         while (tc::global_timer_ns() - t0 < 2000000ull) {
         }
       }
-    } else if (warp == 1 && lane == 0 && leader) {
+    } else if (warp == 1 && leader) {
       // ---------------- MMA issuer (leader CTA) ----------------
       const uint32_t idesc = tc::idesc_f16(2 * BM, p.bn, p.bf16) | (A_MN ? 1u << 15 : 0u);
+      const uint32_t ring_a = sdesc_lo(tc::smem_u32(smem), A_MN), ring_b = sdesc_lo(tc::smem_u32(smem) + A_BYTES, false);
+      const uint32_t full = tc::smem_u32(&ss->full[0]), empty = tc::smem_u32(&ss->empty[0]);
       int stage = 0;
       uint32_t phase = 0;
       bool ok = true, issued_any = false;
@@ -608,27 +624,33 @@ ce_tc_kernel(const __grid_constant__ Maps tm, const Params p) {
       for (int u = cluster_id; ok && unit_at(p, u, w); u += n_clusters) {
         for (int g0 = w.kb0; ok && g0 < w.kb1; g0 += p.group_kb) {
           const int g1 = min(g0 + p.group_kb, w.kb1);
-          if (!tc::mbar_wait(tc::smem_u32(&ss->tmem_empty[r.buf]), r.phase ^ 1u, abort_flag, p.status)) { ok = false; break; }
+          if (!warp_wait(tc::smem_u32(&ss->tmem_empty[r.buf]), r.phase ^ 1u, abort_flag, p.status)) { ok = false; break; }
           tc::tc_fence_after();
           const uint32_t d_tmem = tmem_base + (uint32_t)(r.buf * p.bn);
           for (int kb = g0; kb < g1; ++kb) {
-            if (!tc::mbar_wait(tc::smem_u32(&ss->full[stage]), phase, abort_flag, p.status)) { ok = false; break; }
+            if (!warp_wait(full + (uint32_t)stage * 8u, phase, abort_flag, p.status)) { ok = false; break; }
             tc::tc_fence_after();
-            const uint32_t sa = tc::smem_u32(smem + stage * sbytes), sb = sa + A_BYTES;
+            const uint32_t at = (uint32_t)(stage * sbytes) >> 4;
+            if (elect_one()) {
 #pragma unroll
-            for (int k = 0; k < BK / 16; ++k)
-              tc2::mma2_f16(d_tmem, sdesc<A_MN>(sa, k), tc::sdesc_k_sw128(sb + (uint32_t)k * 32u), idesc, (kb != g0 || k != 0) ? 1u : 0u);
-            tc2::commit2_both(tc::smem_u32(&ss->empty[stage]));
+              for (int k = 0; k < BK / 16; ++k)
+                tc2::mma2_f16(d_tmem, sdesc(ring_a + at + (uint32_t)k * sdesc_step(A_MN)),
+                              sdesc(ring_b + at + (uint32_t)k * sdesc_step(false)), idesc, (kb != g0 || k != 0) ? 1u : 0u);
+              tc2::commit2_both(empty + (uint32_t)stage * 8u);
+            }
+            __syncwarp();
             issued_any = true;
             if (++stage == p.stages) { stage = 0; phase ^= 1u; }
           }
           if (!ok) break;
-          tc2::commit2_both(tc::smem_u32(&ss->tmem_full[r.buf]));
+          if (elect_one()) tc2::commit2_both(tc::smem_u32(&ss->tmem_full[r.buf]));
+          __syncwarp();
           r.next(p.nbuf);
         }
       }
       if (issued_any) {
-        tc2::commit2_own(tc::smem_u32(&ss->drain));
+        if (elect_one()) tc2::commit2_own(tc::smem_u32(&ss->drain));
+        __syncwarp();
         tc::mbar_wait_drain(tc::smem_u32(&ss->drain), 0, 100000000ull);
       }
     }
