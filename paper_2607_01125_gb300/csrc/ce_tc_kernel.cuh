@@ -439,10 +439,10 @@ __device__ __forceinline__ void store_32(void* p, const uint32_t* w, bool whole)
 }
 
 // D scaled, from registers: a thread has a row's 128 columns of its warpgroup and writes them in whole sectors.  Staged in
-// shared memory for bulk stores, a tile's 64 KB of writes and reads there add 2600 cycles to a main loop that is bound by the
-// same memory (the gradient for W alone, 4096 x 128256 in bf16: 768 rows 1202 us for 1136, 2048 rows 2873 for 2847).  Where K
-// is short the output's bytes are the bound, and boxes of 128 rows reach DRAM in better order (1 row: 359 us for 490, 256 rows
-// 500 for 576), so both stay: see STAGED_BELOW.
+// shared memory for bulk stores, a tile's 64 KB of writes and reads there compete with the operands of a long main loop (loss
+// and gradient for W alone, 4096 x 128256 in bf16: 1024 rows 1432 us for 1399).  Where K is short the output's bytes are the
+// bound, and boxes of 128 rows reach DRAM in better order (1 row: 354 us for 475, 256 rows 464 for 566, 768 rows 1114 for
+// 1123), so both stay: see STAGED_BELOW.
 template <typename TO>
 __device__ __forceinline__ void epi_row(const Params& p, const Part& a, int half, int row_in_cta, int64_t m0, int64_t n0, float f) {
   const int64_t m = m0 + row_in_cta, n = n0 + half * 128;

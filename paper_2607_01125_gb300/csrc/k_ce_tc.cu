@@ -10,9 +10,12 @@ namespace {
 // and reading a group's sum about 300 cycles of it.  Logits end in fp32 (12 blocks: 7e-7; 8 cost 2% more time); products that
 // end in 16 bits take 64 (4e-6), and fp32 operands, whose six products are summed alike, 4 (3e-7).
 constexpr int LOGIT_GROUP = 12, GRAD_GROUP = 64, FP32_GROUP = 4;
+// Rows on the M side are taken up to this much more padding: their epilogue has no reduction over lanes.  Loss and dH of a
+// 4096 x 128256 head in bf16, rows on N / on M: 100 rows 357 us / 368, 200 rows 412 / 410, 400 rows 683 / 699, 512 rows
+// 761 / 749, 1024 rows 1469 / 1404, 2048 rows 2795 / 2668; 333 rows of 5120 x 50272 in fp16 326 / 349.
 constexpr double ROWS_M_GAIN = 1.15;
-// K-blocks below which the product by W stores through shared memory: 384 rows 718 us for 753, 512 rows 850 for 838 (epi_row).
-constexpr int STAGED_BELOW = 8;
+// K-blocks below which the product by W stores through shared memory (epi_row).
+constexpr int STAGED_BELOW = 14;
 
 int even_groups(int kb, int most) {
   const int groups = (kb + most - 1) / most;
@@ -44,10 +47,10 @@ int launch(Ctx* ctx, const Maps& tm, Params p) {
 int up32(int64_t n) { return n >= BN ? BN : (int)((n + 31) / 32 * 32); }
 
 // The time of `tiles` tiles of 2 BM x bn in whole waves of pairs, in units of one column: a tile's time is taken as its width
-// plus a part that does not depend on it.
+// plus a part that does not depend on it (a K-block of 64, 333 rows: 217 ns at 96 columns, 244 at 128, 306 at 192, 340 at 256).
 double wave_cost(const Ctx* ctx, int64_t tiles, int bn) {
   const int pairs = ctx->sm_count / 2;
-  return (double)((tiles + pairs - 1) / pairs) * (bn + 32);
+  return (double)((tiles + pairs - 1) / pairs) * (bn + 128);
 }
 
 // Rows per tile of m_tiles x rows outputs, the rows on the N side.
