@@ -45,11 +45,27 @@ ce_join_kernel(const float2* __restrict__ part, int64_t tiles, int64_t part_ld, 
     const int r = threadIdx.x % ROWS, group = threadIdx.x / ROWS;
     const int64_t row = (int64_t)blockIdx.x * ROWS + r;
     MaxSum a = {-INFINITY, 0.f, 0.f};
-    if (row < rows) {
-#pragma unroll 8
-      for (int64_t i = group; i < tiles; i += GROUPS) {
-        const float2 p = part[i * part_ld + row];
-        a = join_sums(a, MaxSum{p.x, p.y, 0.f});
+    constexpr int AHEAD = 8;               // tiles loaded together
+    for (int64_t i0 = group; i0 < tiles && row < rows; i0 += AHEAD * GROUPS) {
+      float2 p[AHEAD];
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k) {
+        const int64_t i = i0 + k * GROUPS;
+        p[k] = i < tiles ? part[i * part_ld + row] : make_float2(-INFINITY, 0.f);
+      }
+      float m = a.m;
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k) m = fmaxf(m, p[k].x);
+      const float f = a.m == m ? 1.f : expf(a.m - m);
+      a.m = m;
+      a.hi *= f;
+      a.lo *= f;
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k) {
+        const float y = p[k].x == m ? p[k].y : p[k].y * expf(p[k].x - m);
+        const float t = a.hi + y, b = t - a.hi;
+        a.lo += (a.hi - (t - b)) + (y - b);                          // what t rounded off
+        a.hi = t;
       }
     }
     mx[r][group] = a.m;
@@ -180,56 +196,91 @@ ce_scale_kernel(void* __restrict__ G, int64_t blk0, int64_t rows, const float2* 
   }
 }
 
-// Block b: L_b = sum / N and D_b = sum over t of (loss_b - loss_0) / N, in fp64 and in a fixed order.
+// Block b: L_b = sum / N and D_b = sum over t of (loss_b - loss_0) / N, in a fixed order: pairs of fp32 whose additions keep what
+// they round off (about 48 bits), since fp64's run at 1/64 of the rate (64 rows took 11.4 us with them), and fp64 from the
+// block's sums on.
 //   mean [nb] (or nullptr); est: 1 = the pair's {L+, L-, D, a}, 2 = {L_0 .. L_q, a_1 .. a_q}, 0 = none.
-__global__ void __launch_bounds__(1024)
+constexpr int FINISH_THREADS = 512;
+
+struct Twofold {
+  float hi = 0.f, lo = 0.f;
+  __device__ __forceinline__ void add(float h, float l) {
+    const float s = hi + h, b = s - hi, e = (hi - (s - b)) + (h - b) + (lo + l);
+    hi = isfinite(s) ? s + e : s;
+    lo = isfinite(s) ? s - hi + e : 0.f;
+  }
+  __device__ __forceinline__ double value() const { return (double)hi + (double)lo; }
+};
+
+__global__ void __launch_bounds__(FINISH_THREADS)
 ce_finish_kernel(const float* __restrict__ loss, int64_t T, int nb, const void* __restrict__ targets, int id64,
                  int64_t vocab, double* mean, int est, double step, double* out, int* status) {
   pdl_wait();
   pdl_trigger();
-  __shared__ double red[3][32];
+  constexpr int WARPS = FINISH_THREADS / 32, AHEAD = 4;
+  __shared__ Twofold red[2][WARPS];
+  __shared__ int count[WARPS];
   const int b = blockIdx.x;
   const int other = est == 1 ? 1 : 0;       // the pair's D is L+ - L-, the others' L_b - L_0
-  double s = 0.0, dd = 0.0, n = 0.0;
-  for (int64_t t = threadIdx.x; t < T; t += 1024) {
-    const int64_t id = load_id(targets, id64, t);
-    if (id < 0 || id >= vocab) continue;
-    const double l = loss[b * T + t];
-    n += 1.0;
-    s += l;
-    if (est) dd += l - (double)loss[other * T + t];
+  Twofold s, dd;
+  int n = 0;
+  for (int64_t t0 = threadIdx.x; t0 < T; t0 += AHEAD * FINISH_THREADS) {
+    int64_t id[AHEAD];
+    float l[AHEAD], o[AHEAD];
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+      const int64_t t = t0 + k * FINISH_THREADS;
+      id[k] = -1;
+      if (t < T) {
+        id[k] = load_id(targets, id64, t);
+        l[k] = loss[b * T + t];
+        if (est) o[k] = loss[other * T + t];
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+      if (id[k] < 0 || id[k] >= vocab) continue;
+      ++n;
+      s.add(l[k], 0.f);
+      if (est) {
+        const float d = l[k] - o[k], c = d - l[k];
+        dd.add(d, (l[k] - (d - c)) - (o[k] + c));                    // the difference's own rounding
+      }
+    }
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
-    s += __shfl_xor_sync(0xffffffffu, s, o);
-    dd += __shfl_xor_sync(0xffffffffu, dd, o);
-    n += __shfl_xor_sync(0xffffffffu, n, o);
+    s.add(__shfl_xor_sync(0xffffffffu, s.hi, o), __shfl_xor_sync(0xffffffffu, s.lo, o));
+    if (est) dd.add(__shfl_xor_sync(0xffffffffu, dd.hi, o), __shfl_xor_sync(0xffffffffu, dd.lo, o));
   }
+  n = __reduce_add_sync(0xffffffffu, n);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  if (lane == 0) { red[0][warp] = s; red[1][warp] = dd; red[2][warp] = n; }
+  if (lane == 0) { red[0][warp] = s; red[1][warp] = dd; count[warp] = n; }
   __syncthreads();
-  if (threadIdx.x != 0) return;
-  s = dd = n = 0.0;
-  for (int w = 0; w < 32; ++w) { s += red[0][w]; dd += red[1][w]; n += red[2][w]; }
-  const double den = n > 0.0 ? n : 1.0;
-  const double L = s / den, D = dd / den;
-  if (mean) mean[b] = L;
-  bool fine = isfinite(L);
-  if (est == 1) {
-    out[b] = L;
+  if (threadIdx.x >= 2) return;             // thread 0: the mean; 1: the difference and the estimate
+  Twofold sum;
+  int64_t all = 0;
+#pragma unroll
+  for (int w = 0; w < WARPS; ++w) {
+    sum.add(red[threadIdx.x][w].hi, red[threadIdx.x][w].lo);
+    all += count[w];
+  }
+  const double v = sum.value() / (double)(all > 0 ? all : 1);
+  bool fine = isfinite(v);
+  if (threadIdx.x == 0) {
+    if (mean) mean[b] = v;
+    if (est) out[b] = v;
+  } else if (est == 1) {
     if (b == 0) {
-      const double e = D / (2.0 * step);
-      out[2] = D;
+      const double e = v / (2.0 * step);
+      out[2] = v;
       out[3] = e;
       fine = fine && isfinite(e);
     }
-  } else if (est == 2) {
-    out[b] = L;
-    if (b > 0) {
-      const double e = D / step;
-      out[nb + b - 1] = e;
-      fine = fine && isfinite(e);
-    }
+  } else if (est == 2 && b > 0) {
+    const double e = v / step;
+    out[nb + b - 1] = e;
+    fine = fine && isfinite(e);
   }
   if (!fine) record_error(status, ZOACT_ERR_NONFINITE);
 }
@@ -277,7 +328,7 @@ int make_alpha(Ctx* ctx, const CeArgs& c, const CeScratch& s, float scale) {
 // The losses' means and estimates.
 int finish(Ctx* ctx, const CeArgs& c, const float* loss) {
   if (!c.mean && !c.est) return ZOACT_OK;
-  ZOACT_CUDA_TRY(launch_pdl(ctx, ce_finish_kernel, dim3((unsigned)c.nb), dim3(1024), 0, loss, c.T, c.nb, c.targets, c.id64,
+  ZOACT_CUDA_TRY(launch_pdl(ctx, ce_finish_kernel, dim3((unsigned)c.nb), dim3(FINISH_THREADS), 0, loss, c.T, c.nb, c.targets, c.id64,
                             c.vocab, c.mean, c.est, (double)c.step, c.out, ctx->d_status));
   ++ctx->n_launch;
   return ZOACT_OK;
