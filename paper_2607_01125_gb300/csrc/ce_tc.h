@@ -14,6 +14,7 @@ struct Operand {
   int64_t part_stride;
 };
 
+constexpr float LOG_STEPS = 2048.f;  // steps of a kept logit's fixed point
 constexpr int V_TILE = 128;          // vocabulary entries of one pair of a row's statistics
 enum { KEEP_NONE = 0, KEEP_LOG = 1, KEEP_Z = 2 };
 
@@ -28,7 +29,7 @@ struct Blocks {
 };
 
 // Logits z = H W^T: of each row the maximum and the sum of exp(z - maximum) over every V_TILE entries (part, [tile][part_ld])
-// and the target's logit (zt; row r has targets[r % T]); keep: min(65535, round(4096 (maximum - z))) as 16-bit integers, or z
+// and the target's logit (zt; row r has targets[r % T]); keep: min(65535, round(LOG_STEPS (maximum - z))) as 16-bit integers, or z
 // in fp32, to G.
 int launch_logits(Ctx* ctx, const Operand& W, const Operand& H, float2* part, int64_t part_ld, float* zt, const void* targets,
                   int id64, int64_t T, int keep, const Blocks& G);

@@ -229,9 +229,8 @@ __device__ __forceinline__ bool sum_groups(const Params& p, Shared* ss, const Un
   return true;
 }
 
-// Fixed point of the tile's maximum - z: 1 / LOG_STEPS, up to 16 (below exp(-16) of the tile's largest: 65535, no value);
+// Fixed point of the tile's maximum - z: 1 / LOG_STEPS, up to 32 (below exp(-32) of the tile's largest: 65535, no value);
 // rounded in the low bits of a sum with 2^23.  x = z - maximum.
-constexpr float LOG_STEPS = 4096.f;
 __device__ __forceinline__ uint32_t log_fixed(float x) {
   return __float_as_uint(fminf(x * -LOG_STEPS, 65535.f) + 8388608.f) & 0xffffu;
 }

@@ -115,9 +115,10 @@ ce_alpha_kernel(const void* __restrict__ targets, int id64, int64_t T, int64_t v
   }
 }
 
-// What a chunk of rows kept of its logits, 4096 (m_tile - z) in 16 bits, to G = exp(z - lse) - onehot in the operands' type,
-// in place.  The fixed point errs by 1.2e-4 of the exponential at most, a third of fp16's rounding (exp(z - m_tile) in fp16
-// would have rounded twice; beyond 16 below the tile's largest nothing is kept).  fp16's G is scaled by 2^15 (undone in
+// What a chunk of rows kept of its logits, 2048 (m_tile - z) in 16 bits, to G = exp(z - lse) - onehot in the operands' type,
+// in place.  The fixed point errs by 2.4e-4 of the exponential at most, half of fp16's rounding (exp(z - m_tile) in fp16 would
+// have rounded twice).  It reaches 32 below the tile's largest: with twice the steps and half the reach, the entries beside a
+// target that the model is nearly sure of were lost.  fp16's G is scaled by 2^15 (undone in
 // the products' scale): 1 / vocab would lie among its subnormals.  The target's element is expm1(z_t - lse): p - 1 from a
 // rounded p would lose what is left of it where the model is nearly right.
 constexpr float G_SCALE_FP16 = 32768.f;
@@ -172,7 +173,7 @@ ce_scale_kernel(void* __restrict__ G, int64_t blk0, int64_t rows, const float2* 
         // 2^23 + the fixed point, by its bytes: the conversion instruction shares the exponential's unit
         const uint32_t bits = __byte_perm(w[i / 2], 0x4b000000u, i & 1 ? 0x7632 : 0x7610);
         const float x = __uint_as_float(bits) - 8388608.f;
-        e[i] = bits == 0x4b00ffffu ? none : exp2_ftz(fmaf(x, -1.44269504f / 4096.f, c2)) * scale;
+        e[i] = bits == 0x4b00ffffu ? none : exp2_ftz(fmaf(x, -1.44269504f / ce::LOG_STEPS, c2)) * scale;
       }
       if (t[k] >= v0 && t[k] < v0 + 8) {
         const float2 st = stat[row];

@@ -7,9 +7,10 @@ namespace ce {
 namespace {
 
 // K-blocks of 64 that the tensor core sums by itself, at most: its cut-off costs about 1.6e-8 of the sum for each 16 products,
-// and reading a group's sum about 300 cycles of it.  Logits end in fp32 (12 blocks: 7e-7; 8 cost 2% more time); products that
-// end in 16 bits take 64 (4e-6), and fp32 operands, whose six products are summed alike, 4 (3e-7).
-constexpr int LOGIT_GROUP = 12, GRAD_GROUP = 64, FP32_GROUP = 4;
+// and reading a group's sum about 300 cycles of it.  Logits end in fp32 (8 blocks: 5e-7; with 12, 8e-7, 333 rows took 153 us
+// for 156 and 2048 rows the same); products that end in 16 bits take 64 (4e-6), and fp32 operands, whose six products are
+// summed alike, 4 (3e-7).
+constexpr int LOGIT_GROUP = 8, GRAD_GROUP = 64, FP32_GROUP = 4;
 // Rows on the M side are taken up to this much more padding: their epilogue has no reduction over lanes.  Loss and dH of a
 // 4096 x 128256 head in bf16, rows on N / on M: 100 rows 357 us / 368, 200 rows 412 / 410, 400 rows 683 / 699, 512 rows
 // 761 / 749, 1024 rows 1469 / 1404, 2048 rows 2795 / 2668; 333 rows of 5120 x 50272 in fp16 326 / 349.

@@ -420,6 +420,35 @@ def test_cross_entropy_of_ignored_rows_that_are_not_finite(ctx, dt, T):
         assert all(torch.equal(a, b) for a, b in zip(out[0], other))
 
 
+@pytest.mark.parametrize("dt", ["bf16", "fp16", "fp32"])
+def test_cross_entropy_gradient_beside_a_target_that_is_nearly_sure(ctx, dt):
+    """Logits 24 below the target's, in its tile of the vocabulary too: their rows of dW keep their own digits, and the loss
+    those that a sum beside 1 can have."""
+    T, d, vocab = 6, 256, 700
+    W = rnd(1, vocab, d, std=1.0 / 16, dt=dt)
+    t = np.array([0, 1, 130, 400, 640, 699])
+    w = n64(W)
+    H = torch.as_tensor(24.0 * w[t] / (w[t] ** 2).sum(axis=1, keepdims=True), device=DEV).to(TYPES[dt])
+    dW, loss = torch.empty(vocab, d, device=DEV), torch.empty(T, device=DEV)
+    zo.zoact_ce_grad(ctx, H, W, ints(t), dW=dW, loss=loss)
+    clean(ctx)
+    h = n64(H)
+    z = h @ w.T
+    wloss, wlse, _ = ends.cross_entropy(h, w, t)
+    ez = _logit_error(h, w)
+    P = np.exp(z - wlse[:, None])
+    P[np.arange(T), t] = 0
+    S = P.sum(axis=1)                                   # 1 - the target's share, to S^2
+    assert S.max() < 1e-6
+    within(loss, S, 130 * F + (2 * ez + 2.0 ** -20) * S)    # a tile's 128 exponentials summed beside a 1
+    others = np.setdiff1d(np.arange(vocab), t)
+    want = (P.T @ h / T)[others]
+    ug = 2.0 ** -21 if dt == "fp32" else 1.01 * UNIT[dt] + 2.0 ** -11
+    # fp16's G lies on multiples of 2^-24 of its scale 2^15
+    eg = (ug + 2 * ez + 2.0 ** -20) * P + (2.0 ** -40 if dt == "fp16" else 0)
+    within(dW[torch.as_tensor(others, device=DEV)], want, ((eg.T @ np.abs(h) + (T + 8) * F * (P.T @ np.abs(h))) / T)[others])
+
+
 def test_cross_entropy_of_non_finite_rows(ctx):
     H, W, t = rnd(1, 40, 64, dt="bf16"), rnd(2, 500, 64, dt="bf16"), ints(np.arange(40))
     H[7, 3] = float("nan")
