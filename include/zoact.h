@@ -534,8 +534,11 @@ int zoact_layer_norm_grad(zoact_ctx* ctx, const void* dY, int64_t ld_dy, const v
  * zoact_ce_multi: out[2 n_blocks - 1] = {L_0 .. L_q, a_1 .. a_q} as zoact_loss_multi, a_j = (L_j - L_0) / mu.
  * zoact_ce_grad: the same losses for one block, and the gradient of grad_scale * L: dH [T, d] of dtype and
  *   dW [vocab, d] of wgdtype (dtype or FP32); either may be NULL.  accumulate != 0 adds to dW, which must then be FP32
- *   (ZOACT_ERR_UNSUPPORTED otherwise).  Context scratch: the gradient by the logits for a chunk of rows (at most 2 GiB or
- *   256 rows), and 4 bytes a weight where several chunks add to a 16-bit dW.
+ *   (ZOACT_ERR_UNSUPPORTED otherwise).
+ * What lies in a row of H whose target is negative reaches no output, be it NaN or infinite.
+ * Context scratch: 8 bytes a row for every 128 vocabulary entries; FP32: 6 bytes an element of H and W.  With a gradient the
+ *   rows are taken in chunks of at most 2 GiB of G, or 256 rows: 2 bytes (FP32: 10) a row and entry, a chunk of H by columns,
+ *   fp32 partial sums of dH's last tiles, and 4 bytes a weight where several chunks add to a 16-bit dW.
  * A mean or estimate that is not finite sets ZOACT_ERR_NONFINITE.  d % 8 == 0 (16-bit) or d % 4 == 0 (FP32); H, W, dH
  * and dW 16-byte aligned.                                                                                         */
 int zoact_ce_loss(zoact_ctx* ctx, const void* H, int dtype, int64_t T, int32_t n_blocks, int32_t d, const void* W,

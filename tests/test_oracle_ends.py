@@ -59,3 +59,20 @@ def test_embedding_gradient_is_that_of_its_rows():
     dE = ends.embed_grad(c, ids, 6, 3.0)
     assert np.abs(dE - _num_grad(f, E)).max() < 1e-7
     assert np.allclose(ends.embed_grad(c, ids, 6, 3.0, start=E), E + dE)
+
+
+def test_the_forward_passes_are_those_of_torch():
+    import torch
+    import torch.nn.functional as tf
+    rng = np.random.default_rng(4)
+    H, W, X = rng.standard_normal((7, 5)), rng.standard_normal((11, 5)), rng.standard_normal((4, 9))
+    g, b, t = rng.standard_normal(9), rng.standard_normal(9), np.array([0, 10, -100, 3, 3, -100, 7])
+    T = torch.as_tensor
+    loss, lse, mean = ends.cross_entropy(H, W, t)
+    z = T(H) @ T(W).T
+    assert np.allclose(loss, tf.cross_entropy(z, T(t), reduction="none", ignore_index=-100), rtol=1e-13, atol=1e-13)
+    assert np.allclose(mean[0], tf.cross_entropy(z, T(t), ignore_index=-100), rtol=1e-13)
+    assert np.allclose(lse, torch.logsumexp(z, 1), rtol=1e-13)
+    assert np.allclose(ends.layer_norm(X, g, b, 1e-5)[0], tf.layer_norm(T(X), (9,), T(g), T(b), 1e-5), rtol=1e-12, atol=1e-13)
+    ids = np.array([4, 0, 10, 4])
+    assert np.allclose(ends.embed(W, ids, 0.5), 0.5 * tf.embedding(T(ids), T(W)))
