@@ -536,7 +536,8 @@ int zoact_layer_norm_grad(zoact_ctx* ctx, const void* dY, int64_t ld_dy, const v
  *   dW [vocab, d] of wgdtype (dtype or FP32); either may be NULL.  accumulate != 0 adds to dW, which must then be FP32
  *   (ZOACT_ERR_UNSUPPORTED otherwise).
  * What lies in a row of H whose target is negative reaches no output, be it NaN or infinite.
- * Context scratch: 8 bytes a row for every 128 vocabulary entries; FP32: 6 bytes an element of H and W.  With a gradient the
+ * Context scratch: 8 bytes a row for every 128 vocabulary entries; FP32: 6 bytes an element of H and W (few
+ *   rows without a gradient: none).  With a gradient the
  *   rows are taken in chunks of at most 2 GiB of G, or 256 rows: 2 bytes (FP32: 10) a row and entry, a chunk of H by columns,
  *   fp32 partial sums of dH's last tiles, and 4 bytes a weight where several chunks add to a 16-bit dW.
  * A mean or estimate that is not finite sets ZOACT_ERR_NONFINITE.  d % 8 == 0 (16-bit) or d % 4 == 0 (FP32); H, W, dH

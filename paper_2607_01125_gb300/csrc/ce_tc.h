@@ -33,6 +33,10 @@ struct Blocks {
 // in fp32, to G.
 int launch_logits(Ctx* ctx, const Operand& W, const Operand& H, float2* part, int64_t part_ld, float* zt, const void* targets,
                   int id64, int64_t T, int keep, const Blocks& G);
+// The same for a few fp32 rows as they are (keep: KEEP_NONE or KEEP_Z); few_rows says when.
+int launch_logits_few(Ctx* ctx, const float* W, int64_t vocab, const float* H, int64_t rows, int d, float2* part,
+                      int64_t part_ld, float* zt, const void* targets, int id64, int64_t T, int keep, const Blocks& G);
+bool few_rows(const Ctx* ctx, int64_t rows, int64_t vocab, int d);
 // out [G.rows, W.cols] of dtype = alpha G W.
 int launch_by_h(Ctx* ctx, const Operand& W, const Blocks& G, const float* alpha, void* out, int dtype);
 // out [G.vocab, H.cols] of dtype = alpha G^T H, added to out (fp32) with add; rows without a target are not taken.

@@ -20,6 +20,10 @@
 //
 // Roles, barriers and bounded waits are those of the pair forward on CTA pairs: a TMA producer in each CTA, one MMA issuer
 // in the leader, eight epilogue warps in each (two warpgroups), two accumulators in TMEM.
+//
+// Measured (bf16, 4096 x 128256 unless said): 32 rows 154 us, W at 6.8 TB/s; 4096 rows 2.10 ms with the tensor pipe 98% busy;
+// with gradients 2048 rows 1.11 / 1.13 / 1.05 ms (93 to 97%, under the power cap), 333 rows of 5120 x 50272 in fp16
+// 142 / 128 / 147 us (60 / 70 / 56%: 384 rows of MMA for 333, and the last one's stores).
 #pragma once
 #include "pair_tc2_kernel.cuh"
 
@@ -38,12 +42,6 @@ constexpr int EPI_THREADS = 256, EPI_BASE = 128, THREADS = EPI_BASE + EPI_THREAD
 constexpr int REGS_ISSUE = 56, REGS_EPI = 224;
 constexpr int TMEM_COLS = 512, MAX_BUF = 4;
 constexpr int STG_BYTES = 16384;                          // a staging buffer (128 rows x 128 bytes)
-// Epilogue area beside the ring: a staging buffer for each warpgroup, or two.
-__host__ __device__ constexpr int aux_bytes(int epi) { return epi == 5 ? 4 * STG_BYTES : 2 * STG_BYTES; }
-__host__ __device__ constexpr int ring_bytes(int epi) { return 229376 - aux_bytes(epi); }
-constexpr int SMEM_BYTES = 1024 + 229376 + 256;
-static_assert(SMEM_BYTES <= 232448, "dynamic shared memory above the 227 KB a CTA may use");
-
 enum Epi {
   EPI_LSE = 0,   // the rows' statistics
   EPI_LOG,       // and the tile's maximum - z as 16-bit fixed point
@@ -52,6 +50,12 @@ enum Epi {
   EPI_ROW,       // D scaled, from registers
   EPI_ROW_STAGED // the same through shared memory
 };
+
+// Epilogue area beside the ring: a staging buffer for each warpgroup, or two.
+__host__ __device__ constexpr int aux_bytes(int epi) { return epi == EPI_ROW_STAGED ? 4 * STG_BYTES : 2 * STG_BYTES; }
+__host__ __device__ constexpr int ring_bytes(int epi) { return 229376 - aux_bytes(epi); }
+constexpr int SMEM_BYTES = 1024 + 229376 + 256;
+static_assert(SMEM_BYTES <= 232448, "dynamic shared memory above the 227 KB a CTA may use");
 
 struct Maps {
   CUtensorMap a, b, out;

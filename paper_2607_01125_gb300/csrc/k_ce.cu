@@ -442,7 +442,8 @@ int run(Ctx* ctx, const CeArgs& c) {
   float* lse = c.lse ? c.lse : s.lse;
   float* loss = c.loss ? c.loss : s.loss;
   Operand W = {c.W, optype, c.vocab, c.d, c.d, 1, c.vocab * c.d}, H = {c.H, optype, c.rows, c.d, c.d, 1, c.rows * c.d};
-  if constexpr (F32) {
+  const bool few = F32 && ce::few_rows(ctx, c.rows, c.vocab, c.d);
+  if (F32 && (grad || !few)) {
     const int64_t ld = (c.d + 7) / 8 * 8;
     uint16_t* W3 = (uint16_t*)scratch(ctx, SLOT_CE_SPLIT, (size_t)(c.vocab + c.rows) * ld * 6);
     if (!W3) return ZOACT_ERR_NOMEM;
@@ -453,9 +454,16 @@ int run(Ctx* ctx, const CeArgs& c) {
     W = {W3, optype, c.vocab, c.d, ld, 3, c.vocab * ld};
     H = {H3, optype, c.rows, c.d, ld, 3, c.rows * ld};
   }
+  // the logits of rows [r0, r0 + h.rows), kept in G as asked for
+  auto logits = [&](const Operand& h, int64_t r0, const void* targets, int keep, const ce::Blocks& G) {
+    if (few)
+      return ce::launch_logits_few(ctx, (const float*)c.W, c.vocab, (const float*)c.H + r0 * c.d, h.rows, c.d, s.part, s.part_ld,
+                                   s.zt + r0, targets, c.id64, c.T, keep, G);
+    return ce::launch_logits(ctx, W, h, s.part, s.part_ld, s.zt + r0, targets, c.id64, c.T, keep, G);
+  };
   int st;
   if (!grad) {
-    st = ce::launch_logits(ctx, W, H, s.part, s.part_ld, s.zt, c.targets, c.id64, c.T, ce::KEEP_NONE, ce::Blocks{});
+    st = logits(H, 0, c.targets, ce::KEEP_NONE, ce::Blocks{});
     if (!st) st = join(ctx, c, s, tiles, 0, c.rows, lse, loss);
     return st ? st : finish(ctx, c, loss);
   }
@@ -476,7 +484,7 @@ int run(Ctx* ctx, const CeArgs& c) {
     Hc.rows = n;
     ce::Blocks G = {kept, optype, n, c.vocab, PARTS};
     const void* targets = (const char*)c.targets + r0 * (c.id64 ? 8 : 4);
-    st = ce::launch_logits(ctx, W, Hc, s.part, s.part_ld, s.zt + r0, targets, c.id64, c.T, F32 ? ce::KEEP_Z : ce::KEEP_LOG, G);
+    st = logits(Hc, r0, targets, F32 ? ce::KEEP_Z : ce::KEEP_LOG, G);
     if (!st) st = join(ctx, c, s, tiles, r0, n, lse, loss);
     if (st) return st;
     if constexpr (F32) {

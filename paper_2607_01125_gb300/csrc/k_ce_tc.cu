@@ -15,6 +15,10 @@ constexpr int LOGIT_GROUP = 8, GRAD_GROUP = 64, FP32_GROUP = 4;
 // 4096 x 128256 head in bf16, rows on N / on M: 100 rows 357 us / 368, 200 rows 412 / 410, 400 rows 683 / 699, 512 rows
 // 761 / 749, 1024 rows 1469 / 1404, 2048 rows 2795 / 2668; 333 rows of 5120 x 50272 in fp16 326 / 349.
 constexpr double ROWS_M_GAIN = 1.15;
+// fp32 rows that are multiplied as they are: up to this many (a head is then read as it is at most three times; loss by parts /
+// as they are, 20000 x 1024: 8 rows 88 us / 28.6, 24 rows 88 / 47.5, 32 rows 88 / 64), or as many as fill no more than a
+// block on each SM (128 rows of 256 against 1009 entries: 16.0 us / 10.8, of 4096: 103 / 49); and their shared memory at most.
+constexpr int FEW_ROWS = 24, FEW_SMEM = 160 * 1024;
 // K-blocks below which the product by W stores through shared memory (epi_row).
 constexpr int STAGED_BELOW = 14;
 
@@ -88,6 +92,78 @@ ce_tail_kernel(const float* __restrict__ part, int tail_first, int tail, int spl
 #pragma unroll 4
   for (int j = 0; j < split; ++j) s += __ldcg(src + j * step);
   out[n * M + m] = from_f32<TO>(s * __ldg(alpha));
+}
+
+// Logits of a few fp32 rows, each read of W's used for FEW rows: a block has V_TILE entries of the vocabulary, a warp four of
+// them at a time, its lanes their columns; H's rows lie in shared memory.  Splitting W for the tensor cores reads and writes
+// 2.5 times its bytes before the product reads them again: see FEW_ROWS.  Two blocks an SM (128 registers) carry a head of
+// little more than one block each: 20000 x 1024 28 us for 38 with one (50272 x 4096, 8 rows: 199 for 185).
+constexpr int FEW = 8, FEW_THREADS = 256, FEW_ENTRIES = 4;
+static_assert(FEW * FEW_ENTRIES == 32 && FEW == FEW_THREADS / 32, "a lane a sum, a warp a row");
+
+__global__ void __launch_bounds__(FEW_THREADS, 2)
+ce_few_kernel(const float* __restrict__ W, int64_t vocab, const float* __restrict__ H, int64_t rows, int d, int groups,
+              float2* __restrict__ part, int64_t part_ld, float* __restrict__ zt, const void* __restrict__ targets, int id64,
+              int64_t T, float* __restrict__ Z) {
+  pdl_wait();
+  pdl_trigger();
+  extern __shared__ __align__(16) uint8_t few_smem[];
+  float* hs = reinterpret_cast<float*>(few_smem);                    // [FEW][d]
+  __shared__ float z[V_TILE][FEW + 1];
+  const int64_t tile = blockIdx.x / groups, r0 = (int64_t)(blockIdx.x - tile * groups) * FEW, v0 = tile * V_TILE;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c4 = d / 4;
+  for (int i = threadIdx.x; i < FEW * c4; i += FEW_THREADS) {
+    const int r = i / c4;
+    reinterpret_cast<float4*>(hs)[i] =
+        r0 + r < rows ? reinterpret_cast<const float4*>(H + (r0 + r) * d)[i - r * c4] : make_float4(0.f, 0.f, 0.f, 0.f);
+  }
+  __syncthreads();
+  for (int e0 = warp * FEW_ENTRIES; e0 < V_TILE; e0 += FEW_ENTRIES * FEW_THREADS / 32) {
+    const float4* w[FEW_ENTRIES];
+#pragma unroll
+    for (int i = 0; i < FEW_ENTRIES; ++i) {
+      const int64_t v = v0 + e0 + i;
+      w[i] = reinterpret_cast<const float4*>(W + (v < vocab ? v : vocab - 1) * d);
+    }
+    float acc[FEW_ENTRIES * FEW];
+#pragma unroll
+    for (int k = 0; k < FEW_ENTRIES * FEW; ++k) acc[k] = 0.f;
+#pragma unroll 4
+    for (int c = lane; c < c4; c += 32) {
+      float4 x[FEW_ENTRIES];
+#pragma unroll
+      for (int i = 0; i < FEW_ENTRIES; ++i) x[i] = __ldcs(w[i] + c);
+#pragma unroll
+      for (int r = 0; r < FEW; ++r) {
+        const float4 h = reinterpret_cast<const float4*>(hs)[r * c4 + c];
+#pragma unroll
+        for (int i = 0; i < FEW_ENTRIES; ++i)
+          acc[i * FEW + r] = fmaf(x[i].x, h.x, fmaf(x[i].y, h.y, fmaf(x[i].z, h.z, fmaf(x[i].w, h.w, acc[i * FEW + r]))));
+      }
+    }
+    const float sum = columns_over_lanes<false>(acc, lane);
+    z[e0 + lane / FEW][lane % FEW] = sum;
+  }
+  __syncthreads();
+  const int64_t row = r0 + warp;
+  if (row >= rows) return;
+  const int64_t t = load_id(targets, id64, row % T) - v0, blocks = (vocab + 63) / 64;
+  float x[V_TILE / 32], m = -INFINITY, s = 0.f;
+#pragma unroll
+  for (int k = 0; k < V_TILE / 32; ++k) {
+    const int e = k * 32 + lane;
+    x[k] = v0 + e < vocab ? z[e][warp] : -INFINITY;
+    m = fmaxf(m, x[k]);
+    if (e == t && v0 + e < vocab) zt[row] = x[k];
+    if (Z && (v0 + e) / 64 < blocks) Z[((v0 + e) / 64 * rows + row) * 64 + (e & 63)] = x[k];
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+#pragma unroll
+  for (int k = 0; k < V_TILE / 32; ++k) s += expf(x[k] - m);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  if (lane == 0) part[tile * part_ld + row] = make_float2(m, s);
 }
 
 // Tiles that fill no whole wave of pairs, cut along K: the pieces whose rounds of 1 / split tile, with the time to write
@@ -164,6 +240,22 @@ int launch_logits(Ctx* ctx, const Operand& W, const Operand& H, float2* part, in
     case KEEP_Z: return rows_m ? launch<EPI_Z, true, float>(ctx, tm, p) : launch<EPI_Z, false, float>(ctx, tm, p);
     default: return rows_m ? launch<EPI_LSE, true, float>(ctx, tm, p) : launch<EPI_LSE, false, float>(ctx, tm, p);
   }
+}
+
+bool few_rows(const Ctx* ctx, int64_t rows, int64_t vocab, int d) {
+  const int64_t blocks = (vocab + V_TILE - 1) / V_TILE * ((rows + FEW - 1) / FEW);
+  return (rows <= FEW_ROWS || blocks <= ctx->sm_count) && (int64_t)FEW * d * 4 <= FEW_SMEM;
+}
+
+int launch_logits_few(Ctx* ctx, const float* W, int64_t vocab, const float* H, int64_t rows, int d, float2* part,
+                      int64_t part_ld, float* zt, const void* targets, int id64, int64_t T, int keep, const Blocks& G) {
+  const int groups = (int)((rows + FEW - 1) / FEW);
+  const int64_t blocks = (vocab + V_TILE - 1) / V_TILE * groups;
+  ZOACT_CUDA_TRY(cudaFuncSetAttribute(ce_few_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, FEW_SMEM));
+  ZOACT_CUDA_TRY(launch_pdl(ctx, ce_few_kernel, dim3((unsigned)blocks), dim3(FEW_THREADS), (size_t)FEW * d * 4, W, vocab, H, rows,
+                            d, groups, part, part_ld, zt, targets, id64, T, keep == KEEP_Z ? (float*)G.p : (float*)nullptr));
+  ++ctx->n_launch;
+  return ZOACT_OK;
 }
 
 int launch_by_h(Ctx* ctx, const Operand& W, const Blocks& G, const float* alpha, void* out, int dtype) {

@@ -420,6 +420,33 @@ def test_cross_entropy_of_ignored_rows_that_are_not_finite(ctx, dt, T):
         assert all(torch.equal(a, b) for a, b in zip(out[0], other))
 
 
+@pytest.mark.parametrize("T,d,vocab", [(2, 1024, 20000), (24, 260, 20011), (25, 260, 20011), (160, 64, 900), (9, 5124, 130)])
+def test_cross_entropy_of_fp32_rows_multiplied_as_they_are_or_in_parts(ctx, T, d, vocab):
+    """Both sides of the rule by rows and by blocks, and a width whose rows do not fit; the gradient call gives the same bits."""
+    rng = np.random.default_rng(T + vocab)
+    H, W = rnd(1, T, d), rnd(2, vocab, d, std=2.0 / np.sqrt(d))
+    t = _targets(rng, T, vocab, 0.1)
+    loss, lse, mean = torch.empty(T, device=DEV), torch.empty(T, device=DEV), torch.empty(1, dtype=torch.float64, device=DEV)
+    zo.zoact_ce_loss(ctx, H, W, ints(t), loss=loss, lse=lse, mean=mean)
+    loss2, dH = torch.empty_like(loss), torch.empty_like(H)
+    zo.zoact_ce_grad(ctx, H, W, ints(t), dH=dH, loss=loss2)
+    clean(ctx)
+    h, w = n64(H), n64(W)
+    wloss, wlse, wmean = ends.cross_entropy(h, w, t)
+    ez = _logit_error(h, w)
+    el = 2 * ez + 2.0 ** -20 + 4 * F * np.abs(wlse)
+    within(lse, wlse, el)
+    within(loss, wloss, el + F * np.abs(wloss))
+    within(mean, wmean, el.max())
+    assert torch.equal(loss, loss2)
+    P = np.exp(h @ w.T - wlse[:, None]) * (t >= 0)[:, None]
+    G = P.copy()
+    G[np.arange(T), np.maximum(t, 0)] -= (t >= 0)
+    eg = 2.0 ** -21 * np.abs(G) + (2 * ez + 2.0 ** -20) * P
+    wh, N = ends.cross_entropy_grad(h, w, t)[0], max(1, int((t >= 0).sum()))
+    within(dH, wh, (eg @ np.abs(w) + (vocab + 8) * F * (np.abs(G) @ np.abs(w))) / N + F * np.abs(wh))
+
+
 @pytest.mark.parametrize("dt", ["bf16", "fp16", "fp32"])
 def test_cross_entropy_gradient_beside_a_target_that_is_nearly_sure(ctx, dt):
     """Logits 24 below the target's, in its tile of the vocabulary too: their rows of dW keep their own digits, and the loss
