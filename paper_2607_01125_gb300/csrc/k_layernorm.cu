@@ -716,15 +716,16 @@ bool parts_for(Ctx* ctx, int64_t blocks, int n, bool wanted, float** part) {
 }
 
 // Blocks that run at once, by their registers a thread and 200 KB of rings an SM (three stages at least), and a ring's stages.
+constexpr int RING_BYTES = 200 * 1024;
 struct RingShape {
   int blocks, stages, smem;
 };
 RingShape ring_shape(const Ctx* ctx, int threads, int regs, int64_t stage, int64_t rows) {
   int per_sm = 65536 / regs / threads;
   per_sm = per_sm > 8 ? 8 : per_sm;
-  while (per_sm > 1 && 200 * 1024 / per_sm / stage < 3) --per_sm;
+  while (per_sm > 1 && RING_BYTES / per_sm / stage < 3) --per_sm;
   RingShape q;
-  q.stages = (int)(200 * 1024 / per_sm / stage);
+  q.stages = (int)(RING_BYTES / per_sm / stage);
   if (q.stages > LN_MAX_STAGES) q.stages = LN_MAX_STAGES;
   q.smem = (int)(q.stages * stage);
   const int64_t most = (int64_t)ctx->sm_count * per_sm;
@@ -738,7 +739,8 @@ int go_ring(Ctx* ctx, int consumers, const void* dY, int64_t ld_dy, const void* 
   auto kern = ln_grad_ring_kernel<T, TP, VPT, MOST>;
   const int regs = VPT * (16 / (int)sizeof(T)) <= 8 ? 72 : 112;
   const RingShape q = ring_shape(ctx, consumers + 32, regs, 2 * (int64_t)n * (int)sizeof(T), rows);
-  ZOACT_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, q.smem));
+  // the most that any width takes: the attribute is the function's, and another host thread may be between it and a launch
+  ZOACT_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, RING_BYTES));
   float* part;
   if (!parts_for(ctx, q.blocks, n, dg || db, &part)) return ZOACT_ERR_NOMEM;
   ZOACT_CUDA_TRY(launch_pdl(ctx, kern, dim3((unsigned)q.blocks), dim3(consumers + 32), q.smem, (const T*)dY, ld_dy, (const T*)X,
