@@ -77,3 +77,25 @@ def test_layer_norm_gradients_of_two_widths_at_once():
 
     assert _at_once([case(n) for n in (1024, 2048, 1024, 2048)], 20000) == [[]] * 4
     assert all(torch.equal(k[-1], k[-2]) for k in keep)
+
+
+def test_embedding_gradients_of_short_and_long_lists_at_once():
+    fn, vocab, d, keep = zo.load().zoact_embed_grad, 50, 8, []
+
+    def case(n):
+        ids = torch.randint(0, vocab, (n,), generator=torch.Generator(DEV).manual_seed(n), device=DEV)
+        dY, dE, want = rnd(n, n, d), torch.empty(vocab, d, device=DEV), torch.empty(vocab, d, device=DEV)
+        keep.append((ids, dY, dE, want))
+
+        def args(c, out):
+            return (c.handle, dY.data_ptr(), zo.DT_FP32, n, d, ids.data_ptr(), zo.ID_INT64, vocab, 1.0, out.data_ptr(),
+                    zo.DT_FP32, 0)
+
+        c = zo.Context(0)
+        assert fn(*args(c, want)) == 0
+        torch.cuda.synchronize()
+        c.close()
+        return lambda c: (fn, args(c, dE))
+
+    assert _at_once([case(n) for n in (40, 10000, 50, 9000)], 4000) == [[]] * 4
+    assert all(torch.equal(k[-1], k[-2]) for k in keep)
