@@ -239,6 +239,9 @@ __device__ __forceinline__ uint32_t log_fixed(float x) {
   return __float_as_uint(fminf(x * -LOG_STEPS, 65535.f) + 8388608.f) & 0xffffu;
 }
 __device__ __forceinline__ float exp_of(float x) { return pairtc::exp2_sfu(x * 1.44269504f); }
+// What a tile's exponentials are taken from: its maximum m, or 0 where all of its logits are minus infinity (the difference of
+// two of these would be NaN; from 0 each exponential is 0, and the tile leaves a sum of 0).
+__device__ __forceinline__ float exp_base(float m) { return m == -INFINITY ? 0.f : m; }
 
 // One tile of logits, M = rows: a thread has a row and the 128 vocabulary entries of its warpgroup from v0.
 template <int EPI>
@@ -278,12 +281,12 @@ __device__ __forceinline__ void epi_rows(const Params& p, const Maps& tm, uint8_
   for (int i = 0; i < CHUNKS; ++i)
 #pragma unroll
     for (int j = 0; j < 32; ++j) mx[j & 3] = fmaxf(mx[j & 3], a.x[i][j]);
-  const float m = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+  const float m = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])), from = exp_base(m);
   float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int i = 0; i < CHUNKS; ++i) {
 #pragma unroll
-    for (int j = 0; j < 32; ++j) a.x[i][j] -= m;
+    for (int j = 0; j < 32; ++j) a.x[i][j] -= from;
     if (EPI == EPI_LOG && (i & 1) == 0) {           // a box of 64 entries: wait until the last one has been read
       if ((etid & 127) == 0 && pending) tc::bulk_wait_read0();
       tc::named_bar_sync(4 + half, 128);
@@ -355,7 +358,7 @@ __device__ __forceinline__ void epi_lanes(const Params& p, Exchange* ex, Part& a
   for (int i = 0; i < CHUNKS; ++i) {
     const int k = i * 32 + lane;
     if (chunk_of<false>(half, i) < nch)
-      all[k] = fmaxf(fmaxf(ex->mx[half][0][k], ex->mx[half][1][k]), fmaxf(ex->mx[half][2][k], ex->mx[half][3][k]));
+      all[k] = exp_base(fmaxf(fmaxf(ex->mx[half][0][k], ex->mx[half][1][k]), fmaxf(ex->mx[half][2][k], ex->mx[half][3][k])));
   }
   __syncwarp();
 #pragma unroll
@@ -393,9 +396,10 @@ __device__ __forceinline__ void epi_lanes(const Params& p, Exchange* ex, Part& a
   // chunk i's statistics by warp i of the warpgroup
   const int c = chunk_of<false>(half, quad), k = quad * 32 + lane;
   const int64_t n = n0 + c * 32 + lane;
-  if (c < nch && n < p.rows && m0 < p.vocab)
-    p.part[m0 / BM * p.part_ld + n] =
-        make_float2(all[k], (ex->sum[half][0][k] + ex->sum[half][1][k]) + (ex->sum[half][2][k] + ex->sum[half][3][k]));
+  if (c < nch && n < p.rows && m0 < p.vocab) {
+    const float s = (ex->sum[half][0][k] + ex->sum[half][1][k]) + (ex->sum[half][2][k] + ex->sum[half][3][k]);
+    p.part[m0 / BM * p.part_ld + n] = make_float2(s == 0.f ? -INFINITY : all[k], s);     // a sum of 0: see exp_base
+  }
 }
 
 // D^T scaled (or a K piece of it, unscaled fp32): a warp stores 32 consecutive elements of each row.

@@ -160,7 +160,7 @@ ce_few_kernel(const float* __restrict__ W, int64_t vocab, const float* __restric
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
 #pragma unroll
-  for (int k = 0; k < V_TILE / 32; ++k) s += expf(x[k] - m);
+  for (int k = 0; k < V_TILE / 32; ++k) s += expf(x[k] - exp_base(m));
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
   if (lane == 0) part[tile * part_ld + row] = make_float2(m, s);
