@@ -346,8 +346,17 @@ __global__ void __launch_bounds__(CE_THREADS) ce_round_kernel(const float4* __re
   }
 }
 
+// What a finite x has beyond the bf16 range, taken off it: the largest value of bf16, 3.3895e38, is the first part of what lies
+// above it (rounded to the nearest, the part would be infinite).  0 for all others; an infinity stays one.
+__device__ __forceinline__ float take_excess(float& x) {
+  constexpr float MOST = 3.38953139e38f;
+  const float all = x;
+  if (fabsf(x) > MOST && fabsf(x) < INFINITY) x = copysignf(MOST, x);
+  return all - x;
+}
+
 // fp32 operands in three bf16 parts: rows of W and then of H [., d] to [3][rows][ld] each, ld = d rounded up to 8 (what lies
-// past d is not read).  blockIdx.y: row (its blocks stride over the rows); four elements a thread.
+// past d is not read).  Four elements a thread.
 __global__ void __launch_bounds__(CE_THREADS)
 ce_split_kernel(const float* __restrict__ W, int64_t w_rows, uint16_t* __restrict__ W3, const float* __restrict__ H,
                 int64_t h_rows, uint16_t* __restrict__ H3, int d, int ld) {
@@ -363,8 +372,10 @@ ce_split_kernel(const float* __restrict__ W, int64_t w_rows, uint16_t* __restric
     float4 v = *reinterpret_cast<const float4*>((of_w ? W : H) + row * d + c);
     uint16_t* o = (of_w ? W3 : H3) + row * ld + c;
     const int64_t part = (of_w ? w_rows : h_rows) * ld;
+    const float4 more = make_float4(take_excess(v.x), take_excess(v.y), take_excess(v.z), take_excess(v.w));
 #pragma unroll
     for (int p = 0; p < 3; ++p) {
+      if (p == 1) v = make_float4(v.x + more.x, v.y + more.y, v.z + more.z, v.w + more.w);
       const uint32_t lo = next_part_bf16x2(v.x, v.y), hi = next_part_bf16x2(v.z, v.w);
       *reinterpret_cast<uint2*>(o + p * part) = make_uint2(lo, hi);
     }

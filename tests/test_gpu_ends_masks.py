@@ -118,3 +118,32 @@ def test_entries_masked_by_minus_infinity(ctx, dt, T, d, vocab):
 def test_entries_whose_logits_overflow_to_minus_infinity(ctx, dt, T, d, vocab):
     H, W, t, stay = _masked(dt, T, d, vocab, 4.0, -2.0 ** 127)
     _against_the_rest(ctx, H, W, t, stay, dt, grad=True)
+
+
+# fp32 above bf16's largest value, 3.3895e38: what the first of three bf16 parts would round to infinity
+@pytest.mark.parametrize("T,d,vocab", [(3, 64, 700), (90, 72, 5000), (601, 260, 1009)])
+def test_entries_masked_by_the_lowest_fp32(ctx, T, d, vocab):
+    H, W, t, stay = _masked("fp32", T, d, vocab, 1.0, torch.finfo(torch.float32).min)
+    _against_the_rest(ctx, H, W, t, stay, "fp32", grad=True)
+
+
+def test_fp32_operands_up_to_the_largest(ctx):
+    """Products that are exact powers of two or the largest value itself, on either side: log-sum-exps of one entry."""
+    T, d, vocab = 200, 8, 5000
+    big = torch.finfo(torch.float32).max
+    for of_h in (False, True):
+        A, B = torch.zeros(T, d, device=DEV), torch.zeros(vocab, d, device=DEV)
+        (A if of_h else B)[:, 0] = big
+        (B if of_h else A)[:, 0] = 2.0 ** -120
+        (B if of_h else A)[7, 0] = 2.0 ** -119
+        want = float(big) * 2.0 ** -120                   # 256, to fp32
+        lse = torch.empty(T, device=DEV)
+        zo.zoact_ce_loss(ctx, A, B, ints(np.zeros(T)), lse=lse)
+        torch.cuda.synchronize()
+        assert ctx.device_status() == 0
+        one = np.full(T, want + np.log(vocab))
+        if of_h:                                         # entry 7 alone counts: 512 beside 256
+            one[:] = 2 * want
+        else:
+            one[7] = 2 * want + np.log(vocab)
+        within(lse, one, 2.0 ** -21 * one)
