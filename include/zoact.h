@@ -535,7 +535,8 @@ int zoact_layer_norm_grad(zoact_ctx* ctx, const void* dY, int64_t ld_dy, const v
  * zoact_ce_grad: the same losses for one block, and the gradient of grad_scale * L: dH [T, d] of dtype and
  *   dW [vocab, d] of wgdtype (dtype or FP32); either may be NULL.  accumulate != 0 adds to dW, which must then be FP32
  *   (ZOACT_ERR_UNSUPPORTED otherwise).
- * What lies in a row of H whose target is negative reaches no output, be it NaN or infinite.
+ * lse is each row's own, with a target or without.  What lies in a row of H without a target reaches that row's lse and
+ * nothing else (no loss, mean or gradient, and no other row's lse), be it NaN or infinite.
  * A vocabulary entry can be masked by its logits: minus infinity, in whole tiles too, has a share of 0.  FP32 operands that
  * are multiplied in three bf16 parts (all but few rows' logits) may have any finite value; an infinity there gives NaN.
  * Context scratch: 8 bytes a row for every 128 vocabulary entries; FP32: 6 bytes an element of H and W (few

@@ -147,3 +147,39 @@ def test_fp32_operands_up_to_the_largest(ctx):
         else:
             one[7] = 2 * want + np.log(vocab)
         within(lse, one, 2.0 ** -21 * one)
+
+
+@pytest.mark.parametrize("dt,T,vocab", [("bf16", 40, 700), ("bf16", 1100, 900), ("fp16", 1100, 900), ("fp32", 8, 700),
+                                        ("fp32", 300, 2000)])
+def test_what_a_row_without_a_target_reaches(ctx, dt, T, vocab):
+    """Its own log-sum-exp, which is finite where the row is, and nothing else."""
+    d = 72
+    H, W = rnd(1, T, d, dt=dt), rnd(2, vocab, d, std=0.2, dt=dt)
+    t = np.random.default_rng(T).integers(0, vocab, T)
+    t[[0, 2, T - 1]] = -1, -100, vocab                   # the last one is none of the vocabulary's
+    none = torch.zeros(T, dtype=torch.bool, device=DEV)
+    none[[0, 2, T - 1]] = True
+    out = []
+    for fill in (None, float("nan"), float("inf")):
+        h = H.clone()
+        if fill is not None:
+            h[none] = fill
+        dH, dW = torch.empty_like(h), torch.empty_like(W)
+        loss, lse, mean = torch.empty(T, device=DEV), torch.empty(T, device=DEV), torch.empty(1, dtype=torch.float64, device=DEV)
+        zo.zoact_ce_grad(ctx, h, W, ints(t), dH=dH, dW=dW, loss=loss, lse=lse, mean=mean)
+        torch.cuda.synchronize()
+        assert ctx.device_status() == -1                 # the target that is not below the vocabulary
+        lse2 = torch.empty_like(lse)
+        zo.zoact_ce_loss(ctx, h, W, ints(t), lse=lse2)
+        torch.cuda.synchronize()
+        assert ctx.device_status() == -1
+        assert torch.equal(lse[~none], lse2[~none])
+        out.append((dH, dW, loss, mean, lse[~none]))
+        if fill is None:
+            wlse = ends.cross_entropy(n64(H), n64(W), np.zeros(T, dtype=int))[1]
+            ez = (d + 8) * F * (np.abs(n64(H)) @ np.abs(n64(W)).T).max()
+            within(lse, wlse, 2 * ez + 2.0 ** -20 + 4 * F * np.abs(wlse))
+        else:
+            assert not torch.isfinite(lse[none]).any()
+    for other in out[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(out[0], other))
