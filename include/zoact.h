@@ -532,6 +532,8 @@ int zoact_layer_norm_grad(zoact_ctx* ctx, const void* dY, int64_t ld_dy, const v
  * zoact_ce_pair: out[4] = {L+, L-, D, a} as zoact_loss_pair writes them: D = L+ - L- as the mean of the rows' loss
  *   differences, a = D / (2 eps); H [2T, d].
  * zoact_ce_multi: out[2 n_blocks - 1] = {L_0 .. L_q, a_1 .. a_q} as zoact_loss_multi, a_j = (L_j - L_0) / mu.
+ * Means of shards with different numbers of counted rows (data-parallel ranks) have to be weighed by these before they are
+ * averaged: zoact_mean_over_ranks gives each rank the same weight.
  * zoact_ce_grad: the same losses for one block, and the gradient of grad_scale * L: dH [T, d] of dtype and
  *   dW [vocab, d] of wgdtype (dtype or FP32); either may be NULL.  accumulate != 0 adds to dW, which must then be FP32
  *   (ZOACT_ERR_UNSUPPORTED otherwise).

@@ -5,6 +5,18 @@ loss pair on its own token shard, and the ranks then average the loss vector --
 [L+, L-, D, a], or [L_0 .. L_q, a_1 .. a_q] for the one-sided q-query estimator
 (each entry a mean over the rank's T * n elements, so with equal shards their
 average is the global value; every a is linear in the losses).
+
+The cross entropy's vectors (zoact_ce_pair, zoact_ce_multi; TokenStep) are means
+over the rows that have a target.  Where ranks have different numbers of those,
+the average of the ranks' means is not the mean over all rows: each rank first
+weighs its vector by its share of them,
+
+    n = (targets >= 0).sum().double()
+    total = n.clone()
+    dist.all_reduce(total)
+    loss_out.mul_(n * (world / total.clamp(min=1)))
+    allreduce_loss(loss_out, ctx)
+
 Each rank then applies the same Adam update with the same regenerated Z, so C
 stays identical on every rank without a gradient all-reduce.  check_replicas
 compares the ranks' fingerprints of their arenas (zoact_arena_hash) to detect a

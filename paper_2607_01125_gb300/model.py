@@ -469,7 +469,9 @@ class TokenStep:
     the norm directly and the table's gradient is whole (the ends warmed up before a stack is put between them).
 
     table [vocab, d] and head [vocab, d] of the activations' type; gain and bias [d] fp32 or that type, or None.
-    ids and targets [T] int32 or int64 on the device; a negative one is no token.
+    ids and targets [T] int32 or int64 on the device; a negative one is no token.  Losses and estimates are means over the rows
+    that have a target: data-parallel ranks whose numbers of these differ weigh their loss vectors before they average them
+    (see dp).
     """
 
     def __init__(self, stack, table, head=None, gain=None, bias=None, scale=1.0, norm_eps=1e-5, ctx=None):
