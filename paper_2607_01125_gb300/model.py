@@ -516,6 +516,8 @@ class TokenStep:
     def loss(self, targets):
         """The loss vector of the latest forward(): ZOStep.loss with the cross entropy in place of the mean square (the
         stack's two vectors take turns); without a stack [L]."""
+        if self.normed is None:
+            raise ValueError("TokenStep: forward() comes first")
         if self.stack is None:
             out = self.buf("loss", (1,), torch.float64)
             Z.zoact_ce_loss(self.ctx, self.normed, self.head, targets, mean=out)
@@ -530,6 +532,8 @@ class TokenStep:
 
     def step(self, ids, targets, step, seed, query, lr=None):
         """One ZO step on tokens.  Returns the device loss vector."""
+        if self.stack is None:
+            raise ValueError("TokenStep.step: there is no stack whose coefficients could step")
         self.forward(ids, seed, query)
         out = self.loss(targets)
         self.stack.update(step, seed, query, lr)
@@ -540,6 +544,8 @@ class TokenStep:
         point; two-sided: the + point) by the ends' parameters, in fp32: dhead, dgain, dbias and, without a stack, dtable
         (tied: dtable is dhead, the sum of both uses).  Returns that block's mean loss (device, fp64 [1])."""
         T, d = ids.shape[0], self.table.shape[1]
+        if self.normed is None or T * self.n_blocks != self.normed.shape[0]:
+            raise ValueError(f"TokenStep.ends_grad: {T} ids are not those of the latest forward()")
         if self.dhead is None:
             f32 = dict(dtype=torch.float32, device=self.table.device)
             self.dhead = torch.empty(self.head.shape, **f32)
