@@ -491,7 +491,6 @@ int run_embed_grad(Ctx* ctx, const void* dY, int64_t n, int d, const void* ids, 
     const int ranks = (int)((n + RANK_TOKENS - 1) / RANK_TOKENS);
     const int smem = ((int)n + 3) / 4 * 16 + RANK_PARTS * RANK_TOKENS * 4;
     static_assert((RANK_MOST + 3) / 4 * 16 + RANK_PARTS * RANK_TOKENS * 4 <= 48 * 1024, "what any kernel may use");
-    if (ranks + zero_ctas == 0) return ZOACT_OK;
     ZOACT_CUDA_TRY(launch_pdl(ctx, embed_rank_kernel, dim3((unsigned)(ranks + zero_ctas)), dim3(SORT_THREADS), (size_t)smem, ids,
                               id64, (int)n, vocab, ranks, a, (uint8_t*)dE, zero_len, ctx->d_status));
   } else {

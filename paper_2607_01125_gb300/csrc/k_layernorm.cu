@@ -79,23 +79,14 @@ __device__ __forceinline__ uint4 pack(const float2* f) {
 template <typename TP>
 __device__ __forceinline__ float param_at(const TP* p, int64_t i, float none) { return p ? to_f32<TP>(p[i]) : none; }
 
-// The P pairs of parameters from element i on (16-byte loads), or `none`.
+// The P pairs of parameters from element i on (16-byte loads), or `none`.  Parameters are of the rows' type or wider.
 template <typename TP, int P>
 __device__ __forceinline__ void load_param(const TP* p, int64_t i, float none, float2* f) {
+  constexpr int N = 8 / (int)sizeof(TP);             // pairs of a vector
+  static_assert(P % N == 0, "whole vectors");
   if (p) {
-    constexpr int N = 8 / (int)sizeof(TP);           // pairs of a vector
 #pragma unroll
-    for (int q = 0; q < (P + N - 1) / N; ++q) {
-      if constexpr (P >= N) {
-        unpack<TP>(*reinterpret_cast<const uint4*>(p + i + q * 2 * N), f + q * N);
-      } else {                                       // 16-bit parameters of an fp32 vector: half a 16-byte vector
-        const uint2 h = *reinterpret_cast<const uint2*>(p + i);
-        float2 four[4];
-        unpack<TP>(make_uint4(h.x, h.y, 0u, 0u), four);
-#pragma unroll
-        for (int k = 0; k < P; ++k) f[k] = four[k];
-      }
-    }
+    for (int q = 0; q < P / N; ++q) unpack<TP>(*reinterpret_cast<const uint4*>(p + i + q * 2 * N), f + q * N);
   } else {
 #pragma unroll
     for (int k = 0; k < P; ++k) f[k] = both(none);

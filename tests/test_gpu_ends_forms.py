@@ -63,11 +63,11 @@ def _ce_reference(H, W, t, nb):
     return h, w, ez, torch.exp(z - lse[:, None]), loss, lse
 
 
-# rows on the M side, by the rule on 152 SMs; two, three, one and many groups of K; both dimensions ragged; the head's gradient
+# rows on the M side, by the rule on 152 SMs (the first two fp32 cases: on the N side); two, three, one and many groups of K; both dimensions ragged; the head's gradient
 # through shared memory (up to 13 K-blocks of 64 rows) and from registers
 @pytest.mark.parametrize("dt,T,d,vocab", [("bf16", 601, 520, 20011), ("fp16", 601, 520, 20011), ("bf16", 1003, 1032, 20011),
                                           ("fp16", 1003, 1032, 20011), ("bf16", 4095, 264, 1009), ("fp16", 4095, 264, 1009),
-                                          ("fp32", 1003, 260, 5003), ("fp32", 601, 1028, 1009)])
+                                          ("fp32", 1003, 260, 5003), ("fp32", 601, 1028, 1009), ("fp32", 1021, 260, 20011)])
 def test_cross_entropy_of_many_rows(ctx, dt, T, d, vocab):
     W = rnd(2, vocab, d, std=2.0 / d ** 0.5, dt=dt)
     t = torch.randint(0, vocab, (T,), generator=gen(3), device=DEV)
