@@ -28,9 +28,9 @@ struct Blocks {
   int64_t blocks() const { return (vocab + 63) / 64; }
 };
 
-// Logits z = H W^T: of each row the maximum and the sum of exp(z - maximum) over every V_TILE entries (part, [tile][part_ld])
-// and the target's logit (zt; row r has targets[r % T]); keep: min(65535, round(LOG_STEPS (maximum - z))) as 16-bit integers, or z
-// in fp32, to G.
+// Logits z = H W^T: of each row the maximum and the sum of exp(z - maximum) over every V_TILE entries without the target (part,
+// [tile][part_ld]; minus infinity and 0 where there is none) and the target's logit (zt; row r has targets[r % T]); keep:
+// min(65535, round(LOG_STEPS (maximum - z))) as 16-bit integers, or z in fp32, to G (the target's entry there is not its logit).
 int launch_logits(Ctx* ctx, const Operand& W, const Operand& H, float2* part, int64_t part_ld, float* zt, const void* targets,
                   int id64, int64_t T, int keep, const Blocks& G);
 // The same for a few fp32 rows as they are (keep: KEEP_NONE or KEEP_Z); few_rows says when.

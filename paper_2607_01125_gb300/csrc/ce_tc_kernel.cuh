@@ -243,7 +243,8 @@ __device__ __forceinline__ float exp_of(float x) { return pairtc::exp2_sfu(x * 1
 // two of these would be NaN; from 0 each exponential is 0, and the tile leaves a sum of 0).
 __device__ __forceinline__ float exp_base(float m) { return m == -INFINITY ? 0.f : m; }
 
-// One tile of logits, M = rows: a thread has a row and the 128 vocabulary entries of its warpgroup from v0.
+// One tile of logits, M = rows: a thread has a row and the 128 vocabulary entries of its warpgroup from v0.  A row's target leaves
+// by itself (zt) and is none of its tile's entries: beside its exponential, a nearly sure row's others would be rounded off.
 template <int EPI>
 __device__ __forceinline__ void epi_rows(const Params& p, const Maps& tm, uint8_t* stg, Part& a, int etid, int half, int row_in_cta,
                                          int64_t m0, int64_t v0, bool& pending) {
@@ -264,7 +265,11 @@ __device__ __forceinline__ void epi_rows(const Params& p, const Maps& tm, uint8_
 #pragma unroll
     for (int i = 0; i < CHUNKS; ++i)
 #pragma unroll
-      for (int j = 0; j < 32; ++j) z = i * 32 + j == (int)t ? a.x[i][j] : z;
+      for (int j = 0; j < 32; ++j) {
+        if (i * 32 + j != (int)t) continue;
+        z = a.x[i][j];
+        a.x[i][j] = -INFINITY;
+      }
     p.zt[row] = z;
   }
   if (EPI == EPI_Z && ok) {
@@ -344,7 +349,11 @@ __device__ __forceinline__ void epi_lanes(const Params& p, Exchange* ex, Part& a
       const int src = (int)(__shfl_sync(0xffffffffu, t, l) - vb);
       float z = 0.f;
 #pragma unroll
-      for (int j = 0; j < 32; ++j) z = j == l ? a.x[i][j] : z;
+      for (int j = 0; j < 32; ++j) {
+        if (j != l) continue;
+        z = a.x[i][j];
+        if (lane == src) a.x[i][j] = -INFINITY;
+      }
       if (lane == src) p.zt[n0 + c * 32 + l] = z;
     }
     float y[32];

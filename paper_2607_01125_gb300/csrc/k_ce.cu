@@ -12,8 +12,9 @@ namespace {
 
 constexpr int CE_THREADS = 256;
 
-// The tiles' maxima m_i and sums s_i of a row joined: m, log s with s = sum s_i exp(m_i - m) (a row that the model predicts
-// well has s = 1 + many terms that fp32 alone would drop one by one), lse = m + log s and loss = (m - z_t) + log s.
+// The tiles' maxima m_i and sums s_i of a row, which are without its target, and the target's logit z_t (as one more of them, with
+// a sum of 1) joined: m, log s with s = sum s_i exp(m_i - m), lse = m + log s and loss = (m - z_t) + log s.  A row that the
+// model predicts well has s = 1 + many terms that fp32 alone would drop one by one: these are summed first.
 // The gradient takes z - lse as (z - m) - log s, exact where z = m.
 // All of it in fp32 with what the additions round off beside the sum (fp64 FMAs run at 1/64 of the rate: with them this kernel
 // took 24 us for 2048 rows of 1002 tiles).  A block has ROWS rows; 1024 / ROWS groups of threads take their tiles in turn,
@@ -86,13 +87,15 @@ ce_join_kernel(const float2* __restrict__ part, int64_t tiles, int64_t part_ld, 
     a = (lane & o) ? join_sums(b, a) : join_sums(a, b);              // one order for both
   }
   if (lane != 0) return;
-  const float ls = logf(a.hi) + a.lo / a.hi;
-  const float l = a.m + ls;
-  stat[row] = make_float2(a.m, ls);
-  lse[row] = l;
   const int64_t t = load_id(targets, id64, row % T);
   if (t >= vocab) record_error(status, ZOACT_ERR_INVALID_ARG);
-  loss[row] = t >= 0 && t < vocab ? (a.m - zt[row]) + ls : 0.f;      // not l - zt: l's rounding would stay in a small loss
+  const bool counted = t >= 0 && t < vocab;
+  const float z = counted ? zt[row] : 0.f;
+  if (counted) a = join_sums(a, MaxSum{z, 1.f, 0.f});
+  const float ls = logf(a.hi) + a.lo / a.hi;
+  stat[row] = make_float2(a.m, ls);
+  lse[row] = a.m + ls;
+  loss[row] = counted ? (a.m - z) + ls : 0.f;      // not lse - z: lse's rounding would stay in a small loss
 }
 
 // alpha = scale / N, N the number of counted rows (at least 1): the factor of the gradient's products.
@@ -386,7 +389,8 @@ ce_split_kernel(const float* __restrict__ W, int64_t w_rows, uint16_t* __restric
 // layout.  Thread: 4 entries of a row.
 __global__ void __launch_bounds__(CE_THREADS)
 ce_split_g_kernel(const float* __restrict__ Z, uint16_t* __restrict__ G, int64_t blocks, int64_t rows,
-                  const float2* __restrict__ stat, const void* __restrict__ targets, int id64, int64_t vocab) {
+                  const float2* __restrict__ stat, const float* __restrict__ zt, const void* __restrict__ targets, int id64,
+                  int64_t vocab) {
   pdl_wait();
   pdl_trigger();
   const int64_t n4 = blocks * rows * 16;
@@ -400,8 +404,9 @@ ce_split_g_kernel(const float* __restrict__ Z, uint16_t* __restrict__ G, int64_t
       const float x[4] = {z.x, z.y, z.z, z.w};
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const float y = (x[k] - st.x) - st.y;
-        e[k] = v0 + k >= vocab ? 0.f : v0 + k == t ? expm1f(y) : expf(y);
+        const bool of_target = v0 + k == t;
+        const float y = ((of_target ? zt[row] : x[k]) - st.x) - st.y;
+        e[k] = v0 + k >= vocab ? 0.f : of_target ? expm1f(y) : expf(y);
       }
     }
 #pragma unroll
@@ -501,8 +506,8 @@ int run(Ctx* ctx, const CeArgs& c) {
     if constexpr (F32) {
       G.p = kept + (size_t)blocks * n * 64 * 4;
       ZOACT_CUDA_TRY(launch_pdl(ctx, ce_split_g_kernel, dim3(stride_blocks(ctx, blocks * n * 16)), dim3(CE_THREADS), 0,
-                                (const float*)kept, (uint16_t*)G.p, blocks, n, (const float2*)s.stat + r0, targets, c.id64,
-                                c.vocab));
+                                (const float*)kept, (uint16_t*)G.p, blocks, n, (const float2*)s.stat + r0, (const float*)s.zt + r0,
+                                targets, c.id64, c.vocab));
       ++ctx->n_launch;
     } else {
       st = make_g<T>(ctx, c, s, G, r0, n, targets);

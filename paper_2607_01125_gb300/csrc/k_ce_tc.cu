@@ -153,8 +153,11 @@ ce_few_kernel(const float* __restrict__ W, int64_t vocab, const float* __restric
   for (int k = 0; k < V_TILE / 32; ++k) {
     const int e = k * 32 + lane;
     x[k] = v0 + e < vocab ? z[e][warp] : -INFINITY;
+    if (e == t && v0 + e < vocab) {                                  // the target leaves by itself
+      zt[row] = x[k];
+      x[k] = -INFINITY;
+    }
     m = fmaxf(m, x[k]);
-    if (e == t && v0 + e < vocab) zt[row] = x[k];
     if (Z && (v0 + e) / 64 < blocks) Z[((v0 + e) / 64 * rows + row) * 64 + (e & 63)] = x[k];
   }
 #pragma unroll
