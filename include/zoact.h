@@ -495,7 +495,8 @@ int zoact_mix_rms_strided(zoact_ctx* ctx, const void* q, const void* k, const vo
  *
  * Token ids and targets: idtype ZOACT_ID_INT32 / INT64.  A negative one is no token: its embedding row is zero, it adds
  * nothing to a gradient, its loss is 0 and it is not counted in a mean.  One that is not below `vocab` is treated the
- * same way and sets ZOACT_ERR_INVALID_ARG in the device status word.                                              */
+ * same way and sets ZOACT_ERR_INVALID_ARG in the device status word.  Where a call names context scratch, the first one of its
+ * size allocates it and comes before any stream capture.                                                          */
 #define ZOACT_ID_INT32 0
 #define ZOACT_ID_INT64 1
 

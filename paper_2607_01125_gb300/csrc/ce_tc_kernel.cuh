@@ -19,11 +19,12 @@
 // epilogue adds up in registers, rounded; a group's sum is read while the next one runs into the other accumulator.
 //
 // Roles, barriers and bounded waits are those of the pair forward on CTA pairs: a TMA producer in each CTA, one MMA issuer
-// in the leader, eight epilogue warps in each (two warpgroups), two accumulators in TMEM.
+// in the leader, eight epilogue warps in each (two warpgroups), two to four accumulators in TMEM (as many as fit).
 //
 // Measured (bf16, 4096 x 128256 unless said): 32 rows 154 us, W at 6.8 TB/s; 4096 rows 2.10 ms with the tensor pipe 98% busy;
 // with gradients 2048 rows 1.11 / 1.13 / 1.05 ms (93 to 97%, under the power cap), 333 rows of 5120 x 50272 in fp16
-// 142 / 128 / 147 us (60 / 70 / 56%: 384 rows of MMA for 333, and the last one's stores).
+// 142 to 155 / 128 to 132 / 147 to 149 us (60 / 70 / 56%: 384 rows of MMA for 333, and the last one's stores); fp32, 1024 rows of
+// 4096 x 50272 1.70 ms the loss and 4.84 ms with gradients (1.5 PFLOP/s of the six products).
 #pragma once
 #include "pair_tc2_kernel.cuh"
 

@@ -120,10 +120,9 @@ ce_alpha_kernel(const void* __restrict__ targets, int id64, int64_t T, int64_t v
 
 // What a chunk of rows kept of its logits, 2048 (m_tile - z) in 16 bits, to G = exp(z - lse) - onehot in the operands' type,
 // in place.  The fixed point errs by 2.4e-4 of the exponential at most, half of fp16's rounding (exp(z - m_tile) in fp16 would
-// have rounded twice).  It reaches 32 below the tile's largest: with twice the steps and half the reach, the entries beside a
-// target that the model is nearly sure of were lost.  fp16's G is scaled by 2^15 (undone in
-// the products' scale): 1 / vocab would lie among its subnormals.  The target's element is expm1(z_t - lse): p - 1 from a
-// rounded p would lose what is left of it where the model is nearly right.
+// have rounded twice).  It reaches 32 below the largest of the tile's entries other than the target.  fp16's G is scaled by 2^15
+// (undone in the products' scale): 1 / vocab would lie among its subnormals.  The target's element is expm1(z_t - lse): p - 1
+// from a rounded p would lose what is left of it where the model is nearly right.
 constexpr float G_SCALE_FP16 = 32768.f;
 
 __device__ __forceinline__ float exp2_ftz(float x) {

@@ -7,8 +7,9 @@ namespace ce {
 namespace {
 
 // K-blocks of 64 that the tensor core sums by itself, at most: its cut-off costs about 1.6e-8 of the sum for each 16 products,
-// and reading a group's sum about 300 cycles of it.  Logits end in fp32 (8 blocks: 5e-7; with 12, 8e-7, 333 rows took 153 us
-// for 156 and 2048 rows the same); products that end in 16 bits take 64 (4e-6), and fp32 operands, whose six products are
+// and reading a group's sum about 300 cycles of it.  Logits end in fp32: log-sum-exps err by 4e-7 (d 4096) to 6e-7 (5120) with 8
+// blocks, half of that with 4 (333 rows 174 us for 163, 4096 rows 2.26 ms for 2.10), 8e-7 with 12 (333 rows 2% faster).
+// Products of G, itself rounded to 16 bits, take 64 (4e-6), a dW in fp32 among them; fp32 operands, whose six products are
 // summed alike, 4 (3e-7).
 constexpr int LOGIT_GROUP = 8, GRAD_GROUP = 64, FP32_GROUP = 4;
 // Rows on the M side are taken up to this much more padding: their epilogue has no reduction over lanes.  Loss and dH of a

@@ -7,8 +7,8 @@
 // order is counted, a long one's sorted in one cluster of eight CTAs, which exchange their digit counts through shared memory;
 // in the same launch all other SMs write the zeros of a dense gradient, which takes longer.
 //
-// Measured: 4096 rows of 4096 in bf16 9.9 us (5.2 TB/s); their gradient into a dense 128256 x 4096 table 154 us (zeros 137, sums
-// 15, join 6; 7.0 TB/s), that of 9001 tokens added to an 8192 x 5120 fp16 table 52 us (order 12, sums 26, join 16).
+// Measured: 4096 rows of 4096 in bf16 9.9 us (5.2 TB/s); their gradient into a dense 128256 x 4096 table 154 us (zeros 138, sums
+// 15, join 6; 7.0 TB/s; 10240 tokens 183, 16384 196, 40000 271), that of 9001 tokens added to an 8192 x 5120 fp16 table 52 us (order 12, sums 26, join 16).
 #include "internal.h"
 #include "tc_common.cuh"
 
@@ -203,7 +203,8 @@ __device__ __forceinline__ void sort_tokens(SortShared& sh, const void* __restri
 }
 
 // Zeros to [p, p + bytes) by the launch's other CTAs, ZERO_VECTORS 16-byte stores a thread and no loop: a CTA for each 64 KB in
-// address order writes 7.3 TB/s where a loop over the SMs' CTAs wrote 6.4 (and 4.6 in clusters, which do not fill every SM).
+// address order writes 7.6 TB/s, alone or in the sort's clusters (1.05 GB beside the order of 4096 and of 12000 tokens: 138 and
+// 139 us).  A loop over the SMs' CTAs wrote 6.4, and 4.6 in clusters, which do not fill every SM.
 constexpr int ZERO_VECTORS = 4;
 constexpr int64_t ZERO_BYTES = (int64_t)SORT_THREADS * ZERO_VECTORS * 16;     // of a CTA
 
