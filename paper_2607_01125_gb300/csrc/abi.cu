@@ -871,7 +871,7 @@ int zoact_ce_grad(zoact_ctx* ctx, const void* H, int dtype, int64_t T, int32_t d
   if (!dH && !dW) return ZOACT_ERR_INVALID_ARG;
   if ((dH && !aligned16(dH)) || (dW && !aligned16(dW))) return ZOACT_ERR_INVALID_ARG;
   if (wgdtype != dtype && wgdtype != ZOACT_DT_FP32) return ZOACT_ERR_INVALID_ARG;
-  if (accumulate && wgdtype != ZOACT_DT_FP32) return ZOACT_ERR_UNSUPPORTED;   // sums over calls are held in fp32
+  if (dW && accumulate && wgdtype != ZOACT_DT_FP32) return ZOACT_ERR_UNSUPPORTED;   // sums over calls are held in fp32
   c.loss = loss; c.lse = lse; c.mean = mean;
   c.dH = dH; c.dW = dW; c.wgdtype = wgdtype; c.accumulate = accumulate; c.grad_scale = grad_scale;
   return launch_ce(ctx, c);
