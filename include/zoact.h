@@ -558,6 +558,84 @@ int zoact_ce_grad(zoact_ctx* ctx, const void* H, int dtype, int64_t T, int32_t d
                   const void* targets, int idtype, float grad_scale, float* loss, float* lse, double* mean, void* dH,
                   void* dW, int wgdtype, int accumulate);
 
+/* ---- inside a decoder: rotary positions and attention ----
+ * The synthetic stacks mix q, k and v by zoact_mix_rms.  A decoder that reads tokens has attention there, over sequences that are
+ * packed one after another, with rotary positions in q and k.  These calls are that part, for any number of evaluation blocks
+ * (the blocks' rows are more sequences), and their gradients.                                                             */
+
+/* zoact_rope_init (host only, no context): the frequencies of `rot` rotated dimensions of a head, f_i = base^(-2i / rot) radians a
+ *   position, i < rot / 2.  layout: ZOACT_ROPE_HALF turns the pairs (i, i + rot / 2), ZOACT_ROPE_INTERLEAVED (2i, 2i + 1).
+ *   scaling, for contexts longer than the original length L = `original`:
+ *     ZOACT_ROPE_PLAIN    none (factor, low, high and original are ignored);
+ *     ZOACT_ROPE_LINEAR   f_i / factor;
+ *     ZOACT_ROPE_BASE     base factor^(rot / (rot - 2)) in place of base (rot > 2): the lowest frequency becomes f / factor;
+ *     ZOACT_ROPE_PARTS    by a frequency's turns over L, t = L f / 2 pi: f / factor below `low`, f above `high`, and between
+ *                         f (s + (1 - s) / factor) with s = (t - low) / (high - low).
+ *   turns[i] is f_i in 2^-64 turns a position (the angle of any 64-bit position is exact to 53 bits of the frequency).
+ *   A caller with frequencies of its own may fill the struct itself.  rot: even, 2 .. ZOACT_ROPE_MAX.
+ * zoact_rope_apply: Y [rows, heads head_dim] = X with each head's first rope->rot dimensions turned by the angle of
+ *   positions[r % n_pos] for row r (rows a multiple of n_pos: the evaluation blocks see one set of positions), the others
+ *   copied: (a, b) -> (a cos - b sin, a sin + b cos), with inverse != 0 by the opposite angle, which is the gradient of the
+ *   call without it.  Positions: ZOACT_ID_INT32 / INT64, any value (a negative one turns backwards).  Rows are ld_x and ld_y
+ *   elements apart (column views of a q/k/v output: q and k turn in one call).  Y may be X (with ld_y = ld_x); otherwise they
+ *   do not overlap.  One rounding.  `rope` is a HOST pointer, read during the call.                                        */
+#define ZOACT_ROPE_MAX 256
+#define ZOACT_ROPE_HALF 0
+#define ZOACT_ROPE_INTERLEAVED 1
+#define ZOACT_ROPE_PLAIN 0
+#define ZOACT_ROPE_LINEAR 1
+#define ZOACT_ROPE_BASE 2
+#define ZOACT_ROPE_PARTS 3
+typedef struct zoact_rope {
+  int32_t rot, layout;
+  uint64_t turns[ZOACT_ROPE_MAX / 2];
+} zoact_rope;
+int zoact_rope_init(zoact_rope* rope, int32_t rot, int32_t layout, double base, int32_t scaling, double factor, double low,
+                    double high, int64_t original);
+int zoact_rope_apply(zoact_ctx* ctx, const void* X, int dtype, int64_t rows, int32_t heads, int32_t head_dim, int64_t ld_x,
+                     const void* positions, int idtype, int64_t n_pos, const zoact_rope* rope, int inverse, void* Y,
+                     int64_t ld_y);
+
+/* Attention of packed sequences: with q of head h and position i of a sequence, and k, v of key head h kv_heads / heads,
+ *       s_j = scale q . k_j,   p_j = exp(s_j - lse),   lse = log sum_j exp(s_j),   o = sum_j p_j v_j
+ *   over the sequence's keys j; causal != 0: those with j <= i + (number of keys - number of queries), so that the queries are
+ *   the last of the keys (all of a prompt, or the new tokens behind a cache: a single token is a sequence of one query).  A row
+ *   that sees no key has o = 0 and lse = -infinity.
+ * shape (HOST pointer, read during the call): q and O [rows_q, heads head_dim], k and v [rows_k, kv_heads head_dim], of one dtype
+ *   (FP32, BF16, FP16), rows ld elements apart; heads a multiple of kv_heads, at most 128 heads a key head; head_dim <= 256.
+ * spans [n_seq, 4] of idtype (DEVICE): each sequence's first row of q, its number of queries, its first row of k and v, its number of
+ *   keys; any number may be 0.  The rows of q are in order and do not overlap (rows between are allowed); those of k may lie in
+ *   any order and be shared (a cache's slots, a common prompt), but with a gradient they too are in order and do not overlap.
+ * zoact_attention_plan reads the spans and writes the lists of work that the other calls run through (plan: DEVICE memory of the
+ *   caller, zoact_attention_plan_bytes bytes, 16-byte aligned; the gradient's with grad != 0, which serve the forward pass too).
+ *   One plan serves every layer of a batch; it can be captured, and replayed after the spans have changed.  Spans outside of the
+ *   rows or out of order set ZOACT_ERR_INVALID_ARG in the device status word, and calls with that plan write nothing.  So do calls
+ *   with a plan of another shape, without a gradient's lists where they are needed, or of another kind of device.
+ * zoact_attention: O, and lse [rows_q, heads] fp32 (NULL: not kept).  Rows of O and lse outside of the spans are left as they were.
+ * zoact_attention_grad: for dO, the gradients by q, k and v, with P and delta = dO . O from the O and lse that the forward call
+ *   gave:  dv = P^T dO,  dS = P (dO v^T - delta),  dq = scale dS k,  dk = scale dS^T q  (the heads of a group are summed).  Rows
+ *   outside of the spans are left as they were; keys that no query sees get zeros.  Sums in fp32 in a fixed order, without
+ *   atomics: the same bits on every run.  dq, dk and dv overlap no input.  It writes to the plan (delta).
+ * What lies in rows outside of a sequence's spans, be it NaN or infinite, does not reach it.  Within a sequence an infinity or NaN in
+ * a row of v (with a gradient: of any operand) may reach rows that do not see it.
+ * 16-bit operands with head_dim a multiple of 8 up to 128 and rows that start on 16 bytes run on the tensor cores (P and dS are
+ * rounded to the operands' type for them, which is half a step of that type for each); others in fp32 on the CUDA cores.
+ * head_dim <= 128: context scratch of about 90 MB (FP32 and 16-bit, any size of call), allocated by the first call, which comes
+ * before any stream capture; graphs captured from one context share it and are replayed one after another.              */
+typedef struct zoact_attention_shape {
+  int64_t rows_q, rows_k;
+  int32_t n_seq, heads, kv_heads, head_dim, causal, reserved;
+} zoact_attention_shape;
+int64_t zoact_attention_plan_bytes(zoact_ctx* ctx, const zoact_attention_shape* shape, int grad);
+int zoact_attention_plan(zoact_ctx* ctx, const zoact_attention_shape* shape, const void* spans, int idtype, int grad, void* plan);
+int zoact_attention(zoact_ctx* ctx, const zoact_attention_shape* shape, const void* plan, const void* q, int64_t ld_q,
+                    const void* k, int64_t ld_k, const void* v, int64_t ld_v, int dtype, float scale, void* O, int64_t ld_o,
+                    float* lse);
+int zoact_attention_grad(zoact_ctx* ctx, const zoact_attention_shape* shape, const void* plan, const void* dO, int64_t ld_do,
+                         const void* q, int64_t ld_q, const void* k, int64_t ld_k, const void* v, int64_t ld_v, int dtype,
+                         float scale, const void* O, int64_t ld_o, const float* lse, void* dq, int64_t ld_dq, void* dk,
+                         int64_t ld_dk, void* dv, int64_t ld_dv);
+
 /* ---- data-parallel replicas ----
  * A data-parallel ZO step shares everything but the tokens: every rank holds
  * the same W, U, C, m, v and seed, runs its token shard, and the ranks

@@ -20,5 +20,7 @@ from ._lib import (  # noqa: F401
     MAX_GROUP,
     zoact_embed, zoact_embed_grad, zoact_layer_norm, zoact_layer_norm_grad,
     zoact_ce_loss, zoact_ce_pair, zoact_ce_multi, zoact_ce_grad, ID_INT32, ID_INT64,
+    rope, zoact_rope_apply, attention_shape, attention_spans, zoact_attention_plan_bytes, zoact_attention_plan, zoact_attention,
+    zoact_attention_grad,
     DT_FP32, DT_BF16, DT_FP16, DT_INT4_G128, ACT_NONE, ACT_RELU, ACT_GELU, EXPORTS, LIB_PATH, TORCH_DT,
 )

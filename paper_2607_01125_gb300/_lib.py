@@ -33,6 +33,10 @@ ACT_NONE, ACT_RELU, ACT_GELU = 0, 1, 2
 
 ID_INT32, ID_INT64 = 0, 1
 
+ROPE_MAX = 256
+ROPE_LAYOUT = {"half": 0, "interleaved": 1}
+ROPE_SCALING = {"none": 0, "linear": 1, "base": 2, "parts": 3}
+
 TORCH_DT = {torch.float32: DT_FP32, torch.bfloat16: DT_BF16, torch.float16: DT_FP16}
 
 # every entry point include/zoact.h declares
@@ -49,6 +53,8 @@ EXPORTS = [
     "zoact_multi_forward_group_rs", "zoact_mix_rms_strided",
     "zoact_embed", "zoact_embed_grad", "zoact_layer_norm", "zoact_layer_norm_grad",
     "zoact_ce_loss", "zoact_ce_pair", "zoact_ce_multi", "zoact_ce_grad",
+    "zoact_rope_init", "zoact_rope_apply", "zoact_attention_plan_bytes", "zoact_attention_plan", "zoact_attention",
+    "zoact_attention_grad",
 ]
 
 
@@ -76,6 +82,16 @@ class zoact_rowscale(ctypes.Structure):
 class zoact_eval_blocks(ctypes.Structure):
     _fields_ = [("n_blocks", ctypes.c_int32), ("reserved", ctypes.c_int32),
                 ("coef", ctypes.c_float * MAX_EVAL_BLOCKS), ("query", ctypes.c_uint64 * MAX_EVAL_BLOCKS)]
+
+
+class zoact_rope(ctypes.Structure):
+    _fields_ = [("rot", ctypes.c_int32), ("layout", ctypes.c_int32), ("turns", ctypes.c_uint64 * (ROPE_MAX // 2))]
+
+
+class zoact_attention_shape(ctypes.Structure):
+    _fields_ = [("rows_q", ctypes.c_int64), ("rows_k", ctypes.c_int64), ("n_seq", ctypes.c_int32), ("heads", ctypes.c_int32),
+                ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("causal", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
 
 
 def eval_blocks(points):
@@ -175,6 +191,20 @@ def load():
         fn = getattr(lib, name)
         fn.argtypes = argtypes
         fn.restype = ctypes.c_int
+    F64, SHAPE, ROPE = ctypes.c_double, ctypes.POINTER(zoact_attention_shape), ctypes.POINTER(zoact_rope)
+    sig = {
+        "zoact_rope_init": [ROPE, I32, I32, F64, I32, F64, F64, F64, I64],
+        "zoact_rope_apply": [P, P, I32, I64, I32, I32, I64, P, I32, I64, ROPE, I32, P, I64],
+        "zoact_attention_plan": [P, SHAPE, P, I32, I32, P],
+        "zoact_attention": [P, SHAPE, P, P, I64, P, I64, P, I64, I32, F32, P, I64, P],
+        "zoact_attention_grad": [P, SHAPE, P, P, I64, P, I64, P, I64, P, I64, I32, F32, P, I64, P, P, I64, P, I64, P, I64],
+    }
+    for name, argtypes in sig.items():
+        fn = getattr(lib, name)
+        fn.argtypes = argtypes
+        fn.restype = ctypes.c_int
+    lib.zoact_attention_plan_bytes.argtypes = [P, SHAPE, I32]
+    lib.zoact_attention_plan_bytes.restype = ctypes.c_int64
     lib.zoact_basis_prepared_bytes.argtypes = [I32, I32]
     lib.zoact_basis_prepared_bytes.restype = ctypes.c_int64
     lib.zoact_status_string.argtypes = [ctypes.c_int]
@@ -689,3 +719,122 @@ def zoact_ce_grad(ctx, H, W, targets, dH=None, dW=None, loss=None, lse=None, mea
         _out(loss, (rows,), torch.float32, "loss"), _out(lse, (rows,), torch.float32, "lse"),
         _out(mean, (1,), torch.float64, "mean"), _out(dH, (rows, d), H.dtype, "dH"), _ptr(dW),
         _dt(dW) if dW is not None else _dt(H), int(accumulate)))
+
+
+# ---- inside a decoder: rotary positions, attention over packed sequences ----
+def rope(rot, base=10000.0, layout="half", scaling="none", factor=1.0, low=1.0, high=4.0, original=8192):
+    """The frequencies of `rot` rotated dimensions of a head (a host struct for zoact_rope_apply).  layout: "half" or
+    "interleaved"; scaling: "none", "linear", "base" or "parts" (include/zoact.h)."""
+    if layout not in ROPE_LAYOUT or scaling not in ROPE_SCALING:
+        raise ValueError(f"rope: layout of {sorted(ROPE_LAYOUT)}, scaling of {sorted(ROPE_SCALING)}")
+    r = zoact_rope()
+    _check("zoact_rope_init", load().zoact_rope_init(ctypes.byref(r), int(rot), ROPE_LAYOUT[layout], float(base),
+                                                     ROPE_SCALING[scaling], float(factor), float(low), float(high),
+                                                     int(original)))
+    return r
+
+
+def _on(ctx, *tensors):
+    """Refuses tensors that are not on the context's device (None: not given)."""
+    for t in tensors:
+        if t is not None and (t.device.type != "cuda" or t.device.index != ctx.device):
+            raise ValueError(f"a tensor on {t.device}, the context is on cuda:{ctx.device}")
+
+
+def zoact_rope_apply(ctx, X, positions, rope, Y, heads, inverse=False):
+    """Y = X [rows, heads head_dim] with every head turned by its row's position (back with inverse: the gradient).  X and Y are
+    matrices with unit column stride, or one matrix; positions int32 or int64 [n_pos], rows a multiple of n_pos."""
+    rows, n = X.shape
+    px, ldx = _rows(X)
+    py, ldy = _rows(Y)
+    pp, idt = _id_args(positions)
+    if tuple(Y.shape) != (rows, n) or Y.dtype != X.dtype or heads <= 0 or n % heads != 0:
+        raise ValueError("X and Y have one shape and type, and columns for all heads")
+    _on(ctx, X, Y, positions)
+    _check("zoact_rope_apply", load().zoact_rope_apply(ctx.handle, px, _dt(X), rows, int(heads), n // int(heads), ldx, pp, idt,
+                                                       positions.shape[0], ctypes.byref(rope), int(inverse), py, ldy))
+
+
+def attention_shape(rows_q, rows_k, n_seq, heads, kv_heads, head_dim, causal=True):
+    """The sizes that a plan and the calls with it agree on."""
+    return zoact_attention_shape(rows_q=int(rows_q), rows_k=int(rows_k), n_seq=int(n_seq), heads=int(heads),
+                                 kv_heads=int(kv_heads), head_dim=int(head_dim), causal=int(bool(causal)))
+
+
+def attention_spans(queries, keys=None, key_rows=None):
+    """Spans [n_seq, 4] (a host int64 tensor) of sequences packed in order: their numbers of queries and of keys (None: the
+    same), and the first row of each one's keys (None: packed too)."""
+    queries = [int(n) for n in queries]
+    keys = queries if keys is None else [int(n) for n in keys]
+    if len(keys) != len(queries) or (key_rows is not None and len(key_rows) != len(queries)):
+        raise ValueError("attention_spans: one entry for every sequence")
+    out, q0, k0 = [], 0, 0
+    for i, (nq, nk) in enumerate(zip(queries, keys)):
+        out.append((q0, nq, k0 if key_rows is None else int(key_rows[i]), nk))
+        q0, k0 = q0 + nq, k0 + nk
+    return torch.tensor(out, dtype=torch.int64).view(-1, 4)
+
+
+def zoact_attention_plan_bytes(ctx, shape, grad=False):
+    n = int(load().zoact_attention_plan_bytes(ctx.handle, ctypes.byref(shape), int(bool(grad))))
+    if n < 0:
+        raise ValueError("zoact_attention_plan_bytes: a shape that attention does not take")
+    return n
+
+
+def zoact_attention_plan(ctx, shape, spans, plan, grad=False):
+    """The plan (a uint8 tensor of zoact_attention_plan_bytes) of spans [n_seq, 4] (int32 or int64, on the device)."""
+    if spans.dim() != 2 or tuple(spans.shape) != (shape.n_seq, 4) or spans.dtype not in _ID_DT:
+        raise ValueError(f"spans: [{shape.n_seq}, 4] of int32 or int64")
+    if plan.dtype != torch.uint8 or plan.numel() < zoact_attention_plan_bytes(ctx, shape, grad):
+        raise ValueError("plan: uint8, zoact_attention_plan_bytes of it")
+    _on(ctx, spans, plan)
+    _check("zoact_attention_plan", load().zoact_attention_plan(ctx.handle, ctypes.byref(shape), _ptr(spans), _ID_DT[spans.dtype],
+                                                               int(bool(grad)), _ptr(plan)))
+
+
+def _heads(ctx, t, rows, heads, shape, dtype, name):
+    """Address and row stride of [rows, heads head_dim] (a matrix with unit column stride)."""
+    if tuple(t.shape) != (rows, heads * shape.head_dim) or t.dtype != dtype:
+        raise ValueError(f"{name}: expected {(rows, heads * shape.head_dim)} of {dtype}, got {tuple(t.shape)} of {t.dtype}")
+    _on(ctx, t)
+    return _rows(t)
+
+
+def _scale(shape, scale):
+    return float(shape.head_dim) ** -0.5 if scale is None else float(scale)
+
+
+def _attention_plan(ctx, shape, plan, grad):
+    if plan.dtype != torch.uint8 or plan.numel() < zoact_attention_plan_bytes(ctx, shape, grad):
+        raise ValueError("plan: uint8, zoact_attention_plan_bytes of it")
+    _on(ctx, plan)
+    return _ptr(plan)
+
+
+def zoact_attention(ctx, shape, plan, q, k, v, O, lse=None, scale=None):
+    """Attention of the plan's sequences: q and O [rows_q, heads head_dim], k and v [rows_k, kv_heads head_dim] (matrices with
+    unit column stride), lse [rows_q, heads] fp32 or None; scale: 1 / sqrt(head_dim) by default."""
+    s = shape
+    args = []
+    for t, rows, heads, name in ((q, s.rows_q, s.heads, "q"), (k, s.rows_k, s.kv_heads, "k"), (v, s.rows_k, s.kv_heads, "v")):
+        args += _heads(ctx, t, rows, heads, s, q.dtype, name)
+    po, ldo = _heads(ctx, O, s.rows_q, s.heads, s, q.dtype, "O")
+    _on(ctx, lse)
+    _check("zoact_attention", load().zoact_attention(
+        ctx.handle, ctypes.byref(s), _attention_plan(ctx, s, plan, False), *args, _dt(q), _scale(s, scale), po, ldo,
+        _out(lse, (s.rows_q, s.heads), torch.float32, "lse")))
+
+
+def zoact_attention_grad(ctx, shape, plan, dO, q, k, v, O, lse, dq, dk, dv, scale=None):
+    """The gradient of zoact_attention for dO, from its O and lse, with a plan made with grad: dq, dk and dv like q, k and v."""
+    s = shape
+    args = []
+    for t, rows, heads, name in ((dO, s.rows_q, s.heads, "dO"), (q, s.rows_q, s.heads, "q"), (k, s.rows_k, s.kv_heads, "k"),
+                                 (v, s.rows_k, s.kv_heads, "v"), (O, s.rows_q, s.heads, "O"), (dq, s.rows_q, s.heads, "dq"),
+                                 (dk, s.rows_k, s.kv_heads, "dk"), (dv, s.rows_k, s.kv_heads, "dv")):
+        args += _heads(ctx, t, rows, heads, s, q.dtype, name)
+    _on(ctx, lse)
+    _check("zoact_attention_grad", load().zoact_attention_grad(
+        ctx.handle, ctypes.byref(s), _attention_plan(ctx, s, plan, True), *args[:8], _dt(q), _scale(s, scale), *args[8:10],
+        _out(lse, (s.rows_q, s.heads), torch.float32, "lse"), *args[10:]))

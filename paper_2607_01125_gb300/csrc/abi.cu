@@ -5,6 +5,7 @@
 #include <cstdlib>
 #include <new>
 
+#include "attn.h"
 #include "internal.h"
 
 namespace zoact {
@@ -228,6 +229,8 @@ int zoact_get_device_status(zoact_ctx* ctx, int* status, int reset) {
     ZOACT_CUDA_TRY(cudaMemsetAsync(ctx->d_tickets, 0, 256, ctx->stream));
     if (ctx->slot_ptr[SLOT_SK_TICKETS])
       ZOACT_CUDA_TRY(cudaMemsetAsync(ctx->slot_ptr[SLOT_SK_TICKETS], 0, ctx->slot_bytes[SLOT_SK_TICKETS], ctx->stream));
+    if (ctx->slot_ptr[SLOT_ATTN_TICKETS])
+      ZOACT_CUDA_TRY(cudaMemsetAsync(ctx->slot_ptr[SLOT_ATTN_TICKETS], 0, ctx->slot_bytes[SLOT_ATTN_TICKETS], ctx->stream));
     ZOACT_CUDA_TRY(cudaStreamSynchronize(ctx->stream));
   }
   if (reset) {
@@ -875,6 +878,110 @@ int zoact_ce_grad(zoact_ctx* ctx, const void* H, int dtype, int64_t T, int32_t d
   c.loss = loss; c.lse = lse; c.mean = mean;
   c.dH = dH; c.dW = dW; c.wgdtype = wgdtype; c.accumulate = accumulate; c.grad_scale = grad_scale;
   return launch_ce(ctx, c);
+}
+
+int zoact_rope_apply(zoact_ctx* ctx, const void* X, int dtype, int64_t rows, int32_t heads, int32_t head_dim, int64_t ld_x,
+                     const void* positions, int idtype, int64_t n_pos, const zoact_rope* rope, int inverse, void* Y,
+                     int64_t ld_y) {
+  ZOACT_ENTER(ctx);
+  if (!rope || rows < 0 || heads <= 0 || head_dim <= 0 || !valid_act_dtype(dtype) || !valid_id_type(idtype))
+    return ZOACT_ERR_INVALID_ARG;
+  if (rope->rot < 2 || rope->rot % 2 != 0 || rope->rot > ZOACT_ROPE_MAX || rope->rot > head_dim ||
+      (rope->layout != ZOACT_ROPE_HALF && rope->layout != ZOACT_ROPE_INTERLEAVED))
+    return ZOACT_ERR_INVALID_ARG;
+  const int64_t n = (int64_t)heads * head_dim;
+  if (ld_x < n || ld_y < n || (X == Y && ld_x != ld_y)) return ZOACT_ERR_INVALID_ARG;
+  if (rows > 0 && (!X || !Y || !positions || n_pos <= 0 || rows % n_pos != 0 || !aligned_to(X, dtype) || !aligned_to(Y, dtype) ||
+                   !aligned_ids(positions, idtype)))
+    return ZOACT_ERR_INVALID_ARG;
+  if (rows > 0x7fffffff || n > (1 << 24)) return ZOACT_ERR_UNSUPPORTED;
+  RopeArgs a = {};
+  a.X = X; a.Y = Y; a.rows = rows; a.ld_x = ld_x; a.ld_y = ld_y; a.n_pos = n_pos; a.heads = heads; a.head_dim = head_dim;
+  a.dtype = dtype; a.id64 = idtype == ZOACT_ID_INT64; a.inverse = inverse != 0; a.positions = positions; a.rope = rope;
+  return launch_rope(ctx, a);
+}
+
+static int check_attention(const zoact_attention_shape* s, attn::Shape* out) {
+  if (!s || s->rows_q < 0 || s->rows_k < 0 || s->n_seq < 0 || s->heads <= 0 || s->kv_heads <= 0 || s->head_dim <= 0 ||
+      s->heads % s->kv_heads != 0)
+    return ZOACT_ERR_INVALID_ARG;
+  if (s->rows_q > 0x7fffffff || s->rows_k > 0x7fffffff || s->n_seq > (1 << 24) || s->head_dim > attn::MAX_DIM ||
+      s->heads / s->kv_heads > attn::MAX_REP || s->heads > (1 << 16))
+    return ZOACT_ERR_UNSUPPORTED;
+  *out = {s->rows_q, s->rows_k, s->n_seq, s->heads, s->kv_heads, s->head_dim, s->causal != 0};
+  return ZOACT_OK;
+}
+
+int64_t zoact_attention_plan_bytes(zoact_ctx* ctx, const zoact_attention_shape* shape, int grad) {
+  attn::Shape s;
+  if (!ctx || check_attention(shape, &s)) return -1;
+  return (int64_t)attn::plan_layout(s, ctx->sm_count, grad != 0).total;
+}
+
+int zoact_attention_plan(zoact_ctx* ctx, const zoact_attention_shape* shape, const void* spans, int idtype, int grad, void* plan) {
+  ZOACT_ENTER(ctx);
+  attn::Shape s;
+  const int st = check_attention(shape, &s);
+  if (st) return st;
+  if (!plan || !aligned16(plan) || !valid_id_type(idtype)) return ZOACT_ERR_INVALID_ARG;
+  if (s.n_seq > 0 && (!spans || !aligned_ids(spans, idtype))) return ZOACT_ERR_INVALID_ARG;
+  return attn::launch_plan(ctx, s, spans, idtype == ZOACT_ID_INT64, static_cast<uint8_t*>(plan), grad != 0);
+}
+
+// A matrix of `rows` rows of n elements of dtype, ld apart.
+static bool valid_rows(const void* p, int64_t rows, int64_t n, int64_t ld, int dtype) {
+  return ld >= n && (rows == 0 || (p && aligned_to(p, dtype)));
+}
+
+static int attention_args(zoact_ctx* ctx, const zoact_attention_shape* shape, const void* plan, const void* q, int64_t ld_q,
+                          const void* k, int64_t ld_k, const void* v, int64_t ld_v, int dtype, float scale, const void* O,
+                          int64_t ld_o, int grad, attn::Args* a) {
+  attn::Shape s;
+  const int st = check_attention(shape, &s);
+  if (st) return st;
+  if (!plan || !aligned16(plan) || !valid_act_dtype(dtype) || !(scale > 0.f) || !(scale <= 3.4e38f)) return ZOACT_ERR_INVALID_ARG;
+  const int64_t nq = (int64_t)s.heads * s.head_dim, nk = (int64_t)s.kv_heads * s.head_dim;
+  if (!valid_rows(q, s.rows_q, nq, ld_q, dtype) || !valid_rows(k, s.rows_k, nk, ld_k, dtype) ||
+      !valid_rows(v, s.rows_k, nk, ld_v, dtype) || !valid_rows(O, s.rows_q, nq, ld_o, dtype))
+    return ZOACT_ERR_INVALID_ARG;
+  a->s = s;
+  a->plan = static_cast<const uint8_t*>(plan);
+  a->at = attn::plan_layout(s, ctx->sm_count, grad);
+  a->tag = attn::plan_tag(s);
+  a->q = q; a->k = k; a->v = v; a->ld_q = ld_q; a->ld_k = ld_k; a->ld_v = ld_v; a->dtype = dtype; a->scale = scale;
+  a->O = const_cast<void*>(O); a->ld_o = ld_o;
+  return ZOACT_OK;
+}
+
+int zoact_attention(zoact_ctx* ctx, const zoact_attention_shape* shape, const void* plan, const void* q, int64_t ld_q,
+                    const void* k, int64_t ld_k, const void* v, int64_t ld_v, int dtype, float scale, void* O, int64_t ld_o,
+                    float* lse) {
+  ZOACT_ENTER(ctx);
+  attn::Args a = {};
+  const int st = attention_args(ctx, shape, plan, q, ld_q, k, ld_k, v, ld_v, dtype, scale, O, ld_o, 0, &a);
+  if (st) return st;
+  a.lse = lse;
+  return attn::launch_fwd_simt(ctx, a);
+}
+
+int zoact_attention_grad(zoact_ctx* ctx, const zoact_attention_shape* shape, const void* plan, const void* dO, int64_t ld_do,
+                         const void* q, int64_t ld_q, const void* k, int64_t ld_k, const void* v, int64_t ld_v, int dtype,
+                         float scale, const void* O, int64_t ld_o, const float* lse, void* dq, int64_t ld_dq, void* dk,
+                         int64_t ld_dk, void* dv, int64_t ld_dv) {
+  ZOACT_ENTER(ctx);
+  attn::Args a = {};
+  const int st = attention_args(ctx, shape, plan, q, ld_q, k, ld_k, v, ld_v, dtype, scale, O, ld_o, 1, &a);
+  if (st) return st;
+  const int64_t nq = (int64_t)a.s.heads * a.s.head_dim, nk = (int64_t)a.s.kv_heads * a.s.head_dim;
+  if (!valid_rows(dO, a.s.rows_q, nq, ld_do, dtype) || !valid_rows(dq, a.s.rows_q, nq, ld_dq, dtype) ||
+      !valid_rows(dk, a.s.rows_k, nk, ld_dk, dtype) || !valid_rows(dv, a.s.rows_k, nk, ld_dv, dtype) ||
+      (a.s.rows_q > 0 && !lse))
+    return ZOACT_ERR_INVALID_ARG;
+  a.lse = const_cast<float*>(lse);
+  a.dO = dO; a.ld_do = ld_do; a.dq = dq; a.ld_dq = ld_dq; a.dk = dk; a.ld_dk = ld_dk; a.dv = dv; a.ld_dv = ld_dv;
+  a.delta = reinterpret_cast<float*>(const_cast<uint8_t*>(a.plan) + a.at.delta);
+  const int sd = attn::launch_delta(ctx, a);
+  return sd ? sd : attn::launch_grad_simt(ctx, a);
 }
 
 }  // extern "C"

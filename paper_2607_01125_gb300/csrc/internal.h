@@ -45,6 +45,8 @@ enum ScratchSlot {
   SLOT_CE_HT,        // H by columns, for its product by W
   SLOT_CE_TAIL,      // K pieces of the last tiles of its product by H
   SLOT_CE_DW,        // fp32 sums of dW over several chunks of rows
+  SLOT_ATTN,         // attention: sums of rows of work that are cut, and of halves of a block's keys
+  SLOT_ATTN_TICKETS, // their tickets (zero between launches)
   SLOT_COUNT
 };
 
@@ -344,6 +346,17 @@ struct CeArgs {
   float grad_scale;
 };
 int launch_ce(Ctx* ctx, const CeArgs& c);
+
+// Rotary positions (k_rope.cu): row r turns by positions[r % n_pos].
+struct RopeArgs {
+  const void* X;        // [rows, heads head_dim], rows ld_x apart
+  void* Y;
+  int64_t rows, ld_x, ld_y, n_pos;
+  int heads, head_dim, dtype, id64, inverse;
+  const void* positions;
+  const zoact_rope* rope;
+};
+int launch_rope(Ctx* ctx, const RopeArgs& a);
 
 // Section 5.3 diagnostics (k_diag.cu): out[0] = ||Ua^T Ub||_F^2, out[2] = out[0] / ra;
 // energy: out[0] = ||U^T G||_F^2, out[1] = ||G||_F^2, out[2] = their ratio.  out: device fp64 [3].

@@ -1,0 +1,184 @@
+// Rotary positions: the pair (a, b) of frequency f in every head of row r turns by the angle position f,
+//     a' = a cos - b sin,  b' = a sin + b cos        (inverse: by the opposite angle, which is the gradient).
+//
+// The angle is kept in turns, as a 64-bit fraction of one: a position times the frequency's fraction (zoact_rope_init), modulo
+// 2^64, is the fraction of a turn that the rotation leaves -- an exact product, so that a far position loses nothing to the
+// reduction that a 32-bit angle would (position 10^6 in fp32: 0.03 radians).  Its two top bits are the quadrant, and the rest
+// goes to sine and cosine as a fraction of at most 1/8 turn.
+//
+// Bound by memory: every element is read and written once.  A block makes the sines and cosines of its rows once, in shared
+// memory, for all of a row's heads, and then moves 16 bytes of both halves (or of neighbouring pairs) at a time.
+//
+// Measured (GB300): see the launcher.
+#include <cmath>
+
+#include "internal.h"
+
+namespace zoact {
+namespace {
+
+constexpr int THREADS = 256, TABLE = 1024;      // TABLE: sines and cosines of a block
+
+struct Turns {
+  uint64_t t[ZOACT_ROPE_MAX / 2];
+};
+
+// (cos, sin) of a fraction of a turn.
+__device__ __forceinline__ float2 cos_sin_turns(uint64_t t) {
+  const uint32_t quadrant = (uint32_t)((t + (1ull << 61)) >> 62) & 3u;
+  const int32_t rest = (int32_t)(uint32_t)((t - ((uint64_t)quadrant << 62)) >> 32);     // +- 1/8 turn, in 2^-32 turns
+  float s, c;
+  sincospif((float)rest * 0x1p-31f, &s, &c);
+  if (quadrant & 1u) {
+    const float k = c;
+    c = -s;
+    s = k;
+  }
+  return quadrant & 2u ? make_float2(-c, -s) : make_float2(c, s);
+}
+
+template <typename T, int N> struct alignas(sizeof(T) * N) Vec { T v[N]; };
+
+// V elements at a time (V = 1: any alignment).  np: pieces of a head that turn; nc: pieces behind them that are copied.
+template <typename T, int V, bool HALF>
+__global__ void __launch_bounds__(THREADS)
+rope_kernel(const T* X, int64_t ld_x, T* Y, int64_t ld_y, int64_t rows, int heads, int head_dim, int rot, int np, int nc,
+            const void* __restrict__ positions, int id64, uint32_t n_pos, int rows_block, int inverse,
+            const __grid_constant__ Turns turns) {
+  __shared__ float2 table[TABLE];
+  pdl_wait();
+  pdl_trigger();
+  const int64_t r0 = (int64_t)blockIdx.x * rows_block;
+  const int nr = (int)(rows - r0 < rows_block ? rows - r0 : rows_block), nf = rot / 2;
+  for (int i = threadIdx.x; i < nr * nf; i += THREADS) {
+    const int r = i / nf, f = i - r * nf;
+    const uint64_t pos = (uint64_t)load_id(positions, id64, (uint32_t)((uint64_t)(r0 + r) % n_pos));
+    const float2 cs = cos_sin_turns(pos * turns.t[f]);
+    table[i] = make_float2(cs.x, inverse ? -cs.y : cs.y);
+  }
+  __syncthreads();
+  const int pieces = np + nc, per_row = heads * pieces, total = nr * per_row;
+#pragma unroll 4
+  for (int i = threadIdx.x; i < total; i += THREADS) {
+    const int r = i / per_row, in_row = i - r * per_row, head = in_row / pieces, p = in_row - head * pieces;
+    const T* x = X + (r0 + r) * ld_x + (int64_t)head * head_dim;
+    T* y = Y + (r0 + r) * ld_y + (int64_t)head * head_dim;
+    if (p >= np) {
+      const int d = rot + (p - np) * V;
+      *reinterpret_cast<Vec<T, V>*>(y + d) = *reinterpret_cast<const Vec<T, V>*>(x + d);
+      continue;
+    }
+    const float2* cs = table + r * nf;
+    if constexpr (HALF) {
+      const int d = p * V;
+      const Vec<T, V> a = *reinterpret_cast<const Vec<T, V>*>(x + d), b = *reinterpret_cast<const Vec<T, V>*>(x + nf + d);
+      Vec<T, V> s, t;
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const float2 w = cs[d + j];
+        const float u = to_f32<T>(a.v[j]), v = to_f32<T>(b.v[j]);
+        s.v[j] = from_f32<T>(u * w.x - v * w.y);
+        t.v[j] = from_f32<T>(u * w.y + v * w.x);
+      }
+      *reinterpret_cast<Vec<T, V>*>(y + d) = s;
+      *reinterpret_cast<Vec<T, V>*>(y + nf + d) = t;
+    } else {
+      constexpr int W = V > 1 ? V : 2;           // pairs: two elements at least
+      const int d = p * W;
+      T e[W];
+      if constexpr (V > 1) {
+        const Vec<T, V> a = *reinterpret_cast<const Vec<T, V>*>(x + d);
+#pragma unroll
+        for (int j = 0; j < V; ++j) e[j] = a.v[j];
+      } else {
+        e[0] = x[d];
+        e[1] = x[d + 1];
+      }
+#pragma unroll
+      for (int j = 0; j < W; j += 2) {
+        const float2 w = cs[(d + j) / 2];
+        const float u = to_f32<T>(e[j]), v = to_f32<T>(e[j + 1]);
+        e[j] = from_f32<T>(u * w.x - v * w.y);
+        e[j + 1] = from_f32<T>(u * w.y + v * w.x);
+      }
+      if constexpr (V > 1) {
+        Vec<T, V> s;
+#pragma unroll
+        for (int j = 0; j < V; ++j) s.v[j] = e[j];
+        *reinterpret_cast<Vec<T, V>*>(y + d) = s;
+      } else {
+        y[d] = e[0];
+        y[d + 1] = e[1];
+      }
+    }
+  }
+}
+
+template <typename T, bool HALF>
+int launch(Ctx* ctx, const RopeArgs& a, const Turns& turns) {
+  const int nf = a.rope->rot / 2, rest = a.head_dim - a.rope->rot;
+  constexpr int V = 16 / (int)sizeof(T);
+  const auto lies = [&](const void* p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld % V == 0; };
+  const bool vec = lies(a.X, a.ld_x) && lies(a.Y, a.ld_y) && a.head_dim % V == 0 && (HALF ? nf : 2 * nf) % V == 0;
+  const int v = vec ? V : 1;
+  const int np = HALF ? nf / v : vec ? 2 * nf / v : nf, nc = a.X == a.Y ? 0 : rest / v;
+  // Rows of a block: as many as the table holds, fewer where the SMs would not have two blocks each.
+  int rows_block = TABLE / nf < 8 ? TABLE / nf : 8;
+  while (rows_block > 1 && a.rows < (int64_t)2 * ctx->sm_count * rows_block) rows_block /= 2;
+  const int64_t blocks = (a.rows + rows_block - 1) / rows_block;
+  const auto run = [&](auto kern) {
+    return launch_pdl(ctx, kern, dim3((unsigned)blocks), dim3(THREADS), 0, (const T*)a.X, a.ld_x, (T*)a.Y, a.ld_y, a.rows,
+                      a.heads, a.head_dim, a.rope->rot, np, nc, a.positions, a.id64, (uint32_t)a.n_pos, rows_block, a.inverse,
+                      turns);
+  };
+  ZOACT_CUDA_TRY(vec ? run(rope_kernel<T, V, HALF>) : run(rope_kernel<T, 1, HALF>));
+  ++ctx->n_launch;
+  return ZOACT_OK;
+}
+
+}  // namespace
+
+int launch_rope(Ctx* ctx, const RopeArgs& a) {
+  if (a.rows == 0) return ZOACT_OK;
+  Turns turns = {};
+  for (int i = 0; i < a.rope->rot / 2; ++i) turns.t[i] = a.rope->turns[i];
+  const bool half = a.rope->layout == ZOACT_ROPE_HALF;
+  switch (a.dtype) {
+    case ZOACT_DT_FP32: return half ? launch<float, true>(ctx, a, turns) : launch<float, false>(ctx, a, turns);
+    case ZOACT_DT_BF16: return half ? launch<__nv_bfloat16, true>(ctx, a, turns) : launch<__nv_bfloat16, false>(ctx, a, turns);
+    default: return half ? launch<__half, true>(ctx, a, turns) : launch<__half, false>(ctx, a, turns);
+  }
+}
+
+}  // namespace zoact
+
+// Frequencies in radians a position: base^(-2 i / rot), scaled for contexts longer than the original length.
+extern "C" int zoact_rope_init(zoact_rope* rope, int32_t rot, int32_t layout, double base, int32_t scaling, double factor,
+                               double low, double high, int64_t original) {
+  if (!rope || rot < 2 || rot % 2 != 0 || (layout != ZOACT_ROPE_HALF && layout != ZOACT_ROPE_INTERLEAVED))
+    return ZOACT_ERR_INVALID_ARG;
+  if (rot > ZOACT_ROPE_MAX) return ZOACT_ERR_UNSUPPORTED;
+  if (!(base > 1.0) || !std::isfinite(base) || scaling < ZOACT_ROPE_PLAIN || scaling > ZOACT_ROPE_PARTS)
+    return ZOACT_ERR_INVALID_ARG;
+  if (scaling != ZOACT_ROPE_PLAIN && (!(factor > 0.0) || !std::isfinite(factor))) return ZOACT_ERR_INVALID_ARG;
+  if (scaling == ZOACT_ROPE_PARTS && (!(high > low) || !std::isfinite(low) || !std::isfinite(high) || original <= 0))
+    return ZOACT_ERR_INVALID_ARG;
+  const double two_pi = 6.283185307179586476925;
+  if (scaling == ZOACT_ROPE_BASE && rot > 2) base *= std::pow(factor, (double)rot / (rot - 2));
+  if (!std::isfinite(base) || !(base > 0.0)) return ZOACT_ERR_INVALID_ARG;
+  rope->rot = rot;
+  rope->layout = layout;
+  for (int i = 0; i < ZOACT_ROPE_MAX / 2; ++i) {
+    double f = 0.0;
+    if (i < rot / 2) f = std::pow(base, -2.0 * i / rot);
+    if (scaling == ZOACT_ROPE_LINEAR) f /= factor;
+    if (scaling == ZOACT_ROPE_PARTS) {
+      const double turns = (double)original * f / two_pi;
+      const double keep = std::fmin(std::fmax((turns - low) / (high - low), 0.0), 1.0);
+      f *= keep + (1.0 - keep) / factor;
+    }
+    const double t = f / two_pi, part = t - std::floor(t);          // below 1: its 53 bits are part of the 64
+    rope->turns[i] = (uint64_t)std::ldexp(part, 64);
+  }
+  return ZOACT_OK;
+}
