@@ -961,7 +961,7 @@ int zoact_attention(zoact_ctx* ctx, const zoact_attention_shape* shape, const vo
   const int st = attention_args(ctx, shape, plan, q, ld_q, k, ld_k, v, ld_v, dtype, scale, O, ld_o, 0, &a);
   if (st) return st;
   a.lse = lse;
-  return attn::launch_fwd_simt(ctx, a);
+  return attn::tc_supported(a, false) ? attn::launch_fwd_tc(ctx, a) : attn::launch_fwd_simt(ctx, a);
 }
 
 int zoact_attention_grad(zoact_ctx* ctx, const zoact_attention_shape* shape, const void* plan, const void* dO, int64_t ld_do,

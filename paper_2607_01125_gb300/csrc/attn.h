@@ -59,6 +59,8 @@ struct Slots {
   float* sums;                          // [slots][2 TILE][TC_DIM]
   float2* stat;                         // [slots][2 TILE]: maximum (times scale log2 e) and sum of exponentials
   unsigned* tickets;                    // [slots][4], zero between launches
+  float* merge;                         // [SMs][TILE][TC_DIM]: a tile's half of the keys (forward)
+  float2* merge_stat;                   // [SMs][TILE]
 };
 int slots(Ctx* ctx, Slots* s);
 

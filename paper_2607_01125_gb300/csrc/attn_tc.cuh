@@ -1,0 +1,168 @@
+// Blackwell building blocks of the attention kernels, beside tc_common.cuh: tiles of rows of (position, head of the group) pairs
+// and of keys, MMAs with the left operand in TMEM, and TMEM transfers of 32 columns that are waited for together.
+//
+// A tile has 128 rows of 64-column boxes (128 bytes, 128-byte swizzle), DP / 64 boxes of BOX bytes.  As a left or right operand
+// of a product over the head's columns it is K-major; as the right operand of a product over its rows (P V, dS K, ...) it is read
+// N-major where it lies: boxes BOX apart along N, 1024 bytes for 8 rows of K.
+#pragma once
+#include "attn.h"
+#include "tc_common.cuh"
+
+namespace zoact {
+namespace attn {
+namespace tcx {
+
+constexpr int BOX = TILE * 128;         // bytes of 128 rows x 64 columns of 16-bit elements
+
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+      "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+      : "memory");
+}
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, int w, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
+      "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar)
+      : "memory");
+}
+
+// Descriptors of a tile at `start` (shared memory): over its columns (K-major), over its rows (N-major).
+constexpr uint32_t DESC_HI = (1024u >> 4) | 1u << 14 | 2u << 29;
+__device__ __forceinline__ uint64_t desc_cols(uint32_t start) { return (uint64_t)DESC_HI << 32 | (start >> 4) | 1u << 16; }
+__device__ __forceinline__ uint64_t desc_rows(uint32_t start) {
+  return (uint64_t)DESC_HI << 32 | (start >> 4) | (uint32_t)(BOX >> 4) << 16;
+}
+constexpr uint32_t B_BY_ROWS = 1u << 16;          // instruction descriptor: the right operand is N-major
+
+// D[tmem] (+)= A[tmem] * B[smem]: A is 128 lanes x 16-bit pairs, two K to a column.
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+      "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+
+// Products of `steps` times 16 in K.  Over columns: A and B tiles in shared memory.
+__device__ __forceinline__ void mma_cols(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, int steps) {
+  for (int k = 0; k < steps; ++k) {
+    const uint32_t at = (uint32_t)(k >> 2) * BOX + (uint32_t)(k & 3) * 32u;
+    tc::mma_f16(d, desc_cols(a + at), desc_cols(b + at), idesc, k != 0);
+  }
+}
+// Over the rows of B: A in TMEM.
+__device__ __forceinline__ void mma_rows(uint32_t d, uint32_t a_tmem, uint32_t b, uint32_t idesc, int steps, bool accumulate) {
+  for (int k = 0; k < steps; ++k)
+    mma_ts(d, a_tmem + (uint32_t)k * 8u, desc_rows(b + (uint32_t)k * 2048u), idesc, accumulate || k != 0);
+}
+
+__device__ __forceinline__ bool elect_one() {
+  uint32_t is;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(is));
+  return is != 0;
+}
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* status) {
+  return __all_sync(0xffffffffu, tc::mbar_wait(bar, parity, abort_flag, status));
+}
+
+// 32 columns of this thread's lane; nothing reads them before ld_wait().
+__device__ __forceinline__ void ld32(uint32_t taddr, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+      "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+        "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+        "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// Registers of an ld32 as values from here on (after ld_wait, which this statement cannot pass).
+__device__ __forceinline__ void ld_use(uint32_t* r) {
+  asm volatile("" : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
+                    "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]));
+  asm volatile("" : "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]),
+                    "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31]));
+}
+__device__ __forceinline__ void st32(uint32_t taddr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
+      "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]),
+      "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]),
+      "r"(r[30]), "r"(r[31])
+      : "memory");
+}
+__device__ __forceinline__ void st16(uint32_t taddr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+template <bool BF16> __device__ __forceinline__ uint32_t pack2(float a, float b) {
+  if constexpr (BF16) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  } else {
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
+}
+
+__device__ __forceinline__ Item load_item(const Item* p) {
+  const int4 a = reinterpret_cast<const int4*>(p)[0], b = reinterpret_cast<const int4*>(p)[1];
+  return {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+}
+
+// Zero rows [from, to) of a tile of `boxes` boxes, by one warp, before the tensor core reads them.
+__device__ __forceinline__ void zero_rows(uint32_t tile, int boxes, int from, int to, int lane) {
+  for (int b = 0; b < boxes; ++b)
+    for (int i = from * 8 + lane; i < to * 8; i += 32) tc::st_shared_v4(tile + (uint32_t)(b * BOX + i * 16), make_uint4(0, 0, 0, 0));
+  tc::fence_proxy_async_smem();
+  __syncwarp();
+}
+
+// Columns [0, n) of a thread's row of a 16-bit output, n a multiple of 8; `whole`: rows lie on 32 bytes.
+template <bool BF16>
+__device__ __forceinline__ void store_row(void* row, const float* x, int n, bool whole) {
+#pragma unroll
+  for (int j = 0; j < 32; j += 16) {
+    if (j >= n) break;
+    uint32_t w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = pack2<BF16>(x[j + 2 * i], x[j + 2 * i + 1]);
+    char* p = static_cast<char*>(row) + 2 * j;
+    if (whole && j + 16 <= n) {
+      asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]),
+                   "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+                   : "memory");
+    } else {
+      *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+      if (j + 16 <= n) *reinterpret_cast<uint4*>(p + 16) = make_uint4(w[4], w[5], w[6], w[7]);
+    }
+  }
+}
+
+}  // namespace tcx
+
+// Host: the boxes of a tile: `positions` rows of 64 columns of every head of a group, and 128 rows of 64 columns of a key head.
+inline int encode_rows(CUtensorMap* map, const void* base, int dtype, const Shape& s, int64_t ld) {
+  return encode_tmap_heads_16bit(map, base, dtype, s.rows_q, s.heads, s.rep(), s.head_dim, ld, tile_positions(s.rep()));
+}
+inline int encode_keys(CUtensorMap* map, const void* base, int dtype, const Shape& s, int64_t ld) {
+  return encode_tmap_heads_16bit(map, base, dtype, s.rows_k, s.kv_heads, 0, s.head_dim, ld, BK);
+}
+
+}  // namespace attn
+}  // namespace zoact

@@ -250,11 +250,21 @@ int launch_plan(Ctx* ctx, const Shape& s, const void* spans, int id64, uint8_t* 
 
 int slots(Ctx* ctx, Slots* s) {
   const size_t n = (size_t)slot_count(ctx->sm_count);
-  s->sums = (float*)scratch(ctx, SLOT_ATTN, n * 2 * TILE * (TC_DIM * sizeof(float) + sizeof(float2)));
+  const size_t rows = n * 2 * TILE, own = (size_t)ctx->sm_count * TILE;
+  s->sums = (float*)scratch(ctx, SLOT_ATTN, (rows + own) * (TC_DIM * sizeof(float) + sizeof(float2)));
   if (!s->sums) return ZOACT_ERR_NOMEM;
-  s->stat = reinterpret_cast<float2*>(s->sums + n * 2 * TILE * TC_DIM);
+  s->merge = s->sums + rows * TC_DIM;
+  s->stat = reinterpret_cast<float2*>(s->merge + own * TC_DIM);
+  s->merge_stat = s->stat + rows;
   s->tickets = (unsigned*)scratch_zeroed(ctx, SLOT_ATTN_TICKETS, n * 4 * sizeof(unsigned));
   return s->tickets ? ZOACT_OK : ZOACT_ERR_NOMEM;
+}
+
+bool tc_supported(const Args& a, bool grad) {
+  const auto lies = [](const void* p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld % 8 == 0; };
+  if (a.dtype == ZOACT_DT_FP32 || a.s.head_dim % 8 != 0 || a.s.head_dim > TC_DIM || a.s.rows_q == 0 || a.s.rows_k == 0) return false;
+  return lies(a.q, a.ld_q) && lies(a.k, a.ld_k) && lies(a.v, a.ld_v) && lies(a.O, a.ld_o) &&
+         (!grad || (lies(a.dO, a.ld_do) && lies(a.dq, a.ld_dq) && lies(a.dk, a.ld_dk) && lies(a.dv, a.ld_dv)));
 }
 
 }  // namespace attn

@@ -92,6 +92,35 @@ int encode_tmap_3d_16bit(CUtensorMap* map, const void* base, int dtype, int64_t 
   return res == CUDA_SUCCESS ? ZOACT_OK : ZOACT_ERR_INVALID_ARG;
 }
 
+namespace {
+int encode_box_16bit(CUtensorMap* map, const void* base, int dtype, int rank, const cuuint64_t* dims, const cuuint64_t* strides,
+                     const cuuint32_t* box) {
+  EncodeTiledFn fn = get_encode_fn();
+  if (!fn) return ZOACT_ERR_CUDA;
+  const cuuint32_t estr[4] = {1u, 1u, 1u, 1u};
+  const CUtensorMapDataType dt =
+      dtype == ZOACT_DT_FP16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+  const CUresult res = fn(map, dt, (cuuint32_t)rank, const_cast<void*>(base), dims, strides, box, estr,
+                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return res == CUDA_SUCCESS ? ZOACT_OK : ZOACT_ERR_INVALID_ARG;
+}
+}  // namespace
+
+int encode_tmap_heads_16bit(CUtensorMap* map, const void* base, int dtype, int64_t rows, int heads, int group, int head_dim,
+                            int64_t ld, int box_rows) {
+  const cuuint64_t d = (cuuint64_t)head_dim;
+  if (group == 0) {
+    const cuuint64_t dims[3] = {d, (cuuint64_t)heads, (cuuint64_t)rows}, strides[2] = {2 * d, 2 * (cuuint64_t)ld};
+    const cuuint32_t box[3] = {64u, 1u, (cuuint32_t)box_rows};
+    return encode_box_16bit(map, base, dtype, 3, dims, strides, box);
+  }
+  const cuuint64_t dims[4] = {d, (cuuint64_t)group, (cuuint64_t)(heads / group), (cuuint64_t)rows};
+  const cuuint64_t strides[3] = {2 * d, 2 * d * (cuuint64_t)group, 2 * (cuuint64_t)ld};
+  const cuuint32_t box[4] = {64u, (cuuint32_t)group, 1u, (cuuint32_t)box_rows};
+  return encode_box_16bit(map, base, dtype, 4, dims, strides, box);
+}
+
 int encode_tmap_2d_int(CUtensorMap* map, const void* base, int elem_bytes, int64_t rows, int64_t cols, int box_cols,
                        int box_rows) {
   EncodeTiledFn fn = get_encode_fn();

@@ -357,6 +357,10 @@ int encode_tmap_2d_16bit(CUtensorMap* map, const void* base, int dtype, int64_t 
 // multiples of 8); a box lies in one slab and is zero-filled at the slab's own edges.
 int encode_tmap_3d_16bit(CUtensorMap* map, const void* base, int dtype, int64_t parts, int64_t rows, int64_t cols,
                          int64_t ld, int64_t part_stride, int box_rows);
+// Host: rows of heads of head_dim columns (rows ld elements apart): boxes of 64 columns of one head and box_rows rows (group 0),
+// or of the heads of a group, beside one another in the box's rows: row i of it is head i % group of row i / group.
+int encode_tmap_heads_16bit(CUtensorMap* map, const void* base, int dtype, int64_t rows, int heads, int group, int head_dim,
+                            int64_t ld, int box_rows);
 // Host: unswizzled boxes of 8- or 16-bit integers (INT4 packed weights, fp16 scales read as raw bits).
 int encode_tmap_2d_int(CUtensorMap* map, const void* base, int elem_bytes, int64_t rows, int64_t cols, int box_cols,
                        int box_rows);
