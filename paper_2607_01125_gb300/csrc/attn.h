@@ -47,7 +47,7 @@ struct Shape {
 
 // Where the parts of a plan lie (bytes).
 struct Layout {
-  size_t seqs, prefix, items[LISTS], delta, total;
+  size_t seqs, prefix, items[LISTS], delta, largest, total;
   int64_t most[LISTS];                  // items a list can have
 };
 Layout plan_layout(const Shape& s, int sm_count, int grad);
@@ -82,6 +82,7 @@ struct Args {
   void *dq, *dk, *dv;
   int64_t ld_dq, ld_dk, ld_dv;
   float* delta;                         // [rows_q, heads], in the plan
+  float* largest;                       // |dO| (fp16), in the plan
 };
 
 // What a kernel needs of a list.

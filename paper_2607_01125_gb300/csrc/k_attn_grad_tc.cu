@@ -1,0 +1,780 @@
+// The gradient of attention over packed sequences on the tensor cores (16-bit operands, heads of up to 128 columns), from the
+// forward pass's log-sum-exps and delta = dO . O:
+//     P = exp2(S scale log2 e - lse log2 e),  dP = dO V^T,  dS = P (dP - delta),
+//     dq = scale dS K,  dk = scale dS^T Q,  dv = P^T dO.
+// Two kernels make S and dP twice (7 products for 5), which leaves no sum to atomics: one has a tile of 128 rows (position, head of
+// the group) and runs over the keys for dq, the other 128 keys and runs over the rows of all heads of the group for dk and dv.
+// P and dS are rounded to the operands' type and stay in TMEM, over the sums that they were made of.
+//
+//   dq:      S twice (two steps), dP, dq in TMEM; while the row threads make dS of one step, the tensor core has dq of the step
+//            before and S of the step after.
+//   dk, dv:  S^T, dP^T, dk, dv in TMEM.  P^T of a step is made while dk of the step before and its dP^T run, dS^T while dv and the
+//            next S^T do: the two halves of a step hide one another.
+//
+// 256 threads work on 128 rows (keys): two warpgroups with 64 columns each.  In fp16, P^T is made 2^10 larger, and dS by a power of
+// two that brings the largest |dO| to 8 .. 16 (never smaller): both keep small values out of the subnormal range, and the
+// factors leave with the result.  Rows behind a sequence's end are zeroed in shared memory where a product would sum over them.
+#include "attn_join.cuh"
+#include "attn_tc.cuh"
+
+namespace zoact {
+namespace attn {
+
+namespace {
+
+using namespace tcx;
+
+constexpr int THREADS = 384, REGS_FEW = 56, REGS_ROWS = 224;      // 3 x 168 as launched
+constexpr int TMEM_COLS = 512;
+
+template <int DP> struct Cfg {
+  static constexpr int BOXES = DP / 64, TILE_BYTES = BOXES * BOX;
+  static constexpr int STAGES = DP == 128 ? 5 : 10;
+  static constexpr int TILES = (2 + STAGES) * TILE_BYTES;
+  static constexpr int HALF = DP / 2;                             // columns of the results of a warpgroup
+};
+
+struct Params {
+  Work work;
+  Slots slots;
+  int* status;
+  int rep, kv_heads, heads, head_dim, causal, positions;
+  float scale, scale_log2;
+  const float *lse, *delta, *largest;                             // largest |dO| (fp16)
+  void *dq, *dk, *dv;
+  int64_t ld_dq, ld_dk, ld_dv;
+  int whole_q, whole_k, whole_v;                                  // rows lie on 32 bytes
+};
+
+struct Maps { CUtensorMap q, g, k, v; };
+
+struct Shared {
+  uint64_t own_full, own_empty, full[10], empty[10], s_full[2], p_full, dp_full, ds_full, acc_full, stat_full[2], stat_empty[2];
+  uint64_t join_in, join_out, drain;
+  uint32_t tmem_base;
+  int abort_flag, last;
+  uint8_t pos_of[TILE];                                           // position of a tile's row
+  alignas(16) float lse[2][TILE];                                 // of a step's rows (dk, dv), read four at a time
+  alignas(16) float delta[2][TILE];
+};
+constexpr int SHARED_BYTES = 2560 + 128;
+static_assert(sizeof(Shared) <= SHARED_BYTES, "barriers and statistics");
+static_assert(Cfg<128>::TILES + SHARED_BYTES <= 232448 && Cfg<64>::TILES + SHARED_BYTES <= 232448, "shared memory");
+
+// Powers of two that P and dS are made larger by, and their inverses.
+template <bool BF16> struct Factors {
+  float p_shift = 0.f, p_inv = 1.f, ds = 1.f, ds_inv = 1.f;       // ds: of dS from P as made
+  __device__ explicit Factors(const float* largest, bool transposed) {
+    if constexpr (!BF16) {
+      const float g = __ldcg(largest);
+      int e = g > 0.f ? 3 - (int)((__float_as_uint(g) >> 23) - 127u) : 0;
+      e = e < 0 ? 0 : e > 24 ? 24 : e;
+      const float up = __uint_as_float((uint32_t)(127 + e) << 23), down = __uint_as_float((uint32_t)(127 - e) << 23);
+      p_shift = transposed ? 10.f : 0.f;
+      p_inv = transposed ? 0x1p-10f : 1.f;
+      ds = up * p_inv;
+      ds_inv = down;
+    }
+  }
+};
+
+// A warpgroup's half of P or dS in TMEM: 64 columns of sums became 32 of pairs at the same place.
+__device__ __forceinline__ void mma_rows_halves(uint32_t d, uint32_t a_tmem, uint32_t b, uint32_t idesc, int steps, bool accumulate) {
+  for (int k = 0; k < steps; ++k)
+    mma_ts(d, a_tmem + (uint32_t)(k >> 2) * 64u + (uint32_t)(k & 3) * 8u, desc_rows(b + (uint32_t)k * 2048u), idesc, accumulate || k != 0);
+}
+
+// The barriers, and each row's position.
+template <int STAGES>
+__device__ __forceinline__ void init_shared(Shared* sh, int rep) {
+  const auto bar = [](const uint64_t& b) { return tc::smem_u32(&b); };
+  if (threadIdx.x == 0) {
+    tc::mbar_init(bar(sh->own_full), 1);
+    tc::mbar_init(bar(sh->own_empty), 1);
+    for (int s = 0; s < STAGES; ++s) {
+      tc::mbar_init(bar(sh->full[s]), 1);
+      tc::mbar_init(bar(sh->empty[s]), 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      tc::mbar_init(bar(sh->s_full[b]), 1);
+      tc::mbar_init(bar(sh->stat_full[b]), 1);
+      tc::mbar_init(bar(sh->stat_empty[b]), 8);
+    }
+    tc::mbar_init(bar(sh->p_full), 8);
+    tc::mbar_init(bar(sh->dp_full), 1);
+    tc::mbar_init(bar(sh->ds_full), 8);
+    tc::mbar_init(bar(sh->acc_full), 1);
+    tc::mbar_init(bar(sh->join_in), 8);
+    tc::mbar_init(bar(sh->join_out), 1);
+    tc::mbar_init(bar(sh->drain), 1);
+    sh->abort_flag = 0;
+    tc::fence_mbar_init();
+  }
+  if (threadIdx.x < TILE) sh->pos_of[threadIdx.x] = (uint8_t)(threadIdx.x / rep);
+}
+
+// Whether this row of work's last part is here: the row threads' part of last_part, with bounded waits.  ok: the waits held.
+__device__ __forceinline__ bool last_of_parts(Shared* sh, unsigned* ticket, int nparts, uint32_t parity, int rwarp, int lane, int* status,
+                                              bool& ok) {
+  volatile int* abort_flag = &sh->abort_flag;
+  __threadfence();
+  __syncwarp();
+  if (lane == 0) tc::mbar_arrive(tc::smem_u32(&sh->join_in));
+  if (rwarp == 0) {
+    ok = warp_wait(tc::smem_u32(&sh->join_in), parity, abort_flag, status);
+    if (!ok) return false;
+    if (lane == 0) {
+      __threadfence();
+      const bool last = atomicAdd(ticket, 1u) == (unsigned)(nparts - 1);
+      if (last) *ticket = 0;
+      __threadfence();
+      sh->last = last;
+      tc::mbar_arrive(tc::smem_u32(&sh->join_out));
+    }
+  }
+  ok = warp_wait(tc::smem_u32(&sh->join_out), parity, abort_flag, status);
+  if (!ok) return false;
+  const bool last = *(volatile int*)&sh->last != 0;
+  if (last) __threadfence();
+  return last;
+}
+
+// 32 columns of a result from TMEM, times f.
+__device__ __forceinline__ void acc_chunk(uint32_t taddr, float f, float* v) {
+  uint32_t o[32];
+  ld32(taddr, o);
+  ld_wait();
+  ld_use(o);
+#pragma unroll
+  for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(o[i]) * f;
+}
+__device__ __forceinline__ void put_part(float* d, const float* v, int n) {
+#pragma unroll
+  for (int i = 0; i < 32; i += 4)
+    if (i < n) *reinterpret_cast<float4*>(d + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+}
+
+template <int DP, bool BF16>
+__global__ void __launch_bounds__(THREADS, 1) dq_tc_kernel(const __grid_constant__ Maps tm, const Params p) {
+  using G = Cfg<DP>;
+  constexpr int STAGES = G::STAGES;
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  Shared* sh = reinterpret_cast<Shared*>(smem_raw + G::TILES);
+  const uint32_t q_tile = tc::smem_u32(smem_raw), g_tile = q_tile + G::TILE_BYTES, ring = q_tile + 2 * G::TILE_BYTES;
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+  if (q_tile & 1023u) {                  // (swizzled tiles: dynamic shared memory begins there, as nothing static lies before it)
+    if (threadIdx.x == 0 && blockIdx.x == 0) record_error(p.status, ZOACT_ERR_UNSUPPORTED);
+    return;
+  }
+  volatile int* abort_flag = &sh->abort_flag;
+  const auto bar = [](const uint64_t& b) { return tc::smem_u32(&b); };
+  init_shared<STAGES>(sh, p.rep);
+  if (threadIdx.x == 32) {
+    tc::prefetch_tmap(&tm.q);
+    tc::prefetch_tmap(&tm.g);
+    tc::prefetch_tmap(&tm.k);
+    tc::prefetch_tmap(&tm.v);
+  }
+  __syncwarp();
+  if (warp == 1) {
+    tc::tmem_alloc(tc::smem_u32(&sh->tmem_base), TMEM_COLS);
+    tc::tmem_relinquish();
+  }
+  tc::tc_fence_before();
+  __syncthreads();
+  tc::tc_fence_after();
+  const uint32_t tmem = __shfl_sync(0xffffffffu, sh->tmem_base, 0);
+  const uint32_t t_s = tmem, t_dp = tmem + 2 * BK, t_dq = tmem + 3 * BK;        // S: two of BK columns
+  pdl_wait();
+  pdl_trigger();
+
+  const int total = work_count(p.work, p.kv_heads, threadIdx.x == 0 && blockIdx.x == 0 ? p.status : nullptr);
+  const auto item_of = [&](int u) { return load_item(p.work.items + u / p.kv_heads); };
+  const int G0 = gridDim.x;
+  const int ksteps = (p.head_dim + 15) / 16;
+
+  if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_FEW));
+    if (warp == 0) {
+      // ---------------- TMA producer ----------------
+      uint32_t at = 0, units = 0;
+      bool ok = true;
+      const uint32_t row_bytes = (uint32_t)(G::BOXES * p.positions * p.rep * 128);
+      for (int r = 0; ok && (int64_t)r * G0 < total; ++r) {
+        const int u = unit_of(r, blockIdx.x, G0);
+        if (u >= total) continue;
+        const Item w = item_of(u);
+        const int h = u % p.kv_heads, n = (w.nk + BK - 1) / BK;
+        if (n == 0) continue;
+        ok = warp_wait(bar(sh->own_empty), (units & 1) ^ 1u, abort_flag, p.status);
+        if (!ok) break;
+        ++units;
+        if (elect_one()) {
+          tc::mbar_arrive_expect_tx(bar(sh->own_full), 2 * row_bytes);
+          for (int b = 0; b < G::BOXES; ++b) {
+            tma_load_4d(q_tile + (uint32_t)(b * BOX), &tm.q, b * 64, 0, h, w.q0, bar(sh->own_full));
+            tma_load_4d(g_tile + (uint32_t)(b * BOX), &tm.g, b * 64, 0, h, w.q0, bar(sh->own_full));
+          }
+        }
+        __syncwarp();
+        for (int j = 0; ok && j < 2 * n; ++j, ++at) {
+          const uint32_t s = at % STAGES;
+          ok = warp_wait(bar(sh->empty[s]), (at / STAGES & 1) ^ 1u, abort_flag, p.status);
+          if (!ok) break;
+          if (elect_one()) {
+            const CUtensorMap* map = j & 1 ? &tm.v : &tm.k;
+            tc::mbar_arrive_expect_tx(bar(sh->full[s]), (uint32_t)G::TILE_BYTES);
+            for (int b = 0; b < G::BOXES; ++b)
+              tma_load_3d(ring + s * G::TILE_BYTES + (uint32_t)(b * BOX), map, b * 64, h, w.k0 + j / 2 * BK, bar(sh->full[s]));
+          }
+          __syncwarp();
+        }
+      }
+      if (!ok) {                       // give our copies time to land before the CTA winds down
+        const uint64_t t0 = tc::global_timer_ns();
+        while (tc::global_timer_ns() - t0 < 2000000ull) {
+        }
+      }
+    } else if (warp == 1) {
+      // ---------------- MMA issuer ----------------
+      const uint32_t id_s = tc::idesc_f16(TILE, BK, BF16), id_q = tc::idesc_f16(TILE, ksteps * 16, BF16) | B_BY_ROWS;
+      uint32_t base = 0, step = 0, units = 0;
+      bool ok = true, any = false;
+      for (int r = 0; ok && (int64_t)r * G0 < total; ++r) {
+        const int u = unit_of(r, blockIdx.x, G0);
+        if (u >= total) continue;
+        const Item w = item_of(u);
+        const int n = (w.nk + BK - 1) / BK;
+        if (n == 0) continue;
+        const auto tile = [&](uint32_t at) { return ring + at % STAGES * G::TILE_BYTES; };
+        const auto product_s = [&](int j) {
+          const uint32_t at = base + 2 * j;
+          if (!warp_wait(bar(sh->full[at % STAGES]), at / STAGES & 1, abort_flag, p.status)) return false;
+          const int keys = min(BK, w.nk - j * BK);
+          if (keys % 16 != 0) zero_rows(tile(at), G::BOXES, keys, (keys + 15) / 16 * 16, lane);
+          tc::tc_fence_after();
+          if (elect_one()) {
+            mma_cols(t_s + ((step + j) & 1) * BK, q_tile, tile(at), id_s, ksteps);
+            tc::mma_commit(bar(sh->s_full[(step + j) & 1]));
+          }
+          __syncwarp();
+          any = true;
+          return true;
+        };
+        const auto product_dp = [&](int j) {
+          const uint32_t at = base + 2 * j + 1;
+          if (!warp_wait(bar(sh->full[at % STAGES]), at / STAGES & 1, abort_flag, p.status)) return false;
+          tc::tc_fence_after();
+          if (elect_one()) {
+            mma_cols(t_dp, g_tile, tile(at), id_s, ksteps);
+            tc::mma_commit(bar(sh->dp_full));
+            tc::mma_commit(bar(sh->empty[at % STAGES]));
+            if (j == n - 1) tc::mma_commit(bar(sh->own_empty));
+          }
+          __syncwarp();
+          return true;
+        };
+        ok = warp_wait(bar(sh->own_full), units & 1, abort_flag, p.status) && product_s(0) && product_dp(0) && (n < 2 || product_s(1));
+        ++units;
+        for (int j = 0; ok && j < n; ++j) {
+          ok = warp_wait(bar(sh->ds_full), (step + j) & 1, abort_flag, p.status);
+          if (!ok) break;
+          if (j + 1 < n) ok = product_dp(j + 1);
+          if (!ok) break;
+          tc::tc_fence_after();
+          if (elect_one()) {
+            const int keys = min(BK, w.nk - j * BK);
+            mma_rows_halves(t_dq, t_s + ((step + j) & 1) * BK, tile(base + 2 * j), id_q, (keys + 15) / 16, j != 0);
+            tc::mma_commit(bar(sh->empty[(base + 2 * j) % STAGES]));
+            if (j == n - 1) tc::mma_commit(bar(sh->acc_full));
+          }
+          __syncwarp();
+          if (j + 2 < n) ok = product_s(j + 2);
+        }
+        base += 2 * n;
+        step += n;
+      }
+      if (any) {
+        if (elect_one()) tc::mma_commit(bar(sh->drain));
+        __syncwarp();
+        tc::mbar_wait_drain(bar(sh->drain), 0, 100000000ull);
+      }
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_ROWS));
+    // ---------------- a thread half a row: dS, and dq at the end ----------------
+    const int half = (warp - 4) >> 2, quad = warp & 3, row = quad * 32 + lane, rwarp = warp - 4;
+    const uint32_t lanes = (uint32_t)(quad * 32) << 16;
+    const int D = p.head_dim, pos = row / p.rep, in_group = row - pos * p.rep;
+    const Factors<BF16> f(p.largest, false);
+    uint32_t step = 0, units = 0, joins = 0;
+    bool ok = true;
+    for (int r = 0; ok && (int64_t)r * G0 < total; ++r) {
+      const int u = unit_of(r, blockIdx.x, G0);
+      if (u >= total) continue;
+      const Item w = item_of(u);
+      const int h = u % p.kv_heads, n = (w.nk + BK - 1) / BK, rows = w.npos * p.rep;
+      const bool active = quad * 32 < rows, valid = row < rows;
+      const int see = valid ? visible(w, p.causal, pos) : 0, all_see = visible(w, p.causal, 0);
+      const int64_t e = (int64_t)(w.q0 + pos) * p.heads + h * p.rep + in_group;
+      const float lse2 = valid ? p.lse[e] * 1.44269504f : 0.f, delta = valid ? p.delta[e] : 0.f;
+      for (int j = 0; j < n; ++j, ++step) {
+        ok = warp_wait(bar(sh->s_full[step & 1]), step >> 1 & 1, abort_flag, p.status) &&
+             warp_wait(bar(sh->dp_full), step & 1, abort_flag, p.status);
+        if (!ok) break;
+        if (active) {
+          tc::tc_fence_after();
+          const uint32_t s0 = t_s + (step & 1) * BK + lanes + half * 64, d0 = t_dp + lanes + half * 64;
+          const bool masked = all_see < (j + 1) * BK;
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            uint32_t x[32], d[32];
+            ld32(s0 + c * 32, x);
+            ld32(d0 + c * 32, d);
+            ld_wait();
+            ld_use(x);
+            ld_use(d);
+            uint32_t y[16];
+            const int lim = masked ? see - j * BK - half * 64 - c * 32 : 32;
+#pragma unroll
+            for (int i = 0; i < 32; i += 2) {
+              float v[2];
+#pragma unroll
+              for (int k = 0; k < 2; ++k) {
+                const float pr = ex2(fmaf(__uint_as_float(x[i + k]), p.scale_log2, -lse2));
+                v[k] = pr * (__uint_as_float(d[i + k]) - delta) * f.ds;
+                if (i + k >= lim) v[k] = 0.f;
+              }
+              y[i / 2] = pack2<BF16>(v[0], v[1]);
+            }
+            st16(s0 + c * 16, y);
+          }
+          tc::tmem_wait_st();
+          tc::tc_fence_before();
+        }
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(bar(sh->ds_full));
+      }
+      if (!ok) break;
+      if (n > 0) {
+        ok = warp_wait(bar(sh->acc_full), units & 1, abort_flag, p.status);
+        if (!ok) break;
+        ++units;
+        tc::tc_fence_after();
+      }
+      const float out_f = p.scale * f.ds_inv;
+      const bool cut = w.nparts > 1;
+      const int slot = w.slot + h * w.nparts;
+      uint16_t* const dq = static_cast<uint16_t*>(p.dq);
+      if (active) {
+#pragma unroll 1
+        for (int c = half * G::HALF; c < min(D, (half + 1) * G::HALF); c += 32) {
+          float v[32];
+          if (n > 0) {
+            acc_chunk(t_dq + lanes + c, out_f, v);
+          } else {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = 0.f;
+          }
+          if (!valid) continue;
+          if (cut) put_part(slot_sums(p.slots, slot + w.part) + (size_t)row * D + c, v, D - c);
+          else store_row<BF16>(dq + (int64_t)(w.q0 + pos) * p.ld_dq + (int64_t)(h * p.rep + in_group) * D + c, v, min(32, D - c), p.whole_q);
+        }
+      }
+      tc::tc_fence_before();
+      if (cut) {
+        const bool last = last_of_parts(sh, p.slots.tickets + 4 * slot, w.nparts, joins & 1, rwarp, lane, p.status, ok);
+        if (!ok) break;
+        ++joins;
+        if (last) {
+          for (int i = rwarp * 32 + lane; i < rows * D; i += 256) {
+            float x = 0.f;
+            for (int k = 0; k < w.nparts; ++k) x += __ldcg(slot_sums(p.slots, slot + k) + i);
+            const int rr = i / D, ps = rr / p.rep;
+            dq[(int64_t)(w.q0 + ps) * p.ld_dq + (int64_t)(h * p.rep + rr - ps * p.rep) * D + (i - rr * D)] = (uint16_t)pack2<BF16>(x, 0.f);
+          }
+        }
+      }
+    }
+  }
+  tc::tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    __syncwarp();
+    tc::tc_fence_after();
+    tc::tmem_dealloc(tmem, TMEM_COLS);
+  }
+}
+
+template <int DP, bool BF16>
+__global__ void __launch_bounds__(THREADS, 1) dkv_tc_kernel(const __grid_constant__ Maps tm, const Params p) {
+  using G = Cfg<DP>;
+  constexpr int STAGES = G::STAGES;
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  Shared* sh = reinterpret_cast<Shared*>(smem_raw + G::TILES);
+  const uint32_t k_tile = tc::smem_u32(smem_raw), v_tile = k_tile + G::TILE_BYTES, ring = k_tile + 2 * G::TILE_BYTES;
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+  if (k_tile & 1023u) {                  // (swizzled tiles: dynamic shared memory begins there, as nothing static lies before it)
+    if (threadIdx.x == 0 && blockIdx.x == 0) record_error(p.status, ZOACT_ERR_UNSUPPORTED);
+    return;
+  }
+  volatile int* abort_flag = &sh->abort_flag;
+  const auto bar = [](const uint64_t& b) { return tc::smem_u32(&b); };
+  init_shared<STAGES>(sh, p.rep);
+  if (threadIdx.x == 32) {
+    tc::prefetch_tmap(&tm.q);
+    tc::prefetch_tmap(&tm.g);
+    tc::prefetch_tmap(&tm.k);
+    tc::prefetch_tmap(&tm.v);
+  }
+  __syncwarp();
+  if (warp == 1) {
+    tc::tmem_alloc(tc::smem_u32(&sh->tmem_base), TMEM_COLS);
+    tc::tmem_relinquish();
+  }
+  tc::tc_fence_before();
+  __syncthreads();
+  tc::tc_fence_after();
+  const uint32_t tmem = __shfl_sync(0xffffffffu, sh->tmem_base, 0);
+  const uint32_t t_s = tmem, t_dp = tmem + BK, t_dv = tmem + 2 * BK, t_dk = tmem + 3 * BK;
+  pdl_wait();
+  pdl_trigger();
+
+  const int total = work_count(p.work, p.kv_heads, threadIdx.x == 0 && blockIdx.x == 0 ? p.status : nullptr);
+  const auto item_of = [&](int u) { return load_item(p.work.items + u / p.kv_heads); };
+  const int G0 = gridDim.x, P = p.positions;
+  const int ksteps = (p.head_dim + 15) / 16;
+
+  if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_FEW));
+    if (warp == 0) {
+      // ---------------- TMA producer ----------------
+      uint32_t at = 0, units = 0;
+      bool ok = true;
+      const uint32_t row_bytes = (uint32_t)(G::BOXES * P * p.rep * 128);
+      for (int r = 0; ok && (int64_t)r * G0 < total; ++r) {
+        const int u = unit_of(r, blockIdx.x, G0);
+        if (u >= total) continue;
+        const Item w = item_of(u);
+        const int h = u % p.kv_heads, n = (w.npos + P - 1) / P;
+        if (n == 0) continue;
+        ok = warp_wait(bar(sh->own_empty), (units & 1) ^ 1u, abort_flag, p.status);
+        if (!ok) break;
+        ++units;
+        if (elect_one()) {
+          tc::mbar_arrive_expect_tx(bar(sh->own_full), (uint32_t)(2 * G::TILE_BYTES));
+          for (int b = 0; b < G::BOXES; ++b) {
+            tma_load_3d(k_tile + (uint32_t)(b * BOX), &tm.k, b * 64, h, w.k0, bar(sh->own_full));
+            tma_load_3d(v_tile + (uint32_t)(b * BOX), &tm.v, b * 64, h, w.k0, bar(sh->own_full));
+          }
+        }
+        __syncwarp();
+        for (int j = 0; ok && j < 2 * n; ++j, ++at) {
+          const uint32_t s = at % STAGES;
+          ok = warp_wait(bar(sh->empty[s]), (at / STAGES & 1) ^ 1u, abort_flag, p.status);
+          if (!ok) break;
+          if (elect_one()) {
+            const CUtensorMap* map = j & 1 ? &tm.g : &tm.q;
+            tc::mbar_arrive_expect_tx(bar(sh->full[s]), row_bytes);
+            for (int b = 0; b < G::BOXES; ++b)
+              tma_load_4d(ring + s * G::TILE_BYTES + (uint32_t)(b * BOX), map, b * 64, 0, h, w.q0 + j / 2 * P, bar(sh->full[s]));
+          }
+          __syncwarp();
+        }
+      }
+      if (!ok) {                       // give our copies time to land before the CTA winds down
+        const uint64_t t0 = tc::global_timer_ns();
+        while (tc::global_timer_ns() - t0 < 2000000ull) {
+        }
+      }
+    } else if (warp == 1) {
+      // ---------------- MMA issuer ----------------
+      const uint32_t id_d = tc::idesc_f16(BK, ksteps * 16, BF16) | B_BY_ROWS;
+      uint32_t base = 0, step = 0, units = 0;
+      bool ok = true, any = false;
+      for (int r = 0; ok && (int64_t)r * G0 < total; ++r) {
+        const int u = unit_of(r, blockIdx.x, G0);
+        if (u >= total) continue;
+        const Item w = item_of(u);
+        const int n = (w.npos + P - 1) / P;
+        if (n == 0) continue;
+        const auto tile = [&](uint32_t at) { return ring + at % STAGES * G::TILE_BYTES; };
+        const auto rows_of = [&](int i) { return min(P, w.npos - i * P) * p.rep; };
+        // S^T (first = 0: K by Q) or dP^T (1: V by dO) of step i, as wide as the step has rows
+        const auto product = [&](int first, int i) {
+          const uint32_t at = base + 2 * i + first;
+          if (!warp_wait(bar(sh->full[at % STAGES]), at / STAGES & 1, abort_flag, p.status)) return false;
+          const int rows = rows_of(i), up = (rows + 15) / 16 * 16;
+          if (rows != up) zero_rows(tile(at), G::BOXES, rows, up, lane);
+          tc::tc_fence_after();
+          if (elect_one()) {
+            mma_cols(first ? t_dp : t_s, first ? v_tile : k_tile, tile(at), tc::idesc_f16(BK, up, BF16), ksteps);
+            tc::mma_commit(first ? bar(sh->dp_full) : bar(sh->s_full[0]));
+            if (first && i == n - 1) tc::mma_commit(bar(sh->own_empty));
+          }
+          __syncwarp();
+          any = true;
+          return true;
+        };
+        // dv += P^T dO (first = 1) or dk += dS^T Q (0)
+        const auto sum = [&](int first, int i) {
+          const uint32_t at = base + 2 * i + first;
+          tc::tc_fence_after();
+          if (elect_one()) {
+            mma_rows_halves(first ? t_dv : t_dk, first ? t_s : t_dp, tile(at), id_d, (rows_of(i) + 15) / 16, i != 0);
+            tc::mma_commit(bar(sh->empty[at % STAGES]));
+            if (!first && i == n - 1) tc::mma_commit(bar(sh->acc_full));
+          }
+          __syncwarp();
+        };
+        ok = warp_wait(bar(sh->own_full), units & 1, abort_flag, p.status) && product(0, 0) && product(1, 0);
+        ++units;
+        for (int i = 0; ok && i < n; ++i) {
+          ok = warp_wait(bar(sh->p_full), (step + i) & 1, abort_flag, p.status);
+          if (!ok) break;
+          sum(1, i);
+          if (i + 1 < n) ok = product(0, i + 1);
+          if (!ok) break;
+          ok = warp_wait(bar(sh->ds_full), (step + i) & 1, abort_flag, p.status);
+          if (!ok) break;
+          sum(0, i);
+          if (i + 1 < n) ok = product(1, i + 1);
+        }
+        base += 2 * n;
+        step += n;
+      }
+      if (any) {
+        if (elect_one()) tc::mma_commit(bar(sh->drain));
+        __syncwarp();
+        tc::mbar_wait_drain(bar(sh->drain), 0, 100000000ull);
+      }
+    } else if (warp == 2) {
+      // ---------------- the rows' statistics, two steps ahead ----------------
+      const Factors<BF16> f(p.largest, true);
+      uint32_t step = 0;
+      bool ok = true;
+      for (int r = 0; ok && (int64_t)r * G0 < total; ++r) {
+        const int u = unit_of(r, blockIdx.x, G0);
+        if (u >= total) continue;
+        const Item w = item_of(u);
+        const int h = u % p.kv_heads, n = (w.npos + P - 1) / P;
+        for (int i = 0; i < n; ++i, ++step) {
+          const int b = step & 1, rows = min(P, w.npos - i * P) * p.rep;
+          float lse[4], delta[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const int row = lane + 32 * k, pos = sh->pos_of[row];
+            const int64_t e = (int64_t)(w.q0 + i * P + pos) * p.heads + h * p.rep + row - pos * p.rep;
+            // (rows behind the last: no share)
+            lse[k] = row < rows ? p.lse[e] * 1.44269504f - f.p_shift : INFINITY;
+            delta[k] = row < rows ? p.delta[e] : 0.f;
+          }
+          ok = warp_wait(bar(sh->stat_empty[b]), (step >> 1 & 1) ^ 1u, abort_flag, p.status);
+          if (!ok) break;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            sh->lse[b][lane + 32 * k] = lse[k];
+            sh->delta[b][lane + 32 * k] = delta[k];
+          }
+          __syncwarp();
+          if (lane == 0) tc::mbar_arrive(bar(sh->stat_full[b]));
+        }
+      }
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_ROWS));
+    // ---------------- a thread half of a key's rows: P^T and dS^T, dk and dv at the end ----------------
+    const int half = (warp - 4) >> 2, quad = warp & 3, key = quad * 32 + lane, rwarp = warp - 4;
+    const uint32_t lanes = (uint32_t)(quad * 32) << 16;
+    const int D = p.head_dim;
+    const Factors<BF16> f(p.largest, true);
+    uint32_t step = 0, units = 0, joins = 0;
+    bool ok = true;
+    for (int r = 0; ok && (int64_t)r * G0 < total; ++r) {
+      const int u = unit_of(r, blockIdx.x, G0);
+      if (u >= total) continue;
+      const Item w = item_of(u);
+      const int h = u % p.kv_heads, n = (w.npos + P - 1) / P;
+      const bool active = quad * 32 < w.nk, valid = key < w.nk;
+      for (int i = 0; i < n; ++i, ++step) {
+        const int b = step & 1;
+        ok = warp_wait(bar(sh->stat_full[b]), step >> 1 & 1, abort_flag, p.status) &&
+             warp_wait(bar(sh->s_full[0]), step & 1, abort_flag, p.status);
+        if (!ok) break;
+        float pr[64];
+        const uint32_t s0 = t_s + lanes + half * 64, d0 = t_dp + lanes + half * 64;
+        const float4* const lse = reinterpret_cast<const float4*>(&sh->lse[b][half * 64]);
+        const float4* const delta = reinterpret_cast<const float4*>(&sh->delta[b][half * 64]);
+        if (active) {
+          tc::tc_fence_after();
+          const bool masked = visible(w, p.causal, i * P) < w.nk;
+          // a row at position x of the step sees this key from x = `from` on
+          const int from = key + 1 - w.diag - i * P;
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            uint32_t x[32];
+            ld32(s0 + c * 32, x);
+            ld_wait();
+            ld_use(x);
+            uint32_t y[16];
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+              const float4 l4 = lse[c * 8 + q];
+              const float l[4] = {l4.x, l4.y, l4.z, l4.w};
+#pragma unroll
+              for (int k = 0; k < 4; ++k) pr[c * 32 + q * 4 + k] = ex2(fmaf(__uint_as_float(x[q * 4 + k]), p.scale_log2, -l[k]));
+            }
+            if (masked) {
+#pragma unroll
+              for (int k = 0; k < 32; ++k)
+                if ((int)sh->pos_of[half * 64 + c * 32 + k] < from) pr[c * 32 + k] = 0.f;
+            }
+#pragma unroll
+            for (int k = 0; k < 16; ++k) y[k] = pack2<BF16>(pr[c * 32 + 2 * k], pr[c * 32 + 2 * k + 1]);
+            st16(s0 + c * 16, y);
+          }
+          tc::tmem_wait_st();
+          tc::tc_fence_before();
+        }
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(bar(sh->p_full));
+        ok = warp_wait(bar(sh->dp_full), step & 1, abort_flag, p.status);
+        if (!ok) break;
+        if (active) {
+          tc::tc_fence_after();
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            uint32_t x[32];
+            ld32(d0 + c * 32, x);
+            ld_wait();
+            ld_use(x);
+            uint32_t y[16];
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+              const float4 d4 = delta[c * 8 + q];
+              const float d[4] = {d4.x, d4.y, d4.z, d4.w};
+              float v[4];
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                const float share = pr[c * 32 + q * 4 + k];
+                v[k] = share * (__uint_as_float(x[q * 4 + k]) - d[k]) * f.ds;
+                // (a key that is not seen: 0, whatever its sums are)
+                if (share == 0.f) v[k] = 0.f;
+              }
+              y[2 * q] = pack2<BF16>(v[0], v[1]);
+              y[2 * q + 1] = pack2<BF16>(v[2], v[3]);
+            }
+            st16(d0 + c * 16, y);
+          }
+          tc::tmem_wait_st();
+          tc::tc_fence_before();
+        }
+        __syncwarp();
+        if (lane == 0) {
+          tc::mbar_arrive(bar(sh->ds_full));
+          tc::mbar_arrive(bar(sh->stat_empty[b]));
+        }
+      }
+      if (!ok) break;
+      if (n > 0) {
+        ok = warp_wait(bar(sh->acc_full), units & 1, abort_flag, p.status);
+        if (!ok) break;
+        ++units;
+        tc::tc_fence_after();
+      }
+      const float fk = p.scale * f.ds_inv, fv = f.p_inv;
+      const bool cut = w.nparts > 1;
+      const int slot = w.slot + h * w.nparts;
+      uint16_t* const dk = static_cast<uint16_t*>(p.dk) + (int64_t)w.k0 * p.ld_dk + (int64_t)h * D;
+      uint16_t* const dv = static_cast<uint16_t*>(p.dv) + (int64_t)w.k0 * p.ld_dv + (int64_t)h * D;
+      if (active) {
+#pragma unroll 1
+        for (int c = half * G::HALF; c < min(D, (half + 1) * G::HALF); c += 32) {
+          float v[32];
+#pragma unroll
+          for (int which = 0; which < 2; ++which) {
+            if (n > 0) {
+              acc_chunk((which ? t_dv : t_dk) + lanes + c, which ? fv : fk, v);
+            } else {
+#pragma unroll
+              for (int i = 0; i < 32; ++i) v[i] = 0.f;
+            }
+            if (!valid) continue;
+            if (cut) put_part(slot_sums(p.slots, slot + w.part) + (size_t)(which * BK + key) * D + c, v, D - c);
+            else if (which) store_row<BF16>(dv + (int64_t)key * p.ld_dv + c, v, min(32, D - c), p.whole_v);
+            else store_row<BF16>(dk + (int64_t)key * p.ld_dk + c, v, min(32, D - c), p.whole_k);
+          }
+        }
+      }
+      tc::tc_fence_before();
+      if (cut) {
+        const bool last = last_of_parts(sh, p.slots.tickets + 4 * slot, w.nparts, joins & 1, rwarp, lane, p.status, ok);
+        if (!ok) break;
+        ++joins;
+        if (last) {
+          for (int i = rwarp * 32 + lane; i < w.nk * D; i += 256) {
+            float x = 0.f, y = 0.f;
+            for (int k = 0; k < w.nparts; ++k) {
+              const float* s = slot_sums(p.slots, slot + k) + i;
+              x += __ldcg(s);
+              y += __ldcg(s + (size_t)BK * D);
+            }
+            const int kk = i / D, d = i - kk * D;
+            dk[(int64_t)kk * p.ld_dk + d] = (uint16_t)pack2<BF16>(x, 0.f);
+            dv[(int64_t)kk * p.ld_dv + d] = (uint16_t)pack2<BF16>(y, 0.f);
+          }
+        }
+      }
+    }
+  }
+  tc::tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    __syncwarp();
+    tc::tc_fence_after();
+    tc::tmem_dealloc(tmem, TMEM_COLS);
+  }
+}
+
+template <int DP, bool BF16>
+int run(Ctx* ctx, const Args& a) {
+  Params p = {};
+  const int st = slots(ctx, &p.slots);
+  if (st) return st;
+  p.status = ctx->d_status;
+  p.rep = a.s.rep(); p.kv_heads = a.s.kv_heads; p.heads = a.s.heads; p.head_dim = a.s.head_dim; p.causal = a.s.causal;
+  p.positions = tile_positions(p.rep);
+  p.scale = a.scale; p.scale_log2 = a.scale * 1.44269504f;
+  p.lse = a.lse; p.delta = a.delta; p.largest = a.largest;
+  p.dq = a.dq; p.dk = a.dk; p.dv = a.dv; p.ld_dq = a.ld_dq; p.ld_dk = a.ld_dk; p.ld_dv = a.ld_dv;
+  const auto whole = [&](const void* q, int64_t ld) { return ((uintptr_t)q & 31) == 0 && ld % 16 == 0 && a.s.head_dim % 16 == 0; };
+  p.whole_q = whole(a.dq, a.ld_dq); p.whole_k = whole(a.dk, a.ld_dk); p.whole_v = whole(a.dv, a.ld_dv);
+  Maps tm;
+  int e = encode_rows(&tm.q, a.q, a.dtype, a.s, a.ld_q);
+  if (!e) e = encode_rows(&tm.g, a.dO, a.dtype, a.s, a.ld_do);
+  if (!e) e = encode_keys(&tm.k, a.k, a.dtype, a.s, a.ld_k);
+  if (!e) e = encode_keys(&tm.v, a.v, a.dtype, a.s, a.ld_v);
+  if (e) return e;
+  constexpr int SMEM = Cfg<DP>::TILES + SHARED_BYTES;
+  for (int list : {LIST_DQ, LIST_DKV}) {
+    auto kern = list == LIST_DQ ? dq_tc_kernel<DP, BF16> : dkv_tc_kernel<DP, BF16>;
+    p.work = work_of(a, list);
+    ZOACT_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM));
+    const int64_t most = a.at.most[list] * a.s.kv_heads;
+    ZOACT_CUDA_TRY(launch_pdl(ctx, kern, dim3((unsigned)(most < ctx->sm_count ? most : ctx->sm_count)), dim3(THREADS), (size_t)SMEM,
+                              tm, p));
+    ++ctx->n_launch;
+  }
+  return ZOACT_OK;
+}
+
+}  // namespace
+
+int launch_grad_tc(Ctx* ctx, const Args& a) {
+  const bool bf = a.dtype == ZOACT_DT_BF16;
+  if (a.s.head_dim <= 64) return bf ? run<64, true>(ctx, a) : run<64, false>(ctx, a);
+  return bf ? run<128, true>(ctx, a) : run<128, false>(ctx, a);
+}
+
+}  // namespace attn
+}  // namespace zoact

@@ -223,6 +223,8 @@ Layout plan_layout(const Shape& s, int sm_count, int grad) {
   }
   l.delta = at;
   if (grad) at += up((size_t)s.rows_q * s.heads * sizeof(float));
+  l.largest = at;
+  if (grad) at += up(sizeof(float));
   l.total = at;
   return l;
 }

@@ -7,6 +7,8 @@
 // and columns, spread 16 apart, so that its 16-byte reads of shared memory fall on different banks.  The gradient recomputes
 // P = exp(S - lse) in two passes, one over the keys for dq and one over the rows for dk and dv, so that no sum needs atomics.
 // Bound by the FMA pipes: 2 reads of 16 bytes from shared memory feed 8 FMAs.
+#include <type_traits>
+
 #include "attn.h"
 #include "attn_join.cuh"
 
@@ -220,25 +222,41 @@ __global__ void __launch_bounds__(THREADS) fwd_kernel(const Dev p) {
   }
 }
 
-// delta = the row sum of dO O, a warp a (row, head).
+// delta = the row sum of dO O, a warp a (row, head); in fp16 also the largest finite |dO| (0 before).
 template <typename T>
 __global__ void __launch_bounds__(THREADS) delta_kernel(const Work work, int* status, const T* dO, int64_t ld_do, const T* O,
-                                                        int64_t ld_o, int64_t rows, int heads, int head_dim, float* delta) {
+                                                        int64_t ld_o, int64_t rows, int heads, int head_dim, float* delta,
+                                                        float* largest) {
   pdl_wait();
   pdl_trigger();
   // the sums lie in the plan, where it has room for them
   if (work_count(work, 1, threadIdx.x == 0 && blockIdx.x == 0 ? status : nullptr) == 0) return;
   const int lane = threadIdx.x & 31;
   const int64_t n = rows * heads;
+  float top = 0.f;
   for (int64_t i = (int64_t)blockIdx.x * (THREADS / 32) + (threadIdx.x >> 5); i < n; i += (int64_t)gridDim.x * (THREADS / 32)) {
     const int64_t r = i / heads;
     const int h = (int)(i - r * heads);
     const T *a = dO + r * ld_do + (int64_t)h * head_dim, *b = O + r * ld_o + (int64_t)h * head_dim;
     float s = 0.f;
-    for (int d = lane; d < head_dim; d += 32) s += to_f32<T>(a[d]) * to_f32<T>(b[d]);
+    for (int d = lane; d < head_dim; d += 32) {
+      const float g = to_f32<T>(a[d]);
+      s += g * to_f32<T>(b[d]);
+      if (std::is_same<T, __half>::value && fabsf(g) < INFINITY) top = fmaxf(top, fabsf(g));
+    }
     for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
     if (lane == 0) delta[i] = s;
   }
+  if (!std::is_same<T, __half>::value) return;
+  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  if (lane == 0 && top > 0.f) atomicMax(reinterpret_cast<int*>(largest), __float_as_int(top));      // above 0: ordered as integers
+}
+
+// In fp16, the largest |dO| of the call before gives way.
+__global__ void reset_kernel(const Work work, float* largest) {
+  pdl_wait();
+  pdl_trigger();
+  if (work_count(work, 1, nullptr) != 0) *largest = 0.f;
 }
 
 // P and dS = P (dP - delta) of a tile, from its scaled products z (times log2 e) and dP; 0 where a key is not seen.
@@ -466,10 +484,14 @@ int run(Ctx* ctx, const Args& a, int list) {
 
 template <typename T>
 int delta(Ctx* ctx, const Args& a) {
+  if (a.dtype == ZOACT_DT_FP16) {
+    ZOACT_CUDA_TRY(launch_pdl(ctx, reset_kernel, dim3(1), dim3(1), 0, work_of(a, LIST_DQ), a.largest));
+    ++ctx->n_launch;
+  }
   const int64_t blocks = (a.s.rows_q * a.s.heads + THREADS / 32 - 1) / (THREADS / 32), most = (int64_t)ctx->sm_count * 64;
   ZOACT_CUDA_TRY(launch_pdl(ctx, delta_kernel<T>, dim3((unsigned)(blocks < most ? blocks : most)), dim3(THREADS), 0,
                             work_of(a, LIST_DQ), ctx->d_status, (const T*)a.dO,
-                            a.ld_do, (const T*)a.O, a.ld_o, a.s.rows_q, a.s.heads, a.s.head_dim, a.delta));
+                            a.ld_do, (const T*)a.O, a.ld_o, a.s.rows_q, a.s.heads, a.s.head_dim, a.delta, a.largest));
   ++ctx->n_launch;
   return ZOACT_OK;
 }
