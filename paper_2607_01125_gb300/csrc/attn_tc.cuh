@@ -120,9 +120,108 @@ template <bool BF16> __device__ __forceinline__ uint32_t pack2(float a, float b)
   }
 }
 
+// Pairs of fp32 in one instruction, each half rounded as by itself.
+__device__ __forceinline__ uint64_t pair(float a, float b) { return (uint64_t)__float_as_uint(b) << 32 | __float_as_uint(a); }
+__device__ __forceinline__ uint64_t pair_bits(uint32_t a, uint32_t b) { return (uint64_t)b << 32 | a; }
+__device__ __forceinline__ float lo(uint64_t x) { return __uint_as_float((uint32_t)x); }
+__device__ __forceinline__ float hi(uint64_t x) { return __uint_as_float((uint32_t)(x >> 32)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+
+// Slots of shared memory in the order in which they are filled next, as the producer and the issuer both count them.  A unit's own
+// tiles (those that stay for all of its steps) take slots off the front and give them back behind its last load; its other
+// loads go round the slots in between.  So the next unit's tiles arrive while this one's last steps run.
+struct Ring {
+  uint64_t order;                         // slot numbers, 4 bits each, the next one lowest
+  uint32_t phase = 0;                     // bit s: parity of slot s's next filling
+  int len;
+  __device__ explicit Ring(int n) : order(0xba9876543210ull), len(n) {}
+  __device__ __forceinline__ uint32_t at(int i) const { return (uint32_t)(order >> (4 * i)) & 15u; }
+  __device__ __forceinline__ uint32_t parity(uint32_t s) const { return phase >> s & 1u; }
+  // The next slot and the parity of its filling.
+  __device__ __forceinline__ uint32_t take(uint32_t& par) {
+    const uint32_t s = at(0);
+    par = parity(s);
+    phase ^= 1u << s;
+    order >>= 4;
+    --len;
+    return s;
+  }
+  __device__ __forceinline__ void give(uint32_t s) {
+    order = (order & ((1ull << (4 * len)) - 1)) | (uint64_t)s << (4 * len);
+    ++len;
+  }
+  // n slots taken and given back, one after another.
+  __device__ __forceinline__ void pass(int n) {
+    const int rounds = n / len, rest = n - rounds * len;
+    for (int i = 0; i < len; ++i)
+      if ((rounds + (i < rest ? 1 : 0)) & 1) phase ^= 1u << at(i);
+    const uint64_t all = (1ull << (4 * len)) - 1, o = order & all;
+    order = (o >> (4 * rest) | o << (4 * (len - rest))) & all;
+  }
+};
+// A place among a unit's loads, moved on by less than a round at a time.
+struct Cursor {
+  int i;
+  uint32_t wrapped = 0;
+  __device__ __forceinline__ void move(int n, int len) {
+    i += n;
+    if (i >= len) { i -= len; wrapped ^= 1u; }
+  }
+};
+
+// The units of a list that a CTA runs, with the next one's item on its way.
+struct Units {
+  const Work* work;
+  int total, kv_heads, round = 0, u, next_u = -1;
+  Item w, next_w;
+  __device__ __forceinline__ Units(const Work& wk, int n, int heads);
+  __device__ __forceinline__ int unit(int r) const {
+    const int x = unit_of(r, (int)blockIdx.x, (int)gridDim.x);
+    return (int64_t)r * gridDim.x < total && x < total ? x : -1;
+  }
+  __device__ __forceinline__ bool here() const { return u >= 0; }
+  __device__ __forceinline__ int head() const { return u % kv_heads; }
+  __device__ __forceinline__ void next() {
+    u = next_u;
+    w = next_w;
+    ++round;
+    fetch();
+  }
+  __device__ __forceinline__ void fetch();
+};
+
 __device__ __forceinline__ Item load_item(const Item* p) {
   const int4 a = reinterpret_cast<const int4*>(p)[0], b = reinterpret_cast<const int4*>(p)[1];
   return {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+}
+
+__device__ __forceinline__ void Units::fetch() {
+  next_u = u >= 0 ? unit(round + 1) : -1;
+  if (next_u >= 0) next_w = load_item(work->items + next_u / kv_heads);
+}
+__device__ __forceinline__ Units::Units(const Work& wk, int n, int heads) : work(&wk), total(n), kv_heads(heads) {
+  u = unit(0);
+  if (u >= 0) w = load_item(work->items + u / kv_heads);
+  fetch();
 }
 
 // Zero rows [from, to) of a tile of `boxes` boxes, by one warp, before the tensor core reads them.

@@ -25,15 +25,15 @@ namespace {
 
 using namespace tcx;
 
-constexpr int THREADS = 384, REGS_FEW = 56, REGS_ROWS = 224;      // 3 x 168 as launched
+constexpr int THREADS = 384, REGS_FEW = 88, REGS_ROWS = 208;      // 3 x 168 as launched
 static_assert(REGS_FEW + 2 * REGS_ROWS <= 3 * 168, "registers");
 constexpr int TMEM_COLS = 512;
 constexpr float RAISE = 8.f;
 
 template <int DP> struct Cfg {
   static constexpr int BOXES = DP / 64, TILE_BYTES = BOXES * BOX;
-  static constexpr int STAGES = DP == 128 ? 5 : 10;
-  static constexpr int SMEM = 1024 + (2 + STAGES) * TILE_BYTES;
+  static constexpr int SLOTS = DP == 128 ? 7 : 12;
+  static constexpr int SMEM = 1024 + SLOTS * TILE_BYTES;
 };
 static_assert(Cfg<128>::SMEM + 1024 <= 232448 && Cfg<64>::SMEM + 1024 <= 232448, "shared memory");
 
@@ -54,7 +54,7 @@ struct Params {
 struct Maps { CUtensorMap q, k, v; };
 
 struct Shared {
-  uint64_t q_full[2], q_empty[2], full[10], empty[10], s_full[2], p_full[2], pv_done[2], merge_full, merge_empty;
+  uint64_t full[12], empty[12], s_full[2], p_full[2], pv_done[2], merge_full, merge_empty;
   uint64_t join_in[2], join_out[2], drain;
   uint32_t tmem_base;
   int abort_flag, last[2];
@@ -84,10 +84,9 @@ struct Tiles {
       n1 = (visible(w, p.causal, w.npos - 1) + BK - 1) / BK;
     }
   }
-  // Loads in order: K, V of each step (halves: K of both tiles, V of both); position of a tile's step j among them.
+  // Loads in order: K, V of each step, of each tile in turn where they have blocks of their own.
+  __device__ __forceinline__ int own() const { return blocks == 0 ? 0 : halves ? 1 : 2; }
   __device__ __forceinline__ int loads() const { return halves ? 2 * blocks : 2 * n1; }
-  __device__ __forceinline__ int at_k(int t, int j) const { return !halves ? 2 * j : j < n1 ? 4 * j + t : 4 * j; }
-  __device__ __forceinline__ int at_v(int t, int j) const { return !halves ? 2 * j + 1 : j < n1 ? 4 * j + 2 + t : 4 * j + 1; }
   __device__ __forceinline__ int block(int t, int j) const { return halves && t ? n0 + j : j; }
 };
 
@@ -95,28 +94,26 @@ struct Tiles {
 __device__ __forceinline__ int keys_in(const Item& w, int block) { return min(BK, w.nk - block * BK); }
 
 template <int DP, bool BF16>
-__global__ void __launch_bounds__(THREADS, 1) fwd_tc_kernel(const __grid_constant__ Maps tm, const Params p) {
+__global__ void __launch_bounds__(THREADS, 1) fwd_tc_kernel(const __grid_constant__ Maps tm, const __grid_constant__ Params p) {
   using G = Cfg<DP>;
-  constexpr int STAGES = G::STAGES;
+  constexpr int SLOTS = G::SLOTS;
   extern __shared__ uint8_t smem_raw[];
   __shared__ Shared sh;
   const uint32_t smem = (tc::smem_u32(smem_raw) + 1023u) & ~1023u;
-  const uint32_t q_tile = smem, ring = smem + 2 * G::TILE_BYTES;
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   volatile int* abort_flag = &sh.abort_flag;
   const auto bar = [](const uint64_t& b) { return tc::smem_u32(&b); };
+  const auto slot = [&](uint32_t s) { return smem + s * (uint32_t)G::TILE_BYTES; };
 
   if (threadIdx.x == 0) {
     for (int t = 0; t < 2; ++t) {
-      tc::mbar_init(bar(sh.q_full[t]), 1);
-      tc::mbar_init(bar(sh.q_empty[t]), 1);
       tc::mbar_init(bar(sh.s_full[t]), 1);
       tc::mbar_init(bar(sh.p_full[t]), 4);
       tc::mbar_init(bar(sh.pv_done[t]), 1);
       tc::mbar_init(bar(sh.join_in[t]), 4);
       tc::mbar_init(bar(sh.join_out[t]), 1);
     }
-    for (int s = 0; s < STAGES; ++s) {
+    for (int s = 0; s < SLOTS; ++s) {
       tc::mbar_init(bar(sh.full[s]), 1);
       tc::mbar_init(bar(sh.empty[s]), 1);
     }
@@ -141,56 +138,47 @@ __global__ void __launch_bounds__(THREADS, 1) fwd_tc_kernel(const __grid_constan
   pdl_trigger();
 
   const int total = work_count(p.work, p.kv_heads, threadIdx.x == 0 && blockIdx.x == 0 ? p.status : nullptr);
-  const auto item_of = [&](int u) { return load_item(p.work.items + u / p.kv_heads); };
-  const int G0 = gridDim.x;
 
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_FEW));
     if (warp == 0) {
       // ---------------- TMA producer ----------------
-      uint32_t base = 0, q_count[2] = {0, 0};
+      Ring ring(SLOTS);
       bool ok = true;
       const uint32_t q_bytes = (uint32_t)(G::BOXES * p.positions * p.rep * 128);
-      for (int r = 0; ok && (int64_t)r * G0 < total; ++r) {
-        const int u = unit_of(r, blockIdx.x, G0);
-        if (u >= total) continue;
-        const Item w = item_of(u);
-        const int h = u % p.kv_heads;
+      for (Units U(p.work, total, p.kv_heads); ok && U.here(); U.next()) {
+        const Item& w = U.w;
+        const int h = U.head();
         const Tiles T(w, p);
-        for (int t = 0; ok && t < 2; ++t) {
-          if (T.n(t) == 0) continue;
-          ok = warp_wait(bar(sh.q_empty[t]), (q_count[t] & 1) ^ 1u, abort_flag, p.status);
-          if (!ok) break;
-          ++q_count[t];
-          if (elect_one()) {
-            tc::mbar_arrive_expect_tx(bar(sh.q_full[t]), q_bytes);
+        uint32_t par, own[2] = {0, 0};
+        for (int t = 0; ok && t < T.own(); ++t) {
+          const uint32_t s = own[t] = ring.take(par);
+          ok = warp_wait(bar(sh.empty[s]), par ^ 1u, abort_flag, p.status);
+          if (ok && elect_one()) {
+            tc::mbar_arrive_expect_tx(bar(sh.full[s]), q_bytes);
             for (int b = 0; b < G::BOXES; ++b)
-              tma_load_4d(q_tile + (uint32_t)(t * G::TILE_BYTES + b * BOX), &tm.q, b * 64, 0, h, w.q0 + T.pos0(t), bar(sh.q_full[t]));
+              tma_load_4d(slot(s) + (uint32_t)(b * BOX), &tm.q, b * 64, 0, h, w.q0 + T.pos0(t), bar(sh.full[s]));
           }
           __syncwarp();
         }
-        const auto load = [&](const CUtensorMap* map, uint32_t at, int block) {
-          const uint32_t s = at % STAGES;
-          if (!warp_wait(bar(sh.empty[s]), (at / STAGES & 1) ^ 1u, abort_flag, p.status)) return false;
+        const auto load = [&](const CUtensorMap* map, int block) {
+          const uint32_t s = ring.take(par);
+          if (!warp_wait(bar(sh.empty[s]), par ^ 1u, abort_flag, p.status)) return false;
           if (elect_one()) {
             tc::mbar_arrive_expect_tx(bar(sh.full[s]), (uint32_t)G::TILE_BYTES);
             for (int b = 0; b < G::BOXES; ++b)
-              tma_load_3d(ring + s * G::TILE_BYTES + (uint32_t)(b * BOX), map, b * 64, h, w.k0 + block * BK, bar(sh.full[s]));
+              tma_load_3d(slot(s) + (uint32_t)(b * BOX), map, b * 64, h, w.k0 + block * BK, bar(sh.full[s]));
           }
           __syncwarp();
+          ring.give(s);
           return true;
         };
-        if (T.halves) {
-          for (int j = 0; ok && j < T.n(0); ++j) {
-            const bool two = j < T.n(1);
-            ok = load(&tm.k, base + T.at_k(0, j), T.block(0, j)) && (!two || load(&tm.k, base + T.at_k(1, j), T.block(1, j))) &&
-                 load(&tm.v, base + T.at_v(0, j), T.block(0, j)) && (!two || load(&tm.v, base + T.at_v(1, j), T.block(1, j)));
-          }
-        } else {
-          for (int j = 0; ok && j < T.n(1); ++j)
-            ok = load(&tm.k, base + 2 * j, j) && load(&tm.v, base + 2 * j + 1, j);
+        const int steps = T.halves ? T.n0 : T.n1;
+        for (int j = 0; ok && j < steps; ++j) {
+          ok = load(&tm.k, j) && load(&tm.v, j);
+          if (ok && T.halves && j < T.n1) ok = load(&tm.k, T.n0 + j) && load(&tm.v, T.n0 + j);
         }
-        base += T.loads();
+        for (int t = 0; t < T.own(); ++t) ring.give(own[t]);
       }
       if (!ok) {                       // give our copies time to land before the CTA winds down
         const uint64_t t0 = tc::global_timer_ns();
@@ -201,58 +189,78 @@ __global__ void __launch_bounds__(THREADS, 1) fwd_tc_kernel(const __grid_constan
       // ---------------- MMA issuer ----------------
       const int ksteps = (p.head_dim + 15) / 16;
       const uint32_t id_s = tc::idesc_f16(TILE, BK, BF16), id_o = tc::idesc_f16(TILE, ksteps * 16, BF16) | B_BY_ROWS;
-      uint32_t base = 0, q_count[2] = {0, 0}, steps[2] = {0, 0};
+      Ring ring(SLOTS);
+      uint32_t done0 = 0, done1 = 0;               // steps of the tiles so far
       bool ok = true, any = false;
-      for (int r = 0; ok && (int64_t)r * G0 < total; ++r) {
-        const int u = unit_of(r, blockIdx.x, G0);
-        if (u >= total) continue;
-        const Item w = item_of(u);
+      for (Units U(p.work, total, p.kv_heads); ok && U.here(); U.next()) {
+        const Item& w = U.w;
         const Tiles T(w, p);
-        const auto product_s = [&](int t, int j) {
-          const uint32_t at = base + T.at_k(t, j), s = at % STAGES;
-          if (j == 0 && !warp_wait(bar(sh.q_full[t]), q_count[t] & 1, abort_flag, p.status)) return false;
-          if (!warp_wait(bar(sh.full[s]), at / STAGES & 1, abort_flag, p.status)) return false;
+        if (T.blocks == 0) continue;
+        uint32_t par0, par1 = 0;
+        const uint32_t q0 = ring.take(par0), q1 = T.halves ? q0 : ring.take(par1);
+        const int len = ring.len, stride = T.halves ? 4 : 2;
+        Cursor k0 = {0}, k1 = {T.halves ? 2 : 0}, v0 = {1}, v1 = {T.halves ? 3 : 1};
+        const auto product_s = [&](int t, int j, Cursor& c) {
+          const uint32_t s = ring.at(c.i);
+          if (!warp_wait(bar(sh.full[s]), ring.parity(s) ^ c.wrapped, abort_flag, p.status)) return false;
+          c.move(stride, len);
           tc::tc_fence_after();
           if (elect_one()) {
-            mma_cols(tmem + t * BK, q_tile + t * G::TILE_BYTES, ring + s * G::TILE_BYTES, id_s, ksteps);
+            mma_cols(tmem + t * BK, slot(t ? q1 : q0), slot(s), id_s, ksteps);
             tc::mma_commit(bar(sh.s_full[t]));
-            // a block that both tiles read is free after the second one, or the first where the second has none
-            if (T.halves || t == 1 || j >= T.n(1)) tc::mma_commit(bar(sh.empty[s]));
-            if (j == T.n(t) - 1) tc::mma_commit(bar(sh.q_empty[t]));
+            if (T.halves || t == 1) tc::mma_commit(bar(sh.empty[s]));          // else the second tile still reads it
           }
           __syncwarp();
           any = true;
-          if (j == T.n(t) - 1) ++q_count[t];
           return true;
         };
-        const auto product_o = [&](int t, int j) {
-          const uint32_t at = base + T.at_v(t, j), s = at % STAGES;
-          if (!warp_wait(bar(sh.p_full[t]), steps[t] & 1, abort_flag, p.status)) return false;
-          ++steps[t];
-          if (!warp_wait(bar(sh.full[s]), at / STAGES & 1, abort_flag, p.status)) return false;
+        const auto product_o = [&](int t, int j, Cursor& c, uint32_t& done) {
+          if (!warp_wait(bar(sh.p_full[t]), done & 1, abort_flag, p.status)) return false;
+          ++done;
+          const uint32_t s = ring.at(c.i);
+          if (!warp_wait(bar(sh.full[s]), ring.parity(s) ^ c.wrapped, abort_flag, p.status)) return false;
+          c.move(stride, len);
           const int block = T.block(t, j), keys = keys_in(w, block);
           // (a tile may end before the block does: its shares are 0 there)
           const int mine = min(keys, T.halves ? BK : visible(w, p.causal, T.pos0(t) + T.npos(t) - 1) - block * BK);
-          if (keys % 16 != 0 && (T.halves || t == 0 || j >= T.n(0)))     // once, before the first product by these rows
-            zero_rows(ring + s * G::TILE_BYTES, G::BOXES, keys, (keys + 15) / 16 * 16, lane);
+          if (keys % 16 != 0 && (T.halves || t == 0 || j >= T.n0))     // once, before the first product by these rows
+            zero_rows(slot(s), G::BOXES, keys, (keys + 15) / 16 * 16, lane);
           tc::tc_fence_after();
           if (elect_one()) {
-            mma_rows(tmem + (2 + t) * BK, tmem + t * BK, ring + s * G::TILE_BYTES, id_o, (mine + 15) / 16, j != 0);
+            mma_rows(tmem + (2 + t) * BK, tmem + t * BK, slot(s), id_o, (mine + 15) / 16, j != 0);
             tc::mma_commit(bar(sh.pv_done[t]));
-            if (T.halves || t == 1 || j >= T.n(1)) tc::mma_commit(bar(sh.empty[s]));
+            if (T.halves || t == 1) tc::mma_commit(bar(sh.empty[s]));
           }
           __syncwarp();
           return true;
         };
-        for (int t = 0; ok && t < 2; ++t)
-          if (T.n(t) > 0) ok = product_s(t, 0);
-        const int most = max(T.n(0), T.n(1));
-        for (int j = 0; ok && j < most; ++j)
-          for (int t = 0; ok && t < 2; ++t) {
-            if (j < T.n(t)) ok = product_o(t, j);
-            if (ok && j + 1 < T.n(t)) ok = product_s(t, j + 1);
+        // the own tiles are free once the last product by them is done
+        const auto free_own = [&](uint32_t s) {
+          if (elect_one()) tc::mma_commit(bar(sh.empty[s]));
+          __syncwarp();
+        };
+        ok = warp_wait(bar(sh.full[q0]), par0, abort_flag, p.status) &&
+             (T.halves || warp_wait(bar(sh.full[q1]), par1, abort_flag, p.status));
+        if (ok && T.n0 > 0) ok = product_s(0, 0, k0);
+        if (ok && T.n1 > 0) ok = product_s(1, 0, k1);
+        const int most = max(T.n0, T.n1);
+        if (ok && most == 1) {
+          free_own(q0);
+          if (!T.halves) free_own(q1);
+        }
+        for (int j = 0; ok && j < most; ++j) {
+          if (j < T.n0) ok = product_o(0, j, v0, done0);
+          if (ok && j + 1 < T.n0) ok = product_s(0, j + 1, k0);
+          if (ok && j < T.n1) ok = product_o(1, j, v1, done1);
+          if (ok && j + 1 < T.n1) ok = product_s(1, j + 1, k1);
+          if (ok && j + 2 == most) {
+            free_own(q0);
+            if (!T.halves) free_own(q1);
           }
-        base += T.loads();
+        }
+        ring.pass(T.loads());
+        ring.give(q0);
+        if (!T.halves) ring.give(q1);
       }
       if (any) {
         if (elect_one()) tc::mma_commit(bar(sh.drain));
@@ -266,17 +274,16 @@ __global__ void __launch_bounds__(THREADS, 1) fwd_tc_kernel(const __grid_constan
     const int t = (warp - 4) >> 2, quad = warp & 3, row = quad * 32 + lane;
     const uint32_t lanes = (uint32_t)(quad * 32) << 16;
     const uint32_t ts = tmem + lanes + (uint32_t)(t * BK), to = tmem + lanes + (uint32_t)((2 + t) * BK);
-    const int D = p.head_dim;
+    const int D = p.head_dim, pos = row / p.rep;
+    const uint64_t scale2 = pair(p.scale_log2, p.scale_log2);
     constexpr float SHIFT = BF16 ? 0.f : 7.f;
     uint32_t steps = 0, merges = 0, joins = 0;
     bool ok = true;
-    for (int r = 0; ok && (int64_t)r * G0 < total; ++r) {
-      const int u = unit_of(r, blockIdx.x, G0);
-      if (u >= total) continue;
-      const Item w = item_of(u);
-      const int h = u % p.kv_heads;
+    for (Units U(p.work, total, p.kv_heads); ok && U.here(); U.next()) {
+      const Item& w = U.w;
+      const int h = U.head();
       const Tiles T(w, p);
-      const int pos = row / p.rep, rows = T.npos(t) * p.rep;
+      const int rows = T.npos(t) * p.rep;
       const bool active = quad * 32 < rows, valid = row < rows;
       const int ipos = T.pos0(t) + pos;                                   // in the item
       const int see = valid ? visible(w, p.causal, ipos) : 0, all_see = visible(w, p.causal, T.pos0(t));
@@ -304,9 +311,9 @@ __global__ void __launch_bounds__(THREADS, 1) fwd_tc_kernel(const __grid_constan
           }
           float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-          for (int i = 0; i < 32; ++i)
+          for (int i = 0; i < 32; i += 2)
 #pragma unroll
-            for (int c = 0; c < 4; ++c) mx[c] = fmaxf(mx[c], __uint_as_float(x[c][i]));
+            for (int c = 0; c < 4; ++c) mx[c] = max3(mx[c], __uint_as_float(x[c][i]), __uint_as_float(x[c][i + 1]));
           const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * p.scale_log2;
           if (__any_sync(0xffffffffu, top > m + RAISE || (m == -INFINITY && top > m))) {
             const float now = fmaxf(m, top);
@@ -331,7 +338,8 @@ __global__ void __launch_bounds__(THREADS, 1) fwd_tc_kernel(const __grid_constan
             m = now;
           }
           const float from = (m == -INFINITY ? 0.f : m) - SHIFT;
-          float s[4] = {0.f, 0.f, 0.f, 0.f};
+          const uint64_t from2 = pair(-from, -from);
+          uint64_t s[4] = {0, 0, 0, 0};
 #pragma unroll
           for (int c = 0; c < 4; c += 2) {
             uint32_t y[32];
@@ -339,15 +347,15 @@ __global__ void __launch_bounds__(THREADS, 1) fwd_tc_kernel(const __grid_constan
             for (int k = 0; k < 2; ++k)
 #pragma unroll
               for (int i = 0; i < 32; i += 2) {
-                const float a = ex2(fmaf(__uint_as_float(x[c + k][i]), p.scale_log2, -from));
-                const float b = ex2(fmaf(__uint_as_float(x[c + k][i + 1]), p.scale_log2, -from));
-                s[2 * k] += a;
-                s[2 * k + 1] += b;
+                const uint64_t z = fma2(pair_bits(x[c + k][i], x[c + k][i + 1]), scale2, from2);
+                const float a = ex2(lo(z)), b = ex2(hi(z));
+                s[i / 2 & 3] = add2(s[i / 2 & 3], pair(a, b));
                 y[k * 16 + i / 2] = pack2<BF16>(a, b);
               }
             st32(ts + c * 16, y);
           }
-          l += (s[0] + s[1]) + (s[2] + s[3]);
+          const uint64_t sum2 = add2(add2(s[0], s[1]), add2(s[2], s[3]));
+          l += lo(sum2) + hi(sum2);
           tc::tmem_wait_st();
           tc::tc_fence_before();
         }
@@ -489,13 +497,14 @@ __global__ void __launch_bounds__(THREADS, 1) fwd_tc_kernel(const __grid_constan
         ++joins;
         if (*(volatile int*)&sh.last[t]) {
           __threadfence();
-          join_rows(p.slots, first_slot, w.nparts, row0, rows, D, row, TILE,
-                    [&](int r, int d, float x) {
-                      static_cast<uint16_t*>(p.O)[out_at(r, d)] = (uint16_t)pack2<BF16>(x, 0.f);
-                    },
-                    [&](int r, float top, float s) {
-                      if (p.lse) p.lse[stat_at(r)] = s == 0.f ? -INFINITY : (top + log2f(s)) * 0.69314718f;
-                    });
+          join_rows4(p.slots, first_slot, w.nparts, row0, rows, D, row, TILE,
+                     [&](int r, int d, float4 x) {
+                       *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.O) + out_at(r, d)) =
+                           make_uint2(pack2<BF16>(x.x, x.y), pack2<BF16>(x.z, x.w));
+                     },
+                     [&](int r, float top, float s) {
+                       if (p.lse) p.lse[stat_at(r)] = s == 0.f ? -INFINITY : (top + log2f(s)) * 0.69314718f;
+                     });
         }
       }
     }

@@ -24,13 +24,13 @@ namespace {
 
 using namespace tcx;
 
-constexpr int THREADS = 384, REGS_FEW = 56, REGS_ROWS = 224;      // 3 x 168 as launched
+constexpr int THREADS = 384, REGS_FEW = 104, REGS_ROWS = 200;      // 3 x 168 as launched
 constexpr int TMEM_COLS = 512;
 
 template <int DP> struct Cfg {
   static constexpr int BOXES = DP / 64, TILE_BYTES = BOXES * BOX;
-  static constexpr int STAGES = DP == 128 ? 5 : 10;
-  static constexpr int TILES = (2 + STAGES) * TILE_BYTES;
+  static constexpr int SLOTS = DP == 128 ? 7 : 12;
+  static constexpr int TILES = SLOTS * TILE_BYTES;
   static constexpr int HALF = DP / 2;                             // columns of the results of a warpgroup
 };
 
@@ -49,7 +49,7 @@ struct Params {
 struct Maps { CUtensorMap q, g, k, v; };
 
 struct Shared {
-  uint64_t own_full, own_empty, full[10], empty[10], s_full[2], p_full, dp_full, ds_full, acc_full, stat_full[2], stat_empty[2];
+  uint64_t full[12], empty[12], s_full[2], p_full, dp_full, ds_full, acc_full, stat_full[2], stat_empty[2];
   uint64_t join_in, join_out, drain;
   uint32_t tmem_base;
   int abort_flag, last;
@@ -85,13 +85,11 @@ __device__ __forceinline__ void mma_rows_halves(uint32_t d, uint32_t a_tmem, uin
 }
 
 // The barriers, and each row's position.
-template <int STAGES>
+template <int SLOTS>
 __device__ __forceinline__ void init_shared(Shared* sh, int rep) {
   const auto bar = [](const uint64_t& b) { return tc::smem_u32(&b); };
   if (threadIdx.x == 0) {
-    tc::mbar_init(bar(sh->own_full), 1);
-    tc::mbar_init(bar(sh->own_empty), 1);
-    for (int s = 0; s < STAGES; ++s) {
+    for (int s = 0; s < SLOTS; ++s) {
       tc::mbar_init(bar(sh->full[s]), 1);
       tc::mbar_init(bar(sh->empty[s]), 1);
     }
@@ -155,20 +153,20 @@ __device__ __forceinline__ void put_part(float* d, const float* v, int n) {
 }
 
 template <int DP, bool BF16>
-__global__ void __launch_bounds__(THREADS, 1) dq_tc_kernel(const __grid_constant__ Maps tm, const Params p) {
+__global__ void __launch_bounds__(THREADS, 1) dq_tc_kernel(const __grid_constant__ Maps tm, const __grid_constant__ Params p) {
   using G = Cfg<DP>;
-  constexpr int STAGES = G::STAGES;
+  constexpr int SLOTS = G::SLOTS;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   Shared* sh = reinterpret_cast<Shared*>(smem_raw + G::TILES);
-  const uint32_t q_tile = tc::smem_u32(smem_raw), g_tile = q_tile + G::TILE_BYTES, ring = q_tile + 2 * G::TILE_BYTES;
+  const uint32_t smem = tc::smem_u32(smem_raw);
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
-  if (q_tile & 1023u) {                  // (swizzled tiles: dynamic shared memory begins there, as nothing static lies before it)
+  if (smem & 1023u) {                  // (swizzled tiles: dynamic shared memory begins there, as nothing static lies before it)
     if (threadIdx.x == 0 && blockIdx.x == 0) record_error(p.status, ZOACT_ERR_UNSUPPORTED);
     return;
   }
   volatile int* abort_flag = &sh->abort_flag;
   const auto bar = [](const uint64_t& b) { return tc::smem_u32(&b); };
-  init_shared<STAGES>(sh, p.rep);
+  init_shared<SLOTS>(sh, p.rep);
   if (threadIdx.x == 32) {
     tc::prefetch_tmap(&tm.q);
     tc::prefetch_tmap(&tm.g);
@@ -189,46 +187,45 @@ __global__ void __launch_bounds__(THREADS, 1) dq_tc_kernel(const __grid_constant
   pdl_trigger();
 
   const int total = work_count(p.work, p.kv_heads, threadIdx.x == 0 && blockIdx.x == 0 ? p.status : nullptr);
-  const auto item_of = [&](int u) { return load_item(p.work.items + u / p.kv_heads); };
-  const int G0 = gridDim.x;
+  const auto slot = [&](uint32_t s) { return smem + s * (uint32_t)G::TILE_BYTES; };
   const int ksteps = (p.head_dim + 15) / 16;
 
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_FEW));
     if (warp == 0) {
       // ---------------- TMA producer ----------------
-      uint32_t at = 0, units = 0;
+      Ring ring(SLOTS);
       bool ok = true;
       const uint32_t row_bytes = (uint32_t)(G::BOXES * p.positions * p.rep * 128);
-      for (int r = 0; ok && (int64_t)r * G0 < total; ++r) {
-        const int u = unit_of(r, blockIdx.x, G0);
-        if (u >= total) continue;
-        const Item w = item_of(u);
-        const int h = u % p.kv_heads, n = (w.nk + BK - 1) / BK;
+      for (Units U(p.work, total, p.kv_heads); ok && U.here(); U.next()) {
+        const Item& w = U.w;
+        const int h = U.head(), n = (w.nk + BK - 1) / BK;
         if (n == 0) continue;
-        ok = warp_wait(bar(sh->own_empty), (units & 1) ^ 1u, abort_flag, p.status);
-        if (!ok) break;
-        ++units;
-        if (elect_one()) {
-          tc::mbar_arrive_expect_tx(bar(sh->own_full), 2 * row_bytes);
-          for (int b = 0; b < G::BOXES; ++b) {
-            tma_load_4d(q_tile + (uint32_t)(b * BOX), &tm.q, b * 64, 0, h, w.q0, bar(sh->own_full));
-            tma_load_4d(g_tile + (uint32_t)(b * BOX), &tm.g, b * 64, 0, h, w.q0, bar(sh->own_full));
-          }
-        }
-        __syncwarp();
-        for (int j = 0; ok && j < 2 * n; ++j, ++at) {
-          const uint32_t s = at % STAGES;
-          ok = warp_wait(bar(sh->empty[s]), (at / STAGES & 1) ^ 1u, abort_flag, p.status);
-          if (!ok) break;
-          if (elect_one()) {
-            const CUtensorMap* map = j & 1 ? &tm.v : &tm.k;
-            tc::mbar_arrive_expect_tx(bar(sh->full[s]), (uint32_t)G::TILE_BYTES);
+        uint32_t par, own[2] = {0, 0};
+        for (int t = 0; ok && t < 2; ++t) {
+          const uint32_t s = own[t] = ring.take(par);
+          ok = warp_wait(bar(sh->empty[s]), par ^ 1u, abort_flag, p.status);
+          if (ok && elect_one()) {
+            tc::mbar_arrive_expect_tx(bar(sh->full[s]), row_bytes);
             for (int b = 0; b < G::BOXES; ++b)
-              tma_load_3d(ring + s * G::TILE_BYTES + (uint32_t)(b * BOX), map, b * 64, h, w.k0 + j / 2 * BK, bar(sh->full[s]));
+              tma_load_4d(slot(s) + (uint32_t)(b * BOX), t ? &tm.g : &tm.q, b * 64, 0, h, w.q0, bar(sh->full[s]));
           }
           __syncwarp();
         }
+        for (int j = 0; ok && j < 2 * n; ++j) {
+          const uint32_t s = ring.take(par);
+          ok = warp_wait(bar(sh->empty[s]), par ^ 1u, abort_flag, p.status);
+          if (!ok) break;
+          if (elect_one()) {
+            tc::mbar_arrive_expect_tx(bar(sh->full[s]), (uint32_t)G::TILE_BYTES);
+            for (int b = 0; b < G::BOXES; ++b)
+              tma_load_3d(slot(s) + (uint32_t)(b * BOX), j & 1 ? &tm.v : &tm.k, b * 64, h, w.k0 + j / 2 * BK, bar(sh->full[s]));
+          }
+          __syncwarp();
+          ring.give(s);
+        }
+        ring.give(own[0]);
+        ring.give(own[1]);
       }
       if (!ok) {                       // give our copies time to land before the CTA winds down
         const uint64_t t0 = tc::global_timer_ns();
@@ -238,60 +235,69 @@ __global__ void __launch_bounds__(THREADS, 1) dq_tc_kernel(const __grid_constant
     } else if (warp == 1) {
       // ---------------- MMA issuer ----------------
       const uint32_t id_s = tc::idesc_f16(TILE, BK, BF16), id_q = tc::idesc_f16(TILE, ksteps * 16, BF16) | B_BY_ROWS;
-      uint32_t base = 0, step = 0, units = 0;
+      Ring ring(SLOTS);
+      uint32_t step = 0;
       bool ok = true, any = false;
-      for (int r = 0; ok && (int64_t)r * G0 < total; ++r) {
-        const int u = unit_of(r, blockIdx.x, G0);
-        if (u >= total) continue;
-        const Item w = item_of(u);
+      for (Units U(p.work, total, p.kv_heads); ok && U.here(); U.next()) {
+        const Item& w = U.w;
         const int n = (w.nk + BK - 1) / BK;
         if (n == 0) continue;
-        const auto tile = [&](uint32_t at) { return ring + at % STAGES * G::TILE_BYTES; };
+        uint32_t par_q, par_g;
+        const uint32_t q_slot = ring.take(par_q), g_slot = ring.take(par_g);
+        const int len = ring.len;
+        Cursor ks = {0}, kq = {0}, vs = {1};         // K for S and for dq, V
         const auto product_s = [&](int j) {
-          const uint32_t at = base + 2 * j;
-          if (!warp_wait(bar(sh->full[at % STAGES]), at / STAGES & 1, abort_flag, p.status)) return false;
+          const uint32_t s = ring.at(ks.i);
+          if (!warp_wait(bar(sh->full[s]), ring.parity(s) ^ ks.wrapped, abort_flag, p.status)) return false;
+          ks.move(2, len);
           const int keys = min(BK, w.nk - j * BK);
-          if (keys % 16 != 0) zero_rows(tile(at), G::BOXES, keys, (keys + 15) / 16 * 16, lane);
+          if (keys % 16 != 0) zero_rows(slot(s), G::BOXES, keys, (keys + 15) / 16 * 16, lane);
           tc::tc_fence_after();
           if (elect_one()) {
-            mma_cols(t_s + ((step + j) & 1) * BK, q_tile, tile(at), id_s, ksteps);
+            mma_cols(t_s + ((step + j) & 1) * BK, slot(q_slot), slot(s), id_s, ksteps);
             tc::mma_commit(bar(sh->s_full[(step + j) & 1]));
+            if (j == n - 1) tc::mma_commit(bar(sh->empty[q_slot]));
           }
           __syncwarp();
           any = true;
           return true;
         };
         const auto product_dp = [&](int j) {
-          const uint32_t at = base + 2 * j + 1;
-          if (!warp_wait(bar(sh->full[at % STAGES]), at / STAGES & 1, abort_flag, p.status)) return false;
+          const uint32_t s = ring.at(vs.i);
+          if (!warp_wait(bar(sh->full[s]), ring.parity(s) ^ vs.wrapped, abort_flag, p.status)) return false;
+          vs.move(2, len);
           tc::tc_fence_after();
           if (elect_one()) {
-            mma_cols(t_dp, g_tile, tile(at), id_s, ksteps);
+            mma_cols(t_dp, slot(g_slot), slot(s), id_s, ksteps);
             tc::mma_commit(bar(sh->dp_full));
-            tc::mma_commit(bar(sh->empty[at % STAGES]));
-            if (j == n - 1) tc::mma_commit(bar(sh->own_empty));
+            tc::mma_commit(bar(sh->empty[s]));
+            if (j == n - 1) tc::mma_commit(bar(sh->empty[g_slot]));
           }
           __syncwarp();
           return true;
         };
-        ok = warp_wait(bar(sh->own_full), units & 1, abort_flag, p.status) && product_s(0) && product_dp(0) && (n < 2 || product_s(1));
-        ++units;
+        ok = warp_wait(bar(sh->full[q_slot]), par_q, abort_flag, p.status) && product_s(0) &&
+             warp_wait(bar(sh->full[g_slot]), par_g, abort_flag, p.status) && product_dp(0) && (n < 2 || product_s(1));
         for (int j = 0; ok && j < n; ++j) {
           ok = warp_wait(bar(sh->ds_full), (step + j) & 1, abort_flag, p.status);
           if (!ok) break;
           if (j + 1 < n) ok = product_dp(j + 1);
           if (!ok) break;
           tc::tc_fence_after();
+          const uint32_t s = ring.at(kq.i);
+          kq.move(2, len);
           if (elect_one()) {
             const int keys = min(BK, w.nk - j * BK);
-            mma_rows_halves(t_dq, t_s + ((step + j) & 1) * BK, tile(base + 2 * j), id_q, (keys + 15) / 16, j != 0);
-            tc::mma_commit(bar(sh->empty[(base + 2 * j) % STAGES]));
+            mma_rows_halves(t_dq, t_s + ((step + j) & 1) * BK, slot(s), id_q, (keys + 15) / 16, j != 0);
+            tc::mma_commit(bar(sh->empty[s]));
             if (j == n - 1) tc::mma_commit(bar(sh->acc_full));
           }
           __syncwarp();
           if (j + 2 < n) ok = product_s(j + 2);
         }
-        base += 2 * n;
+        ring.pass(2 * n);
+        ring.give(q_slot);
+        ring.give(g_slot);
         step += n;
       }
       if (any) {
@@ -307,45 +313,74 @@ __global__ void __launch_bounds__(THREADS, 1) dq_tc_kernel(const __grid_constant
     const uint32_t lanes = (uint32_t)(quad * 32) << 16;
     const int D = p.head_dim, pos = row / p.rep, in_group = row - pos * p.rep;
     const Factors<BF16> f(p.largest, false);
+    const uint64_t scale2 = pair(p.scale_log2, p.scale_log2), ds2 = pair(f.ds, f.ds);
     uint32_t step = 0, units = 0, joins = 0;
     bool ok = true;
-    for (int r = 0; ok && (int64_t)r * G0 < total; ++r) {
-      const int u = unit_of(r, blockIdx.x, G0);
-      if (u >= total) continue;
-      const Item w = item_of(u);
-      const int h = u % p.kv_heads, n = (w.nk + BK - 1) / BK, rows = w.npos * p.rep;
+    // of this thread's row of an item: log-sum-exp (times log2 e) and delta
+    const auto stat_of = [&](const Item& w, int h, float& lse2, float& delta) {
+      lse2 = delta = 0.f;
+      if (row >= w.npos * p.rep) return;
+      const int64_t e = (int64_t)(w.q0 + pos) * p.heads + h * p.rep + in_group;
+      lse2 = p.lse[e];
+      delta = p.delta[e];
+    };
+    Units U(p.work, total, p.kv_heads);
+    float lse_next = 0.f, delta_next = 0.f;
+    if (U.here()) stat_of(U.w, U.head(), lse_next, delta_next);
+    for (; ok && U.here(); U.next()) {
+      const Item& w = U.w;
+      const int h = U.head(), n = (w.nk + BK - 1) / BK, rows = w.npos * p.rep;
       const bool active = quad * 32 < rows, valid = row < rows;
       const int see = valid ? visible(w, p.causal, pos) : 0, all_see = visible(w, p.causal, 0);
-      const int64_t e = (int64_t)(w.q0 + pos) * p.heads + h * p.rep + in_group;
-      const float lse2 = valid ? p.lse[e] * 1.44269504f : 0.f, delta = valid ? p.delta[e] : 0.f;
+      const float lse2 = lse_next * 1.44269504f;
+      const uint64_t lse22 = pair(-lse2, -lse2), delta2 = pair(-delta_next, -delta_next);
       for (int j = 0; j < n; ++j, ++step) {
-        ok = warp_wait(bar(sh->s_full[step & 1]), step >> 1 & 1, abort_flag, p.status) &&
-             warp_wait(bar(sh->dp_full), step & 1, abort_flag, p.status);
+        ok = warp_wait(bar(sh->s_full[step & 1]), step >> 1 & 1, abort_flag, p.status);
+        if (!ok) break;
+        const uint32_t s0 = t_s + (step & 1) * BK + lanes + half * 64, d0 = t_dp + lanes + half * 64;
+        const int lim = see - j * BK - half * 64;                         // columns of this half that are seen
+        const bool masked = all_see < (j + 1) * BK;
+        uint64_t pr[32];
+        if (active) {
+          // P while the tensor core has this step's dP
+          tc::tc_fence_after();
+          uint32_t x[2][32];
+          ld32(s0, x[0]);
+          ld32(s0 + 32, x[1]);
+          ld_wait();
+          ld_use(x[0]);
+          ld_use(x[1]);
+#pragma unroll
+          for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int i = 0; i < 32; i += 2) {
+              const uint64_t z = fma2(pair_bits(x[c][i], x[c][i + 1]), scale2, lse22);
+              pr[c * 16 + i / 2] = pair(ex2(lo(z)), ex2(hi(z)));
+            }
+        }
+        ok = warp_wait(bar(sh->dp_full), step & 1, abort_flag, p.status);
         if (!ok) break;
         if (active) {
           tc::tc_fence_after();
-          const uint32_t s0 = t_s + (step & 1) * BK + lanes + half * 64, d0 = t_dp + lanes + half * 64;
-          const bool masked = all_see < (j + 1) * BK;
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
-            uint32_t x[32], d[32];
-            ld32(s0 + c * 32, x);
+            uint32_t d[32], y[16];
             ld32(d0 + c * 32, d);
             ld_wait();
-            ld_use(x);
             ld_use(d);
-            uint32_t y[16];
-            const int lim = masked ? see - j * BK - half * 64 - c * 32 : 32;
+            if (masked) {                                                 // 0, whatever the sums are
 #pragma unroll
-            for (int i = 0; i < 32; i += 2) {
-              float v[2];
-#pragma unroll
-              for (int k = 0; k < 2; ++k) {
-                const float pr = ex2(fmaf(__uint_as_float(x[i + k]), p.scale_log2, -lse2));
-                v[k] = pr * (__uint_as_float(d[i + k]) - delta) * f.ds;
-                if (i + k >= lim) v[k] = 0.f;
+              for (int i = 0; i < 16; ++i) {
+                const int col = c * 32 + 2 * i;
+                if (col >= lim) { pr[c * 16 + i] = 0; d[2 * i] = 0; }
+                if (col + 1 >= lim) { pr[c * 16 + i] &= 0xffffffffull; d[2 * i + 1] = 0; }
               }
-              y[i / 2] = pack2<BF16>(v[0], v[1]);
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              uint64_t v = mul2(pr[c * 16 + i], add2(pair_bits(d[2 * i], d[2 * i + 1]), delta2));
+              if (!BF16) v = mul2(v, ds2);
+              y[i] = pack2<BF16>(lo(v), hi(v));
             }
             st16(s0 + c * 16, y);
           }
@@ -356,6 +391,7 @@ __global__ void __launch_bounds__(THREADS, 1) dq_tc_kernel(const __grid_constant
         if (lane == 0) tc::mbar_arrive(bar(sh->ds_full));
       }
       if (!ok) break;
+      if (U.next_u >= 0) stat_of(U.next_w, U.next_u % p.kv_heads, lse_next, delta_next);
       if (n > 0) {
         ok = warp_wait(bar(sh->acc_full), units & 1, abort_flag, p.status);
         if (!ok) break;
@@ -364,7 +400,7 @@ __global__ void __launch_bounds__(THREADS, 1) dq_tc_kernel(const __grid_constant
       }
       const float out_f = p.scale * f.ds_inv;
       const bool cut = w.nparts > 1;
-      const int slot = w.slot + h * w.nparts;
+      const int first = w.slot + h * w.nparts;
       uint16_t* const dq = static_cast<uint16_t*>(p.dq);
       if (active) {
 #pragma unroll 1
@@ -377,22 +413,21 @@ __global__ void __launch_bounds__(THREADS, 1) dq_tc_kernel(const __grid_constant
             for (int i = 0; i < 32; ++i) v[i] = 0.f;
           }
           if (!valid) continue;
-          if (cut) put_part(slot_sums(p.slots, slot + w.part) + (size_t)row * D + c, v, D - c);
+          if (cut) put_part(slot_sums(p.slots, first + w.part) + (size_t)row * D + c, v, D - c);
           else store_row<BF16>(dq + (int64_t)(w.q0 + pos) * p.ld_dq + (int64_t)(h * p.rep + in_group) * D + c, v, min(32, D - c), p.whole_q);
         }
       }
       tc::tc_fence_before();
       if (cut) {
-        const bool last = last_of_parts(sh, p.slots.tickets + 4 * slot, w.nparts, joins & 1, rwarp, lane, p.status, ok);
+        const bool last = last_of_parts(sh, p.slots.tickets + 4 * first, w.nparts, joins & 1, rwarp, lane, p.status, ok);
         if (!ok) break;
         ++joins;
         if (last) {
-          for (int i = rwarp * 32 + lane; i < rows * D; i += 256) {
-            float x = 0.f;
-            for (int k = 0; k < w.nparts; ++k) x += __ldcg(slot_sums(p.slots, slot + k) + i);
-            const int rr = i / D, ps = rr / p.rep;
-            dq[(int64_t)(w.q0 + ps) * p.ld_dq + (int64_t)(h * p.rep + rr - ps * p.rep) * D + (i - rr * D)] = (uint16_t)pack2<BF16>(x, 0.f);
-          }
+          join_sums4(p.slots, first, w.nparts, 0, rows * D / 4, rwarp * 32 + lane, 256, [&](int e, float4 v) {
+            const int rr = e * 4 / D, ps = rr / p.rep;
+            *reinterpret_cast<uint2*>(dq + (int64_t)(w.q0 + ps) * p.ld_dq + (int64_t)(h * p.rep + rr - ps * p.rep) * D + (e * 4 - rr * D)) =
+                make_uint2(pack2<BF16>(v.x, v.y), pack2<BF16>(v.z, v.w));
+          });
         }
       }
     }
@@ -407,20 +442,20 @@ __global__ void __launch_bounds__(THREADS, 1) dq_tc_kernel(const __grid_constant
 }
 
 template <int DP, bool BF16>
-__global__ void __launch_bounds__(THREADS, 1) dkv_tc_kernel(const __grid_constant__ Maps tm, const Params p) {
+__global__ void __launch_bounds__(THREADS, 1) dkv_tc_kernel(const __grid_constant__ Maps tm, const __grid_constant__ Params p) {
   using G = Cfg<DP>;
-  constexpr int STAGES = G::STAGES;
+  constexpr int SLOTS = G::SLOTS;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   Shared* sh = reinterpret_cast<Shared*>(smem_raw + G::TILES);
-  const uint32_t k_tile = tc::smem_u32(smem_raw), v_tile = k_tile + G::TILE_BYTES, ring = k_tile + 2 * G::TILE_BYTES;
+  const uint32_t smem = tc::smem_u32(smem_raw);
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
-  if (k_tile & 1023u) {                  // (swizzled tiles: dynamic shared memory begins there, as nothing static lies before it)
+  if (smem & 1023u) {                  // (swizzled tiles: dynamic shared memory begins there, as nothing static lies before it)
     if (threadIdx.x == 0 && blockIdx.x == 0) record_error(p.status, ZOACT_ERR_UNSUPPORTED);
     return;
   }
   volatile int* abort_flag = &sh->abort_flag;
   const auto bar = [](const uint64_t& b) { return tc::smem_u32(&b); };
-  init_shared<STAGES>(sh, p.rep);
+  init_shared<SLOTS>(sh, p.rep);
   if (threadIdx.x == 32) {
     tc::prefetch_tmap(&tm.q);
     tc::prefetch_tmap(&tm.g);
@@ -441,46 +476,46 @@ __global__ void __launch_bounds__(THREADS, 1) dkv_tc_kernel(const __grid_constan
   pdl_trigger();
 
   const int total = work_count(p.work, p.kv_heads, threadIdx.x == 0 && blockIdx.x == 0 ? p.status : nullptr);
-  const auto item_of = [&](int u) { return load_item(p.work.items + u / p.kv_heads); };
-  const int G0 = gridDim.x, P = p.positions;
+  const auto slot = [&](uint32_t s) { return smem + s * (uint32_t)G::TILE_BYTES; };
+  const int P = p.positions;
   const int ksteps = (p.head_dim + 15) / 16;
 
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_FEW));
     if (warp == 0) {
       // ---------------- TMA producer ----------------
-      uint32_t at = 0, units = 0;
+      Ring ring(SLOTS);
       bool ok = true;
       const uint32_t row_bytes = (uint32_t)(G::BOXES * P * p.rep * 128);
-      for (int r = 0; ok && (int64_t)r * G0 < total; ++r) {
-        const int u = unit_of(r, blockIdx.x, G0);
-        if (u >= total) continue;
-        const Item w = item_of(u);
-        const int h = u % p.kv_heads, n = (w.npos + P - 1) / P;
+      for (Units U(p.work, total, p.kv_heads); ok && U.here(); U.next()) {
+        const Item& w = U.w;
+        const int h = U.head(), n = (w.npos + P - 1) / P;
         if (n == 0) continue;
-        ok = warp_wait(bar(sh->own_empty), (units & 1) ^ 1u, abort_flag, p.status);
-        if (!ok) break;
-        ++units;
-        if (elect_one()) {
-          tc::mbar_arrive_expect_tx(bar(sh->own_full), (uint32_t)(2 * G::TILE_BYTES));
-          for (int b = 0; b < G::BOXES; ++b) {
-            tma_load_3d(k_tile + (uint32_t)(b * BOX), &tm.k, b * 64, h, w.k0, bar(sh->own_full));
-            tma_load_3d(v_tile + (uint32_t)(b * BOX), &tm.v, b * 64, h, w.k0, bar(sh->own_full));
-          }
-        }
-        __syncwarp();
-        for (int j = 0; ok && j < 2 * n; ++j, ++at) {
-          const uint32_t s = at % STAGES;
-          ok = warp_wait(bar(sh->empty[s]), (at / STAGES & 1) ^ 1u, abort_flag, p.status);
-          if (!ok) break;
-          if (elect_one()) {
-            const CUtensorMap* map = j & 1 ? &tm.g : &tm.q;
-            tc::mbar_arrive_expect_tx(bar(sh->full[s]), row_bytes);
+        uint32_t par, own[2] = {0, 0};
+        for (int t = 0; ok && t < 2; ++t) {
+          const uint32_t s = own[t] = ring.take(par);
+          ok = warp_wait(bar(sh->empty[s]), par ^ 1u, abort_flag, p.status);
+          if (ok && elect_one()) {
+            tc::mbar_arrive_expect_tx(bar(sh->full[s]), (uint32_t)G::TILE_BYTES);
             for (int b = 0; b < G::BOXES; ++b)
-              tma_load_4d(ring + s * G::TILE_BYTES + (uint32_t)(b * BOX), map, b * 64, 0, h, w.q0 + j / 2 * P, bar(sh->full[s]));
+              tma_load_3d(slot(s) + (uint32_t)(b * BOX), t ? &tm.v : &tm.k, b * 64, h, w.k0, bar(sh->full[s]));
           }
           __syncwarp();
         }
+        for (int j = 0; ok && j < 2 * n; ++j) {
+          const uint32_t s = ring.take(par);
+          ok = warp_wait(bar(sh->empty[s]), par ^ 1u, abort_flag, p.status);
+          if (!ok) break;
+          if (elect_one()) {
+            tc::mbar_arrive_expect_tx(bar(sh->full[s]), row_bytes);
+            for (int b = 0; b < G::BOXES; ++b)
+              tma_load_4d(slot(s) + (uint32_t)(b * BOX), j & 1 ? &tm.g : &tm.q, b * 64, 0, h, w.q0 + j / 2 * P, bar(sh->full[s]));
+          }
+          __syncwarp();
+          ring.give(s);
+        }
+        ring.give(own[0]);
+        ring.give(own[1]);
       }
       if (!ok) {                       // give our copies time to land before the CTA winds down
         const uint64_t t0 = tc::global_timer_ns();
@@ -490,57 +525,64 @@ __global__ void __launch_bounds__(THREADS, 1) dkv_tc_kernel(const __grid_constan
     } else if (warp == 1) {
       // ---------------- MMA issuer ----------------
       const uint32_t id_d = tc::idesc_f16(BK, ksteps * 16, BF16) | B_BY_ROWS;
-      uint32_t base = 0, step = 0, units = 0;
+      Ring ring(SLOTS);
+      uint32_t step = 0;
       bool ok = true, any = false;
-      for (int r = 0; ok && (int64_t)r * G0 < total; ++r) {
-        const int u = unit_of(r, blockIdx.x, G0);
-        if (u >= total) continue;
-        const Item w = item_of(u);
+      for (Units U(p.work, total, p.kv_heads); ok && U.here(); U.next()) {
+        const Item& w = U.w;
         const int n = (w.npos + P - 1) / P;
         if (n == 0) continue;
-        const auto tile = [&](uint32_t at) { return ring + at % STAGES * G::TILE_BYTES; };
+        uint32_t par_k, par_v;
+        const uint32_t k_slot = ring.take(par_k), v_slot = ring.take(par_v);
+        const int len = ring.len;
+        Cursor c1[2] = {{0}, {1}}, c2[2] = {{0}, {1}};       // Q and dO: for the products over columns, and over rows
         const auto rows_of = [&](int i) { return min(P, w.npos - i * P) * p.rep; };
-        // S^T (first = 0: K by Q) or dP^T (1: V by dO) of step i, as wide as the step has rows
-        const auto product = [&](int first, int i) {
-          const uint32_t at = base + 2 * i + first;
-          if (!warp_wait(bar(sh->full[at % STAGES]), at / STAGES & 1, abort_flag, p.status)) return false;
+        // S^T (G = 0: K by Q) or dP^T (1: V by dO) of step i, as wide as the step has rows
+        const auto product = [&](int g, int i, Cursor& c) {
+          const uint32_t s = ring.at(c.i);
+          if (!warp_wait(bar(sh->full[s]), ring.parity(s) ^ c.wrapped, abort_flag, p.status)) return false;
+          c.move(2, len);
           const int rows = rows_of(i), up = (rows + 15) / 16 * 16;
-          if (rows != up) zero_rows(tile(at), G::BOXES, rows, up, lane);
+          if (rows != up) zero_rows(slot(s), G::BOXES, rows, up, lane);
           tc::tc_fence_after();
           if (elect_one()) {
-            mma_cols(first ? t_dp : t_s, first ? v_tile : k_tile, tile(at), tc::idesc_f16(BK, up, BF16), ksteps);
-            tc::mma_commit(first ? bar(sh->dp_full) : bar(sh->s_full[0]));
-            if (first && i == n - 1) tc::mma_commit(bar(sh->own_empty));
+            const uint32_t own = g ? v_slot : k_slot;
+            mma_cols(g ? t_dp : t_s, slot(own), slot(s), tc::idesc_f16(BK, up, BF16), ksteps);
+            tc::mma_commit(g ? bar(sh->dp_full) : bar(sh->s_full[0]));
+            if (i == n - 1) tc::mma_commit(bar(sh->empty[own]));
           }
           __syncwarp();
           any = true;
           return true;
         };
-        // dv += P^T dO (first = 1) or dk += dS^T Q (0)
-        const auto sum = [&](int first, int i) {
-          const uint32_t at = base + 2 * i + first;
+        // dv += P^T dO (g = 1) or dk += dS^T Q (0)
+        const auto sum = [&](int g, int i, Cursor& c) {
+          const uint32_t s = ring.at(c.i);
+          c.move(2, len);
           tc::tc_fence_after();
           if (elect_one()) {
-            mma_rows_halves(first ? t_dv : t_dk, first ? t_s : t_dp, tile(at), id_d, (rows_of(i) + 15) / 16, i != 0);
-            tc::mma_commit(bar(sh->empty[at % STAGES]));
-            if (!first && i == n - 1) tc::mma_commit(bar(sh->acc_full));
+            mma_rows_halves(g ? t_dv : t_dk, g ? t_s : t_dp, slot(s), id_d, (rows_of(i) + 15) / 16, i != 0);
+            tc::mma_commit(bar(sh->empty[s]));
+            if (!g && i == n - 1) tc::mma_commit(bar(sh->acc_full));
           }
           __syncwarp();
         };
-        ok = warp_wait(bar(sh->own_full), units & 1, abort_flag, p.status) && product(0, 0) && product(1, 0);
-        ++units;
+        ok = warp_wait(bar(sh->full[k_slot]), par_k, abort_flag, p.status) && product(0, 0, c1[0]) &&
+             warp_wait(bar(sh->full[v_slot]), par_v, abort_flag, p.status) && product(1, 0, c1[1]);
         for (int i = 0; ok && i < n; ++i) {
           ok = warp_wait(bar(sh->p_full), (step + i) & 1, abort_flag, p.status);
           if (!ok) break;
-          sum(1, i);
-          if (i + 1 < n) ok = product(0, i + 1);
+          sum(1, i, c2[1]);
+          if (i + 1 < n) ok = product(0, i + 1, c1[0]);
           if (!ok) break;
           ok = warp_wait(bar(sh->ds_full), (step + i) & 1, abort_flag, p.status);
           if (!ok) break;
-          sum(0, i);
-          if (i + 1 < n) ok = product(1, i + 1);
+          sum(0, i, c2[0]);
+          if (i + 1 < n) ok = product(1, i + 1, c1[1]);
         }
-        base += 2 * n;
+        ring.pass(2 * n);
+        ring.give(k_slot);
+        ring.give(v_slot);
         step += n;
       }
       if (any) {
@@ -553,11 +595,9 @@ __global__ void __launch_bounds__(THREADS, 1) dkv_tc_kernel(const __grid_constan
       const Factors<BF16> f(p.largest, true);
       uint32_t step = 0;
       bool ok = true;
-      for (int r = 0; ok && (int64_t)r * G0 < total; ++r) {
-        const int u = unit_of(r, blockIdx.x, G0);
-        if (u >= total) continue;
-        const Item w = item_of(u);
-        const int h = u % p.kv_heads, n = (w.npos + P - 1) / P;
+      for (Units U(p.work, total, p.kv_heads); ok && U.here(); U.next()) {
+        const Item& w = U.w;
+        const int h = U.head(), n = (w.npos + P - 1) / P;
         for (int i = 0; i < n; ++i, ++step) {
           const int b = step & 1, rows = min(P, w.npos - i * P) * p.rep;
           float lse[4], delta[4];
@@ -566,8 +606,8 @@ __global__ void __launch_bounds__(THREADS, 1) dkv_tc_kernel(const __grid_constan
             const int row = lane + 32 * k, pos = sh->pos_of[row];
             const int64_t e = (int64_t)(w.q0 + i * P + pos) * p.heads + h * p.rep + row - pos * p.rep;
             // (rows behind the last: no share)
-            lse[k] = row < rows ? p.lse[e] * 1.44269504f - f.p_shift : INFINITY;
-            delta[k] = row < rows ? p.delta[e] : 0.f;
+            lse[k] = row < rows ? f.p_shift - p.lse[e] * 1.44269504f : -INFINITY;
+            delta[k] = row < rows ? -p.delta[e] : 0.f;
           }
           ok = warp_wait(bar(sh->stat_empty[b]), (step >> 1 & 1) ^ 1u, abort_flag, p.status);
           if (!ok) break;
@@ -588,49 +628,54 @@ __global__ void __launch_bounds__(THREADS, 1) dkv_tc_kernel(const __grid_constan
     const uint32_t lanes = (uint32_t)(quad * 32) << 16;
     const int D = p.head_dim;
     const Factors<BF16> f(p.largest, true);
+    const uint64_t scale2 = pair(p.scale_log2, p.scale_log2), ds2 = pair(f.ds, f.ds);
     uint32_t step = 0, units = 0, joins = 0;
     bool ok = true;
-    for (int r = 0; ok && (int64_t)r * G0 < total; ++r) {
-      const int u = unit_of(r, blockIdx.x, G0);
-      if (u >= total) continue;
-      const Item w = item_of(u);
-      const int h = u % p.kv_heads, n = (w.npos + P - 1) / P;
+    for (Units U(p.work, total, p.kv_heads); ok && U.here(); U.next()) {
+      const Item& w = U.w;
+      const int h = U.head(), n = (w.npos + P - 1) / P;
       const bool active = quad * 32 < w.nk, valid = key < w.nk;
       for (int i = 0; i < n; ++i, ++step) {
         const int b = step & 1;
         ok = warp_wait(bar(sh->stat_full[b]), step >> 1 & 1, abort_flag, p.status) &&
              warp_wait(bar(sh->s_full[0]), step & 1, abort_flag, p.status);
         if (!ok) break;
-        float pr[64];
+        uint64_t pr[32];
         const uint32_t s0 = t_s + lanes + half * 64, d0 = t_dp + lanes + half * 64;
-        const float4* const lse = reinterpret_cast<const float4*>(&sh->lse[b][half * 64]);
-        const float4* const delta = reinterpret_cast<const float4*>(&sh->delta[b][half * 64]);
+        const ulonglong2* const lse = reinterpret_cast<const ulonglong2*>(&sh->lse[b][half * 64]);          // negative, in pairs
+        const ulonglong2* const delta = reinterpret_cast<const ulonglong2*>(&sh->delta[b][half * 64]);
+        const bool masked = visible(w, p.causal, i * P) < w.nk;
         if (active) {
           tc::tc_fence_after();
-          const bool masked = visible(w, p.causal, i * P) < w.nk;
-          // a row at position x of the step sees this key from x = `from` on
-          const int from = key + 1 - w.diag - i * P;
+          uint32_t x[2][32];
+          ld32(s0, x[0]);
+          ld32(s0 + 32, x[1]);
+          ld_wait();
+          ld_use(x[0]);
+          ld_use(x[1]);
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
-            uint32_t x[32];
-            ld32(s0 + c * 32, x);
-            ld_wait();
-            ld_use(x);
             uint32_t y[16];
 #pragma unroll
             for (int q = 0; q < 8; ++q) {
-              const float4 l4 = lse[c * 8 + q];
-              const float l[4] = {l4.x, l4.y, l4.z, l4.w};
-#pragma unroll
-              for (int k = 0; k < 4; ++k) pr[c * 32 + q * 4 + k] = ex2(fmaf(__uint_as_float(x[q * 4 + k]), p.scale_log2, -l[k]));
+              const ulonglong2 l = lse[c * 8 + q];
+              const uint64_t z0 = fma2(pair_bits(x[c][4 * q], x[c][4 * q + 1]), scale2, l.x);
+              const uint64_t z1 = fma2(pair_bits(x[c][4 * q + 2], x[c][4 * q + 3]), scale2, l.y);
+              pr[c * 16 + 2 * q] = pair(ex2(lo(z0)), ex2(hi(z0)));
+              pr[c * 16 + 2 * q + 1] = pair(ex2(lo(z1)), ex2(hi(z1)));
             }
             if (masked) {
+              // a row at position x of the step sees this key from x = `from` on
+              const int from = key + 1 - w.diag - i * P;
 #pragma unroll
-              for (int k = 0; k < 32; ++k)
-                if ((int)sh->pos_of[half * 64 + c * 32 + k] < from) pr[c * 32 + k] = 0.f;
+              for (int k = 0; k < 16; ++k) {
+                const int col = half * 64 + c * 32 + 2 * k;
+                if ((int)sh->pos_of[col] < from) pr[c * 16 + k] &= ~0xffffffffull;
+                if ((int)sh->pos_of[col + 1] < from) pr[c * 16 + k] &= 0xffffffffull;
+              }
             }
 #pragma unroll
-            for (int k = 0; k < 16; ++k) y[k] = pack2<BF16>(pr[c * 32 + 2 * k], pr[c * 32 + 2 * k + 1]);
+            for (int k = 0; k < 16; ++k) y[k] = pack2<BF16>(lo(pr[c * 16 + k]), hi(pr[c * 16 + k]));
             st16(s0 + c * 16, y);
           }
           tc::tmem_wait_st();
@@ -644,25 +689,21 @@ __global__ void __launch_bounds__(THREADS, 1) dkv_tc_kernel(const __grid_constan
           tc::tc_fence_after();
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
-            uint32_t x[32];
+            uint32_t x[32], y[16];
             ld32(d0 + c * 32, x);
             ld_wait();
             ld_use(x);
-            uint32_t y[16];
 #pragma unroll
             for (int q = 0; q < 8; ++q) {
-              const float4 d4 = delta[c * 8 + q];
-              const float d[4] = {d4.x, d4.y, d4.z, d4.w};
-              float v[4];
-#pragma unroll
-              for (int k = 0; k < 4; ++k) {
-                const float share = pr[c * 32 + q * 4 + k];
-                v[k] = share * (__uint_as_float(x[q * 4 + k]) - d[k]) * f.ds;
-                // (a key that is not seen: 0, whatever its sums are)
-                if (share == 0.f) v[k] = 0.f;
+              const ulonglong2 d = delta[c * 8 + q];
+              uint64_t v0 = mul2(pr[c * 16 + 2 * q], add2(pair_bits(x[4 * q], x[4 * q + 1]), d.x));
+              uint64_t v1 = mul2(pr[c * 16 + 2 * q + 1], add2(pair_bits(x[4 * q + 2], x[4 * q + 3]), d.y));
+              if (!BF16) {
+                v0 = mul2(v0, ds2);
+                v1 = mul2(v1, ds2);
               }
-              y[2 * q] = pack2<BF16>(v[0], v[1]);
-              y[2 * q + 1] = pack2<BF16>(v[2], v[3]);
+              y[2 * q] = pack2<BF16>(lo(v0), hi(v0));
+              y[2 * q + 1] = pack2<BF16>(lo(v1), hi(v1));
             }
             st16(d0 + c * 16, y);
           }
@@ -684,7 +725,7 @@ __global__ void __launch_bounds__(THREADS, 1) dkv_tc_kernel(const __grid_constan
       }
       const float fk = p.scale * f.ds_inv, fv = f.p_inv;
       const bool cut = w.nparts > 1;
-      const int slot = w.slot + h * w.nparts;
+      const int first = w.slot + h * w.nparts;
       uint16_t* const dk = static_cast<uint16_t*>(p.dk) + (int64_t)w.k0 * p.ld_dk + (int64_t)h * D;
       uint16_t* const dv = static_cast<uint16_t*>(p.dv) + (int64_t)w.k0 * p.ld_dv + (int64_t)h * D;
       if (active) {
@@ -700,7 +741,7 @@ __global__ void __launch_bounds__(THREADS, 1) dkv_tc_kernel(const __grid_constan
               for (int i = 0; i < 32; ++i) v[i] = 0.f;
             }
             if (!valid) continue;
-            if (cut) put_part(slot_sums(p.slots, slot + w.part) + (size_t)(which * BK + key) * D + c, v, D - c);
+            if (cut) put_part(slot_sums(p.slots, first + w.part) + (size_t)(which * BK + key) * D + c, v, D - c);
             else if (which) store_row<BF16>(dv + (int64_t)key * p.ld_dv + c, v, min(32, D - c), p.whole_v);
             else store_row<BF16>(dk + (int64_t)key * p.ld_dk + c, v, min(32, D - c), p.whole_k);
           }
@@ -708,21 +749,16 @@ __global__ void __launch_bounds__(THREADS, 1) dkv_tc_kernel(const __grid_constan
       }
       tc::tc_fence_before();
       if (cut) {
-        const bool last = last_of_parts(sh, p.slots.tickets + 4 * slot, w.nparts, joins & 1, rwarp, lane, p.status, ok);
+        const bool last = last_of_parts(sh, p.slots.tickets + 4 * first, w.nparts, joins & 1, rwarp, lane, p.status, ok);
         if (!ok) break;
         ++joins;
         if (last) {
-          for (int i = rwarp * 32 + lane; i < w.nk * D; i += 256) {
-            float x = 0.f, y = 0.f;
-            for (int k = 0; k < w.nparts; ++k) {
-              const float* s = slot_sums(p.slots, slot + k) + i;
-              x += __ldcg(s);
-              y += __ldcg(s + (size_t)BK * D);
-            }
-            const int kk = i / D, d = i - kk * D;
-            dk[(int64_t)kk * p.ld_dk + d] = (uint16_t)pack2<BF16>(x, 0.f);
-            dv[(int64_t)kk * p.ld_dv + d] = (uint16_t)pack2<BF16>(y, 0.f);
-          }
+          for (int which = 0; which < 2; ++which)
+            join_sums4(p.slots, first, w.nparts, (size_t)(which * BK) * D, w.nk * D / 4, rwarp * 32 + lane, 256, [&](int e, float4 v) {
+              const int kk = e * 4 / D, d = e * 4 - kk * D;
+              *reinterpret_cast<uint2*>(which ? dv + (int64_t)kk * p.ld_dv + d : dk + (int64_t)kk * p.ld_dk + d) =
+                  make_uint2(pack2<BF16>(v.x, v.y), pack2<BF16>(v.z, v.w));
+            });
         }
       }
     }

@@ -13,6 +13,10 @@ namespace {
 
 constexpr int THREADS = 1024, BINS = 1024;
 
+// Steps that rows of work are not cut below: a step takes 0.6 to 1.2 us, and a part's sums 4 to 8 us to be left and joined (few
+// rows: 2 us).
+__device__ constexpr int min_steps(int list) { return list == LIST_FWD ? 4 : 12; }
+
 size_t up(size_t n) { return (n + 255) / 256 * 256; }
 
 __device__ __forceinline__ int64_t block_sum(int64_t v, int64_t* sh) {
@@ -113,7 +117,7 @@ struct Builder {
 struct PlanArgs {
   Shape s;
   const void* spans;
-  int id64, grad, sm_count, min_steps;
+  int id64, grad, sm_count;
   uint64_t tag;
   uint8_t* plan;
   Layout at;
@@ -173,7 +177,7 @@ __global__ void __launch_bounds__(THREADS) plan_kernel(const PlanArgs p) {
     for (int r = tid; r < rows; r += THREADS) steps += b.row_at(r, w);
     steps = block_sum(steps, sums) * p.s.kv_heads;
     // a part is no shorter than its share of the GPU: at most 2 parts of a share each, so that the slots suffice
-    const int64_t share = max((int64_t)p.min_steps, (steps + SPLIT_OVER * p.sm_count - 1) / (SPLIT_OVER * p.sm_count));
+    const int64_t share = max((int64_t)min_steps(list), (steps + SPLIT_OVER * p.sm_count - 1) / (SPLIT_OVER * p.sm_count));
     const bool cuts = p.s.head_dim <= TC_DIM;
     const auto parts_of = [&](int len) { return cuts && len > share ? (int)((len + share - 1) / share) : 1; };
     const auto bin_of = [&](int len, int parts) { return BINS - 1 - min((len + parts - 1) / parts, BINS - 1); };
@@ -243,8 +247,7 @@ uint64_t plan_tag(const Shape& s) {
 }
 
 int launch_plan(Ctx* ctx, const Shape& s, const void* spans, int id64, uint8_t* plan, int grad) {
-  // Steps that no part falls below: 4 blocks of keys take about as long as a part's sums to be joined.
-  PlanArgs p = {s, spans, id64, grad, ctx->sm_count, 4, plan_tag(s), plan, plan_layout(s, ctx->sm_count, grad), ctx->d_status};
+  PlanArgs p = {s, spans, id64, grad, ctx->sm_count, plan_tag(s), plan, plan_layout(s, ctx->sm_count, grad), ctx->d_status};
   ZOACT_CUDA_TRY(launch_pdl(ctx, plan_kernel, dim3(1), dim3(THREADS), 0, p));
   ++ctx->n_launch;
   return ZOACT_OK;

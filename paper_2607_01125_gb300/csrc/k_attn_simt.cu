@@ -223,7 +223,8 @@ __global__ void __launch_bounds__(THREADS) fwd_kernel(const Dev p) {
 }
 
 // delta = the row sum of dO O, a warp a (row, head); in fp16 also the largest finite |dO| (0 before).
-template <typename T>
+constexpr int EACH = 4;
+template <typename T, int V>
 __global__ void __launch_bounds__(THREADS) delta_kernel(const Work work, int* status, const T* dO, int64_t ld_do, const T* O,
                                                         int64_t ld_o, int64_t rows, int heads, int head_dim, float* delta,
                                                         float* largest) {
@@ -234,18 +235,32 @@ __global__ void __launch_bounds__(THREADS) delta_kernel(const Work work, int* st
   const int lane = threadIdx.x & 31;
   const int64_t n = rows * heads;
   float top = 0.f;
-  for (int64_t i = (int64_t)blockIdx.x * (THREADS / 32) + (threadIdx.x >> 5); i < n; i += (int64_t)gridDim.x * (THREADS / 32)) {
-    const int64_t r = i / heads;
-    const int h = (int)(i - r * heads);
-    const T *a = dO + r * ld_do + (int64_t)h * head_dim, *b = O + r * ld_o + (int64_t)h * head_dim;
-    float s = 0.f;
-    for (int d = lane; d < head_dim; d += 32) {
-      const float g = to_f32<T>(a[d]);
-      s += g * to_f32<T>(b[d]);
-      if (std::is_same<T, __half>::value && fabsf(g) < INFINITY) top = fmaxf(top, fabsf(g));
+  const int64_t warps = (int64_t)gridDim.x * (THREADS / 32);
+  // EACH (row, head) pairs at a time, so that their loads are in flight together
+  for (int64_t i0 = ((int64_t)blockIdx.x * (THREADS / 32) + (threadIdx.x >> 5)) * EACH; i0 < n; i0 += warps * EACH) {
+    float s[EACH];
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) {
+      const int64_t i = min(i0 + e, n - 1), r = i / heads;
+      const int h = (int)(i - r * heads);
+      const T *a = dO + r * ld_do + (int64_t)h * head_dim, *b = O + r * ld_o + (int64_t)h * head_dim;
+      s[e] = 0.f;
+      for (int d = lane * V; d < head_dim; d += 32 * V) {
+        struct alignas(sizeof(T) * V) Vec { T v[V]; };
+        const Vec x = *reinterpret_cast<const Vec*>(a + d), y = *reinterpret_cast<const Vec*>(b + d);
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+          const float g = to_f32<T>(x.v[k]);
+          s[e] += g * to_f32<T>(y.v[k]);
+          if (std::is_same<T, __half>::value && fabsf(g) < INFINITY) top = fmaxf(top, fabsf(g));
+        }
+      }
     }
-    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-    if (lane == 0) delta[i] = s;
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) {
+      for (int o = 16; o > 0; o >>= 1) s[e] += __shfl_xor_sync(0xffffffffu, s[e], o);
+      if (lane == 0 && i0 + e < n) delta[i0 + e] = s[e];
+    }
   }
   if (!std::is_same<T, __half>::value) return;
   for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
@@ -488,10 +503,13 @@ int delta(Ctx* ctx, const Args& a) {
     ZOACT_CUDA_TRY(launch_pdl(ctx, reset_kernel, dim3(1), dim3(1), 0, work_of(a, LIST_DQ), a.largest));
     ++ctx->n_launch;
   }
-  const int64_t blocks = (a.s.rows_q * a.s.heads + THREADS / 32 - 1) / (THREADS / 32), most = (int64_t)ctx->sm_count * 64;
-  ZOACT_CUDA_TRY(launch_pdl(ctx, delta_kernel<T>, dim3((unsigned)(blocks < most ? blocks : most)), dim3(THREADS), 0,
-                            work_of(a, LIST_DQ), ctx->d_status, (const T*)a.dO,
-                            a.ld_do, (const T*)a.O, a.ld_o, a.s.rows_q, a.s.heads, a.s.head_dim, a.delta, a.largest));
+  const auto lies = [](const void* p, int64_t ld) { return (uintptr_t)p % (4 * sizeof(T)) == 0 && ld % 4 == 0; };
+  const bool vec = a.s.head_dim % 4 == 0 && lies(a.O, a.ld_o) && lies(a.dO, a.ld_do);
+  const int64_t per = EACH * THREADS / 32, blocks = (a.s.rows_q * a.s.heads + per - 1) / per, most = (int64_t)ctx->sm_count * 8;
+  auto kern = vec ? delta_kernel<T, 4> : delta_kernel<T, 1>;
+  ZOACT_CUDA_TRY(launch_pdl(ctx, kern, dim3((unsigned)(blocks < most ? blocks : most)), dim3(THREADS), 0, work_of(a, LIST_DQ),
+                            ctx->d_status, (const T*)a.dO, a.ld_do, (const T*)a.O, a.ld_o, a.s.rows_q, a.s.heads, a.s.head_dim,
+                            a.delta, a.largest));
   ++ctx->n_launch;
   return ZOACT_OK;
 }
