@@ -45,17 +45,28 @@ __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint3
       : "memory");
 }
 
-// Products of `steps` times 16 in K.  Over columns: A and B tiles in shared memory.
+// A warp's own value, which the instructions of the tensor core take from uniform registers: a loop whose addresses the compiler
+// did not know to be one for the whole warp took 100 cycles an MMA to issue, more than the MMA itself.
+__device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xffffffffu, x, 0); }
+__device__ __forceinline__ uint32_t uniform(uint32_t x) { return __shfl_sync(0xffffffffu, x, 0); }
+
+// Products of `steps` times 16 in K, at most STEPS (all arguments the warp's own).  Over columns: A and B tiles in shared memory.
+template <int STEPS>
 __device__ __forceinline__ void mma_cols(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, int steps) {
-  for (int k = 0; k < steps; ++k) {
+#pragma unroll
+  for (int k = 0; k < STEPS; ++k) {
     const uint32_t at = (uint32_t)(k >> 2) * BOX + (uint32_t)(k & 3) * 32u;
-    tc::mma_f16(d, desc_cols(a + at), desc_cols(b + at), idesc, k != 0);
+    if (k < steps) tc::mma_f16(d, desc_cols(a + at), desc_cols(b + at), idesc, k != 0);
   }
 }
-// Over the rows of B: A in TMEM.
-__device__ __forceinline__ void mma_rows(uint32_t d, uint32_t a_tmem, uint32_t b, uint32_t idesc, int steps, bool accumulate) {
-  for (int k = 0; k < steps; ++k)
-    mma_ts(d, a_tmem + (uint32_t)k * 8u, desc_rows(b + (uint32_t)k * 2048u), idesc, accumulate || k != 0);
+// Over the rows of B: A in TMEM, the columns of 64 K of it SECOND apart.
+template <int SECOND>
+__device__ __forceinline__ void mma_rows(uint32_t d, uint32_t a_tmem, uint32_t b, uint32_t idesc, int steps, uint32_t accumulate) {
+#pragma unroll
+  for (int k = 0; k < TILE / 16; ++k)
+    if (k < steps)
+      mma_ts(d, a_tmem + (uint32_t)(k >> 2) * SECOND + (uint32_t)(k & 3) * 8u, desc_rows(b + (uint32_t)k * 2048u), idesc,
+             k != 0 ? 1u : accumulate);
 }
 
 __device__ __forceinline__ bool elect_one() {
@@ -200,12 +211,7 @@ struct Units {
   }
   __device__ __forceinline__ bool here() const { return u >= 0; }
   __device__ __forceinline__ int head() const { return u % kv_heads; }
-  __device__ __forceinline__ void next() {
-    u = next_u;
-    w = next_w;
-    ++round;
-    fetch();
-  }
+  __device__ __forceinline__ void next();
   __device__ __forceinline__ void fetch();
 };
 
@@ -214,13 +220,22 @@ __device__ __forceinline__ Item load_item(const Item* p) {
   return {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
 }
 
+__device__ __forceinline__ Item uniform_item(const Item& w) {
+  return {uniform(w.q0), uniform(w.npos), uniform(w.k0), uniform(w.nk), uniform(w.diag), uniform(w.part), uniform(w.nparts), uniform(w.slot)};
+}
+__device__ __forceinline__ void Units::next() {
+  u = next_u;
+  if (u >= 0) w = uniform_item(next_w);
+  ++round;
+  fetch();
+}
 __device__ __forceinline__ void Units::fetch() {
   next_u = u >= 0 ? unit(round + 1) : -1;
   if (next_u >= 0) next_w = load_item(work->items + next_u / kv_heads);
 }
 __device__ __forceinline__ Units::Units(const Work& wk, int n, int heads) : work(&wk), total(n), kv_heads(heads) {
   u = unit(0);
-  if (u >= 0) w = load_item(work->items + u / kv_heads);
+  if (u >= 0) w = uniform_item(load_item(work->items + u / kv_heads));
   fetch();
 }
 

@@ -137,7 +137,7 @@ __global__ void __launch_bounds__(THREADS, 1) fwd_tc_kernel(const __grid_constan
   pdl_wait();
   pdl_trigger();
 
-  const int total = work_count(p.work, p.kv_heads, threadIdx.x == 0 && blockIdx.x == 0 ? p.status : nullptr);
+  const int total = uniform(work_count(p.work, p.kv_heads, threadIdx.x == 0 && blockIdx.x == 0 ? p.status : nullptr));
 
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_FEW));
@@ -206,7 +206,7 @@ __global__ void __launch_bounds__(THREADS, 1) fwd_tc_kernel(const __grid_constan
           c.move(stride, len);
           tc::tc_fence_after();
           if (elect_one()) {
-            mma_cols(tmem + t * BK, slot(t ? q1 : q0), slot(s), id_s, ksteps);
+            mma_cols<DP / 16>(tmem + t * BK, slot(t ? q1 : q0), slot(s), id_s, ksteps);
             tc::mma_commit(bar(sh.s_full[t]));
             if (T.halves || t == 1) tc::mma_commit(bar(sh.empty[s]));          // else the second tile still reads it
           }
@@ -227,7 +227,7 @@ __global__ void __launch_bounds__(THREADS, 1) fwd_tc_kernel(const __grid_constan
             zero_rows(slot(s), G::BOXES, keys, (keys + 15) / 16 * 16, lane);
           tc::tc_fence_after();
           if (elect_one()) {
-            mma_rows(tmem + (2 + t) * BK, tmem + t * BK, slot(s), id_o, (mine + 15) / 16, j != 0);
+            mma_rows<32>(tmem + (2 + t) * BK, tmem + t * BK, slot(s), id_o, (mine + 15) / 16, j != 0);
             tc::mma_commit(bar(sh.pv_done[t]));
             if (T.halves || t == 1) tc::mma_commit(bar(sh.empty[s]));
           }

@@ -78,12 +78,6 @@ template <bool BF16> struct Factors {
   }
 };
 
-// A warpgroup's half of P or dS in TMEM: 64 columns of sums became 32 of pairs at the same place.
-__device__ __forceinline__ void mma_rows_halves(uint32_t d, uint32_t a_tmem, uint32_t b, uint32_t idesc, int steps, bool accumulate) {
-  for (int k = 0; k < steps; ++k)
-    mma_ts(d, a_tmem + (uint32_t)(k >> 2) * 64u + (uint32_t)(k & 3) * 8u, desc_rows(b + (uint32_t)k * 2048u), idesc, accumulate || k != 0);
-}
-
 // The barriers, and each row's position.
 template <int SLOTS>
 __device__ __forceinline__ void init_shared(Shared* sh, int rep) {
@@ -186,7 +180,7 @@ __global__ void __launch_bounds__(THREADS, 1) dq_tc_kernel(const __grid_constant
   pdl_wait();
   pdl_trigger();
 
-  const int total = work_count(p.work, p.kv_heads, threadIdx.x == 0 && blockIdx.x == 0 ? p.status : nullptr);
+  const int total = uniform(work_count(p.work, p.kv_heads, threadIdx.x == 0 && blockIdx.x == 0 ? p.status : nullptr));
   const auto slot = [&](uint32_t s) { return smem + s * (uint32_t)G::TILE_BYTES; };
   const int ksteps = (p.head_dim + 15) / 16;
 
@@ -254,7 +248,7 @@ __global__ void __launch_bounds__(THREADS, 1) dq_tc_kernel(const __grid_constant
           if (keys % 16 != 0) zero_rows(slot(s), G::BOXES, keys, (keys + 15) / 16 * 16, lane);
           tc::tc_fence_after();
           if (elect_one()) {
-            mma_cols(t_s + ((step + j) & 1) * BK, slot(q_slot), slot(s), id_s, ksteps);
+            mma_cols<DP / 16>(t_s + ((step + j) & 1) * BK, slot(q_slot), slot(s), id_s, ksteps);
             tc::mma_commit(bar(sh->s_full[(step + j) & 1]));
             if (j == n - 1) tc::mma_commit(bar(sh->empty[q_slot]));
           }
@@ -268,7 +262,7 @@ __global__ void __launch_bounds__(THREADS, 1) dq_tc_kernel(const __grid_constant
           vs.move(2, len);
           tc::tc_fence_after();
           if (elect_one()) {
-            mma_cols(t_dp, slot(g_slot), slot(s), id_s, ksteps);
+            mma_cols<DP / 16>(t_dp, slot(g_slot), slot(s), id_s, ksteps);
             tc::mma_commit(bar(sh->dp_full));
             tc::mma_commit(bar(sh->empty[s]));
             if (j == n - 1) tc::mma_commit(bar(sh->empty[g_slot]));
@@ -288,7 +282,7 @@ __global__ void __launch_bounds__(THREADS, 1) dq_tc_kernel(const __grid_constant
           kq.move(2, len);
           if (elect_one()) {
             const int keys = min(BK, w.nk - j * BK);
-            mma_rows_halves(t_dq, t_s + ((step + j) & 1) * BK, slot(s), id_q, (keys + 15) / 16, j != 0);
+            mma_rows<64>(t_dq, t_s + ((step + j) & 1) * BK, slot(s), id_q, (keys + 15) / 16, j != 0);
             tc::mma_commit(bar(sh->empty[s]));
             if (j == n - 1) tc::mma_commit(bar(sh->acc_full));
           }
@@ -475,7 +469,7 @@ __global__ void __launch_bounds__(THREADS, 1) dkv_tc_kernel(const __grid_constan
   pdl_wait();
   pdl_trigger();
 
-  const int total = work_count(p.work, p.kv_heads, threadIdx.x == 0 && blockIdx.x == 0 ? p.status : nullptr);
+  const int total = uniform(work_count(p.work, p.kv_heads, threadIdx.x == 0 && blockIdx.x == 0 ? p.status : nullptr));
   const auto slot = [&](uint32_t s) { return smem + s * (uint32_t)G::TILE_BYTES; };
   const int P = p.positions;
   const int ksteps = (p.head_dim + 15) / 16;
@@ -547,7 +541,7 @@ __global__ void __launch_bounds__(THREADS, 1) dkv_tc_kernel(const __grid_constan
           tc::tc_fence_after();
           if (elect_one()) {
             const uint32_t own = g ? v_slot : k_slot;
-            mma_cols(g ? t_dp : t_s, slot(own), slot(s), tc::idesc_f16(BK, up, BF16), ksteps);
+            mma_cols<DP / 16>(g ? t_dp : t_s, slot(own), slot(s), tc::idesc_f16(BK, up, BF16), ksteps);
             tc::mma_commit(g ? bar(sh->dp_full) : bar(sh->s_full[0]));
             if (i == n - 1) tc::mma_commit(bar(sh->empty[own]));
           }
@@ -561,7 +555,7 @@ __global__ void __launch_bounds__(THREADS, 1) dkv_tc_kernel(const __grid_constan
           c.move(2, len);
           tc::tc_fence_after();
           if (elect_one()) {
-            mma_rows_halves(g ? t_dv : t_dk, g ? t_s : t_dp, slot(s), id_d, (rows_of(i) + 15) / 16, i != 0);
+            mma_rows<64>(g ? t_dv : t_dk, g ? t_s : t_dp, slot(s), id_d, (rows_of(i) + 15) / 16, i != 0);
             tc::mma_commit(bar(sh->empty[s]));
             if (!g && i == n - 1) tc::mma_commit(bar(sh->acc_full));
           }
