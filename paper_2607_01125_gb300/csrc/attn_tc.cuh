@@ -35,13 +35,33 @@ __device__ __forceinline__ uint64_t desc_rows(uint32_t start) {
 }
 constexpr uint32_t B_BY_ROWS = 1u << 16;          // instruction descriptor: the right operand is N-major
 
-// D[tmem] (+)= A[tmem] * B[smem]: A is 128 lanes x 16-bit pairs, two K to a column.
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+// D[tmem] (+)= A * B[smem], issued by the warp's elected lane (`lead`: a predicate, so that the warp stays together and the
+// operands in uniform registers).  A in shared memory, or in TMEM: 128 lanes x 16-bit pairs, two K to a column.
+__device__ __forceinline__ void mma_ss(bool lead, uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\t"
+      "{\n\t.reg .pred p, q;\n\t"
       "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
-      "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
+      "setp.ne.b32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"((uint32_t)lead)
+      : "memory");
+}
+__device__ __forceinline__ void mma_ts(bool lead, uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "setp.ne.b32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+      "r"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"((uint32_t)lead)
+      : "memory");
+}
+// Arrive on `bar` once what the elected lane issued so far has completed.
+__device__ __forceinline__ void commit(bool lead, uint32_t bar) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\t"
+      "setp.ne.b32 q, %1, 0;\n\t"
+      "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar),
+      "r"((uint32_t)lead)
       : "memory");
 }
 
@@ -52,20 +72,20 @@ __device__ __forceinline__ uint32_t uniform(uint32_t x) { return __shfl_sync(0xf
 
 // Products of `steps` times 16 in K, at most STEPS (all arguments the warp's own).  Over columns: A and B tiles in shared memory.
 template <int STEPS>
-__device__ __forceinline__ void mma_cols(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, int steps) {
+__device__ __forceinline__ void mma_cols(bool lead, uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, int steps) {
 #pragma unroll
   for (int k = 0; k < STEPS; ++k) {
     const uint32_t at = (uint32_t)(k >> 2) * BOX + (uint32_t)(k & 3) * 32u;
-    if (k < steps) tc::mma_f16(d, desc_cols(a + at), desc_cols(b + at), idesc, k != 0);
+    if (k < steps) mma_ss(lead, d, desc_cols(a + at), desc_cols(b + at), idesc, k != 0);
   }
 }
 // Over the rows of B: A in TMEM, the columns of 64 K of it SECOND apart.
 template <int SECOND>
-__device__ __forceinline__ void mma_rows(uint32_t d, uint32_t a_tmem, uint32_t b, uint32_t idesc, int steps, uint32_t accumulate) {
+__device__ __forceinline__ void mma_rows(bool lead, uint32_t d, uint32_t a_tmem, uint32_t b, uint32_t idesc, int steps, uint32_t accumulate) {
 #pragma unroll
   for (int k = 0; k < TILE / 16; ++k)
     if (k < steps)
-      mma_ts(d, a_tmem + (uint32_t)(k >> 2) * SECOND + (uint32_t)(k & 3) * 8u, desc_rows(b + (uint32_t)k * 2048u), idesc,
+      mma_ts(lead, d, a_tmem + (uint32_t)(k >> 2) * SECOND + (uint32_t)(k & 3) * 8u, desc_rows(b + (uint32_t)k * 2048u), idesc,
              k != 0 ? 1u : accumulate);
 }
 

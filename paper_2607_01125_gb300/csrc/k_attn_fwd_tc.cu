@@ -187,6 +187,7 @@ __global__ void __launch_bounds__(THREADS, 1) fwd_tc_kernel(const __grid_constan
       }
     } else if (warp == 1) {
       // ---------------- MMA issuer ----------------
+      const bool lead = elect_one();
       const int ksteps = (p.head_dim + 15) / 16;
       const uint32_t id_s = tc::idesc_f16(TILE, BK, BF16), id_o = tc::idesc_f16(TILE, ksteps * 16, BF16) | B_BY_ROWS;
       Ring ring(SLOTS);
@@ -205,12 +206,9 @@ __global__ void __launch_bounds__(THREADS, 1) fwd_tc_kernel(const __grid_constan
           if (!warp_wait(bar(sh.full[s]), ring.parity(s) ^ c.wrapped, abort_flag, p.status)) return false;
           c.move(stride, len);
           tc::tc_fence_after();
-          if (elect_one()) {
-            mma_cols<DP / 16>(tmem + t * BK, slot(t ? q1 : q0), slot(s), id_s, ksteps);
-            tc::mma_commit(bar(sh.s_full[t]));
-            if (T.halves || t == 1) tc::mma_commit(bar(sh.empty[s]));          // else the second tile still reads it
-          }
-          __syncwarp();
+          mma_cols<DP / 16>(lead, tmem + t * BK, slot(t ? q1 : q0), slot(s), id_s, ksteps);
+          commit(lead, bar(sh.s_full[t]));
+          if (T.halves || t == 1) commit(lead, bar(sh.empty[s]));          // else the second tile still reads it
           any = true;
           return true;
         };
@@ -226,18 +224,14 @@ __global__ void __launch_bounds__(THREADS, 1) fwd_tc_kernel(const __grid_constan
           if (keys % 16 != 0 && (T.halves || t == 0 || j >= T.n0))     // once, before the first product by these rows
             zero_rows(slot(s), G::BOXES, keys, (keys + 15) / 16 * 16, lane);
           tc::tc_fence_after();
-          if (elect_one()) {
-            mma_rows<32>(tmem + (2 + t) * BK, tmem + t * BK, slot(s), id_o, (mine + 15) / 16, j != 0);
-            tc::mma_commit(bar(sh.pv_done[t]));
-            if (T.halves || t == 1) tc::mma_commit(bar(sh.empty[s]));
-          }
-          __syncwarp();
+          mma_rows<32>(lead, tmem + (2 + t) * BK, tmem + t * BK, slot(s), id_o, (mine + 15) / 16, j != 0);
+          commit(lead, bar(sh.pv_done[t]));
+          if (T.halves || t == 1) commit(lead, bar(sh.empty[s]));
           return true;
         };
         // the own tiles are free once the last product by them is done
         const auto free_own = [&](uint32_t s) {
-          if (elect_one()) tc::mma_commit(bar(sh.empty[s]));
-          __syncwarp();
+          commit(lead, bar(sh.empty[s]));
         };
         ok = warp_wait(bar(sh.full[q0]), par0, abort_flag, p.status) &&
              (T.halves || warp_wait(bar(sh.full[q1]), par1, abort_flag, p.status));

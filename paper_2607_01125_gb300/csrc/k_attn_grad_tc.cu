@@ -228,6 +228,7 @@ __global__ void __launch_bounds__(THREADS, 1) dq_tc_kernel(const __grid_constant
       }
     } else if (warp == 1) {
       // ---------------- MMA issuer ----------------
+      const bool lead = elect_one();
       const uint32_t id_s = tc::idesc_f16(TILE, BK, BF16), id_q = tc::idesc_f16(TILE, ksteps * 16, BF16) | B_BY_ROWS;
       Ring ring(SLOTS);
       uint32_t step = 0;
@@ -247,12 +248,9 @@ __global__ void __launch_bounds__(THREADS, 1) dq_tc_kernel(const __grid_constant
           const int keys = min(BK, w.nk - j * BK);
           if (keys % 16 != 0) zero_rows(slot(s), G::BOXES, keys, (keys + 15) / 16 * 16, lane);
           tc::tc_fence_after();
-          if (elect_one()) {
-            mma_cols<DP / 16>(t_s + ((step + j) & 1) * BK, slot(q_slot), slot(s), id_s, ksteps);
-            tc::mma_commit(bar(sh->s_full[(step + j) & 1]));
-            if (j == n - 1) tc::mma_commit(bar(sh->empty[q_slot]));
-          }
-          __syncwarp();
+          mma_cols<DP / 16>(lead, t_s + ((step + j) & 1) * BK, slot(q_slot), slot(s), id_s, ksteps);
+          commit(lead, bar(sh->s_full[(step + j) & 1]));
+          if (j == n - 1) commit(lead, bar(sh->empty[q_slot]));
           any = true;
           return true;
         };
@@ -261,13 +259,10 @@ __global__ void __launch_bounds__(THREADS, 1) dq_tc_kernel(const __grid_constant
           if (!warp_wait(bar(sh->full[s]), ring.parity(s) ^ vs.wrapped, abort_flag, p.status)) return false;
           vs.move(2, len);
           tc::tc_fence_after();
-          if (elect_one()) {
-            mma_cols<DP / 16>(t_dp, slot(g_slot), slot(s), id_s, ksteps);
-            tc::mma_commit(bar(sh->dp_full));
-            tc::mma_commit(bar(sh->empty[s]));
-            if (j == n - 1) tc::mma_commit(bar(sh->empty[g_slot]));
-          }
-          __syncwarp();
+          mma_cols<DP / 16>(lead, t_dp, slot(g_slot), slot(s), id_s, ksteps);
+          commit(lead, bar(sh->dp_full));
+          commit(lead, bar(sh->empty[s]));
+          if (j == n - 1) commit(lead, bar(sh->empty[g_slot]));
           return true;
         };
         ok = warp_wait(bar(sh->full[q_slot]), par_q, abort_flag, p.status) && product_s(0) &&
@@ -280,13 +275,10 @@ __global__ void __launch_bounds__(THREADS, 1) dq_tc_kernel(const __grid_constant
           tc::tc_fence_after();
           const uint32_t s = ring.at(kq.i);
           kq.move(2, len);
-          if (elect_one()) {
-            const int keys = min(BK, w.nk - j * BK);
-            mma_rows<64>(t_dq, t_s + ((step + j) & 1) * BK, slot(s), id_q, (keys + 15) / 16, j != 0);
-            tc::mma_commit(bar(sh->empty[s]));
-            if (j == n - 1) tc::mma_commit(bar(sh->acc_full));
-          }
-          __syncwarp();
+          const int keys = min(BK, w.nk - j * BK);
+          mma_rows<64>(lead, t_dq, t_s + ((step + j) & 1) * BK, slot(s), id_q, (keys + 15) / 16, j != 0);
+          commit(lead, bar(sh->empty[s]));
+          if (j == n - 1) commit(lead, bar(sh->acc_full));
           if (j + 2 < n) ok = product_s(j + 2);
         }
         ring.pass(2 * n);
@@ -518,6 +510,7 @@ __global__ void __launch_bounds__(THREADS, 1) dkv_tc_kernel(const __grid_constan
       }
     } else if (warp == 1) {
       // ---------------- MMA issuer ----------------
+      const bool lead = elect_one();
       const uint32_t id_d = tc::idesc_f16(BK, ksteps * 16, BF16) | B_BY_ROWS;
       Ring ring(SLOTS);
       uint32_t step = 0;
@@ -539,13 +532,10 @@ __global__ void __launch_bounds__(THREADS, 1) dkv_tc_kernel(const __grid_constan
           const int rows = rows_of(i), up = (rows + 15) / 16 * 16;
           if (rows != up) zero_rows(slot(s), G::BOXES, rows, up, lane);
           tc::tc_fence_after();
-          if (elect_one()) {
-            const uint32_t own = g ? v_slot : k_slot;
-            mma_cols<DP / 16>(g ? t_dp : t_s, slot(own), slot(s), tc::idesc_f16(BK, up, BF16), ksteps);
-            tc::mma_commit(g ? bar(sh->dp_full) : bar(sh->s_full[0]));
-            if (i == n - 1) tc::mma_commit(bar(sh->empty[own]));
-          }
-          __syncwarp();
+          const uint32_t own = g ? v_slot : k_slot;
+          mma_cols<DP / 16>(lead, g ? t_dp : t_s, slot(own), slot(s), tc::idesc_f16(BK, up, BF16), ksteps);
+          commit(lead, g ? bar(sh->dp_full) : bar(sh->s_full[0]));
+          if (i == n - 1) commit(lead, bar(sh->empty[own]));
           any = true;
           return true;
         };
@@ -554,12 +544,9 @@ __global__ void __launch_bounds__(THREADS, 1) dkv_tc_kernel(const __grid_constan
           const uint32_t s = ring.at(c.i);
           c.move(2, len);
           tc::tc_fence_after();
-          if (elect_one()) {
-            mma_rows<64>(g ? t_dv : t_dk, g ? t_s : t_dp, slot(s), id_d, (rows_of(i) + 15) / 16, i != 0);
-            tc::mma_commit(bar(sh->empty[s]));
-            if (!g && i == n - 1) tc::mma_commit(bar(sh->acc_full));
-          }
-          __syncwarp();
+          mma_rows<64>(lead, g ? t_dv : t_dk, g ? t_s : t_dp, slot(s), id_d, (rows_of(i) + 15) / 16, i != 0);
+          commit(lead, bar(sh->empty[s]));
+          if (!g && i == n - 1) commit(lead, bar(sh->acc_full));
         };
         ok = warp_wait(bar(sh->full[k_slot]), par_k, abort_flag, p.status) && product(0, 0, c1[0]) &&
              warp_wait(bar(sh->full[v_slot]), par_v, abort_flag, p.status) && product(1, 0, c1[1]);
