@@ -734,25 +734,38 @@ def rope(rot, base=10000.0, layout="half", scaling="none", factor=1.0, low=1.0, 
     return r
 
 
-def _on(ctx, *tensors):
-    """Refuses tensors that are not on the context's device (None: not given)."""
-    for t in tensors:
-        if t is not None and (t.device.type != "cuda" or t.device.index != ctx.device):
-            raise ValueError(f"a tensor on {t.device}, the context is on cuda:{ctx.device}")
+def _on(ctx, t):
+    """Refuses a tensor that is not on the context's device (None: not given)."""
+    if t is not None and t.get_device() != ctx.device:
+        raise ValueError(f"a tensor on {t.device}, the context is on cuda:{ctx.device}")
+
+
+def _mat(ctx, t, rows, cols, dtype, name):
+    """Address and row stride of a matrix of a known shape and type with unit column stride, on the context's device."""
+    if t.shape != (rows, cols) or t.dtype != dtype:
+        raise ValueError(f"{name}: expected {(rows, cols)} of {dtype}, got {tuple(t.shape)} of {t.dtype}")
+    ld, step = t.stride()
+    if rows <= 1:
+        ld = cols
+    if (step != 1 and cols > 1) or ld < cols:
+        raise ValueError("libzoact takes matrices with unit column stride")
+    _on(ctx, t)
+    return t.data_ptr(), ld
 
 
 def zoact_rope_apply(ctx, X, positions, rope, Y, heads, inverse=False):
     """Y = X [rows, heads head_dim] with every head turned by its row's position (back with inverse: the gradient).  X and Y are
     matrices with unit column stride, or one matrix; positions int32 or int64 [n_pos], rows a multiple of n_pos."""
     rows, n = X.shape
-    px, ldx = _rows(X)
-    py, ldy = _rows(Y)
+    heads = int(heads)
+    if heads <= 0 or n % heads != 0:
+        raise ValueError("X has columns for all heads")
+    px, ldx = _mat(ctx, X, rows, n, X.dtype, "X")
+    py, ldy = (px, ldx) if Y is X else _mat(ctx, Y, rows, n, X.dtype, "Y")
     pp, idt = _id_args(positions)
-    if tuple(Y.shape) != (rows, n) or Y.dtype != X.dtype or heads <= 0 or n % heads != 0:
-        raise ValueError("X and Y have one shape and type, and columns for all heads")
-    _on(ctx, X, Y, positions)
-    _check("zoact_rope_apply", load().zoact_rope_apply(ctx.handle, px, _dt(X), rows, int(heads), n // int(heads), ldx, pp, idt,
-                                                       positions.shape[0], ctypes.byref(rope), int(inverse), py, ldy))
+    _on(ctx, positions)
+    _check("zoact_rope_apply", load().zoact_rope_apply(ctx.handle, px, _dt(X), rows, heads, n // heads, ldx, pp, idt,
+                                                       positions.shape[0], rope, 1 if inverse else 0, py, ldy))
 
 
 def attention_shape(rows_q, rows_k, n_seq, heads, kv_heads, head_dim, causal=True):
@@ -775,66 +788,61 @@ def attention_spans(queries, keys=None, key_rows=None):
     return torch.tensor(out, dtype=torch.int64).view(-1, 4)
 
 
+_PLAN_BYTES = {}
+
+
 def zoact_attention_plan_bytes(ctx, shape, grad=False):
-    n = int(load().zoact_attention_plan_bytes(ctx.handle, ctypes.byref(shape), int(bool(grad))))
-    if n < 0:
-        raise ValueError("zoact_attention_plan_bytes: a shape that attention does not take")
+    key = (ctx.device, shape.rows_q, shape.rows_k, shape.n_seq, shape.heads, shape.kv_heads, shape.head_dim, bool(grad))
+    n = _PLAN_BYTES.get(key)
+    if n is None:
+        n = int(load().zoact_attention_plan_bytes(ctx.handle, shape, int(bool(grad))))
+        if n < 0:
+            raise ValueError("zoact_attention_plan_bytes: a shape that attention does not take")
+        if len(_PLAN_BYTES) > 1000:
+            _PLAN_BYTES.clear()
+        _PLAN_BYTES[key] = n
     return n
 
 
-def zoact_attention_plan(ctx, shape, spans, plan, grad=False):
-    """The plan (a uint8 tensor of zoact_attention_plan_bytes) of spans [n_seq, 4] (int32 or int64, on the device)."""
-    if spans.dim() != 2 or tuple(spans.shape) != (shape.n_seq, 4) or spans.dtype not in _ID_DT:
-        raise ValueError(f"spans: [{shape.n_seq}, 4] of int32 or int64")
-    if plan.dtype != torch.uint8 or plan.numel() < zoact_attention_plan_bytes(ctx, shape, grad):
-        raise ValueError("plan: uint8, zoact_attention_plan_bytes of it")
-    _on(ctx, spans, plan)
-    _check("zoact_attention_plan", load().zoact_attention_plan(ctx.handle, ctypes.byref(shape), _ptr(spans), _ID_DT[spans.dtype],
-                                                               int(bool(grad)), _ptr(plan)))
-
-
-def _heads(ctx, t, rows, heads, shape, dtype, name):
-    """Address and row stride of [rows, heads head_dim] (a matrix with unit column stride)."""
-    if tuple(t.shape) != (rows, heads * shape.head_dim) or t.dtype != dtype:
-        raise ValueError(f"{name}: expected {(rows, heads * shape.head_dim)} of {dtype}, got {tuple(t.shape)} of {t.dtype}")
-    _on(ctx, t)
-    return _rows(t)
-
-
-def _scale(shape, scale):
-    return float(shape.head_dim) ** -0.5 if scale is None else float(scale)
-
-
-def _attention_plan(ctx, shape, plan, grad):
+def _plan(ctx, shape, plan, grad):
     if plan.dtype != torch.uint8 or plan.numel() < zoact_attention_plan_bytes(ctx, shape, grad):
         raise ValueError("plan: uint8, zoact_attention_plan_bytes of it")
     _on(ctx, plan)
     return _ptr(plan)
 
 
+def zoact_attention_plan(ctx, shape, spans, plan, grad=False):
+    """The plan (a uint8 tensor of zoact_attention_plan_bytes) of spans [n_seq, 4] (int32 or int64, on the device)."""
+    if spans.shape != (shape.n_seq, 4) or spans.dtype not in _ID_DT:
+        raise ValueError(f"spans: [{shape.n_seq}, 4] of int32 or int64")
+    _on(ctx, spans)
+    _check("zoact_attention_plan", load().zoact_attention_plan(ctx.handle, shape, _ptr(spans), _ID_DT[spans.dtype],
+                                                               int(bool(grad)), _plan(ctx, shape, plan, grad)))
+
+
+def _scale(shape, scale):
+    return shape.head_dim ** -0.5 if scale is None else float(scale)
+
+
 def zoact_attention(ctx, shape, plan, q, k, v, O, lse=None, scale=None):
     """Attention of the plan's sequences: q and O [rows_q, heads head_dim], k and v [rows_k, kv_heads head_dim] (matrices with
     unit column stride), lse [rows_q, heads] fp32 or None; scale: 1 / sqrt(head_dim) by default."""
-    s = shape
-    args = []
-    for t, rows, heads, name in ((q, s.rows_q, s.heads, "q"), (k, s.rows_k, s.kv_heads, "k"), (v, s.rows_k, s.kv_heads, "v")):
-        args += _heads(ctx, t, rows, heads, s, q.dtype, name)
-    po, ldo = _heads(ctx, O, s.rows_q, s.heads, s, q.dtype, "O")
+    dt, d = q.dtype, shape.head_dim
+    rq, cq, rk, ck = shape.rows_q, shape.heads * d, shape.rows_k, shape.kv_heads * d
     _on(ctx, lse)
     _check("zoact_attention", load().zoact_attention(
-        ctx.handle, ctypes.byref(s), _attention_plan(ctx, s, plan, False), *args, _dt(q), _scale(s, scale), po, ldo,
-        _out(lse, (s.rows_q, s.heads), torch.float32, "lse")))
+        ctx.handle, shape, _plan(ctx, shape, plan, False), *_mat(ctx, q, rq, cq, dt, "q"), *_mat(ctx, k, rk, ck, dt, "k"),
+        *_mat(ctx, v, rk, ck, dt, "v"), TORCH_DT[dt], _scale(shape, scale), *_mat(ctx, O, rq, cq, dt, "O"),
+        _out(lse, (rq, shape.heads), torch.float32, "lse")))
 
 
 def zoact_attention_grad(ctx, shape, plan, dO, q, k, v, O, lse, dq, dk, dv, scale=None):
     """The gradient of zoact_attention for dO, from its O and lse, with a plan made with grad: dq, dk and dv like q, k and v."""
-    s = shape
-    args = []
-    for t, rows, heads, name in ((dO, s.rows_q, s.heads, "dO"), (q, s.rows_q, s.heads, "q"), (k, s.rows_k, s.kv_heads, "k"),
-                                 (v, s.rows_k, s.kv_heads, "v"), (O, s.rows_q, s.heads, "O"), (dq, s.rows_q, s.heads, "dq"),
-                                 (dk, s.rows_k, s.kv_heads, "dk"), (dv, s.rows_k, s.kv_heads, "dv")):
-        args += _heads(ctx, t, rows, heads, s, q.dtype, name)
+    dt, d = q.dtype, shape.head_dim
+    rq, cq, rk, ck = shape.rows_q, shape.heads * d, shape.rows_k, shape.kv_heads * d
     _on(ctx, lse)
     _check("zoact_attention_grad", load().zoact_attention_grad(
-        ctx.handle, ctypes.byref(s), _attention_plan(ctx, s, plan, True), *args[:8], _dt(q), _scale(s, scale), *args[8:10],
-        _out(lse, (s.rows_q, s.heads), torch.float32, "lse"), *args[10:]))
+        ctx.handle, shape, _plan(ctx, shape, plan, True), *_mat(ctx, dO, rq, cq, dt, "dO"), *_mat(ctx, q, rq, cq, dt, "q"),
+        *_mat(ctx, k, rk, ck, dt, "k"), *_mat(ctx, v, rk, ck, dt, "v"), TORCH_DT[dt], _scale(shape, scale),
+        *_mat(ctx, O, rq, cq, dt, "O"), _out(lse, (rq, shape.heads), torch.float32, "lse"), *_mat(ctx, dq, rq, cq, dt, "dq"),
+        *_mat(ctx, dk, rk, ck, dt, "dk"), *_mat(ctx, dv, rk, ck, dt, "dv")))

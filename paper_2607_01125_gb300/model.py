@@ -24,6 +24,7 @@ Graph wiring (names follow synth.Workload):
   llama/opt  per decoder layer on input h:
                a = rms(h); q, k, v = Q a, K a, V a
                o = O rms(q + rep(k) + rep(v));  b = rms(o)
+                 (after pack(): o = O attention(rot(q), rot(k), v) over packed sequences)
                llama: h' = down rms(silu(gate b) * up b)
                opt:   h' = fc2 rms(relu(fc1 b))
              the first layer's q, k, v see the same input for both signs;
@@ -112,7 +113,52 @@ class ZOStep:
         # stacks: RMS normalisations as row scales of the pair forwards where the library applies them
         self.row_scales = True
         self._utc = {}
+        self._attention = None                      # after pack(): (shape, plan, positions, rope)
         self.prepare_bases()
+
+    def pack(self, lengths, rope=None, causal=True):
+        """Attention in place of a stack's mixer from now on: the T rows are sequences of these lengths, one after another, in
+        each evaluation block, with rotary positions counted from each sequence's start (rope: zo.rope(...), or None).  Rows
+        behind the last sequence take no part (the mixer gives zeros there).  pack(None): the mixer as before.  One plan serves
+        every decoder until the next call."""
+        if lengths is None:
+            self._attention = None
+            return
+        if not self.groups:
+            raise ValueError(f"ZOStep.pack: a {self.kind} graph has no attention")
+        lengths = [int(n) for n in lengths]
+        if any(n < 0 for n in lengths) or sum(lengths) > self.T:
+            raise ValueError(f"ZOStep.pack: sequences of {sum(lengths)} rows, the step takes {self.T}")
+        q, k, v = (self.by_name[n] for n in self.groups[0])
+        if k.d_out != v.d_out or q.d_out % self.head_dim or k.d_out % self.head_dim:
+            raise ValueError("ZOStep.pack: q, k and v are whole heads, as many of k as of v")
+        spans = torch.cat([Z.attention_spans(lengths) + torch.tensor([b * self.T, 0, b * self.T, 0]) for b in range(self.nb)])
+        positions = torch.zeros(self.T, dtype=torch.int64)
+        if sum(lengths):
+            positions[:sum(lengths)] = torch.cat([torch.arange(n) for n in lengths])
+        rows = self.nb * self.T
+        shape = Z.attention_shape(rows, rows, len(spans), q.d_out // self.head_dim, k.d_out // self.head_dim, self.head_dim,
+                                  causal=causal)
+        plan = torch.empty(Z.zoact_attention_plan_bytes(self.ctx, shape), dtype=torch.uint8, device=self.device)
+        Z.zoact_attention_plan(self.ctx, shape, spans.to(self.device), plan)
+        self.buf("attn", rows, q.d_out).zero_()
+        self._attention = (shape, plan, positions.to(self.device), rope)
+
+    def _attend(self, q, k, v):
+        """The mixer's output after pack(); q and k are turned in place."""
+        shape, plan, positions, rope = self._attention
+        if rope is not None:
+            both = self._bufs.get("qkv")
+            if both is not None and q.data_ptr() == both.data_ptr():        # columns of one output: one call
+                qk = both[:, :q.shape[1] + k.shape[1]]
+                Z.zoact_rope_apply(self.ctx, qk, positions, rope, qk, shape.heads + shape.kv_heads)
+            else:
+                Z.zoact_rope_apply(self.ctx, q, positions, rope, q, shape.heads)
+                Z.zoact_rope_apply(self.ctx, k, positions, rope, k, shape.kv_heads)
+        out = self._bufs["attn"]
+        Z.zoact_attention(self.ctx, shape, plan, q, k, v, out)
+        self._wrote(out)
+        return out
 
     def prepare_bases(self):
         """The frozen bases in the tensor-core projection's operand form, once per distinct U
@@ -387,9 +433,12 @@ class ZOStep:
                     k = self.pair(f"{L}.k", h, False, seed, query, "k", in_scale=inv_h)
                     v = self.pair(f"{L}.v", h, False, seed, query, "v", in_scale=inv_h)
             shared = False
-            mix = self.buf("mix", self.nb * T, q.shape[1])
-            Z.zoact_mix_rms(self.ctx, q, k, v, mix, self.n_rep if self.kind == "llama" else 1, self.head_dim)
-            self._wrote(mix)
+            if self._attention is not None:
+                mix = self._attend(q, k, v)
+            else:
+                mix = self.buf("mix", self.nb * T, q.shape[1])
+                Z.zoact_mix_rms(self.ctx, q, k, v, mix, self.n_rep if self.kind == "llama" else 1, self.head_dim)
+                self._wrote(mix)
             inv_o = None
             if rs:
                 o, inv_o = self.pair(f"{L}.o", mix, False, seed, query, "o", sums=True)
