@@ -79,11 +79,11 @@ __device__ __forceinline__ void mma_cols(bool lead, uint32_t d, uint32_t a, uint
     if (k < steps) mma_ss(lead, d, desc_cols(a + at), desc_cols(b + at), idesc, k != 0);
   }
 }
-// Over the rows of B: A in TMEM, the columns of 64 K of it SECOND apart.
-template <int SECOND>
+// Over the rows of B (steps FIRST to LAST of them): A in TMEM, the columns of 64 K of it SECOND apart.
+template <int SECOND, int FIRST = 0, int LAST = TILE / 16>
 __device__ __forceinline__ void mma_rows(bool lead, uint32_t d, uint32_t a_tmem, uint32_t b, uint32_t idesc, int steps, uint32_t accumulate) {
 #pragma unroll
-  for (int k = 0; k < TILE / 16; ++k)
+  for (int k = FIRST; k < LAST; ++k)
     if (k < steps)
       mma_ts(lead, d, a_tmem + (uint32_t)(k >> 2) * SECOND + (uint32_t)(k & 3) * 8u, desc_rows(b + (uint32_t)k * 2048u), idesc,
              k != 0 ? 1u : accumulate);
@@ -202,7 +202,8 @@ struct Ring {
   }
   // n slots taken and given back, one after another.
   __device__ __forceinline__ void pass(int n) {
-    const int rounds = n / len, rest = n - rounds * len;
+    const int rounds = n / len;
+    const int rest = n - rounds * len;
     for (int i = 0; i < len; ++i)
       if ((rounds + (i < rest ? 1 : 0)) & 1) phase ^= 1u << at(i);
     const uint64_t all = (1ull << (4 * len)) - 1, o = order & all;
@@ -222,15 +223,14 @@ struct Cursor {
 // The units of a list that a CTA runs, with the next one's item on its way.
 struct Units {
   const Work* work;
-  int total, kv_heads, round = 0, u, next_u = -1;
+  int total, round = 0, u, next_u = -1, h = 0, next_h = 0;
   Item w, next_w;
-  __device__ __forceinline__ Units(const Work& wk, int n, int heads);
+  __device__ __forceinline__ Units(const Work& wk, int n);
   __device__ __forceinline__ int unit(int r) const {
     const int x = unit_of(r, (int)blockIdx.x, (int)gridDim.x);
     return (int64_t)r * gridDim.x < total && x < total ? x : -1;
   }
   __device__ __forceinline__ bool here() const { return u >= 0; }
-  __device__ __forceinline__ int head() const { return u % kv_heads; }
   __device__ __forceinline__ void next();
   __device__ __forceinline__ void fetch();
 };
@@ -245,17 +245,19 @@ __device__ __forceinline__ Item uniform_item(const Item& w) {
 }
 __device__ __forceinline__ void Units::next() {
   u = next_u;
+  h = uniform(next_h);
   if (u >= 0) w = uniform_item(next_w);
   ++round;
   fetch();
 }
 __device__ __forceinline__ void Units::fetch() {
   next_u = u >= 0 ? unit(round + 1) : -1;
-  if (next_u >= 0) next_w = load_item(work->items + next_u / kv_heads);
+  if (next_u >= 0) next_w = load_item(work->items + work->item(next_u, next_h));
 }
-__device__ __forceinline__ Units::Units(const Work& wk, int n, int heads) : work(&wk), total(n), kv_heads(heads) {
+__device__ __forceinline__ Units::Units(const Work& wk, int n) : work(&wk), total(n) {
   u = unit(0);
-  if (u >= 0) w = uniform_item(load_item(work->items + u / kv_heads));
+  if (u >= 0) w = uniform_item(load_item(work->items + work->item(u, h)));
+  h = uniform(h);
   fetch();
 }
 

@@ -165,6 +165,19 @@ __device__ __forceinline__ uint32_t next_part_bf16x2(float& x, float& y) {
 
 __device__ __forceinline__ float silu_f(float x) { return x / (1.0f + expf(-x)); }
 
+// Division of numbers below 2^31 by a divisor that the host knows: the product with its inverse is the quotient or one less.
+struct Divisor {
+  int d;
+  uint32_t inverse;                     // 2^32 / d, rounded down (2^32 - 1 for 1)
+  explicit Divisor(int n = 1) : d(n), inverse(n == 1 ? 0xffffffffu : (uint32_t)((1ull << 32) / (uint32_t)n)) {}
+  __device__ __forceinline__ int div(int x, int& rest) const {
+    int q = (int)__umulhi((uint32_t)x, inverse);
+    rest = x - q * d;
+    if (rest >= d) { ++q; rest -= d; }
+    return q;
+  }
+};
+
 inline size_t dtype_size(int dt) {
   return dt == ZOACT_DT_FP32 ? 4 : 2;
 }

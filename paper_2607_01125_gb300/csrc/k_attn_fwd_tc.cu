@@ -54,7 +54,7 @@ struct Params {
 struct Maps { CUtensorMap q, k, v; };
 
 struct Shared {
-  uint64_t full[12], empty[12], s_full[2], p_full[2], pv_done[2], merge_full, merge_empty;
+  uint64_t full[12], empty[12], s_full[2], p_half[2], p_full[2], pv_done[2], merge_full, merge_empty;
   uint64_t join_in[2], join_out[2], drain;
   uint32_t tmem_base;
   int abort_flag, last[2];
@@ -108,6 +108,7 @@ __global__ void __launch_bounds__(THREADS, 1) fwd_tc_kernel(const __grid_constan
   if (threadIdx.x == 0) {
     for (int t = 0; t < 2; ++t) {
       tc::mbar_init(bar(sh.s_full[t]), 1);
+      tc::mbar_init(bar(sh.p_half[t]), 4);
       tc::mbar_init(bar(sh.p_full[t]), 4);
       tc::mbar_init(bar(sh.pv_done[t]), 1);
       tc::mbar_init(bar(sh.join_in[t]), 4);
@@ -146,9 +147,9 @@ __global__ void __launch_bounds__(THREADS, 1) fwd_tc_kernel(const __grid_constan
       Ring ring(SLOTS);
       bool ok = true;
       const uint32_t q_bytes = (uint32_t)(G::BOXES * p.positions * p.rep * 128);
-      for (Units U(p.work, total, p.kv_heads); ok && U.here(); U.next()) {
+      for (Units U(p.work, total); ok && U.here(); U.next()) {
         const Item& w = U.w;
-        const int h = U.head();
+        const int h = U.h;
         const Tiles T(w, p);
         uint32_t par, own[2] = {0, 0};
         for (int t = 0; ok && t < T.own(); ++t) {
@@ -193,7 +194,7 @@ __global__ void __launch_bounds__(THREADS, 1) fwd_tc_kernel(const __grid_constan
       Ring ring(SLOTS);
       uint32_t done0 = 0, done1 = 0;               // steps of the tiles so far
       bool ok = true, any = false;
-      for (Units U(p.work, total, p.kv_heads); ok && U.here(); U.next()) {
+      for (Units U(p.work, total); ok && U.here(); U.next()) {
         const Item& w = U.w;
         const Tiles T(w, p);
         if (T.blocks == 0) continue;
@@ -213,8 +214,6 @@ __global__ void __launch_bounds__(THREADS, 1) fwd_tc_kernel(const __grid_constan
           return true;
         };
         const auto product_o = [&](int t, int j, Cursor& c, uint32_t& done) {
-          if (!warp_wait(bar(sh.p_full[t]), done & 1, abort_flag, p.status)) return false;
-          ++done;
           const uint32_t s = ring.at(c.i);
           if (!warp_wait(bar(sh.full[s]), ring.parity(s) ^ c.wrapped, abort_flag, p.status)) return false;
           c.move(stride, len);
@@ -223,8 +222,14 @@ __global__ void __launch_bounds__(THREADS, 1) fwd_tc_kernel(const __grid_constan
           const int mine = min(keys, T.halves ? BK : visible(w, p.causal, T.pos0(t) + T.npos(t) - 1) - block * BK);
           if (keys % 16 != 0 && (T.halves || t == 0 || j >= T.n0))     // once, before the first product by these rows
             zero_rows(slot(s), G::BOXES, keys, (keys + 15) / 16 * 16, lane);
+          // the shares of the first 64 keys come before the others': their products run meanwhile
+          if (!warp_wait(bar(sh.p_half[t]), done & 1, abort_flag, p.status)) return false;
           tc::tc_fence_after();
-          mma_rows<32>(lead, tmem + (2 + t) * BK, tmem + t * BK, slot(s), id_o, (mine + 15) / 16, j != 0);
+          mma_rows<32, 0, 4>(lead, tmem + (2 + t) * BK, tmem + t * BK, slot(s), id_o, (mine + 15) / 16, j != 0);
+          if (!warp_wait(bar(sh.p_full[t]), done & 1, abort_flag, p.status)) return false;
+          ++done;
+          tc::tc_fence_after();
+          mma_rows<32, 4, 8>(lead, tmem + (2 + t) * BK, tmem + t * BK, slot(s), id_o, (mine + 15) / 16, j != 0);
           commit(lead, bar(sh.pv_done[t]));
           if (T.halves || t == 1) commit(lead, bar(sh.empty[s]));
           return true;
@@ -273,9 +278,9 @@ __global__ void __launch_bounds__(THREADS, 1) fwd_tc_kernel(const __grid_constan
     constexpr float SHIFT = BF16 ? 0.f : 7.f;
     uint32_t steps = 0, merges = 0, joins = 0;
     bool ok = true;
-    for (Units U(p.work, total, p.kv_heads); ok && U.here(); U.next()) {
+    for (Units U(p.work, total); ok && U.here(); U.next()) {
       const Item& w = U.w;
-      const int h = U.head();
+      const int h = U.h;
       const Tiles T(w, p);
       const int rows = T.npos(t) * p.rep;
       const bool active = quad * 32 < rows, valid = row < rows;
@@ -347,6 +352,12 @@ __global__ void __launch_bounds__(THREADS, 1) fwd_tc_kernel(const __grid_constan
                 y[k * 16 + i / 2] = pack2<BF16>(a, b);
               }
             st32(ts + c * 16, y);
+            if (c == 0) {
+              tc::tmem_wait_st();
+              tc::tc_fence_before();
+              __syncwarp();
+              if (lane == 0) tc::mbar_arrive(bar(sh.p_half[t]));
+            }
           }
           const uint64_t sum2 = add2(add2(s[0], s[1]), add2(s[2], s[3]));
           l += lo(sum2) + hi(sum2);
@@ -354,7 +365,10 @@ __global__ void __launch_bounds__(THREADS, 1) fwd_tc_kernel(const __grid_constan
           tc::tc_fence_before();
         }
         __syncwarp();
-        if (lane == 0) tc::mbar_arrive(bar(sh.p_full[t]));
+        if (lane == 0) {
+          if (!active) tc::mbar_arrive(bar(sh.p_half[t]));
+          tc::mbar_arrive(bar(sh.p_full[t]));
+        }
       }
       if (!ok) break;
       // ---- the unit's rows ----

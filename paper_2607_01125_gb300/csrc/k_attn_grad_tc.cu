@@ -191,9 +191,9 @@ __global__ void __launch_bounds__(THREADS, 1) dq_tc_kernel(const __grid_constant
       Ring ring(SLOTS);
       bool ok = true;
       const uint32_t row_bytes = (uint32_t)(G::BOXES * p.positions * p.rep * 128);
-      for (Units U(p.work, total, p.kv_heads); ok && U.here(); U.next()) {
+      for (Units U(p.work, total); ok && U.here(); U.next()) {
         const Item& w = U.w;
-        const int h = U.head(), n = (w.nk + BK - 1) / BK;
+        const int h = U.h, n = (w.nk + BK - 1) / BK;
         if (n == 0) continue;
         uint32_t par, own[2] = {0, 0};
         for (int t = 0; ok && t < 2; ++t) {
@@ -233,7 +233,7 @@ __global__ void __launch_bounds__(THREADS, 1) dq_tc_kernel(const __grid_constant
       Ring ring(SLOTS);
       uint32_t step = 0;
       bool ok = true, any = false;
-      for (Units U(p.work, total, p.kv_heads); ok && U.here(); U.next()) {
+      for (Units U(p.work, total); ok && U.here(); U.next()) {
         const Item& w = U.w;
         const int n = (w.nk + BK - 1) / BK;
         if (n == 0) continue;
@@ -310,12 +310,12 @@ __global__ void __launch_bounds__(THREADS, 1) dq_tc_kernel(const __grid_constant
       lse2 = p.lse[e];
       delta = p.delta[e];
     };
-    Units U(p.work, total, p.kv_heads);
+    Units U(p.work, total);
     float lse_next = 0.f, delta_next = 0.f;
-    if (U.here()) stat_of(U.w, U.head(), lse_next, delta_next);
+    if (U.here()) stat_of(U.w, U.h, lse_next, delta_next);
     for (; ok && U.here(); U.next()) {
       const Item& w = U.w;
-      const int h = U.head(), n = (w.nk + BK - 1) / BK, rows = w.npos * p.rep;
+      const int h = U.h, n = (w.nk + BK - 1) / BK, rows = w.npos * p.rep;
       const bool active = quad * 32 < rows, valid = row < rows;
       const int see = valid ? visible(w, p.causal, pos) : 0, all_see = visible(w, p.causal, 0);
       const float lse2 = lse_next * 1.44269504f;
@@ -377,7 +377,7 @@ __global__ void __launch_bounds__(THREADS, 1) dq_tc_kernel(const __grid_constant
         if (lane == 0) tc::mbar_arrive(bar(sh->ds_full));
       }
       if (!ok) break;
-      if (U.next_u >= 0) stat_of(U.next_w, U.next_u % p.kv_heads, lse_next, delta_next);
+      if (U.next_u >= 0) stat_of(U.next_w, U.next_h, lse_next, delta_next);
       if (n > 0) {
         ok = warp_wait(bar(sh->acc_full), units & 1, abort_flag, p.status);
         if (!ok) break;
@@ -473,9 +473,9 @@ __global__ void __launch_bounds__(THREADS, 1) dkv_tc_kernel(const __grid_constan
       Ring ring(SLOTS);
       bool ok = true;
       const uint32_t row_bytes = (uint32_t)(G::BOXES * P * p.rep * 128);
-      for (Units U(p.work, total, p.kv_heads); ok && U.here(); U.next()) {
+      for (Units U(p.work, total); ok && U.here(); U.next()) {
         const Item& w = U.w;
-        const int h = U.head(), n = (w.npos + P - 1) / P;
+        const int h = U.h, n = (w.npos + P - 1) / P;
         if (n == 0) continue;
         uint32_t par, own[2] = {0, 0};
         for (int t = 0; ok && t < 2; ++t) {
@@ -515,7 +515,7 @@ __global__ void __launch_bounds__(THREADS, 1) dkv_tc_kernel(const __grid_constan
       Ring ring(SLOTS);
       uint32_t step = 0;
       bool ok = true, any = false;
-      for (Units U(p.work, total, p.kv_heads); ok && U.here(); U.next()) {
+      for (Units U(p.work, total); ok && U.here(); U.next()) {
         const Item& w = U.w;
         const int n = (w.npos + P - 1) / P;
         if (n == 0) continue;
@@ -576,9 +576,9 @@ __global__ void __launch_bounds__(THREADS, 1) dkv_tc_kernel(const __grid_constan
       const Factors<BF16> f(p.largest, true);
       uint32_t step = 0;
       bool ok = true;
-      for (Units U(p.work, total, p.kv_heads); ok && U.here(); U.next()) {
+      for (Units U(p.work, total); ok && U.here(); U.next()) {
         const Item& w = U.w;
-        const int h = U.head(), n = (w.npos + P - 1) / P;
+        const int h = U.h, n = (w.npos + P - 1) / P;
         for (int i = 0; i < n; ++i, ++step) {
           const int b = step & 1, rows = min(P, w.npos - i * P) * p.rep;
           float lse[4], delta[4];
@@ -612,9 +612,9 @@ __global__ void __launch_bounds__(THREADS, 1) dkv_tc_kernel(const __grid_constan
     const uint64_t scale2 = pair(p.scale_log2, p.scale_log2), ds2 = pair(f.ds, f.ds);
     uint32_t step = 0, units = 0, joins = 0;
     bool ok = true;
-    for (Units U(p.work, total, p.kv_heads); ok && U.here(); U.next()) {
+    for (Units U(p.work, total); ok && U.here(); U.next()) {
       const Item& w = U.w;
-      const int h = U.head(), n = (w.npos + P - 1) / P;
+      const int h = U.h, n = (w.npos + P - 1) / P;
       const bool active = quad * 32 < w.nk, valid = key < w.nk;
       for (int i = 0; i < n; ++i, ++step) {
         const int b = step & 1;

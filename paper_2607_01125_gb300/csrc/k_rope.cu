@@ -9,7 +9,6 @@
 // Bound by memory: every element is read and written once.  A block makes the sines and cosines of its rows once, in shared
 // memory, for all of a row's heads, and then moves 16 bytes of both halves (or of neighbouring pairs) at a time.
 //
-// Measured (GB300): see the launcher.
 #include <cmath>
 
 #include "internal.h"
@@ -39,12 +38,58 @@ __device__ __forceinline__ float2 cos_sin_turns(uint64_t t) {
 
 template <typename T, int N> struct alignas(sizeof(T) * N) Vec { T v[N]; };
 
-// V elements at a time (V = 1: any alignment).  np: pieces of a head that turn; nc: pieces behind them that are copied.
+// A piece of a head: what is read for it, and turned in place.
+template <typename T, int V, bool HALF> struct Piece {
+  static constexpr int W = HALF || V > 1 ? V : 2;              // elements of one half, or of neighbouring pairs
+  Vec<T, W> a, b;
+  __device__ __forceinline__ void load(const T* x, int nf) {
+    if constexpr (!HALF && V == 1) {
+      a.v[0] = x[0];
+      a.v[1] = x[1];
+    } else {
+      a = *reinterpret_cast<const Vec<T, W>*>(x);
+      if constexpr (HALF) b = *reinterpret_cast<const Vec<T, W>*>(x + nf);
+    }
+  }
+  __device__ __forceinline__ void turn(const float2* cs) {
+    if constexpr (HALF) {
+#pragma unroll
+      for (int j = 0; j < W; ++j) {
+        const float2 w = cs[j];
+        const float u = to_f32<T>(a.v[j]), v = to_f32<T>(b.v[j]);
+        a.v[j] = from_f32<T>(u * w.x - v * w.y);
+        b.v[j] = from_f32<T>(u * w.y + v * w.x);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < W; j += 2) {
+        const float2 w = cs[j / 2];
+        const float u = to_f32<T>(a.v[j]), v = to_f32<T>(a.v[j + 1]);
+        a.v[j] = from_f32<T>(u * w.x - v * w.y);
+        a.v[j + 1] = from_f32<T>(u * w.y + v * w.x);
+      }
+    }
+  }
+  __device__ __forceinline__ void store(T* y, int nf) const {
+    if constexpr (!HALF && V == 1) {
+      y[0] = a.v[0];
+      y[1] = a.v[1];
+    } else {
+      *reinterpret_cast<Vec<T, W>*>(y) = a;
+      if constexpr (HALF) *reinterpret_cast<Vec<T, W>*>(y + nf) = b;
+    }
+  }
+};
+
+// V elements at a time (V = 1: any alignment).  np: pieces of a head that turn; nc: pieces behind them that are copied.  MANY
+// pieces of a thread are read before the first is written (X may be Y, which the compiler has to allow for).
+constexpr int MANY = 2;
 template <typename T, int V, bool HALF>
 __global__ void __launch_bounds__(THREADS)
-rope_kernel(const T* X, int64_t ld_x, T* Y, int64_t ld_y, int64_t rows, int heads, int head_dim, int rot, int np, int nc,
+rope_kernel(const T* X, int64_t ld_x, T* Y, int64_t ld_y, int64_t rows, int head_dim, int rot, int np, Divisor pieces, Divisor per_row,
             const void* __restrict__ positions, int id64, uint32_t n_pos, int rows_block, int inverse,
             const __grid_constant__ Turns turns) {
+  using P = Piece<T, V, HALF>;
   __shared__ float2 table[TABLE];
   pdl_wait();
   pdl_trigger();
@@ -57,58 +102,41 @@ rope_kernel(const T* X, int64_t ld_x, T* Y, int64_t ld_y, int64_t rows, int head
     table[i] = make_float2(cs.x, inverse ? -cs.y : cs.y);
   }
   __syncthreads();
-  const int pieces = np + nc, per_row = heads * pieces, total = nr * per_row;
-#pragma unroll 4
-  for (int i = threadIdx.x; i < total; i += THREADS) {
-    const int r = i / per_row, in_row = i - r * per_row, head = in_row / pieces, p = in_row - head * pieces;
-    const T* x = X + (r0 + r) * ld_x + (int64_t)head * head_dim;
-    T* y = Y + (r0 + r) * ld_y + (int64_t)head * head_dim;
-    if (p >= np) {
-      const int d = rot + (p - np) * V;
-      *reinterpret_cast<Vec<T, V>*>(y + d) = *reinterpret_cast<const Vec<T, V>*>(x + d);
-      continue;
+  const int total = nr * per_row.d;
+  for (int i0 = threadIdx.x; i0 < total; i0 += MANY * THREADS) {
+    P v[MANY];
+    int64_t to[MANY];
+    int cs[MANY];                              // the first of its cosines and sines, or -1: copied
+#pragma unroll
+    for (int k = 0; k < MANY; ++k) {
+      const int i = min(i0 + k * THREADS, total - 1);
+      int in_row, p;
+      const int r = per_row.div(i, in_row), head = pieces.div(in_row, p);
+      const bool copy = p >= np;
+      const int d = copy ? rot + (p - np) * V : p * P::W;
+      const int64_t at = (int64_t)head * head_dim + d;
+      const T* x = X + (r0 + r) * ld_x + at;
+      to[k] = (r0 + r) * ld_y + at;
+      cs[k] = copy ? -1 : r * nf + (HALF ? d : d / 2);
+      if (copy) {
+        const Vec<T, V> c = *reinterpret_cast<const Vec<T, V>*>(x);
+#pragma unroll
+        for (int j = 0; j < V; ++j) v[k].a.v[j] = c.v[j];
+      } else {
+        v[k].load(x, nf);
+      }
     }
-    const float2* cs = table + r * nf;
-    if constexpr (HALF) {
-      const int d = p * V;
-      const Vec<T, V> a = *reinterpret_cast<const Vec<T, V>*>(x + d), b = *reinterpret_cast<const Vec<T, V>*>(x + nf + d);
-      Vec<T, V> s, t;
 #pragma unroll
-      for (int j = 0; j < V; ++j) {
-        const float2 w = cs[d + j];
-        const float u = to_f32<T>(a.v[j]), v = to_f32<T>(b.v[j]);
-        s.v[j] = from_f32<T>(u * w.x - v * w.y);
-        t.v[j] = from_f32<T>(u * w.y + v * w.x);
-      }
-      *reinterpret_cast<Vec<T, V>*>(y + d) = s;
-      *reinterpret_cast<Vec<T, V>*>(y + nf + d) = t;
-    } else {
-      constexpr int W = V > 1 ? V : 2;           // pairs: two elements at least
-      const int d = p * W;
-      T e[W];
-      if constexpr (V > 1) {
-        const Vec<T, V> a = *reinterpret_cast<const Vec<T, V>*>(x + d);
+    for (int k = 0; k < MANY; ++k) {
+      if (i0 + k * THREADS >= total) break;
+      if (cs[k] < 0) {
+        Vec<T, V> c;
 #pragma unroll
-        for (int j = 0; j < V; ++j) e[j] = a.v[j];
+        for (int j = 0; j < V; ++j) c.v[j] = v[k].a.v[j];
+        *reinterpret_cast<Vec<T, V>*>(Y + to[k]) = c;
       } else {
-        e[0] = x[d];
-        e[1] = x[d + 1];
-      }
-#pragma unroll
-      for (int j = 0; j < W; j += 2) {
-        const float2 w = cs[(d + j) / 2];
-        const float u = to_f32<T>(e[j]), v = to_f32<T>(e[j + 1]);
-        e[j] = from_f32<T>(u * w.x - v * w.y);
-        e[j + 1] = from_f32<T>(u * w.y + v * w.x);
-      }
-      if constexpr (V > 1) {
-        Vec<T, V> s;
-#pragma unroll
-        for (int j = 0; j < V; ++j) s.v[j] = e[j];
-        *reinterpret_cast<Vec<T, V>*>(y + d) = s;
-      } else {
-        y[d] = e[0];
-        y[d + 1] = e[1];
+        v[k].turn(table + cs[k]);
+        v[k].store(Y + to[k], nf);
       }
     }
   }
@@ -128,7 +156,7 @@ int launch(Ctx* ctx, const RopeArgs& a, const Turns& turns) {
   const int64_t blocks = (a.rows + rows_block - 1) / rows_block;
   const auto run = [&](auto kern) {
     return launch_pdl(ctx, kern, dim3((unsigned)blocks), dim3(THREADS), 0, (const T*)a.X, a.ld_x, (T*)a.Y, a.ld_y, a.rows,
-                      a.heads, a.head_dim, a.rope->rot, np, nc, a.positions, a.id64, (uint32_t)a.n_pos, rows_block, a.inverse,
+                      a.head_dim, a.rope->rot, np, Divisor(np + nc), Divisor(a.heads * (np + nc)), a.positions, a.id64, (uint32_t)a.n_pos, rows_block, a.inverse,
                       turns);
   };
   ZOACT_CUDA_TRY(vec ? run(rope_kernel<T, V, HALF>) : run(rope_kernel<T, 1, HALF>));
