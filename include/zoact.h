@@ -602,7 +602,8 @@ int zoact_rope_apply(zoact_ctx* ctx, const void* X, int dtype, int64_t rows, int
  *   the last of the keys (all of a prompt, or the new tokens behind a cache: a single token is a sequence of one query).  A row
  *   that sees no key has o = 0 and lse = -infinity.
  * shape (HOST pointer, read during the call): q and O [rows_q, heads head_dim], k and v [rows_k, kv_heads head_dim], of one dtype
- *   (FP32, BF16, FP16), rows ld elements apart; heads a multiple of kv_heads, at most 128 heads a key head; head_dim <= 256.
+ *   (FP32, BF16, FP16), rows ld elements apart; heads a multiple of kv_heads, at most 128 heads a key head; head_dim <= 256;
+ *   0 < scale <= 1e30.  O overlaps no input.
  * spans [n_seq, 4] of idtype (DEVICE): each sequence's first row of q, its number of queries, its first row of k and v, its number of
  *   keys; any number may be 0.  The rows of q are in order and do not overlap (rows between are allowed); those of k may lie in
  *   any order and be shared (a cache's slots, a common prompt), but with a gradient they too are in order and do not overlap.
@@ -615,7 +616,8 @@ int zoact_rope_apply(zoact_ctx* ctx, const void* X, int dtype, int64_t rows, int
  * zoact_attention_grad: for dO, the gradients by q, k and v, with P and delta = dO . O from the O and lse that the forward call
  *   gave:  dv = P^T dO,  dS = P (dO v^T - delta),  dq = scale dS k,  dk = scale dS^T q  (the heads of a group are summed).  Rows
  *   outside of the spans are left as they were; keys that no query sees get zeros.  Sums in fp32 in a fixed order, without
- *   atomics: the same bits on every run.  dq, dk and dv overlap no input.  It writes to the plan (delta).
+ *   atomics: the same bits on every run.  dq, dk and dv overlap no input.  It writes to the plan (delta): calls with one plan run
+ *   one after another.
  * What lies in rows outside of a sequence's spans, be it NaN or infinite, does not reach it.  Within a sequence an infinity or NaN in
  * a row of v (with a gradient: of any operand) may reach rows that do not see it.
  * 16-bit operands with head_dim a multiple of 8 up to 128 and rows that start on 16 bytes run on the tensor cores (P and dS are

@@ -909,7 +909,10 @@ static int check_attention(const zoact_attention_shape* s, attn::Shape* out) {
       s->heads / s->kv_heads > attn::MAX_REP || s->heads > (1 << 16))
     return ZOACT_ERR_UNSUPPORTED;
   *out = {s->rows_q, s->rows_k, s->n_seq, s->heads, s->kv_heads, s->head_dim, s->causal != 0};
-  return ZOACT_OK;
+  // units of work are counted in 31 bits (a unit: a row of work and a key head; the lists' most, wherever they are cut)
+  const int64_t per = attn::tile_positions(out->rep());
+  const int64_t rows = (out->rows_q / per > out->rows_k / attn::BK ? out->rows_q / per : out->rows_k / attn::BK) + out->n_seq;
+  return (rows + (1 << 16)) * out->kv_heads > 0x7fffffff ? ZOACT_ERR_UNSUPPORTED : ZOACT_OK;
 }
 
 int64_t zoact_attention_plan_bytes(zoact_ctx* ctx, const zoact_attention_shape* shape, int grad) {
@@ -939,7 +942,7 @@ static int attention_args(zoact_ctx* ctx, const zoact_attention_shape* shape, co
   attn::Shape s;
   const int st = check_attention(shape, &s);
   if (st) return st;
-  if (!plan || !aligned16(plan) || !valid_act_dtype(dtype) || !(scale > 0.f) || !(scale <= 3.4e38f)) return ZOACT_ERR_INVALID_ARG;
+  if (!plan || !aligned16(plan) || !valid_act_dtype(dtype) || !(scale > 0.f) || !(scale <= 1e30f)) return ZOACT_ERR_INVALID_ARG;
   const int64_t nq = (int64_t)s.heads * s.head_dim, nk = (int64_t)s.kv_heads * s.head_dim;
   if (!valid_rows(q, s.rows_q, nq, ld_q, dtype) || !valid_rows(k, s.rows_k, nk, ld_k, dtype) ||
       !valid_rows(v, s.rows_k, nk, ld_v, dtype) || !valid_rows(O, s.rows_q, nq, ld_o, dtype))

@@ -113,7 +113,7 @@ class ZOStep:
         # stacks: RMS normalisations as row scales of the pair forwards where the library applies them
         self.row_scales = True
         self._utc = {}
-        self._attention = None                      # after pack(): (shape, plan, positions, rope)
+        self._attention = None                      # after pack(): (shape, plan, positions, rope, spans)
         self.prepare_bases()
 
     def pack(self, lengths, rope=None, causal=True):
@@ -140,13 +140,14 @@ class ZOStep:
         shape = Z.attention_shape(rows, rows, len(spans), q.d_out // self.head_dim, k.d_out // self.head_dim, self.head_dim,
                                   causal=causal)
         plan = torch.empty(Z.zoact_attention_plan_bytes(self.ctx, shape), dtype=torch.uint8, device=self.device)
-        Z.zoact_attention_plan(self.ctx, shape, spans.to(self.device), plan)
+        spans = spans.to(self.device)
+        Z.zoact_attention_plan(self.ctx, shape, spans, plan)
         self.buf("attn", rows, q.d_out).zero_()
-        self._attention = (shape, plan, positions.to(self.device), rope)
+        self._attention = (shape, plan, positions.to(self.device), rope, spans)
 
     def _attend(self, q, k, v):
         """The mixer's output after pack(); q and k are turned in place."""
-        shape, plan, positions, rope = self._attention
+        shape, plan, positions, rope, _ = self._attention
         if rope is not None:
             both = self._bufs.get("qkv")
             if both is not None and q.data_ptr() == both.data_ptr():        # columns of one output: one call

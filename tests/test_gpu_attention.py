@@ -97,7 +97,7 @@ class Case:
         assert (gl[empty] == -np.inf).all()
         some = ~none & ~empty
         lt = es + 2.0 ** -20 + (n + 8) * F + 4 * F * np.abs(np.where(some, lse, 0))
-        assert (np.abs(gl - lse)[some] <= lt[some]).all()
+        assert (np.abs(gl[some] - lse[some]) <= lt[some]).all()
 
     def grads(self, pad=0):
         outs = []
@@ -301,6 +301,44 @@ def test_long_rows_of_work_are_cut_and_joined(ctx, dt, idt):
     clean(ctx)
     c.check_forward()
     c.check_grads(outs)
+
+
+@pytest.mark.parametrize("dt,heads,kv_heads", [("bf16", 8, 8), ("fp32", 4, 4)])
+def test_rows_behind_32_bits(ctx, dt, heads, kv_heads):
+    """A cache of more than 2^31 elements (fp32: 2^31 bytes), its last rows used, and rows of q as far apart."""
+    d = 128 if dt == "bf16" else 64
+    rows = 2 ** 31 // (kv_heads * d) + 1000 if dt == "bf16" else 2 ** 29 // (kv_heads * d) * 2 + 1000
+    cache = [torch.empty(rows, kv_heads * d, dtype=TYPES[dt], device=DEV) for _ in range(2)]
+    n, first = 300, rows - 310
+    spans = [(0, 2, first, n)]
+    small = Case(ctx, dt, heads, kv_heads, d, [(0, 2, 0, n)])
+    for t, x in zip(cache, (small.k, small.v)):
+        t[first:first + n] = x
+    shape = zo.attention_shape(2, rows, 1, heads, kv_heads, d)
+    plan = plan_of(ctx, shape, spans)
+    wide = torch.empty(2, 2 ** 31 // 2 + 64, dtype=TYPES[dt], device=DEV)
+    q = wide[:, :heads * d]
+    q.copy_(small.q)
+    zo.zoact_attention(ctx, shape, plan, q, cache[0], cache[1], small.O, lse=small.lse)
+    clean(ctx)
+    small.check_forward()
+
+
+@pytest.mark.parametrize("power", [0, 6, 12])
+def test_small_gradients_in_fp16(ctx, power):
+    """Powers of two of dO pass through: what is rounded to fp16 on the way is scaled to dO's size, so that a small dO loses
+    nothing but the last roundings below fp16's normal range."""
+    c = Case(ctx, "fp16", 4, 2, 64, packed(300, 40), grad=True)
+    c.forward()
+    small = c.dO.float() * 2.0 ** -power
+    c.dO.copy_(torch.where(small.abs() < 2.0 ** -14, torch.zeros_like(small), small))       # exact
+    part = c.grads()
+    c.dO.mul_(2.0 ** power)
+    full = c.grads()
+    clean(ctx)
+    for a, b in zip(full, part):
+        a, b = n64(a), n64(b) * 2.0 ** power
+        assert (np.abs(a - b) <= 2.0 ** -11 * np.abs(a) + 2.0 ** -24 * 2.0 ** power).all()
 
 
 def test_many_short_sequences(ctx):
