@@ -9,7 +9,7 @@ constexpr int BK = 128;                 // keys of a block of work
 constexpr int TILE = 128;               // rows of a tile: (position, head of the group) pairs, the group fastest
 constexpr int MAX_REP = 128;            // query heads of a group at most
 constexpr int MAX_DIM = 256, TC_DIM = 128;
-constexpr int SPLIT_OVER = 2;           // pieces of work an SM that long rows of work are cut for
+constexpr int SPLIT_OVER = 2;           // pieces of work an SM that long rows of work are cut for, at most
 
 // A rectangle of work: positions [q0, q0 + npos) against keys [k0, k0 + nk); position i sees the first visible(i) of them.
 // A row of work (positions of a forward or dq tile, keys of a dk / dv tile) that is cut into nparts leaves each part's sums in

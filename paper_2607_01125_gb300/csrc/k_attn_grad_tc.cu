@@ -618,13 +618,22 @@ __global__ void __launch_bounds__(THREADS, 1) dkv_tc_kernel(const __grid_constan
       const bool active = quad * 32 < w.nk, valid = key < w.nk;
       for (int i = 0; i < n; ++i, ++step) {
         const int b = step & 1;
-        ok = warp_wait(bar(sh->stat_full[b]), step >> 1 & 1, abort_flag, p.status) &&
-             warp_wait(bar(sh->s_full[0]), step & 1, abort_flag, p.status);
+        ok = warp_wait(bar(sh->stat_full[b]), step >> 1 & 1, abort_flag, p.status);
         if (!ok) break;
-        uint64_t pr[32];
+        uint64_t pr[32], st[32];
         const uint32_t s0 = t_s + lanes + half * 64, d0 = t_dp + lanes + half * 64;
-        const ulonglong2* const lse = reinterpret_cast<const ulonglong2*>(&sh->lse[b][half * 64]);          // negative, in pairs
+        // the rows' statistics (negative, in pairs) come before the sums that they go with: a read of shared memory waits behind
+        // the operands of the tensor core
+        const ulonglong2* const lse = reinterpret_cast<const ulonglong2*>(&sh->lse[b][half * 64]);
         const ulonglong2* const delta = reinterpret_cast<const ulonglong2*>(&sh->delta[b][half * 64]);
+#pragma unroll
+        for (int q = 0; q < 16; ++q) {
+          const ulonglong2 l = lse[q];
+          st[2 * q] = l.x;
+          st[2 * q + 1] = l.y;
+        }
+        ok = warp_wait(bar(sh->s_full[0]), step & 1, abort_flag, p.status);
+        if (!ok) break;
         const bool masked = visible(w, p.causal, i * P) < w.nk;
         if (active) {
           tc::tc_fence_after();
@@ -639,9 +648,8 @@ __global__ void __launch_bounds__(THREADS, 1) dkv_tc_kernel(const __grid_constan
             uint32_t y[16];
 #pragma unroll
             for (int q = 0; q < 8; ++q) {
-              const ulonglong2 l = lse[c * 8 + q];
-              const uint64_t z0 = fma2(pair_bits(x[c][4 * q], x[c][4 * q + 1]), scale2, l.x);
-              const uint64_t z1 = fma2(pair_bits(x[c][4 * q + 2], x[c][4 * q + 3]), scale2, l.y);
+              const uint64_t z0 = fma2(pair_bits(x[c][4 * q], x[c][4 * q + 1]), scale2, st[c * 16 + 2 * q]);
+              const uint64_t z1 = fma2(pair_bits(x[c][4 * q + 2], x[c][4 * q + 3]), scale2, st[c * 16 + 2 * q + 1]);
               pr[c * 16 + 2 * q] = pair(ex2(lo(z0)), ex2(hi(z0)));
               pr[c * 16 + 2 * q + 1] = pair(ex2(lo(z1)), ex2(hi(z1)));
             }
@@ -664,6 +672,12 @@ __global__ void __launch_bounds__(THREADS, 1) dkv_tc_kernel(const __grid_constan
         }
         __syncwarp();
         if (lane == 0) tc::mbar_arrive(bar(sh->p_full));
+#pragma unroll
+        for (int q = 0; q < 16; ++q) {
+          const ulonglong2 d = delta[q];
+          st[2 * q] = d.x;
+          st[2 * q + 1] = d.y;
+        }
         ok = warp_wait(bar(sh->dp_full), step & 1, abort_flag, p.status);
         if (!ok) break;
         if (active) {
@@ -676,9 +690,8 @@ __global__ void __launch_bounds__(THREADS, 1) dkv_tc_kernel(const __grid_constan
             ld_use(x);
 #pragma unroll
             for (int q = 0; q < 8; ++q) {
-              const ulonglong2 d = delta[c * 8 + q];
-              uint64_t v0 = mul2(pr[c * 16 + 2 * q], add2(pair_bits(x[4 * q], x[4 * q + 1]), d.x));
-              uint64_t v1 = mul2(pr[c * 16 + 2 * q + 1], add2(pair_bits(x[4 * q + 2], x[4 * q + 3]), d.y));
+              uint64_t v0 = mul2(pr[c * 16 + 2 * q], add2(pair_bits(x[4 * q], x[4 * q + 1]), st[c * 16 + 2 * q]));
+              uint64_t v1 = mul2(pr[c * 16 + 2 * q + 1], add2(pair_bits(x[4 * q + 2], x[4 * q + 3]), st[c * 16 + 2 * q + 1]));
               if (!BF16) {
                 v0 = mul2(v0, ds2);
                 v1 = mul2(v1, ds2);

@@ -16,6 +16,9 @@ constexpr int THREADS = 1024, BINS = 1024;
 // Steps that rows of work are not cut below: a step takes 0.6 to 1.2 us, and a part's sums 4 to 8 us to be left and joined (few
 // rows: 2 us).
 __device__ constexpr int min_steps(int list) { return list == LIST_FWD ? 4 : 12; }
+// Shares of an SM's part of all steps that rows of work are cut to: halves even out a list that has few long rows; dk and dv, whose
+// parts leave twice the sums, are only cut where a row is longer than all that an SM has to do.
+__device__ constexpr int split_over(int list) { return list == LIST_DKV ? 1 : SPLIT_OVER; }
 
 size_t up(size_t n) { return (n + 255) / 256 * 256; }
 
@@ -177,7 +180,8 @@ __global__ void __launch_bounds__(THREADS) plan_kernel(const PlanArgs p) {
     for (int r = tid; r < rows; r += THREADS) steps += b.row_at(r, w);
     steps = block_sum(steps, sums) * p.s.kv_heads;
     // a part is no shorter than its share of the GPU: at most 2 parts of a share each, so that the slots suffice
-    const int64_t share = max((int64_t)min_steps(list), (steps + SPLIT_OVER * p.sm_count - 1) / (SPLIT_OVER * p.sm_count));
+    const int over = split_over(list) * p.sm_count;
+    const int64_t share = max((int64_t)min_steps(list), (steps + over - 1) / over);
     const bool cuts = p.s.head_dim <= TC_DIM;
     const auto parts_of = [&](int len) { return cuts && len > share ? (int)((len + share - 1) / share) : 1; };
     const auto bin_of = [&](int len, int parts) { return BINS - 1 - min((len + parts - 1) / parts, BINS - 1); };
