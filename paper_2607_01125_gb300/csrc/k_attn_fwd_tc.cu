@@ -15,6 +15,11 @@
 //
 // Warps: a TMA producer, an MMA issuer, and four for each tile's rows.  The issuer zeroes V's rows behind the last key where a
 // step of 16 would take them in (P is 0 there, and 0 times what another sequence left may not be).  Every wait is bounded.
+//
+// Measured (GB300, bf16, 32 heads on 8 of 128): 8192 tokens 386 us, 1.42 PFLOP/s of useful operations, the tensor pipe busy 64% of
+// the cycles (a step of both tiles 3150 cycles, its MMAs 2048 by themselves); 48 tokens on 820 to 16384 keys 254 us, 6.6 TB/s; 32
+// sequences of 256 50.5 us, bound by the latencies of units of one or two steps.  (Two threads a row, which agree on the maximum
+// through shared memory in 430 cycles: 8192 tokens 420 us.  O stored by warps of their own: 32 sequences of 256 55 to 61 us.)
 #include "attn_join.cuh"
 #include "attn_tc.cuh"
 
