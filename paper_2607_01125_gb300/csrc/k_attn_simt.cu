@@ -6,8 +6,8 @@
 // A block of 256 threads has a tile of M rows of (position, head of the group) pairs against M keys; a thread has M / 16 rows
 // and columns, spread 16 apart, so that its 16-byte reads of shared memory fall on different banks.  The gradient recomputes
 // P = exp(S - lse) in two passes, one over the keys for dq and one over the rows for dk and dv, so that no sum needs atomics.
-// Bound by the FMA pipes and by shared memory (12 of its cycles for 16 of FMAs): 8192 tokens of 32 heads on 8 of 128 22 ms, 25 TFLOP/s; two
-// sequences of 64 in 4 heads of 64 13 us.
+// Bound by the FMA pipes and by shared memory (12 of its cycles for 16 of FMAs): 8192 tokens of 32 heads on 8 of 128 22 ms
+// (25 TFLOP/s), two sequences of 64 in 4 heads of 64 13 us.
 #include <type_traits>
 
 #include "attn.h"
