@@ -249,46 +249,51 @@ __global__ void __launch_bounds__(THREADS) fwd_kernel(const Dev p) {
   }
 }
 
-// delta = the row sum of dO O for each (row, head), by a group of lanes that has V elements each of a pass over the head; in fp16 also
-// the largest finite |dO| (0 before).  EACH pairs of a group at a time, so that their loads are in flight together: 4096 rows of
-// 32 heads of 128 in bf16 ran at 2.9 TB/s with 8-byte loads.
+// delta = the row sum of dO O for each (row, head) of the sequences, by a group of lanes that has V elements each of a pass over the
+// head; in fp16 also the largest finite |dO| (0 before).  It runs through the items of dq, whose rows are those of the
+// sequences.  EACH pairs of a group at a time; 4096 rows of 32 heads of 128 in bf16 20 us (3.4 TB/s).
 constexpr int EACH = 4;
 template <typename T, int V>
 __global__ void __launch_bounds__(THREADS) delta_kernel(const Work work, int* status, const T* dO, int64_t ld_do, const T* O,
-                                                        int64_t ld_o, int64_t n, Divisor heads, int head_dim, int group,
+                                                        int64_t ld_o, int kv_heads, Divisor rep, int head_dim, int group,
                                                         float* delta, float* largest) {
   pdl_wait();
   pdl_trigger();
-  // the sums lie in the plan, where it has room for them
-  if (work_count(work, 1, threadIdx.x == 0 && blockIdx.x == 0 ? status : nullptr) == 0) return;
+  // (the sums lie in the plan, where it has room for them)
+  const int total = work_count(work, kv_heads, threadIdx.x == 0 && blockIdx.x == 0 ? status : nullptr);
   struct alignas(sizeof(T) * V) Vec { T v[V]; };
-  const int lane = threadIdx.x & 31, in_group = lane & (group - 1);
-  const int64_t step = (int64_t)gridDim.x * (THREADS / group);
+  const int lane = threadIdx.x & 31, in_group = lane & (group - 1), groups = THREADS / group;
+  const int heads = kv_heads * rep.d;
   float top = 0.f;
-  for (int64_t i0 = (int64_t)blockIdx.x * (THREADS / group) + threadIdx.x / group; __any_sync(0xffffffffu, i0 < n); i0 += step * EACH) {
-    float s[EACH];
+  for (int u = blockIdx.x; u < total; u += gridDim.x) {
+    const Item w = work.items[u / kv_heads];
+    if (w.part != 0) continue;
+    const int h0 = u % kv_heads * rep.d, n = w.npos * rep.d;
+    for (int e0 = threadIdx.x / group; __any_sync(0xffffffffu, e0 < n); e0 += groups * EACH) {
+      float s[EACH];
+      int64_t at[EACH];
 #pragma unroll
-    for (int e = 0; e < EACH; ++e) {
-      const int64_t i = min(i0 + e * step, n - 1);
-      int64_t r = i / heads.d;
-      int h = (int)(i - r * heads.d);
-      if (n < (1ll << 31)) r = heads.div((int)i, h);
-      const T *a = dO + r * ld_do + (int64_t)h * head_dim, *b = O + r * ld_o + (int64_t)h * head_dim;
-      s[e] = 0.f;
-      for (int d = in_group * V; d < head_dim; d += group * V) {
-        const Vec x = *reinterpret_cast<const Vec*>(a + d), y = *reinterpret_cast<const Vec*>(b + d);
+      for (int e = 0; e < EACH; ++e) {
+        int g;
+        const int64_t r = w.q0 + rep.div(min(e0 + e * groups, n - 1), g);
+        const T *a = dO + r * ld_do + (int64_t)(h0 + g) * head_dim, *b = O + r * ld_o + (int64_t)(h0 + g) * head_dim;
+        at[e] = r * heads + h0 + g;
+        s[e] = 0.f;
+        for (int d = in_group * V; d < head_dim; d += group * V) {
+          const Vec x = *reinterpret_cast<const Vec*>(a + d), y = *reinterpret_cast<const Vec*>(b + d);
 #pragma unroll
-        for (int k = 0; k < V; ++k) {
-          const float g = to_f32<T>(x.v[k]);
-          s[e] += g * to_f32<T>(y.v[k]);
-          if (std::is_same<T, __half>::value && fabsf(g) < INFINITY) top = fmaxf(top, fabsf(g));
+          for (int k = 0; k < V; ++k) {
+            const float f = to_f32<T>(x.v[k]);
+            s[e] += f * to_f32<T>(y.v[k]);
+            if (std::is_same<T, __half>::value && fabsf(f) < INFINITY) top = fmaxf(top, fabsf(f));
+          }
         }
       }
-    }
 #pragma unroll
-    for (int e = 0; e < EACH; ++e) {
-      for (int o = group / 2; o > 0; o >>= 1) s[e] += __shfl_xor_sync(0xffffffffu, s[e], o);
-      if (in_group == 0 && i0 + e * step < n) delta[i0 + e * step] = s[e];
+      for (int e = 0; e < EACH; ++e) {
+        for (int o = group / 2; o > 0; o >>= 1) s[e] += __shfl_xor_sync(0xffffffffu, s[e], o);
+        if (in_group == 0 && e0 + e * groups < n) delta[at[e]] = s[e];
+      }
     }
   }
   if (!std::is_same<T, __half>::value) return;
@@ -539,12 +544,11 @@ int delta(Ctx* ctx, const Args& a) {
   const bool vec = a.s.head_dim % V == 0 && lies(a.O, a.ld_o) && lies(a.dO, a.ld_do);
   int group = 1;                        // lanes of a head: a power of two
   while (group < 32 && group * (vec ? V : 1) < a.s.head_dim) group *= 2;
-  const int64_t n = a.s.rows_q * a.s.heads, per = EACH * THREADS / group, blocks = (n + per - 1) / per;
-  const int64_t most = (int64_t)ctx->sm_count * 8;
+  const int64_t blocks = a.at.most[LIST_DQ] * a.s.kv_heads, most = (int64_t)ctx->sm_count * 8;
   auto kern = vec ? delta_kernel<T, V> : delta_kernel<T, 1>;
   ZOACT_CUDA_TRY(launch_pdl(ctx, kern, dim3((unsigned)(blocks < most ? blocks : most)), dim3(THREADS), 0, work_of(a, LIST_DQ),
-                            ctx->d_status, (const T*)a.dO, a.ld_do, (const T*)a.O, a.ld_o, n, Divisor(a.s.heads), a.s.head_dim,
-                            group, a.delta, a.largest));
+                            ctx->d_status, (const T*)a.dO, a.ld_do, (const T*)a.O, a.ld_o, a.s.kv_heads, Divisor(a.s.rep()),
+                            a.s.head_dim, group, a.delta, a.largest));
   ++ctx->n_launch;
   return ZOACT_OK;
 }

@@ -341,6 +341,24 @@ def test_small_gradients_in_fp16(ctx, power):
         assert (np.abs(a - b) <= 2.0 ** -11 * np.abs(a) + 2.0 ** -24 * 2.0 ** power).all()
 
 
+def test_large_values_outside_of_the_sequences_cost_small_gradients_nothing(ctx):
+    """fp16: the scale of dS comes from the sequences' rows alone."""
+    spans = [(7, 60, 7, 60), (80, 50, 80, 50)]
+    got = []
+    for outside in (0.0, 60000.0, float("inf"), float("nan")):
+        c = Case(ctx, "fp16", 4, 2, 64, spans, grad=True, rows_q=140, rows_k=140)
+        c.dO.mul_(2.0 ** -10)
+        inside = torch.zeros(140, dtype=torch.bool, device=DEV)
+        inside[7:67] = inside[80:130] = True
+        c.dO[~inside] = outside
+        c.forward()
+        c.O[~inside] = outside
+        outs = c.grads()
+        clean(ctx)
+        got.append([t[inside].clone() for t in outs])
+    assert all(torch.equal(a, b) for other in got[1:] for a, b in zip(other, got[0]))
+
+
 def test_many_short_sequences(ctx):
     rng = np.random.default_rng(3)
     c = Case(ctx, "bf16", 4, 2, 64, packed(*rng.integers(0, 6, 3000)), grad=True)
