@@ -611,7 +611,7 @@ int zoact_rope_apply(zoact_ctx* ctx, const void* X, int dtype, int64_t rows, int
  *   caller, zoact_attention_plan_bytes bytes, 16-byte aligned; the gradient's with grad != 0, which serve the forward pass too).
  *   One plan serves every layer of a batch; it can be captured, and replayed after the spans have changed.  Spans outside of the
  *   rows or out of order set ZOACT_ERR_INVALID_ARG in the device status word, and calls with that plan write nothing.  So do calls
- *   with a plan of another shape, without a gradient's lists where they are needed, or of another kind of device.
+ *   with a plan of another shape, without a gradient's lists where they are needed, or made for a device with another number of SMs.
  * zoact_attention: O, and lse [rows_q, heads] fp32 (NULL: not kept).  Rows of O and lse outside of the spans are left as they were.
  * zoact_attention_grad: for dO, the gradients by q, k and v, with P and delta = dO . O from the O and lse that the forward call
  *   gave:  dv = P^T dO,  dS = P (dO v^T - delta),  dq = scale dS k,  dk = scale dS^T q  (the heads of a group are summed).  Rows
@@ -622,8 +622,8 @@ int zoact_rope_apply(zoact_ctx* ctx, const void* X, int dtype, int64_t rows, int
  * a row of v (with a gradient: of any operand) may reach rows that do not see it.
  * 16-bit operands with head_dim a multiple of 8 up to 128 and rows that start on 16 bytes run on the tensor cores (P and dS are
  * rounded to the operands' type for them, which is half a step of that type for each); others in fp32 on the CUDA cores.
- * head_dim <= 128: context scratch of about 90 MB (FP32 and 16-bit, any size of call), allocated by the first call, which comes
- * before any stream capture; graphs captured from one context share it and are replayed one after another.              */
+ * Context scratch: about 90 MB, whatever the size of a call, allocated by the first one, which comes before any stream capture;
+ * graphs captured from one context share it and are replayed one after another.              */
 typedef struct zoact_attention_shape {
   int64_t rows_q, rows_k;
   int32_t n_seq, heads, kv_heads, head_dim, causal, reserved;

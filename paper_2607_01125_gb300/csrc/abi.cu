@@ -950,7 +950,7 @@ static int attention_args(zoact_ctx* ctx, const zoact_attention_shape* shape, co
   a->s = s;
   a->plan = static_cast<const uint8_t*>(plan);
   a->at = attn::plan_layout(s, ctx->sm_count, grad);
-  a->tag = attn::plan_tag(s);
+  a->tag = attn::plan_tag(s, ctx->sm_count);
   a->q = q; a->k = k; a->v = v; a->ld_q = ld_q; a->ld_k = ld_k; a->ld_v = ld_v; a->dtype = dtype; a->scale = scale;
   a->O = const_cast<void*>(O); a->ld_o = ld_o;
   return ZOACT_OK;

@@ -34,7 +34,7 @@ constexpr int HAS_FWD = 1, HAS_GRAD = 2;
 
 // The head of a plan; the lists of items follow.
 struct Head {
-  uint64_t tag;                         // the shape that the plan is for
+  uint64_t tag;                         // the shape and the number of SMs that the plan is for
   int32_t count[LISTS];
   int32_t has;                          // HAS_FWD, HAS_GRAD; 0: the spans were refused
 };
@@ -51,7 +51,7 @@ struct Layout {
   int64_t most[LISTS];                  // items a list can have
 };
 Layout plan_layout(const Shape& s, int sm_count, int grad);
-uint64_t plan_tag(const Shape& s);
+uint64_t plan_tag(const Shape& s, int sm_count);
 inline int slot_count(int sm_count) { return 2 * SPLIT_OVER * sm_count; }
 
 // Scratch of rows of work that are cut: fixed sizes, so that no later call moves what a captured graph uses.

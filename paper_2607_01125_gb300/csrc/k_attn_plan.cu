@@ -238,9 +238,9 @@ Layout plan_layout(const Shape& s, int sm_count, int grad) {
   return l;
 }
 
-uint64_t plan_tag(const Shape& s) {
+uint64_t plan_tag(const Shape& s, int sm_count) {
   const uint64_t v[] = {(uint64_t)s.rows_q, (uint64_t)s.rows_k, (uint64_t)s.n_seq, (uint64_t)s.heads, (uint64_t)s.kv_heads,
-                        (uint64_t)s.head_dim, (uint64_t)s.causal};
+                        (uint64_t)s.head_dim, (uint64_t)s.causal, (uint64_t)sm_count};
   uint64_t h = 0x7a6f617474656e64ull;
   for (uint64_t x : v) {
     h ^= x + 0x9E3779B97F4A7C15ull;
@@ -252,7 +252,8 @@ uint64_t plan_tag(const Shape& s) {
 }
 
 int launch_plan(Ctx* ctx, const Shape& s, const void* spans, int id64, uint8_t* plan, int grad) {
-  PlanArgs p = {s, spans, id64, grad, ctx->sm_count, plan_tag(s), plan, plan_layout(s, ctx->sm_count, grad), ctx->d_status};
+  const Layout at = plan_layout(s, ctx->sm_count, grad);
+  PlanArgs p = {s, spans, id64, grad, ctx->sm_count, plan_tag(s, ctx->sm_count), plan, at, ctx->d_status};
   ZOACT_CUDA_TRY(launch_pdl(ctx, plan_kernel, dim3(1), dim3(THREADS), 0, p));
   ++ctx->n_launch;
   return ZOACT_OK;
