@@ -14,7 +14,7 @@ import torch
 import paper_2607_01125_gb300 as zo
 from oracle import decoder, graphs
 from oracle.layers import STORE_ROUNDING, rms_norm, silu
-from paper_2607_01125_gb300.model import AdaptedLinear, TokenStep, ZOStep
+from paper_2607_01125_gb300.model import AdaptedLinear, TokenStep, ZOStep, calibrate_bases
 from synth import normal
 
 pytestmark = pytest.mark.gpu
@@ -157,4 +157,24 @@ def test_mixers_come_and_go():
            for i, n in enumerate(("l1", "l2"))]
     with pytest.raises(ValueError):
         ZOStep(ctx, "toy", lin, 8, "fp32").pack([8])
+    ctx.close()
+
+
+def test_bases_calibrated_with_attention():
+    """A calibration pass of a packed stack: every basis is orthonormal, and that of o the one of attention's outputs."""
+    ctx = zo.Context(0)
+    s = stack(ctx, "bf16", 300, n_dec=1)
+    s.C.zero_()
+    s.pack([200, 100], zo.rope(HEAD))
+    x = normal((300, D), 7, DEV).to(torch.bfloat16)
+    calibrate_bases(ctx, s, x, 8)
+    torch.cuda.synchronize()
+    assert ctx.device_status() == 0
+    for l in s.linears:
+        U = n64(l.U)
+        assert np.abs(U.T @ U - np.eye(8)).max() < 1e-4
+    X = n64(s._bufs["attn"][:300])
+    vals = np.linalg.eigvalsh(X.T @ X)
+    U = n64(s.by_name["0.o"].U)
+    assert np.trace(U.T @ X.T @ X @ U) >= 0.99 * vals[-8:].sum()
     ctx.close()
