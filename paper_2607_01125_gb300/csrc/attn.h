@@ -82,7 +82,7 @@ struct Args {
   void *dq, *dk, *dv;
   int64_t ld_dq, ld_dk, ld_dv;
   float* delta;                         // [rows_q, heads], in the plan
-  float* largest;                       // |dO| (fp16), in the plan
+  float* largest;                       // [2]: |dO| and |v| (fp16), in the plan
 };
 
 // What a kernel needs of a list.

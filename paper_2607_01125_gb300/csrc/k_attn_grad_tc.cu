@@ -11,9 +11,9 @@
 //   dk, dv:  S^T, dP^T, dk, dv in TMEM.  P^T of a step is made while dk of the step before and its dP^T run, dS^T while dv and the
 //            next S^T do: the two halves of a step hide one another.
 //
-// 256 threads work on 128 rows (keys): two warpgroups with 64 columns each.  In fp16, P^T is made 2^10 larger, and dS by a power of
-// two that brings the largest |dO| to 8 .. 16 (never smaller): both keep small values out of the subnormal range, and the
-// factors leave with the result.  Rows behind a sequence's end are zeroed in shared memory where a product would sum over them.
+// 256 threads work on 128 rows (keys): two warpgroups with 64 columns each.  In fp16, P^T is made 2^10 larger, and dS by the power
+// of two that brings its bound to 2^14 .. 2^15: |dS| = P |dP - sum P dP| <= 2 P (1 - P) B <= B / 2, where B = head_dim max|dO| max|v|
+// bounds |dP|.  Both keep small values out of the subnormal range and large ones finite, and the factors leave with the result.  Rows behind a sequence's end are zeroed in shared memory where a product would sum over them.
 //
 // Measured (GB300, bf16, 32 heads on 8 of 128): 4096 tokens dq 152 us (tensor pipe 58% busy), dk and dv 219 us (53%; their rows'
 // statistics are read from shared memory beside the operands); 16 sequences of 256 36 and 38 us, bound by latencies.
@@ -43,7 +43,7 @@ struct Params {
   int* status;
   int rep, kv_heads, heads, head_dim, causal, positions;
   float scale, scale_log2;
-  const float *lse, *delta, *largest;                             // largest |dO| (fp16)
+  const float *lse, *delta, *largest;                             // largest |dO| and |v| (fp16)
   void *dq, *dk, *dv;
   int64_t ld_dq, ld_dk, ld_dv;
   int whole_q, whole_k, whole_v;                                  // rows lie on 32 bytes
@@ -69,9 +69,10 @@ template <bool BF16> struct Factors {
   float p_shift = 0.f, p_inv = 1.f, ds = 1.f, ds_inv = 1.f;       // ds: of dS from P as made
   __device__ explicit Factors(const float* largest, bool transposed) {
     if constexpr (!BF16) {
-      const float g = __ldcg(largest);
-      int e = g > 0.f ? 3 - (int)((__float_as_uint(g) >> 23) - 127u) : 0;
-      e = e < 0 ? 0 : e > 24 ? 24 : e;
+      // exponents of -24 to 15: B / 2 < 2^(6 + (eg + 1) + (ev + 1)), and e between -23 and 55
+      const float g = __ldcg(largest), v = __ldcg(largest + 1);
+      const int eg = (int)(__float_as_uint(g) >> 23) - 127, ev = (int)(__float_as_uint(v) >> 23) - 127;
+      const int e = g > 0.f && v > 0.f ? 7 - eg - ev : 0;
       const float up = __uint_as_float((uint32_t)(127 + e) << 23), down = __uint_as_float((uint32_t)(127 - e) << 23);
       p_shift = transposed ? 10.f : 0.f;
       p_inv = transposed ? 0x1p-10f : 1.f;

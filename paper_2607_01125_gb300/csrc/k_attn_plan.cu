@@ -224,16 +224,15 @@ Layout plan_layout(const Shape& s, int sm_count, int grad) {
   at += up((size_t)s.n_seq * sizeof(int));
   for (int i = 0; i < (grad ? LISTS : 1); ++i) {
     const int64_t rows = i == LIST_DKV ? s.rows_k : s.rows_q, per = i == LIST_FWD ? 2 * positions : i == LIST_DQ ? positions : BK;
-    // (parts of cut rows: at most 2 for each share of work)
+    // (parts of cut rows: at most 2 for each share of work; the sequences' rows of q, and with a gradient of k, do not overlap)
     l.most[i] = rows / per + s.n_seq + slot_count(sm_count);
-    // keys that several sequences see (not with a gradient) count once for each in no list
     l.items[i] = at;
     at += up((size_t)l.most[i] * sizeof(Item));
   }
   l.delta = at;
   if (grad) at += up((size_t)s.rows_q * s.heads * sizeof(float));
   l.largest = at;
-  if (grad) at += up(sizeof(float));
+  if (grad) at += up(2 * sizeof(float));
   l.total = at;
   return l;
 }

@@ -250,13 +250,13 @@ __global__ void __launch_bounds__(THREADS) fwd_kernel(const Dev p) {
 }
 
 // delta = the row sum of dO O for each (row, head) of the sequences, by a group of lanes that has V elements each of a pass over the
-// head; in fp16 also the largest finite |dO| (0 before).  It runs through the items of dq, whose rows are those of the
-// sequences.  EACH pairs of a group at a time; 4096 rows of 32 heads of 128 in bf16 20 us (3.4 TB/s).
+// head; in fp16 also the largest finite |dO| and |v| (0 before).  It runs through the items of dq, whose rows are those of the
+// sequences, and for v through those of dk and dv.  EACH pairs of a group at a time; 4096 rows of 32 heads of 128 in bf16 20 us (3.4 TB/s).
 constexpr int EACH = 4;
 template <typename T, int V>
 __global__ void __launch_bounds__(THREADS) delta_kernel(const Work work, int* status, const T* dO, int64_t ld_do, const T* O,
                                                         int64_t ld_o, int kv_heads, Divisor rep, int head_dim, int group,
-                                                        float* delta, float* largest) {
+                                                        float* delta, float* largest, const Work keys, const T* v, int64_t ld_v) {
   pdl_wait();
   pdl_trigger();
   // (the sums lie in the plan, where it has room for them)
@@ -296,16 +296,39 @@ __global__ void __launch_bounds__(THREADS) delta_kernel(const Work work, int* st
       }
     }
   }
-  if (!std::is_same<T, __half>::value) return;
-  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-  if (lane == 0 && top > 0.f) atomicMax(reinterpret_cast<int*>(largest), __float_as_int(top));      // above 0: ordered as integers
+  if constexpr (std::is_same<T, __half>::value) {
+    float top_v = 0.f;
+    const int total_v = work_count(keys, kv_heads, nullptr);
+    for (int u = gridDim.x - 1 - blockIdx.x; u < total_v; u += gridDim.x) {      // from the blocks that have least to do
+      const Item w = keys.items[u / kv_heads];
+      if (w.part != 0) continue;
+      const T* const a = v + (int64_t)w.k0 * ld_v + (int64_t)(u % kv_heads) * head_dim;
+#pragma unroll 4
+      for (int e = threadIdx.x / group; e < w.nk; e += groups)
+        for (int d = in_group * V; d < head_dim; d += group * V) {
+          const Vec x = *reinterpret_cast<const Vec*>(a + e * ld_v + d);
+#pragma unroll
+          for (int k = 0; k < V; ++k) {
+            const float f = fabsf(to_f32<T>(x.v[k]));
+            if (f < INFINITY) top_v = fmaxf(top_v, f);
+          }
+        }
+    }
+    for (int o = 16; o > 0; o >>= 1) {
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+      top_v = fmaxf(top_v, __shfl_xor_sync(0xffffffffu, top_v, o));
+    }
+    // (above 0: ordered as integers)
+    if (lane == 0 && top > 0.f) atomicMax(reinterpret_cast<int*>(largest), __float_as_int(top));
+    if (lane == 0 && top_v > 0.f) atomicMax(reinterpret_cast<int*>(largest + 1), __float_as_int(top_v));
+  }
 }
 
-// In fp16, the largest |dO| of the call before gives way.
+// In fp16, the largest values of the call before give way.
 __global__ void reset_kernel(const Work work, float* largest) {
   pdl_wait();
   pdl_trigger();
-  if (work_count(work, 1, nullptr) != 0) *largest = 0.f;
+  if (work_count(work, 1, nullptr) != 0) largest[0] = largest[1] = 0.f;
 }
 
 // P and dS = P (dP - delta) of a tile, from its scaled products z (times log2 e) and dP; 0 where a key is not seen.
@@ -541,14 +564,15 @@ int delta(Ctx* ctx, const Args& a) {
   }
   constexpr int V = 16 / (int)sizeof(T);
   const auto lies = [](const void* p, int64_t ld) { return (uintptr_t)p % 16 == 0 && ld % V == 0; };
-  const bool vec = a.s.head_dim % V == 0 && lies(a.O, a.ld_o) && lies(a.dO, a.ld_do);
+  const bool vec = a.s.head_dim % V == 0 && lies(a.O, a.ld_o) && lies(a.dO, a.ld_do) &&
+                   (a.dtype != ZOACT_DT_FP16 || lies(a.v, a.ld_v));
   int group = 1;                        // lanes of a head: a power of two
   while (group < 32 && group * (vec ? V : 1) < a.s.head_dim) group *= 2;
   const int64_t blocks = a.at.most[LIST_DQ] * a.s.kv_heads, most = (int64_t)ctx->sm_count * 8;
   auto kern = vec ? delta_kernel<T, V> : delta_kernel<T, 1>;
   ZOACT_CUDA_TRY(launch_pdl(ctx, kern, dim3((unsigned)(blocks < most ? blocks : most)), dim3(THREADS), 0, work_of(a, LIST_DQ),
                             ctx->d_status, (const T*)a.dO, a.ld_do, (const T*)a.O, a.ld_o, a.s.kv_heads, Divisor(a.s.rep()),
-                            a.s.head_dim, group, a.delta, a.largest));
+                            a.s.head_dim, group, a.delta, a.largest, work_of(a, LIST_DKV), (const T*)a.v, a.ld_v));
   ++ctx->n_launch;
   return ZOACT_OK;
 }

@@ -159,8 +159,8 @@ int launch(Ctx* ctx, const RopeArgs& a, const Turns& turns) {
   const int64_t blocks = (a.rows + rows_block - 1) / rows_block;
   const auto run = [&](auto kern) {
     return launch_pdl(ctx, kern, dim3((unsigned)blocks), dim3(THREADS), 0, (const T*)a.X, a.ld_x, (T*)a.Y, a.ld_y, a.rows,
-                      a.head_dim, a.rope->rot, np, Divisor(np + nc), Divisor(a.heads * (np + nc)), a.positions, a.id64, (uint32_t)a.n_pos, rows_block, a.inverse,
-                      turns);
+                      a.head_dim, a.rope->rot, np, Divisor(np + nc), Divisor(a.heads * (np + nc)), a.positions, a.id64,
+                      (uint32_t)a.n_pos, rows_block, a.inverse, turns);
   };
   ZOACT_CUDA_TRY(vec ? run(rope_kernel<T, V, HALF>) : run(rope_kernel<T, 1, HALF>));
   ++ctx->n_launch;

@@ -341,6 +341,20 @@ def test_small_gradients_in_fp16(ctx, power):
         assert (np.abs(a - b) <= 2.0 ** -11 * np.abs(a) + 2.0 ** -24 * 2.0 ** power).all()
 
 
+@pytest.mark.parametrize("dO,v", [(2.0 ** -6, 256.0), (2.0 ** -20, 30000.0), (60.0, 2.0 ** -12), (1.0, 0.0)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_gradients_of_large_and_small_values_in_fp16(ctx, dO, v, d):
+    """dO and v of one sign pattern: dP and dS are as large as they can be for their sizes, and the gradients fit."""
+    c = Case(ctx, "fp16", 4, 2, d, packed(200, 40), grad=True, std=0.5)
+    signs = (torch.arange(d, device=DEV) % 3 - 1).half()
+    c.dO.copy_(dO * signs.repeat(4) * (0.5 + rnd(5, c.nq, 1).sigmoid().half()))
+    c.v.copy_(v * signs.repeat(2) * rnd(6, c.nk, 1).sign().half())
+    c.forward()
+    outs = c.grads()
+    clean(ctx)
+    c.check_grads(outs)
+
+
 def test_large_values_outside_of_the_sequences_cost_small_gradients_nothing(ctx):
     """fp16: the scale of dS comes from the sequences' rows alone."""
     spans = [(7, 60, 7, 60), (80, 50, 80, 50)]
@@ -350,7 +364,7 @@ def test_large_values_outside_of_the_sequences_cost_small_gradients_nothing(ctx)
         c.dO.mul_(2.0 ** -10)
         inside = torch.zeros(140, dtype=torch.bool, device=DEV)
         inside[7:67] = inside[80:130] = True
-        c.dO[~inside] = outside
+        c.dO[~inside] = c.v[~inside] = outside
         c.forward()
         c.O[~inside] = outside
         outs = c.grads()
