@@ -603,7 +603,7 @@ int zoact_rope_apply(zoact_ctx* ctx, const void* X, int dtype, int64_t rows, int
  *   that sees no key has o = 0 and lse = -infinity.
  * shape (HOST pointer, read during the call): q and O [rows_q, heads head_dim], k and v [rows_k, kv_heads head_dim], of one dtype
  *   (FP32, BF16, FP16), rows ld elements apart; heads a multiple of kv_heads, at most 128 heads a key head; head_dim <= 256;
- *   0 < scale <= 1e30.  O overlaps no input.
+ *   rows_q and rows_k below 2^31 - 2^16; 0 < scale <= 1e30.  O overlaps no input.
  * spans [n_seq, 4] of idtype (DEVICE): each sequence's first row of q, its number of queries, its first row of k and v, its number of
  *   keys; any number may be 0.  The rows of q are in order and do not overlap (rows between are allowed); those of k may lie in
  *   any order and be shared (a cache's slots, a common prompt), but with a gradient they too are in order and do not overlap.

@@ -905,7 +905,9 @@ static int check_attention(const zoact_attention_shape* s, attn::Shape* out) {
   if (!s || s->rows_q < 0 || s->rows_k < 0 || s->n_seq < 0 || s->heads <= 0 || s->kv_heads <= 0 || s->head_dim <= 0 ||
       s->heads % s->kv_heads != 0)
     return ZOACT_ERR_INVALID_ARG;
-  if (s->rows_q > 0x7fffffff || s->rows_k > 0x7fffffff || s->n_seq > (1 << 24) || s->head_dim > attn::MAX_DIM ||
+  // (positions are rounded up to tiles, and counted, in 31 bits)
+  constexpr int64_t most = 0x7fffffff - (1 << 16);
+  if (s->rows_q > most || s->rows_k > most || s->n_seq > (1 << 24) || s->head_dim > attn::MAX_DIM ||
       s->heads / s->kv_heads > attn::MAX_REP || s->heads > (1 << 16))
     return ZOACT_ERR_UNSUPPORTED;
   *out = {s->rows_q, s->rows_k, s->n_seq, s->heads, s->kv_heads, s->head_dim, s->causal != 0};
@@ -938,7 +940,7 @@ static bool valid_rows(const void* p, int64_t rows, int64_t n, int64_t ld, int d
 
 static int attention_args(zoact_ctx* ctx, const zoact_attention_shape* shape, const void* plan, const void* q, int64_t ld_q,
                           const void* k, int64_t ld_k, const void* v, int64_t ld_v, int dtype, float scale, const void* O,
-                          int64_t ld_o, int grad, attn::Args* a) {
+                          int64_t ld_o, const float* lse, int grad, attn::Args* a) {
   attn::Shape s;
   const int st = check_attention(shape, &s);
   if (st) return st;
@@ -947,6 +949,7 @@ static int attention_args(zoact_ctx* ctx, const zoact_attention_shape* shape, co
   if (!valid_rows(q, s.rows_q, nq, ld_q, dtype) || !valid_rows(k, s.rows_k, nk, ld_k, dtype) ||
       !valid_rows(v, s.rows_k, nk, ld_v, dtype) || !valid_rows(O, s.rows_q, nq, ld_o, dtype))
     return ZOACT_ERR_INVALID_ARG;
+  if (lse && !aligned_to(lse, ZOACT_DT_FP32)) return ZOACT_ERR_INVALID_ARG;
   a->s = s;
   a->plan = static_cast<const uint8_t*>(plan);
   a->at = attn::plan_layout(s, ctx->sm_count, grad);
@@ -961,7 +964,7 @@ int zoact_attention(zoact_ctx* ctx, const zoact_attention_shape* shape, const vo
                     float* lse) {
   ZOACT_ENTER(ctx);
   attn::Args a = {};
-  const int st = attention_args(ctx, shape, plan, q, ld_q, k, ld_k, v, ld_v, dtype, scale, O, ld_o, 0, &a);
+  const int st = attention_args(ctx, shape, plan, q, ld_q, k, ld_k, v, ld_v, dtype, scale, O, ld_o, lse, 0, &a);
   if (st) return st;
   a.lse = lse;
   return attn::tc_supported(a, false) ? attn::launch_fwd_tc(ctx, a) : attn::launch_fwd_simt(ctx, a);
@@ -973,7 +976,7 @@ int zoact_attention_grad(zoact_ctx* ctx, const zoact_attention_shape* shape, con
                          int64_t ld_dk, void* dv, int64_t ld_dv) {
   ZOACT_ENTER(ctx);
   attn::Args a = {};
-  const int st = attention_args(ctx, shape, plan, q, ld_q, k, ld_k, v, ld_v, dtype, scale, O, ld_o, 1, &a);
+  const int st = attention_args(ctx, shape, plan, q, ld_q, k, ld_k, v, ld_v, dtype, scale, O, ld_o, lse, 1, &a);
   if (st) return st;
   const int64_t nq = (int64_t)a.s.heads * a.s.head_dim, nk = (int64_t)a.s.kv_heads * a.s.head_dim;
   if (!valid_rows(dO, a.s.rows_q, nq, ld_do, dtype) || !valid_rows(dq, a.s.rows_q, nq, ld_dq, dtype) ||

@@ -324,7 +324,8 @@ __global__ void __launch_bounds__(THREADS) delta_kernel(const Work work, int* st
   }
 }
 
-// In fp16, the largest values of the call before give way.
+// In fp16, the largest values of the call before give way.  (The last block of dk and dv could do this, without a launch: the ragged
+// fp16 gradient 71.8 us for 69.9.)
 __global__ void reset_kernel(const Work work, float* largest) {
   pdl_wait();
   pdl_trigger();

@@ -355,6 +355,28 @@ def test_gradients_of_large_and_small_values_in_fp16(ctx, dO, v, d):
     c.check_grads(outs)
 
 
+def test_a_call_leaves_nothing_to_the_next(ctx):
+    """fp16: large values, then small ones with the same plan, give what a fresh plan gives; the forward call's plan too."""
+    got = []
+    for before in (False, True):
+        c = Case(ctx, "fp16", 4, 2, 64, packed(300, 40), grad=True)
+        c.forward()
+        small = c.dO * 2.0 ** -8
+        if before:
+            c.dO.mul_(100)
+            c.v.mul_(64)
+            c.forward()
+            c.grads()
+            c.v.div_(64)
+            c.forward()
+        c.dO.copy_(small)
+        got.append(c.grads())
+        clean(ctx)
+    v = Case(ctx, "fp16", 4, 2, 64, packed(300, 40)).v
+    assert torch.equal(v, c.v)                    # times 64 and back is exact
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
 def test_large_values_outside_of_the_sequences_cost_small_gradients_nothing(ctx):
     """fp16: the scale of dS comes from the sequences' rows alone."""
     spans = [(7, 60, 7, 60), (80, 50, 80, 50)]
@@ -500,9 +522,14 @@ def test_refusals(ctx):
         with pytest.raises((ValueError, zo.ZoactError)):
             call()
             raise AssertionError(i)
-    for shape in ((1, 1, 1, 3, 2, 64), (1, 1, 1, 129, 1, 64), (1, 1, 1, 1, 1, 257), (-1, 1, 1, 1, 1, 8), (1, 1, 1, 0, 1, 8)):
+    for shape in ((1, 1, 1, 3, 2, 64), (1, 1, 1, 129, 1, 64), (1, 1, 1, 1, 1, 257), (-1, 1, 1, 1, 1, 8), (1, 1, 1, 0, 1, 8),
+                  (2 ** 31 - 100, 1, 1, 1, 1, 8), (1, 2 ** 31 - 100, 1, 1, 1, 8), (2 ** 27, 1, 1, 65536, 65536, 8)):
         with pytest.raises(ValueError):
             zo.zoact_attention_plan_bytes(ctx, zo.attention_shape(*shape))
+    # log-sum-exps that begin inside of an element
+    st = zo.load().zoact_attention(ctx.handle, s, p.data_ptr(), c.q.data_ptr(), 256, c.k.data_ptr(), 128, c.v.data_ptr(), 128, 1, 0.125,
+                                   c.O.data_ptr(), 256, c.lse.data_ptr() + 2)
+    assert st == -1
     assert ctx.launch_count() == before
     clean(ctx)
 
