@@ -120,7 +120,7 @@ class ZOStep:
         """Attention in place of a stack's mixer from now on: the T rows are sequences of these lengths, one after another, in
         each evaluation block, with rotary positions counted from each sequence's start (rope: zo.rope(...), or None).  Rows
         behind the last sequence take no part (the mixer gives zeros there).  pack(None): the mixer as before.  One plan serves
-        every decoder until the next call."""
+        every decoder until the next call (a graph captured before that call holds the old one: capture it again)."""
         if lengths is None:
             self._attention = None
             return
