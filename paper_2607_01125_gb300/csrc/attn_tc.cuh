@@ -89,6 +89,9 @@ __device__ __forceinline__ void mma_rows(bool lead, uint32_t d, uint32_t a_tmem,
              k != 0 ? 1u : accumulate);
 }
 
+// The lowest n bits (n of any size): which of 32 columns are seen, tested a bit each with the instruction's own predicates.
+__device__ __forceinline__ uint32_t first_bits(int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u; }
+
 __device__ __forceinline__ bool elect_one() {
   uint32_t is;
   asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(is));
@@ -269,25 +272,29 @@ __device__ __forceinline__ void zero_rows(uint32_t tile, int boxes, int from, in
   __syncwarp();
 }
 
-// Columns [0, n) of a thread's row of a 16-bit output, n a multiple of 8; `whole`: rows lie on 32 bytes.
-template <bool BF16>
-__device__ __forceinline__ void store_row(void* row, const float* x, int n, bool whole) {
+// Columns [0, n) of a thread's row of a 16-bit output, n a multiple of 8 up to 32; `whole`: rows lie on 32 bytes.
+__device__ __forceinline__ void store_pairs(void* row, const uint32_t* y, int n, bool whole) {
 #pragma unroll
-  for (int j = 0; j < 32; j += 16) {
-    if (j >= n) break;
-    uint32_t w[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) w[i] = pack2<BF16>(x[j + 2 * i], x[j + 2 * i + 1]);
-    char* p = static_cast<char*>(row) + 2 * j;
-    if (whole && j + 16 <= n) {
+  for (int j = 0; j < 16; j += 8) {
+    if (2 * j >= n) break;
+    char* p = static_cast<char*>(row) + 4 * j;
+    const uint32_t* w = y + j;
+    if (whole && 2 * j + 16 <= n) {
       asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]),
                    "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
                    : "memory");
     } else {
       *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
-      if (j + 16 <= n) *reinterpret_cast<uint4*>(p + 16) = make_uint4(w[4], w[5], w[6], w[7]);
+      if (2 * j + 16 <= n) *reinterpret_cast<uint4*>(p + 16) = make_uint4(w[4], w[5], w[6], w[7]);
     }
   }
+}
+template <bool BF16>
+__device__ __forceinline__ void store_row(void* row, const float* x, int n, bool whole) {
+  uint32_t y[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) y[i] = pack2<BF16>(x[2 * i], x[2 * i + 1]);
+  store_pairs(row, y, n, whole);
 }
 
 }  // namespace tcx

@@ -278,13 +278,14 @@ __global__ void __launch_bounds__(THREADS, 1) fwd_tc_kernel(const __grid_constan
     const int t = (warp - 4) >> 2, quad = warp & 3, row = quad * 32 + lane;
     const uint32_t lanes = (uint32_t)(quad * 32) << 16;
     const uint32_t ts = tmem + lanes + (uint32_t)(t * BK), to = tmem + lanes + (uint32_t)((2 + t) * BK);
-    const int D = p.head_dim, pos = row / p.rep;
+    const int D = p.head_dim, pos = row / p.rep, in_group = row - pos * p.rep;
     const uint64_t scale2 = pair(p.scale_log2, p.scale_log2);
     constexpr float SHIFT = BF16 ? 0.f : 7.f;
     uint32_t steps = 0, merges = 0, joins = 0;
     bool ok = true;
-    for (Units U(p.work, total); ok && U.here(); U.next()) {
-      const Item& w = U.w;
+    Units U(p.work, total);
+    while (ok && U.here()) {
+      const Item w = U.w;
       const int h = U.h;
       const Tiles T(w, p);
       const int rows = T.npos(t) * p.rep;
@@ -308,10 +309,12 @@ __global__ void __launch_bounds__(THREADS, 1) fwd_tc_kernel(const __grid_constan
           if (all_see < first + BK) {
             const int lim = see - first;
 #pragma unroll
-            for (int c = 0; c < 4; ++c)
+            for (int c = 0; c < 4; ++c) {
+              const uint32_t seen = first_bits(lim - c * 32);
 #pragma unroll
               for (int i = 0; i < 32; ++i)
-                if (c * 32 + i >= lim) x[c][i] = 0xff800000u;             // -inf
+                if (!(seen & 1u << i)) x[c][i] = 0xff800000u;             // -inf
+            }
           }
           float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
@@ -376,14 +379,49 @@ __global__ void __launch_bounds__(THREADS, 1) fwd_tc_kernel(const __grid_constan
         }
       }
       if (!ok) break;
-      // ---- the unit's rows ----
+      // ---- the unit's rows: what does not need O comes before the wait for it, the next unit's item too ----
       const float base2 = m == -INFINITY ? m : m - SHIFT;                 // log2 of the sums' unit
-      if (T.n(t) > 0) {
+      const bool have = T.n(t) > 0, merging = T.halves && T.n(1) > 0, cut = w.nparts > 1;
+      U.next();
+      if (have && !merging && !cut) {
+        const int64_t r = w.q0 + T.pos0(t) + pos;
+        uint16_t* const out = static_cast<uint16_t*>(p.O) + r * p.ld_o + (int64_t)(h * p.rep + in_group) * D;
+        const bool some = l != 0.f;                                       // (a row that saw nothing: 0, whatever its lane held)
+        const uint32_t keep = some ? 0xffffffffu : 0u;
+        const float inv = some ? 1.f / l : 0.f;
+        const uint64_t inv2 = pair(inv, inv);
+        if (valid && p.lse) p.lse[r * p.heads + h * p.rep + in_group] = some ? (base2 + log2f(l)) * 0.69314718f : -INFINITY;
+        ok = warp_wait(bar(sh.pv_done[t]), (steps & 1) ^ 1u, abort_flag, p.status);
+        if (!ok) break;
+        if (active) {
+          tc::tc_fence_after();
+#pragma unroll 1
+          for (int c = 0; c < D; c += 64) {
+            uint32_t o[2][32];
+            ld32(to + c, o[0]);
+            ld32(to + c + 32, o[1]);
+            ld_wait();
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              ld_use(o[k]);
+              uint32_t y[16];
+#pragma unroll
+              for (int i = 0; i < 16; ++i) {
+                const uint64_t z = mul2(pair_bits(o[k][2 * i], o[k][2 * i + 1]), inv2);
+                y[i] = pack2<BF16>(lo(z), hi(z)) & keep;
+              }
+              if (valid) store_pairs(out + c + 32 * k, y, min(32, D - c - 32 * k), p.whole);
+            }
+          }
+          tc::tc_fence_before();
+        }
+        continue;
+      }
+      if (have) {
         ok = warp_wait(bar(sh.pv_done[t]), (steps & 1) ^ 1u, abort_flag, p.status);
         if (!ok) break;
         tc::tc_fence_after();
       }
-      const bool have = T.n(t) > 0;
       const auto o_chunk = [&](int c, float* v) {                         // 32 columns of O (of all lanes)
         uint32_t o[32];
         ld32(to + c, o);
@@ -394,7 +432,6 @@ __global__ void __launch_bounds__(THREADS, 1) fwd_tc_kernel(const __grid_constan
       };
       float* const mg = p.merge + ((size_t)blockIdx.x * TILE + row) * TC_DIM;
       float2* const mgs = p.merge_stat + (size_t)blockIdx.x * TILE + row;
-      const bool merging = T.halves && T.n(1) > 0;
       if (t == 1 && T.halves) {
         if (merging) {                                                    // this half goes to the first tile's warps
           ok = warp_wait(bar(sh.merge_empty), (merges & 1) ^ 1u, abort_flag, p.status);
@@ -433,7 +470,6 @@ __global__ void __launch_bounds__(THREADS, 1) fwd_tc_kernel(const __grid_constan
         }
       }
       const int first_slot = w.slot + h * w.nparts, row0 = t * TILE;      // rows of a slot: the tiles' one after another
-      const bool cut = w.nparts > 1;
       const float inv = cut ? 1.f : sum == 0.f ? 0.f : 1.f / sum;
       const auto out_at = [&](int r, int d) {                             // r: row of the tile
         const int ps = r / p.rep;
