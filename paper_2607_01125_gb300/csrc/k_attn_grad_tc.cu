@@ -252,7 +252,7 @@ __global__ void __launch_bounds__(THREADS, 1) dq_tc_kernel(const __grid_constant
           const int keys = min(BK, w.nk - j * BK);
           if (keys % 16 != 0) zero_rows(slot(s), G::BOXES, keys, (keys + 15) / 16 * 16, lane);
           tc::tc_fence_after();
-          mma_cols<DP / 16>(lead, t_s + ((step + j) & 1) * BK, slot(q_slot), slot(s), id_s, ksteps);
+          mma_cols<DP / 16, false>(lead, t_s + ((step + j) & 1) * BK, slot(q_slot), slot(s), id_s, ksteps);
           commit(lead, bar(sh->s_full[(step + j) & 1]));
           if (j == n - 1) commit(lead, bar(sh->empty[q_slot]));
           any = true;
@@ -263,7 +263,7 @@ __global__ void __launch_bounds__(THREADS, 1) dq_tc_kernel(const __grid_constant
           if (!warp_wait(bar(sh->full[s]), ring.parity(s) ^ vs.wrapped, abort_flag, p.status)) return false;
           vs.move(2, len);
           tc::tc_fence_after();
-          mma_cols<DP / 16>(lead, t_dp, slot(g_slot), slot(s), id_s, ksteps);
+          mma_cols<DP / 16, false>(lead, t_dp, slot(g_slot), slot(s), id_s, ksteps);
           commit(lead, bar(sh->dp_full));
           commit(lead, bar(sh->empty[s]));
           if (j == n - 1) commit(lead, bar(sh->empty[g_slot]));
@@ -280,7 +280,7 @@ __global__ void __launch_bounds__(THREADS, 1) dq_tc_kernel(const __grid_constant
           const uint32_t s = ring.at(kq.i);
           kq.move(2, len);
           const int keys = min(BK, w.nk - j * BK);
-          mma_rows<64>(lead, t_dq, t_s + ((step + j) & 1) * BK, slot(s), id_q, (keys + 15) / 16, j != 0);
+          mma_rows<64, false>(lead, t_dq, t_s + ((step + j) & 1) * BK, slot(s), id_q, (keys + 15) / 16, j != 0);
           commit(lead, bar(sh->empty[s]));
           if (j == n - 1) commit(lead, bar(sh->acc_full));
           if (j + 2 < n) ok = product_s(j + 2);
@@ -321,7 +321,7 @@ __global__ void __launch_bounds__(THREADS, 1) dq_tc_kernel(const __grid_constant
       const Item& w = U.w;
       const int h = U.h, n = (w.nk + BK - 1) / BK, rows = w.npos * p.rep;
       const bool active = quad * 32 < rows, valid = row < rows;
-      const int see = valid ? visible(w, p.causal, pos) : 0, all_see = visible(w, p.causal, 0);
+      const int see = valid ? visible<int>(w, p.causal, pos) : 0, all_see = visible<int>(w, p.causal, 0);
       const float lse2 = lse_next * 1.44269504f;
       const uint64_t lse22 = pair(-lse2, -lse2), delta2 = pair(-delta_next, -delta_next);
       for (int j = 0; j < n; ++j, ++step) {
@@ -537,7 +537,7 @@ __global__ void __launch_bounds__(THREADS, 1) dkv_tc_kernel(const __grid_constan
           if (rows != up) zero_rows(slot(s), G::BOXES, rows, up, lane);
           tc::tc_fence_after();
           const uint32_t own = g ? v_slot : k_slot;
-          mma_cols<DP / 16>(lead, g ? t_dp : t_s, slot(own), slot(s), tc::idesc_f16(BK, up, BF16), ksteps);
+          mma_cols<DP / 16, false>(lead, g ? t_dp : t_s, slot(own), slot(s), tc::idesc_f16(BK, up, BF16), ksteps);
           commit(lead, g ? bar(sh->dp_full) : bar(sh->s_full[0]));
           if (i == n - 1) commit(lead, bar(sh->empty[own]));
           any = true;
@@ -548,7 +548,7 @@ __global__ void __launch_bounds__(THREADS, 1) dkv_tc_kernel(const __grid_constan
           const uint32_t s = ring.at(c.i);
           c.move(2, len);
           tc::tc_fence_after();
-          mma_rows<64>(lead, g ? t_dv : t_dk, g ? t_s : t_dp, slot(s), id_d, (rows_of(i) + 15) / 16, i != 0);
+          mma_rows<64, false>(lead, g ? t_dv : t_dk, g ? t_s : t_dp, slot(s), id_d, (rows_of(i) + 15) / 16, i != 0);
           commit(lead, bar(sh->empty[s]));
           if (!g && i == n - 1) commit(lead, bar(sh->acc_full));
         };
@@ -638,7 +638,7 @@ __global__ void __launch_bounds__(THREADS, 1) dkv_tc_kernel(const __grid_constan
         }
         ok = warp_wait(bar(sh->s_full[0]), step & 1, abort_flag, p.status);
         if (!ok) break;
-        const bool masked = visible(w, p.causal, i * P) < w.nk;
+        const bool masked = visible<int>(w, p.causal, i * P) < w.nk;
         if (active) {
           tc::tc_fence_after();
           uint32_t x[2][32];
