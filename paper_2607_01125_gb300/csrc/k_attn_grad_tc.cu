@@ -150,6 +150,28 @@ __device__ __forceinline__ void put_part(float* d, const float* v, int n) {
     if (i < n) *reinterpret_cast<float4*>(d + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
 }
 
+// A thread's half row of a result, times f, from TMEM to `out`; n: columns of it, which may be fewer than the half.
+template <int HALF, bool BF16>
+__device__ __forceinline__ void store_half(uint32_t taddr, float f, uint16_t* out, int n, bool valid, bool whole) {
+  constexpr int PARTS = HALF / 32;
+  uint32_t o[PARTS][32];
+  const uint64_t f2 = pair(f, f);
+#pragma unroll
+  for (int k = 0; k < PARTS; ++k) ld32(taddr + 32 * k, o[k]);
+  ld_wait();
+#pragma unroll
+  for (int k = 0; k < PARTS; ++k) {
+    ld_use(o[k]);
+    uint32_t y[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const uint64_t z = mul2(pair_bits(o[k][2 * i], o[k][2 * i + 1]), f2);
+      y[i] = pack2<BF16>(lo(z), hi(z));
+    }
+    if (valid) store_pairs(out + 32 * k, y, min(32, n - 32 * k), whole);
+  }
+}
+
 template <int DP, bool BF16>
 __global__ void __launch_bounds__(THREADS, 1) dq_tc_kernel(const __grid_constant__ Maps tm, const __grid_constant__ Params p) {
   using G = Cfg<DP>;
@@ -317,8 +339,8 @@ __global__ void __launch_bounds__(THREADS, 1) dq_tc_kernel(const __grid_constant
     Units U(p.work, total);
     float lse_next = 0.f, delta_next = 0.f;
     if (U.here()) stat_of(U.w, U.h, lse_next, delta_next);
-    for (; ok && U.here(); U.next()) {
-      const Item& w = U.w;
+    while (ok && U.here()) {
+      const Item w = U.w;
       const int h = U.h, n = (w.nk + BK - 1) / BK, rows = w.npos * p.rep;
       const bool active = quad * 32 < rows, valid = row < rows;
       const int see = valid ? visible<int>(w, p.causal, pos) : 0, all_see = visible<int>(w, p.causal, 0);
@@ -381,17 +403,25 @@ __global__ void __launch_bounds__(THREADS, 1) dq_tc_kernel(const __grid_constant
         if (lane == 0) tc::mbar_arrive(bar(sh->ds_full));
       }
       if (!ok) break;
-      if (U.next_u >= 0) stat_of(U.next_w, U.next_h, lse_next, delta_next);
+      // (the next unit's item and statistics are on their way before the wait for dq)
+      U.next();
+      if (U.here()) stat_of(U.w, U.h, lse_next, delta_next);
+      const float out_f = p.scale * f.ds_inv;
+      const bool cut = w.nparts > 1;
+      uint16_t* const dq = static_cast<uint16_t*>(p.dq);
+      uint16_t* const out = dq + (int64_t)(w.q0 + pos) * p.ld_dq + (int64_t)(h * p.rep + in_group) * D;
       if (n > 0) {
         ok = warp_wait(bar(sh->acc_full), units & 1, abort_flag, p.status);
         if (!ok) break;
         ++units;
         tc::tc_fence_after();
+        if (!cut) {
+          if (active) store_half<G::HALF, BF16>(t_dq + lanes + half * G::HALF, out_f, out + half * G::HALF, D - half * G::HALF, valid, p.whole_q);
+          tc::tc_fence_before();
+          continue;
+        }
       }
-      const float out_f = p.scale * f.ds_inv;
-      const bool cut = w.nparts > 1;
       const int first = w.slot + h * w.nparts;
-      uint16_t* const dq = static_cast<uint16_t*>(p.dq);
       if (active) {
 #pragma unroll 1
         for (int c = half * G::HALF; c < min(D, (half + 1) * G::HALF); c += 32) {
@@ -404,7 +434,7 @@ __global__ void __launch_bounds__(THREADS, 1) dq_tc_kernel(const __grid_constant
           }
           if (!valid) continue;
           if (cut) put_part(slot_sums(p.slots, first + w.part) + (size_t)row * D + c, v, D - c);
-          else store_row<BF16>(dq + (int64_t)(w.q0 + pos) * p.ld_dq + (int64_t)(h * p.rep + in_group) * D + c, v, min(32, D - c), p.whole_q);
+          else store_row<BF16>(out + c, v, min(32, D - c), p.whole_q);
         }
       }
       tc::tc_fence_before();
@@ -616,8 +646,9 @@ __global__ void __launch_bounds__(THREADS, 1) dkv_tc_kernel(const __grid_constan
     const uint64_t scale2 = pair(p.scale_log2, p.scale_log2), ds2 = pair(f.ds, f.ds);
     uint32_t step = 0, units = 0, joins = 0;
     bool ok = true;
-    for (Units U(p.work, total); ok && U.here(); U.next()) {
-      const Item& w = U.w;
+    Units U(p.work, total);
+    while (ok && U.here()) {
+      const Item w = U.w;
       const int h = U.h, n = (w.npos + P - 1) / P;
       const bool active = quad * 32 < w.nk, valid = key < w.nk;
       for (int i = 0; i < n; ++i, ++step) {
@@ -715,17 +746,28 @@ __global__ void __launch_bounds__(THREADS, 1) dkv_tc_kernel(const __grid_constan
         }
       }
       if (!ok) break;
+      U.next();
+      const float fk = p.scale * f.ds_inv, fv = f.p_inv;
+      const bool cut = w.nparts > 1;
+      uint16_t* const dk = static_cast<uint16_t*>(p.dk) + (int64_t)w.k0 * p.ld_dk + (int64_t)h * D;
+      uint16_t* const dv = static_cast<uint16_t*>(p.dv) + (int64_t)w.k0 * p.ld_dv + (int64_t)h * D;
       if (n > 0) {
+        const int c = half * G::HALF;
+        uint16_t *const to_k = dk + (int64_t)key * p.ld_dk + c, *const to_v = dv + (int64_t)key * p.ld_dv + c;
         ok = warp_wait(bar(sh->acc_full), units & 1, abort_flag, p.status);
         if (!ok) break;
         ++units;
         tc::tc_fence_after();
+        if (!cut) {
+          if (active) {
+            store_half<G::HALF, BF16>(t_dv + lanes + c, fv, to_v, D - c, valid, p.whole_v);
+            store_half<G::HALF, BF16>(t_dk + lanes + c, fk, to_k, D - c, valid, p.whole_k);
+          }
+          tc::tc_fence_before();
+          continue;
+        }
       }
-      const float fk = p.scale * f.ds_inv, fv = f.p_inv;
-      const bool cut = w.nparts > 1;
       const int first = w.slot + h * w.nparts;
-      uint16_t* const dk = static_cast<uint16_t*>(p.dk) + (int64_t)w.k0 * p.ld_dk + (int64_t)h * D;
-      uint16_t* const dv = static_cast<uint16_t*>(p.dv) + (int64_t)w.k0 * p.ld_dv + (int64_t)h * D;
       if (active) {
 #pragma unroll 1
         for (int c = half * G::HALF; c < min(D, (half + 1) * G::HALF); c += 32) {
