@@ -16,10 +16,12 @@
 // Warps: a TMA producer, an MMA issuer, and four for each tile's rows.  The issuer zeroes V's rows behind the last key where a
 // step of 16 would take them in (P is 0 there, and 0 times what another sequence left may not be).  Every wait is bounded.
 //
-// Measured (GB300, bf16, 32 heads on 8 of 128): 8192 tokens 386 us, 1.42 PFLOP/s of useful operations, the tensor pipe busy 64% of
-// the cycles (a step of both tiles 3150 cycles, its MMAs 2048 by themselves); 48 tokens on 820 to 16384 keys 254 us, 6.6 TB/s; 32
-// sequences of 256 50.5 us, bound by the latencies of units of one or two steps.  (Two threads a row, which agree on the maximum
-// through shared memory in 430 cycles: 8192 tokens 420 us.  O stored by warps of their own: 32 sequences of 256 55 to 61 us.)
+// Measured (GB300, bf16, 32 heads on 8 of 128): 8192 tokens 365 us, 1.51 PFLOP/s of useful operations, the tensor pipe busy 69% of
+// the cycles; 48 tokens on 820 to 16384 keys 250 to 254 us, 6.7 TB/s; 32 sequences of 256 45.6 us, in units of one or two steps
+// whose row warps are never idle: 2700 of a unit's 9000 cycles are its softmax, 3000 its way out.  (Against the same
+// kernel then: two threads a row, which agree on the maximum through shared memory in 430 cycles, 8192 tokens 420 us for 386; O stored
+// by warps of their own 55 to 61 for 50.5; O's rows made whole lines through shared memory, in the place of Q 52.6 for
+// 45.6, with a slot fewer 44.6, but ragged sequences 117 for 115.5.)
 #include "attn_join.cuh"
 #include "attn_tc.cuh"
 

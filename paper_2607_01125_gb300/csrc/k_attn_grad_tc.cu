@@ -12,11 +12,12 @@
 //            next S^T do: the two halves of a step hide one another.
 //
 // 256 threads work on 128 rows (keys): two warpgroups with 64 columns each.  In fp16, P^T is made 2^10 larger, and dS by the power
-// of two that brings its bound to 2^14 .. 2^15: |dS| = P |dP - sum P dP| <= 2 P (1 - P) B <= B / 2, where B = head_dim max|dO| max|v|
-// bounds |dP|.  Both keep small values out of the subnormal range and large ones finite, and the factors leave with the result.  Rows behind a sequence's end are zeroed in shared memory where a product would sum over them.
+// of two that brings its bound to 2^14 .. 2^15: |dS| = P |dP - sum P dP| <= 2 P (1 - P) B <= B / 2, where
+// B = head_dim max|dO| max|v| bounds |dP|.  Both keep small values out of the subnormal range and large ones finite, and the
+// factors leave with the result.  Rows behind a sequence's end are zeroed in shared memory where a product would sum over them.
 //
-// Measured (GB300, bf16, 32 heads on 8 of 128): 4096 tokens dq 152 us (tensor pipe 58% busy), dk and dv 219 us (53%; their rows'
-// statistics are read from shared memory beside the operands); 16 sequences of 256 36 and 38 us, bound by latencies.
+// Measured (GB300, bf16, 32 heads on 8 of 128): 4096 tokens dq 153 us (tensor pipe 58% busy), dk and dv 213 us (55%; their rows'
+// statistics are read from shared memory beside the operands); 16 sequences of 256 36 and 37 us, bound by latencies.
 #include "attn_join.cuh"
 #include "attn_tc.cuh"
 
@@ -416,7 +417,8 @@ __global__ void __launch_bounds__(THREADS, 1) dq_tc_kernel(const __grid_constant
         ++units;
         tc::tc_fence_after();
         if (!cut) {
-          if (active) store_half<G::HALF, BF16>(t_dq + lanes + half * G::HALF, out_f, out + half * G::HALF, D - half * G::HALF, valid, p.whole_q);
+          const int c = half * G::HALF;
+          if (active) store_half<G::HALF, BF16>(t_dq + lanes + c, out_f, out + c, D - c, valid, p.whole_q);
           tc::tc_fence_before();
           continue;
         }

@@ -251,7 +251,8 @@ __global__ void __launch_bounds__(THREADS) fwd_kernel(const Dev p) {
 
 // delta = the row sum of dO O for each (row, head) of the sequences, by a group of lanes that has V elements each of a pass over the
 // head; in fp16 also the largest finite |dO| and |v| (0 before).  It runs through the items of dq, whose rows are those of the
-// sequences, and for v through those of dk and dv.  EACH pairs of a group at a time; 4096 rows of 32 heads of 128 in bf16 20 us (3.4 TB/s).
+// sequences, and for v through those of dk and dv.  EACH pairs of a group at a time; 4096 rows of 32 heads of 128 in bf16 20 us
+// (3.4 TB/s).
 constexpr int EACH = 4;
 template <typename T, int V>
 __global__ void __launch_bounds__(THREADS) delta_kernel(const Work work, int* status, const T* dO, int64_t ld_do, const T* O,
