@@ -12,7 +12,7 @@
 //            next S^T do: the two halves of a step hide one another.
 //
 // 256 threads work on 128 rows (keys): two warpgroups with 64 columns each.  In fp16, P^T is made 2^10 larger, and dS by the power
-// of two that brings its bound to 2^14 .. 2^15: |dS| = P |dP - sum P dP| <= 2 P (1 - P) B <= B / 2, where
+// of two that brings its bound to 2^13 .. 2^15: |dS| = P |dP - sum P dP| <= 2 P (1 - P) B <= B / 2, where
 // B = head_dim max|dO| max|v| bounds |dP|.  Both keep small values out of the subnormal range and large ones finite, and the
 // factors leave with the result.  Rows behind a sequence's end are zeroed in shared memory where a product would sum over them.
 //
