@@ -65,11 +65,13 @@ constexpr int SHARED_BYTES = 2560 + 128;
 static_assert(sizeof(Shared) <= SHARED_BYTES, "barriers and statistics");
 static_assert(Cfg<128>::TILES + SHARED_BYTES <= 232448 && Cfg<64>::TILES + SHARED_BYTES <= 232448, "shared memory");
 
-// Powers of two that P and dS are made larger by, and their inverses.
+// Powers of two that P and dS are made larger by, and their inverses.  `largest` lies in the plan behind its lists, where a plan that
+// was refused may have no room for it: it is only read where the plan has units for this kernel.
 template <bool BF16> struct Factors {
   float p_shift = 0.f, p_inv = 1.f, ds = 1.f, ds_inv = 1.f;       // ds: of dS from P as made
-  __device__ explicit Factors(const float* largest, bool transposed) {
+  __device__ Factors(const float* largest, int units, bool transposed) {
     if constexpr (!BF16) {
+      if (units == 0) return;
       // exponents of -24 to 15: B / 2 < 2^(6 + (eg + 1) + (ev + 1)), and e between -23 and 55
       const float g = __ldcg(largest), v = __ldcg(largest + 1);
       const int eg = (int)(__float_as_uint(g) >> 23) - 127, ev = (int)(__float_as_uint(v) >> 23) - 127;
@@ -325,7 +327,7 @@ __global__ void __launch_bounds__(THREADS, 1) dq_tc_kernel(const __grid_constant
     const int half = (warp - 4) >> 2, quad = warp & 3, row = quad * 32 + lane, rwarp = warp - 4;
     const uint32_t lanes = (uint32_t)(quad * 32) << 16;
     const int D = p.head_dim, pos = row / p.rep, in_group = row - pos * p.rep;
-    const Factors<BF16> f(p.largest, false);
+    const Factors<BF16> f(p.largest, total, false);
     const uint64_t scale2 = pair(p.scale_log2, p.scale_log2), ds2 = pair(f.ds, f.ds);
     uint32_t step = 0, units = 0, joins = 0;
     bool ok = true;
@@ -609,7 +611,7 @@ __global__ void __launch_bounds__(THREADS, 1) dkv_tc_kernel(const __grid_constan
       }
     } else if (warp == 2) {
       // ---------------- the rows' statistics, two steps ahead ----------------
-      const Factors<BF16> f(p.largest, true);
+      const Factors<BF16> f(p.largest, total, true);
       uint32_t step = 0;
       bool ok = true;
       for (Units U(p.work, total); ok && U.here(); U.next()) {
@@ -644,7 +646,7 @@ __global__ void __launch_bounds__(THREADS, 1) dkv_tc_kernel(const __grid_constan
     const int half = (warp - 4) >> 2, quad = warp & 3, key = quad * 32 + lane, rwarp = warp - 4;
     const uint32_t lanes = (uint32_t)(quad * 32) << 16;
     const int D = p.head_dim;
-    const Factors<BF16> f(p.largest, true);
+    const Factors<BF16> f(p.largest, total, true);
     const uint64_t scale2 = pair(p.scale_log2, p.scale_log2), ds2 = pair(f.ds, f.ds);
     uint32_t step = 0, units = 0, joins = 0;
     bool ok = true;
