@@ -621,7 +621,9 @@ int zoact_rope_apply(zoact_ctx* ctx, const void* X, int dtype, int64_t rows, int
  * What lies in rows outside of a sequence's spans, be it NaN or infinite, does not reach it.  Within a sequence an infinity or NaN in
  * a row of v (with a gradient: of any operand) may reach rows that do not see it.
  * 16-bit operands with head_dim a multiple of 8 up to 128 and rows that start on 16 bytes run on the tensor cores (P and dS are
- * rounded to the operands' type for them, which is half a step of that type for each); others in fp32 on the CUDA cores.
+ * rounded to the operands' type for them, which is half a step of that type for each); others in fp32 on the CUDA cores.  In fp16, dS
+ * is made larger by a power of two for each sequence and key head, from the largest finite |dO| and |v| of their rows there: its
+ * rounding is half a step of its own size, or 2^-39 of 128 max|dO| max|v| where that is more, whatever other sequences and heads hold.
  * Context scratch: about 90 MB, whatever the size of a call, allocated by the first one, which comes before any stream capture;
  * graphs captured from one context share it and are replayed one after another.              */
 typedef struct zoact_attention_shape {

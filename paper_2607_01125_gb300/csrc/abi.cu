@@ -986,7 +986,7 @@ int zoact_attention_grad(zoact_ctx* ctx, const zoact_attention_shape* shape, con
   a.lse = const_cast<float*>(lse);
   a.dO = dO; a.ld_do = ld_do; a.dq = dq; a.ld_dq = ld_dq; a.dk = dk; a.ld_dk = ld_dk; a.dv = dv; a.ld_dv = ld_dv;
   a.delta = reinterpret_cast<float*>(const_cast<uint8_t*>(a.plan) + a.at.delta);
-  a.largest = reinterpret_cast<float*>(const_cast<uint8_t*>(a.plan) + a.at.largest);
+  a.largest = reinterpret_cast<float2*>(const_cast<uint8_t*>(a.plan) + a.at.largest);
   const int sd = attn::launch_delta(ctx, a);
   if (sd) return sd;
   return attn::tc_supported(a, true) ? attn::launch_grad_tc(ctx, a) : attn::launch_grad_simt(ctx, a);

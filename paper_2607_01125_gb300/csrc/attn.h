@@ -14,10 +14,11 @@ constexpr int SPLIT_OVER = 2;           // pieces of work an SM that long rows o
 // A rectangle of work: positions [q0, q0 + npos) against keys [k0, k0 + nk); position i sees the first visible(i) of them.
 // A row of work (positions of a forward or dq tile, keys of a dk / dv tile) that is cut into nparts leaves each part's sums in
 // a slot: part p of key head h in slot + h nparts + p.
-struct Item {
+struct alignas(16) Item {
   int32_t q0, npos, k0, nk, diag, part, nparts, slot;
+  int32_t seq;                          // the sequence that the work is of
 };
-static_assert(sizeof(Item) == 32, "items are read as two 16-byte words");
+static_assert(sizeof(Item) == 48, "items are read as two 16-byte words, and the sequence where it is needed");
 
 // (rows are below 2^31 - 2^16, and 32 bits suffice; the long prompt of the forward kernel took 389 us with them for 363, the
 // gradient's short sequences 89.0 for 91.2)
@@ -85,7 +86,7 @@ struct Args {
   void *dq, *dk, *dv;
   int64_t ld_dq, ld_dk, ld_dv;
   float* delta;                         // [rows_q, heads], in the plan
-  float* largest;                       // [2]: |dO| and |v| (fp16), in the plan
+  float2* largest;                      // [n_seq, kv_heads]: |dO| of a group's heads and |v| (fp16), in the plan
 };
 
 // What a kernel needs of a list.

@@ -254,11 +254,12 @@ struct Units {
 
 __device__ __forceinline__ Item load_item(const Item* p) {
   const int4 a = reinterpret_cast<const int4*>(p)[0], b = reinterpret_cast<const int4*>(p)[1];
-  return {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+  return {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w, p->seq};
 }
 
 __device__ __forceinline__ Item uniform_item(const Item& w) {
-  return {uniform(w.q0), uniform(w.npos), uniform(w.k0), uniform(w.nk), uniform(w.diag), uniform(w.part), uniform(w.nparts), uniform(w.slot)};
+  return {uniform(w.q0), uniform(w.npos), uniform(w.k0), uniform(w.nk), uniform(w.diag), uniform(w.part), uniform(w.nparts), uniform(w.slot),
+          w.seq};
 }
 __device__ __forceinline__ void Units::next() {
   u = next_u;

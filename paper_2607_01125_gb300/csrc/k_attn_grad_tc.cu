@@ -13,8 +13,8 @@
 //
 // 256 threads work on 128 rows (keys): two warpgroups with 64 columns each.  In fp16, P^T is made 2^10 larger, and dS by the power
 // of two that brings its bound to 2^13 .. 2^15: |dS| = P |dP - sum P dP| <= 2 P (1 - P) B <= B / 2, where
-// B = head_dim max|dO| max|v| bounds |dP|.  Both keep small values out of the subnormal range and large ones finite, and the
-// factors leave with the result.  Rows behind a sequence's end are zeroed in shared memory where a product would sum over them.
+// B = head_dim max|dO| max|v| of the sequence and the group of heads bounds |dP|.  Both keep small values out of the subnormal
+// range and large ones finite, whatever other sequences hold, and the factors leave with the result.  Rows behind a sequence's end are zeroed in shared memory where a product would sum over them.
 //
 // Measured (GB300, bf16, 32 heads on 8 of 128): 4096 tokens dq 153 us (tensor pipe 58% busy), dk and dv 213 us (55%; their rows'
 // statistics are read from shared memory beside the operands); 16 sequences of 256 36 and 37 us, bound by latencies.
@@ -44,7 +44,8 @@ struct Params {
   int* status;
   int rep, kv_heads, heads, head_dim, causal, positions;
   float scale, scale_log2;
-  const float *lse, *delta, *largest;                             // largest |dO| and |v| (fp16)
+  const float *lse, *delta;
+  const float2* largest;                                          // |dO| and |v| of each sequence and key head (fp16)
   void *dq, *dk, *dv;
   int64_t ld_dq, ld_dk, ld_dv;
   int whole_q, whole_k, whole_v;                                  // rows lie on 32 bytes
@@ -65,22 +66,26 @@ constexpr int SHARED_BYTES = 2560 + 128;
 static_assert(sizeof(Shared) <= SHARED_BYTES, "barriers and statistics");
 static_assert(Cfg<128>::TILES + SHARED_BYTES <= 232448 && Cfg<64>::TILES + SHARED_BYTES <= 232448, "shared memory");
 
-// Powers of two that P and dS are made larger by, and their inverses.  `largest` lies in the plan behind its lists, where a plan that
-// was refused may have no room for it: it is only read where the plan has units for this kernel.
+// The power of two that P^T is made larger by, as an exponent, and its inverse.
+template <bool BF16> constexpr float P_SHIFT = BF16 ? 0.f : 10.f;
+template <bool BF16> constexpr float P_INV = BF16 ? 1.f : 0x1p-10f;
+
+// The largest |dO| and |v| of an item's sequence and key head.  (They lie in the plan behind its lists, where a plan that was refused
+// may have no room for them: they are read for its units alone.)
+template <bool BF16> __device__ __forceinline__ float2 largest_of(const Params& p, const Item& w, int h) {
+  return BF16 ? make_float2(0.f, 0.f) : __ldcg(&p.largest[(int64_t)w.seq * p.kv_heads + h]);
+}
+
+// The power of two that dS is made larger by, and its inverse.
 template <bool BF16> struct Factors {
-  float p_shift = 0.f, p_inv = 1.f, ds = 1.f, ds_inv = 1.f;       // ds: of dS from P as made
-  __device__ Factors(const float* largest, int units, bool transposed) {
+  float up = 1.f, down = 1.f;
+  __device__ explicit Factors(float2 largest) {
     if constexpr (!BF16) {
-      if (units == 0) return;
       // exponents of -24 to 15: B / 2 < 2^(6 + (eg + 1) + (ev + 1)), and e between -23 and 55
-      const float g = __ldcg(largest), v = __ldcg(largest + 1);
-      const int eg = (int)(__float_as_uint(g) >> 23) - 127, ev = (int)(__float_as_uint(v) >> 23) - 127;
-      const int e = g > 0.f && v > 0.f ? 7 - eg - ev : 0;
-      const float up = __uint_as_float((uint32_t)(127 + e) << 23), down = __uint_as_float((uint32_t)(127 - e) << 23);
-      p_shift = transposed ? 10.f : 0.f;
-      p_inv = transposed ? 0x1p-10f : 1.f;
-      ds = up * p_inv;
-      ds_inv = down;
+      const int eg = (int)(__float_as_uint(largest.x) >> 23) - 127, ev = (int)(__float_as_uint(largest.y) >> 23) - 127;
+      const int e = largest.x > 0.f && largest.y > 0.f ? 7 - eg - ev : 0;
+      up = __uint_as_float((uint32_t)(127 + e) << 23);
+      down = __uint_as_float((uint32_t)(127 - e) << 23);
     }
   }
 };
@@ -327,8 +332,7 @@ __global__ void __launch_bounds__(THREADS, 1) dq_tc_kernel(const __grid_constant
     const int half = (warp - 4) >> 2, quad = warp & 3, row = quad * 32 + lane, rwarp = warp - 4;
     const uint32_t lanes = (uint32_t)(quad * 32) << 16;
     const int D = p.head_dim, pos = row / p.rep, in_group = row - pos * p.rep;
-    const Factors<BF16> f(p.largest, total, false);
-    const uint64_t scale2 = pair(p.scale_log2, p.scale_log2), ds2 = pair(f.ds, f.ds);
+    const uint64_t scale2 = pair(p.scale_log2, p.scale_log2);
     uint32_t step = 0, units = 0, joins = 0;
     bool ok = true;
     // of this thread's row of an item: log-sum-exp (times log2 e) and delta
@@ -341,7 +345,11 @@ __global__ void __launch_bounds__(THREADS, 1) dq_tc_kernel(const __grid_constant
     };
     Units U(p.work, total);
     float lse_next = 0.f, delta_next = 0.f;
-    if (U.here()) stat_of(U.w, U.h, lse_next, delta_next);
+    float2 largest_next = make_float2(0.f, 0.f);
+    if (U.here()) {
+      stat_of(U.w, U.h, lse_next, delta_next);
+      largest_next = largest_of<BF16>(p, U.w, U.h);
+    }
     while (ok && U.here()) {
       const Item w = U.w;
       const int h = U.h, n = (w.nk + BK - 1) / BK, rows = w.npos * p.rep;
@@ -349,6 +357,8 @@ __global__ void __launch_bounds__(THREADS, 1) dq_tc_kernel(const __grid_constant
       const int see = valid ? visible<int>(w, p.causal, pos) : 0, all_see = visible<int>(w, p.causal, 0);
       const float lse2 = lse_next * 1.44269504f;
       const uint64_t lse22 = pair(-lse2, -lse2), delta2 = pair(-delta_next, -delta_next);
+      const Factors<BF16> f(largest_next);
+      const uint64_t ds2 = pair(f.up, f.up);
       for (int j = 0; j < n; ++j, ++step) {
         ok = warp_wait(bar(sh->s_full[step & 1]), step >> 1 & 1, abort_flag, p.status);
         if (!ok) break;
@@ -408,8 +418,11 @@ __global__ void __launch_bounds__(THREADS, 1) dq_tc_kernel(const __grid_constant
       if (!ok) break;
       // (the next unit's item and statistics are on their way before the wait for dq)
       U.next();
-      if (U.here()) stat_of(U.w, U.h, lse_next, delta_next);
-      const float out_f = p.scale * f.ds_inv;
+      if (U.here()) {
+        stat_of(U.w, U.h, lse_next, delta_next);
+        largest_next = largest_of<BF16>(p, U.w, U.h);
+      }
+      const float out_f = p.scale * f.down;
       const bool cut = w.nparts > 1;
       uint16_t* const dq = static_cast<uint16_t*>(p.dq);
       uint16_t* const out = dq + (int64_t)(w.q0 + pos) * p.ld_dq + (int64_t)(h * p.rep + in_group) * D;
@@ -611,7 +624,6 @@ __global__ void __launch_bounds__(THREADS, 1) dkv_tc_kernel(const __grid_constan
       }
     } else if (warp == 2) {
       // ---------------- the rows' statistics, two steps ahead ----------------
-      const Factors<BF16> f(p.largest, total, true);
       uint32_t step = 0;
       bool ok = true;
       for (Units U(p.work, total); ok && U.here(); U.next()) {
@@ -625,7 +637,7 @@ __global__ void __launch_bounds__(THREADS, 1) dkv_tc_kernel(const __grid_constan
             const int row = lane + 32 * k, pos = sh->pos_of[row];
             const int64_t e = (int64_t)(w.q0 + i * P + pos) * p.heads + h * p.rep + row - pos * p.rep;
             // (rows behind the last: no share)
-            lse[k] = row < rows ? f.p_shift - p.lse[e] * 1.44269504f : -INFINITY;
+            lse[k] = row < rows ? P_SHIFT<BF16> - p.lse[e] * 1.44269504f : -INFINITY;
             delta[k] = row < rows ? -p.delta[e] : 0.f;
           }
           ok = warp_wait(bar(sh->stat_empty[b]), (step >> 1 & 1) ^ 1u, abort_flag, p.status);
@@ -646,14 +658,17 @@ __global__ void __launch_bounds__(THREADS, 1) dkv_tc_kernel(const __grid_constan
     const int half = (warp - 4) >> 2, quad = warp & 3, key = quad * 32 + lane, rwarp = warp - 4;
     const uint32_t lanes = (uint32_t)(quad * 32) << 16;
     const int D = p.head_dim;
-    const Factors<BF16> f(p.largest, total, true);
-    const uint64_t scale2 = pair(p.scale_log2, p.scale_log2), ds2 = pair(f.ds, f.ds);
+    const uint64_t scale2 = pair(p.scale_log2, p.scale_log2);
     uint32_t step = 0, units = 0, joins = 0;
     bool ok = true;
     Units U(p.work, total);
+    float2 largest_next = U.here() ? largest_of<BF16>(p, U.w, U.h) : make_float2(0.f, 0.f);
     while (ok && U.here()) {
       const Item w = U.w;
       const int h = U.h, n = (w.npos + P - 1) / P;
+      const Factors<BF16> f(largest_next);
+      const float up = f.up * P_INV<BF16>;                        // of dS from P^T as made
+      const uint64_t ds2 = pair(up, up);
       const bool active = quad * 32 < w.nk, valid = key < w.nk;
       for (int i = 0; i < n; ++i, ++step) {
         const int b = step & 1;
@@ -751,7 +766,8 @@ __global__ void __launch_bounds__(THREADS, 1) dkv_tc_kernel(const __grid_constan
       }
       if (!ok) break;
       U.next();
-      const float fk = p.scale * f.ds_inv, fv = f.p_inv;
+      if (U.here()) largest_next = largest_of<BF16>(p, U.w, U.h);
+      const float fk = p.scale * f.down, fv = P_INV<BF16>;
       const bool cut = w.nparts > 1;
       uint16_t* const dk = static_cast<uint16_t*>(p.dk) + (int64_t)w.k0 * p.ld_dk + (int64_t)h * D;
       uint16_t* const dv = static_cast<uint16_t*>(p.dv) + (int64_t)w.k0 * p.ld_dv + (int64_t)h * D;

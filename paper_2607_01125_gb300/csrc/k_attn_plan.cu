@@ -73,7 +73,7 @@ struct Builder {
     const int4 s = seqs[lo];
     const int b = r - prefix[lo];
     const int64_t first = (int64_t)s.w - s.y + 1;          // keys that position 0 of the sequence sees
-    w.part = 0; w.nparts = 1; w.slot = 0;
+    w.part = 0; w.nparts = 1; w.slot = 0; w.seq = lo;
     if (list == LIST_DKV) {
       w.k0 = s.z + b * BK;
       w.nk = min(BK, s.w - b * BK);
@@ -232,7 +232,7 @@ Layout plan_layout(const Shape& s, int sm_count, int grad) {
   l.delta = at;
   if (grad) at += up((size_t)s.rows_q * s.heads * sizeof(float));
   l.largest = at;
-  if (grad) at += up(2 * sizeof(float));
+  if (grad) at += up((size_t)s.n_seq * s.kv_heads * sizeof(float2));
   l.total = at;
   return l;
 }

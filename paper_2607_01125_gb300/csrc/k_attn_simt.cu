@@ -250,14 +250,21 @@ __global__ void __launch_bounds__(THREADS) fwd_kernel(const Dev p) {
 }
 
 // delta = the row sum of dO O for each (row, head) of the sequences, by a group of lanes that has V elements each of a pass over the
-// head; in fp16 also the largest finite |dO| and |v| (0 before).  It runs through the items of dq, whose rows are those of the
-// sequences, and for v through those of dk and dv.  EACH pairs of a group at a time; 4096 rows of 32 heads of 128 in bf16 20 us
-// (3.4 TB/s).
+// head; in fp16 also the largest finite |dO| and |v| of each sequence's group of heads (0 before).  It runs through the items of dq,
+// whose rows are those of the sequences, and for v through those of dk and dv.  EACH pairs of a group at a time; 4096 rows of 32
+// heads of 128 in bf16 20 us (3.4 TB/s).
 constexpr int EACH = 4;
+
+// The largest of a warp's values goes to *to (above 0: ordered as integers).
+__device__ __forceinline__ void keep_largest(float x, float* to) {
+  for (int o = 16; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
+  if ((threadIdx.x & 31) == 0 && x > __ldcg(to)) atomicMax(reinterpret_cast<int*>(to), __float_as_int(x));
+}
+
 template <typename T, int V>
 __global__ void __launch_bounds__(THREADS) delta_kernel(const Work work, int* status, const T* dO, int64_t ld_do, const T* O,
                                                         int64_t ld_o, int kv_heads, Divisor rep, int head_dim, int group,
-                                                        float* delta, float* largest, const Work keys, const T* v, int64_t ld_v) {
+                                                        float* delta, float2* largest, const Work keys, const T* v, int64_t ld_v) {
   pdl_wait();
   pdl_trigger();
   // (the sums lie in the plan, where it has room for them)
@@ -265,11 +272,11 @@ __global__ void __launch_bounds__(THREADS) delta_kernel(const Work work, int* st
   struct alignas(sizeof(T) * V) Vec { T v[V]; };
   const int lane = threadIdx.x & 31, in_group = lane & (group - 1), groups = THREADS / group;
   const int heads = kv_heads * rep.d;
-  float top = 0.f;
   for (int u = blockIdx.x; u < total; u += gridDim.x) {
     const Item w = work.items[u / kv_heads];
     if (w.part != 0) continue;
     const int h0 = u % kv_heads * rep.d, n = w.npos * rep.d;
+    float top = 0.f;
     for (int e0 = threadIdx.x / group; __any_sync(0xffffffffu, e0 < n); e0 += groups * EACH) {
       float s[EACH];
       int64_t at[EACH];
@@ -296,14 +303,15 @@ __global__ void __launch_bounds__(THREADS) delta_kernel(const Work work, int* st
         if (in_group == 0 && e0 + e * groups < n) delta[at[e]] = s[e];
       }
     }
+    if constexpr (std::is_same<T, __half>::value) keep_largest(top, &largest[(int64_t)w.seq * kv_heads + u % kv_heads].x);
   }
   if constexpr (std::is_same<T, __half>::value) {
-    float top_v = 0.f;
     const int total_v = work_count(keys, kv_heads, nullptr);
     for (int u = gridDim.x - 1 - blockIdx.x; u < total_v; u += gridDim.x) {      // from the blocks that have least to do
       const Item w = keys.items[u / kv_heads];
       if (w.part != 0) continue;
       const T* const a = v + (int64_t)w.k0 * ld_v + (int64_t)(u % kv_heads) * head_dim;
+      float top = 0.f;
 #pragma unroll 4
       for (int e = threadIdx.x / group; e < w.nk; e += groups)
         for (int d = in_group * V; d < head_dim; d += group * V) {
@@ -311,26 +319,21 @@ __global__ void __launch_bounds__(THREADS) delta_kernel(const Work work, int* st
 #pragma unroll
           for (int k = 0; k < V; ++k) {
             const float f = fabsf(to_f32<T>(x.v[k]));
-            if (f < INFINITY) top_v = fmaxf(top_v, f);
+            if (f < INFINITY) top = fmaxf(top, f);
           }
         }
+      keep_largest(top, &largest[(int64_t)w.seq * kv_heads + u % kv_heads].y);
     }
-    for (int o = 16; o > 0; o >>= 1) {
-      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-      top_v = fmaxf(top_v, __shfl_xor_sync(0xffffffffu, top_v, o));
-    }
-    // (above 0: ordered as integers)
-    if (lane == 0 && top > 0.f) atomicMax(reinterpret_cast<int*>(largest), __float_as_int(top));
-    if (lane == 0 && top_v > 0.f) atomicMax(reinterpret_cast<int*>(largest + 1), __float_as_int(top_v));
   }
 }
 
 // In fp16, the largest values of the call before give way.  (The last block of dk and dv could do this, without a launch: the ragged
 // fp16 gradient 71.8 us for 69.9.)
-__global__ void reset_kernel(const Work work, float* largest) {
+__global__ void __launch_bounds__(THREADS) reset_kernel(const Work work, float2* largest, int64_t n) {
   pdl_wait();
   pdl_trigger();
-  if (work_count(work, 1, nullptr) != 0) largest[0] = largest[1] = 0.f;
+  if (work_count(work, 1, nullptr) == 0) return;
+  for (int64_t i = (int64_t)blockIdx.x * THREADS + threadIdx.x; i < n; i += (int64_t)gridDim.x * THREADS) largest[i] = make_float2(0.f, 0.f);
 }
 
 // P and dS = P (dP - delta) of a tile, from its scaled products z (times log2 e) and dP; 0 where a key is not seen.
@@ -561,7 +564,9 @@ int run(Ctx* ctx, const Args& a, int list) {
 template <typename T>
 int delta(Ctx* ctx, const Args& a) {
   if (a.dtype == ZOACT_DT_FP16) {
-    ZOACT_CUDA_TRY(launch_pdl(ctx, reset_kernel, dim3(1), dim3(1), 0, work_of(a, LIST_DQ), a.largest));
+    const int64_t n = (int64_t)a.s.n_seq * a.s.kv_heads, blocks = n == 0 ? 1 : (n + THREADS - 1) / THREADS;
+    ZOACT_CUDA_TRY(launch_pdl(ctx, reset_kernel, dim3((unsigned)(blocks < ctx->sm_count ? blocks : ctx->sm_count)), dim3(THREADS), 0,
+                              work_of(a, LIST_DQ), a.largest, n));
     ++ctx->n_launch;
   }
   constexpr int V = 16 / (int)sizeof(T);
