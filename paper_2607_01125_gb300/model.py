@@ -113,14 +113,19 @@ class ZOStep:
         # stacks: RMS normalisations as row scales of the pair forwards where the library applies them
         self.row_scales = True
         self._utc = {}
-        self._attention = None                      # after pack(): (shape, plan, positions, rope, spans)
+        self._attention = None                      # after pack(): (shape, plan, positions, rope)
+        self._plans = {}                            # pack()'s plans, that of the last call and those that graphs hold
         self.prepare_bases()
 
     def pack(self, lengths, rope=None, causal=True):
         """Attention in place of a stack's mixer from now on: the T rows are sequences of these lengths, one after another, in
         each evaluation block, with rotary positions counted from each sequence's start (rope: zo.rope(...), or None).  Rows
         behind the last sequence take no part (the mixer gives zeros there).  pack(None): the mixer as before.  One plan serves
-        every decoder until the next call (a graph captured before that call holds the old one: capture it again)."""
+        every decoder.
+
+        A graph captured after a call takes the sequences and positions of the last one, as long as there are as many of them
+        (lengths of 0 count) and `causal` is the same, with the rope of its capture.  After a call with another number its
+        attention is refused (the device status word; nothing is written) until one with its own comes again."""
         if lengths is None:
             self._attention = None
             return
@@ -139,15 +144,28 @@ class ZOStep:
         rows = self.nb * self.T
         shape = Z.attention_shape(rows, rows, len(spans), q.d_out // self.head_dim, k.d_out // self.head_dim, self.head_dim,
                                   causal=causal)
-        plan = torch.empty(Z.zoact_attention_plan_bytes(self.ctx, shape), dtype=torch.uint8, device=self.device)
-        spans = spans.to(self.device)
-        Z.zoact_attention_plan(self.ctx, shape, spans, plan)
+        size = Z.zoact_attention_plan_bytes(self.ctx, shape)
+        key = (len(spans), bool(causal))
+        for other in [k for k in self._plans if k != key]:
+            self._plans[other]["plan"].zero_()      # no plan: calls with it are refused
+            if not self._plans[other]["held"]:
+                del self._plans[other]
+        p = self._plans.get(key)
+        if p is None:
+            plan = torch.empty(size, dtype=torch.uint8, device=self.device)
+            p = self._plans[key] = {"plan": plan, "spans": torch.empty_like(spans, device=self.device), "held": False}
+        p["spans"].copy_(spans)
+        Z.zoact_attention_plan(self.ctx, shape, p["spans"], p["plan"])
+        at = self.buf("positions", 1, self.T, torch.int64).view(self.T)
+        at.copy_(positions)
         self.buf("attn", rows, q.d_out).zero_()
-        self._attention = (shape, plan, positions.to(self.device), rope, spans)
+        self._attention = (shape, p["plan"], at, rope)
 
     def _attend(self, q, k, v):
         """The mixer's output after pack(); q and k are turned in place."""
-        shape, plan, positions, rope, _ = self._attention
+        shape, plan, positions, rope = self._attention
+        if torch.cuda.is_current_stream_capturing():
+            self._plans[shape.n_seq, bool(shape.causal)]["held"] = True
         if rope is not None:
             both = self._bufs.get("qkv")
             if both is not None and q.data_ptr() == both.data_ptr():        # columns of one output: one call
