@@ -423,6 +423,11 @@ __global__ void __launch_bounds__(THREADS) dq_kernel(const Dev p) {
   }
 }
 
+// A row of work of dk and dv has up to 2^31 positions, with up to MAX_REP heads each: its rows are counted in 32 bits within runs of
+// POSITIONS of them (whole tiles, so that the sums' order does not depend on it).
+constexpr int POSITIONS = 4096;
+static_assert((int64_t)POSITIONS * MAX_REP + TILE <= 0x7fffffff && POSITIONS % TILE == 0, "rows of a run");
+
 template <typename T, int DP>
 __global__ void __launch_bounds__(THREADS) dkv_kernel(const Dev p) {
   constexpr int R = Cfg<DP>::R, C = Cfg<DP>::C, M = Cfg<DP>::M, LD = Cfg<DP>::LD, LP = Cfg<DP>::LP, SUB = tiles_of<DP>(BK);
@@ -437,7 +442,7 @@ __global__ void __launch_bounds__(THREADS) dkv_kernel(const Dev p) {
   for (int64_t u = blockIdx.x; u < total; u += gridDim.x) {
     const int sub = (int)(u % SUB), h = (int)(u / SUB % p.kv_heads);
     const Item w = p.work.items[u / SUB / p.kv_heads];
-    const int key0 = sub * M, n = w.npos * p.rep;
+    const int key0 = sub * M;
     if (key0 >= w.nk) continue;
     const int nk = min(M, w.nk - key0);
     __syncthreads();
@@ -448,35 +453,42 @@ __global__ void __launch_bounds__(THREADS) dkv_kernel(const Dev p) {
     for (int i = 0; i < R; ++i)
 #pragma unroll
       for (int c = 0; c < C; ++c) ok[i][c] = ov[i][c] = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int r0 = 0; r0 < n; r0 += M) {
-      __syncthreads();
-      if (visible(w, p.causal, min(r0 + M, n) / p.rep) <= key0) continue;      // none of these rows sees the keys
-      load_rows<T, DP>(sq, p.q, p.ld_q, w, h, p.by_rep, p.head_dim, p.vec, r0, n);
-      load_rows<T, DP>(sg, p.dO, p.ld_do, w, h, p.by_rep, p.head_dim, p.vec, r0, n);
-      if (tid < M) {
-        const int r = r0 + tid, pos = r / p.rep;
-        const int64_t e = (int64_t)(w.q0 + pos) * p.heads + h * p.rep + r - pos * p.rep;
-        see[tid] = r < n ? visible(w, p.causal, pos) - key0 : 0;
-        lse[tid] = r < n ? p.lse_in[e] * 1.44269504f : 0.f;
-        delta[tid] = r < n ? p.delta[e] : 0.f;
-      }
-      __syncthreads();
-      float s[R][R], dp[R][R];
-      product<DP>(sk, sq, ty, tx, s);
-      product<DP>(sv, sg, ty, tx, dp);
-#pragma unroll
-      for (int i = 0; i < R; ++i)
-#pragma unroll
-        for (int j = 0; j < R; ++j) {
-          const int key = ty + 16 * i, r = tx + 16 * j;
-          float pr, ds;
-          share_of(s[i][j] * p.scale_log2, dp[i][j], lse[r], delta[r], key < see[r], pr, ds);
-          sp[key * LP + r] = pr;
-          sd[key * LP + r] = ds;
+    for (int first = 0; first < w.npos; first += POSITIONS) {
+      Item run = w;
+      run.q0 += first;
+      run.npos = min(POSITIONS, w.npos - first);
+      run.diag += p.causal ? first : 0;
+      const int n = run.npos * p.rep;
+      for (int r0 = 0; r0 < n; r0 += M) {
+        __syncthreads();
+        if (visible(run, p.causal, min(r0 + M, n) / p.rep) <= key0) continue;      // none of these rows sees the keys
+        load_rows<T, DP>(sq, p.q, p.ld_q, run, h, p.by_rep, p.head_dim, p.vec, r0, n);
+        load_rows<T, DP>(sg, p.dO, p.ld_do, run, h, p.by_rep, p.head_dim, p.vec, r0, n);
+        if (tid < M) {
+          const int r = r0 + tid, pos = r / p.rep;
+          const int64_t e = (int64_t)(run.q0 + pos) * p.heads + h * p.rep + r - pos * p.rep;
+          see[tid] = r < n ? visible(run, p.causal, pos) - key0 : 0;
+          lse[tid] = r < n ? p.lse_in[e] * 1.44269504f : 0.f;
+          delta[tid] = r < n ? p.delta[e] : 0.f;
         }
-      __syncthreads();
-      add_product<DP>(sp, sg, ty, tx, ov);
-      add_product<DP>(sd, sq, ty, tx, ok);
+        __syncthreads();
+        float s[R][R], dp[R][R];
+        product<DP>(sk, sq, ty, tx, s);
+        product<DP>(sv, sg, ty, tx, dp);
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+#pragma unroll
+          for (int j = 0; j < R; ++j) {
+            const int key = ty + 16 * i, r = tx + 16 * j;
+            float pr, ds;
+            share_of(s[i][j] * p.scale_log2, dp[i][j], lse[r], delta[r], key < see[r], pr, ds);
+            sp[key * LP + r] = pr;
+            sd[key * LP + r] = ds;
+          }
+        __syncthreads();
+        add_product<DP>(sp, sg, ty, tx, ov);
+        add_product<DP>(sd, sq, ty, tx, ok);
+      }
     }
     const auto put = [&](int key, int d, float k, float v) {
       const int64_t row = w.k0 + key, col = (int64_t)h * p.head_dim + d;
