@@ -115,7 +115,8 @@ __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatil
   return __all_sync(0xffffffffu, tc::mbar_wait(bar, parity, abort_flag, status));
 }
 
-// 32 columns of this thread's lane; nothing reads them before ld_wait().
+// TMEM transfers are instructions of the whole warp: where lanes had branches of their own before one, a __syncwarp() brings them
+// together.  32 columns of this thread's lane; nothing reads them before ld_wait().
 __device__ __forceinline__ void ld32(uint32_t taddr, uint32_t* r) {
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"

@@ -317,6 +317,7 @@ __global__ void __launch_bounds__(THREADS, 1) fwd_tc_kernel(const __grid_constan
               for (int i = 0; i < 32; ++i)
                 if (!(seen & 1u << i)) x[c][i] = 0xff800000u;             // -inf
             }
+            __syncwarp();
           }
           float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
@@ -400,6 +401,7 @@ __global__ void __launch_bounds__(THREADS, 1) fwd_tc_kernel(const __grid_constan
 #pragma unroll 1
           for (int c = 0; c < D; c += 64) {
             uint32_t o[2][32];
+            __syncwarp();                                                 // (lanes without a row stored nothing)
             ld32(to + c, o[0]);
             ld32(to + c + 32, o[1]);
             ld_wait();
@@ -426,6 +428,7 @@ __global__ void __launch_bounds__(THREADS, 1) fwd_tc_kernel(const __grid_constan
       }
       const auto o_chunk = [&](int c, float* v) {                         // 32 columns of O (of all lanes)
         uint32_t o[32];
+        __syncwarp();
         ld32(to + c, o);
         ld_wait();
         ld_use(o);

@@ -146,6 +146,7 @@ __device__ __forceinline__ bool last_of_parts(Shared* sh, unsigned* ticket, int 
 // 32 columns of a result from TMEM, times f.
 __device__ __forceinline__ void acc_chunk(uint32_t taddr, float f, float* v) {
   uint32_t o[32];
+  __syncwarp();                                                   // (lanes without a row stored nothing)
   ld32(taddr, o);
   ld_wait();
   ld_use(o);
@@ -164,6 +165,7 @@ __device__ __forceinline__ void store_half(uint32_t taddr, float f, uint16_t* ou
   constexpr int PARTS = HALF / 32;
   uint32_t o[PARTS][32];
   const uint64_t f2 = pair(f, f);
+  __syncwarp();
 #pragma unroll
   for (int k = 0; k < PARTS; ++k) ld32(taddr + 32 * k, o[k]);
   ld_wait();
@@ -400,6 +402,7 @@ __global__ void __launch_bounds__(THREADS, 1) dq_tc_kernel(const __grid_constant
                 if (col >= lim) { pr[c * 16 + i] = 0; d[2 * i] = 0; }
                 if (col + 1 >= lim) { pr[c * 16 + i] &= 0xffffffffull; d[2 * i + 1] = 0; }
               }
+              __syncwarp();
             }
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
@@ -716,6 +719,7 @@ __global__ void __launch_bounds__(THREADS, 1) dkv_tc_kernel(const __grid_constan
                 if ((int)sh->pos_of[col] < from) pr[c * 16 + k] &= ~0xffffffffull;
                 if ((int)sh->pos_of[col + 1] < from) pr[c * 16 + k] &= 0xffffffffull;
               }
+              __syncwarp();
             }
 #pragma unroll
             for (int k = 0; k < 16; ++k) y[k] = pack2<BF16>(lo(pr[c * 16 + k]), hi(pr[c * 16 + k]));
