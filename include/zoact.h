@@ -600,7 +600,8 @@ int zoact_rope_apply(zoact_ctx* ctx, const void* X, int dtype, int64_t rows, int
  *       s_j = scale q . k_j,   p_j = exp(s_j - lse),   lse = log sum_j exp(s_j),   o = sum_j p_j v_j
  *   over the sequence's keys j; causal != 0: those with j <= i + (number of keys - number of queries), so that the queries are
  *   the last of the keys (all of a prompt, or the new tokens behind a cache: a single token is a sequence of one query).  A row
- *   that sees no key has o = 0 and lse = -infinity.
+ *   that sees no key has o = 0 and lse = -infinity; so has one whose scores are all -infinity (below what fp32 holds, too), and
+ *   neither has a part in a gradient.
  * shape (HOST pointer, read during the call): q and O [rows_q, heads head_dim], k and v [rows_k, kv_heads head_dim], of one dtype
  *   (FP32, BF16, FP16), rows ld elements apart; heads a multiple of kv_heads, at most 128 heads a key head; head_dim <= 256;
  *   rows_q and rows_k below 2^31 - 2^16; 0 < scale <= 1e30.  O overlaps no input.

@@ -29,6 +29,10 @@ __device__ __forceinline__ int visible(const Item& w, int causal, int i) {
   return v < 0 ? 0 : v > w.nk ? w.nk : (int)v;
 }
 
+// What the gradient adds to a row's scores (times log2 e) for its shares: the log-sum-exp, negative.  A row without any share, whose
+// scores may all be -infinity, has none here either.
+__device__ __forceinline__ float share_base(float lse) { return lse == -INFINITY ? -INFINITY : -lse * 1.44269504f; }
+
 // Positions of a tile.
 __host__ __device__ inline int tile_positions(int rep) { return TILE / rep; }
 

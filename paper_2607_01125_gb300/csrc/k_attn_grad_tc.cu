@@ -337,12 +337,12 @@ __global__ void __launch_bounds__(THREADS, 1) dq_tc_kernel(const __grid_constant
     const uint64_t scale2 = pair(p.scale_log2, p.scale_log2);
     uint32_t step = 0, units = 0, joins = 0;
     bool ok = true;
-    // of this thread's row of an item: log-sum-exp (times log2 e) and delta
-    const auto stat_of = [&](const Item& w, int h, float& lse2, float& delta) {
-      lse2 = delta = 0.f;
+    // of this thread's row of an item: log-sum-exp and delta
+    const auto stat_of = [&](const Item& w, int h, float& lse, float& delta) {
+      lse = delta = 0.f;
       if (row >= w.npos * p.rep) return;
       const int64_t e = (int64_t)(w.q0 + pos) * p.heads + h * p.rep + in_group;
-      lse2 = p.lse[e];
+      lse = p.lse[e];
       delta = p.delta[e];
     };
     Units U(p.work, total);
@@ -357,8 +357,8 @@ __global__ void __launch_bounds__(THREADS, 1) dq_tc_kernel(const __grid_constant
       const int h = U.h, n = (w.nk + BK - 1) / BK, rows = w.npos * p.rep;
       const bool active = quad * 32 < rows, valid = row < rows;
       const int see = valid ? visible<int>(w, p.causal, pos) : 0, all_see = visible<int>(w, p.causal, 0);
-      const float lse2 = lse_next * 1.44269504f;
-      const uint64_t lse22 = pair(-lse2, -lse2), delta2 = pair(-delta_next, -delta_next);
+      const float base = share_base(lse_next);
+      const uint64_t base2 = pair(base, base), delta2 = pair(-delta_next, -delta_next);
       const Factors<BF16> f(largest_next);
       const uint64_t ds2 = pair(f.up, f.up);
       for (int j = 0; j < n; ++j, ++step) {
@@ -381,7 +381,7 @@ __global__ void __launch_bounds__(THREADS, 1) dq_tc_kernel(const __grid_constant
           for (int c = 0; c < 2; ++c)
 #pragma unroll
             for (int i = 0; i < 32; i += 2) {
-              const uint64_t z = fma2(pair_bits(x[c][i], x[c][i + 1]), scale2, lse22);
+              const uint64_t z = fma2(pair_bits(x[c][i], x[c][i + 1]), scale2, base2);
               pr[c * 16 + i / 2] = pair(ex2(lo(z)), ex2(hi(z)));
             }
         }
@@ -640,7 +640,7 @@ __global__ void __launch_bounds__(THREADS, 1) dkv_tc_kernel(const __grid_constan
             const int row = lane + 32 * k, pos = sh->pos_of[row];
             const int64_t e = (int64_t)(w.q0 + i * P + pos) * p.heads + h * p.rep + row - pos * p.rep;
             // (rows behind the last: no share)
-            lse[k] = row < rows ? P_SHIFT<BF16> - p.lse[e] * 1.44269504f : -INFINITY;
+            lse[k] = row < rows ? P_SHIFT<BF16> + share_base(p.lse[e]) : -INFINITY;
             delta[k] = row < rows ? -p.delta[e] : 0.f;
           }
           ok = warp_wait(bar(sh->stat_empty[b]), (step >> 1 & 1) ^ 1u, abort_flag, p.status);

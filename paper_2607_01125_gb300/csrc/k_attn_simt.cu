@@ -337,8 +337,8 @@ __global__ void __launch_bounds__(THREADS) reset_kernel(const Work work, float2*
 }
 
 // P and dS = P (dP - delta) of a tile, from its scaled products z (times log2 e) and dP; 0 where a key is not seen.
-__device__ __forceinline__ void share_of(float z, float dp, float lse_log2, float delta, bool seen, float& pr, float& ds) {
-  pr = seen ? exp2f(z - lse_log2) : 0.f;
+__device__ __forceinline__ void share_of(float z, float dp, float base, float delta, bool seen, float& pr, float& ds) {
+  pr = seen ? exp2f(z + base) : 0.f;
   ds = seen ? pr * (dp - delta) : 0.f;
 }
 
@@ -360,7 +360,7 @@ __global__ void __launch_bounds__(THREADS) dq_kernel(const Dev p) {
     __syncthreads();
     load_rows<T, DP>(sq, p.q, p.ld_q, w, h, p.by_rep, p.head_dim, p.vec, r0, n);
     load_rows<T, DP>(sg, p.dO, p.ld_do, w, h, p.by_rep, p.head_dim, p.vec, r0, n);
-    float lse[R], delta[R];
+    float base[R], delta[R];
     float4 o[R][C];
     int see[R];
 #pragma unroll
@@ -368,7 +368,7 @@ __global__ void __launch_bounds__(THREADS) dq_kernel(const Dev p) {
       const int r = r0 + ty + 16 * i, pos = r / p.rep;
       const int64_t e = (int64_t)(w.q0 + pos) * p.heads + h * p.rep + r - pos * p.rep;
       see[i] = r < n ? visible(w, p.causal, pos) : 0;
-      lse[i] = r < n ? p.lse_in[e] * 1.44269504f : 0.f;
+      base[i] = r < n ? share_base(p.lse_in[e]) : 0.f;
       delta[i] = r < n ? p.delta[e] : 0.f;
 #pragma unroll
       for (int c = 0; c < C; ++c) o[i][c] = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -387,7 +387,7 @@ __global__ void __launch_bounds__(THREADS) dq_kernel(const Dev p) {
 #pragma unroll
         for (int j = 0; j < R; ++j) {
           float pr, ds;
-          share_of(s[i][j] * p.scale_log2, dp[i][j], lse[i], delta[i], j0 + tx + 16 * j < see[i], pr, ds);
+          share_of(s[i][j] * p.scale_log2, dp[i][j], base[i], delta[i], j0 + tx + 16 * j < see[i], pr, ds);
           sp[(ty + 16 * i) * LP + tx + 16 * j] = ds;
         }
       __syncthreads();
@@ -433,7 +433,7 @@ __global__ void __launch_bounds__(THREADS) dkv_kernel(const Dev p) {
   constexpr int R = Cfg<DP>::R, C = Cfg<DP>::C, M = Cfg<DP>::M, LD = Cfg<DP>::LD, LP = Cfg<DP>::LP, SUB = tiles_of<DP>(BK);
   extern __shared__ float sm[];
   float *sq = sm, *sg = sq + M * LD, *sk = sg + M * LD, *sv = sk + M * LD, *sp = sv + M * LD, *sd = sp + M * LP;
-  __shared__ float lse[M], delta[M];
+  __shared__ float base[M], delta[M];
   __shared__ int see[M], flag;
   pdl_wait();
   pdl_trigger();
@@ -468,7 +468,7 @@ __global__ void __launch_bounds__(THREADS) dkv_kernel(const Dev p) {
           const int r = r0 + tid, pos = r / p.rep;
           const int64_t e = (int64_t)(run.q0 + pos) * p.heads + h * p.rep + r - pos * p.rep;
           see[tid] = r < n ? visible(run, p.causal, pos) - key0 : 0;
-          lse[tid] = r < n ? p.lse_in[e] * 1.44269504f : 0.f;
+          base[tid] = r < n ? share_base(p.lse_in[e]) : 0.f;
           delta[tid] = r < n ? p.delta[e] : 0.f;
         }
         __syncthreads();
@@ -481,7 +481,7 @@ __global__ void __launch_bounds__(THREADS) dkv_kernel(const Dev p) {
           for (int j = 0; j < R; ++j) {
             const int key = ty + 16 * i, r = tx + 16 * j;
             float pr, ds;
-            share_of(s[i][j] * p.scale_log2, dp[i][j], lse[r], delta[r], key < see[r], pr, ds);
+            share_of(s[i][j] * p.scale_log2, dp[i][j], base[r], delta[r], key < see[r], pr, ds);
             sp[key * LP + r] = pr;
             sd[key * LP + r] = ds;
           }
