@@ -572,7 +572,8 @@ int zoact_ce_grad(zoact_ctx* ctx, const void* H, int dtype, int64_t T, int32_t d
  *     ZOACT_ROPE_PARTS    by a frequency's turns over L, t = L f / 2 pi: f / factor below `low`, f above `high`, and between
  *                         f (s + (1 - s) / factor) with s = (t - low) / (high - low).
  *   turns[i] is f_i in 2^-64 turns a position (the angle of any 64-bit position is exact to 53 bits of the frequency).
- *   A caller with frequencies of its own may fill the struct itself.  rot: even, 2 .. ZOACT_ROPE_MAX.
+ *   A caller with frequencies of its own may fill the struct itself.  rot: even, 2 .. ZOACT_ROPE_MAX.  A frequency that is infinite or
+ *   no number is refused, and nothing is written.
  * zoact_rope_apply: Y [rows, heads head_dim] = X with each head's first rope->rot dimensions turned by the angle of
  *   positions[r % n_pos] for row r (rows a multiple of n_pos: the evaluation blocks see one set of positions), the others
  *   copied: (a, b) -> (a cos - b sin, a sin + b cos), with inverse != 0 by the opposite angle, which is the gradient of the

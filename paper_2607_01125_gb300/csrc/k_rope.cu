@@ -197,8 +197,9 @@ extern "C" int zoact_rope_init(zoact_rope* rope, int32_t rot, int32_t layout, do
   const double two_pi = 6.283185307179586476925;
   if (scaling == ZOACT_ROPE_BASE && rot > 2) base *= std::pow(factor, (double)rot / (rot - 2));
   if (!std::isfinite(base) || !(base > 0.0)) return ZOACT_ERR_INVALID_ARG;
-  rope->rot = rot;
-  rope->layout = layout;
+  zoact_rope r = {};
+  r.rot = rot;
+  r.layout = layout;
   for (int i = 0; i < ZOACT_ROPE_MAX / 2; ++i) {
     double f = 0.0;
     if (i < rot / 2) f = std::pow(base, -2.0 * i / rot);
@@ -208,8 +209,10 @@ extern "C" int zoact_rope_init(zoact_rope* rope, int32_t rot, int32_t layout, do
       const double keep = std::fmin(std::fmax((turns - low) / (high - low), 0.0), 1.0);
       f *= keep + (1.0 - keep) / factor;
     }
+    if (!std::isfinite(f)) return ZOACT_ERR_INVALID_ARG;
     const double t = f / two_pi, part = t - std::floor(t);          // below 1: its 53 bits are part of the 64
-    rope->turns[i] = (uint64_t)std::ldexp(part, 64);
+    r.turns[i] = (uint64_t)std::ldexp(part, 64);
   }
+  *rope = r;
   return ZOACT_OK;
 }
