@@ -45,3 +45,28 @@ def test_gradients_with_plans_of_other_calls_write_nothing(dt, d):
     assert ctx.device_status() == 0
     c.check_grads(outs)
     ctx.close()
+
+
+@pytest.mark.parametrize("dt", ["fp32", "bf16", "fp16"])
+def test_keys_without_any_query_and_queries_without_any_key(dt):
+    """No rows of q at all: dk and dv are zeros in the spans.  No rows of k: outputs and dq are zeros."""
+    ctx = zo.Context(0)
+    c = Case(ctx, dt, 4, 2, 64, [(0, 0, 2, 40), (0, 0, 50, 130)], grad=True, rows_q=0, rows_k=190)
+    c.forward()
+    dq, dk, dv = c.grads()
+    torch.cuda.synchronize()
+    assert ctx.device_status() == 0
+    inside = torch.zeros(190, dtype=torch.bool, device=DEV)
+    inside[2:42] = inside[50:180] = True
+    for t in (dk, dv):
+        assert (t[inside] == 0).all() and torch.isnan(t[~inside]).all()
+    c = Case(ctx, dt, 4, 2, 64, [(1, 30, 0, 0), (40, 200, 0, 0)], grad=True, rows_q=250, rows_k=0)
+    c.forward()
+    c.check_forward()
+    dq, dk, dv = c.grads()
+    torch.cuda.synchronize()
+    assert ctx.device_status() == 0
+    inside = torch.zeros(250, dtype=torch.bool, device=DEV)
+    inside[1:31] = inside[40:240] = True
+    assert (dq[inside] == 0).all() and torch.isnan(dq[~inside]).all()
+    ctx.close()
