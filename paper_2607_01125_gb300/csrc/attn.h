@@ -18,6 +18,8 @@ struct alignas(16) Item {
   int32_t q0, npos, k0, nk, diag, part, nparts, slot;
   int32_t seq;                          // the sequence that the work is of
 };
+// (With part and nparts as two 16-bit fields, in 32 bytes, the kernel for dq joined its parts to zeros; no reason for it was found in
+// the source.)
 static_assert(sizeof(Item) == 48, "items are read as two 16-byte words, and the sequence where it is needed");
 
 // (rows are below 2^31 - 2^16, and 32 bits suffice; the long prompt of the forward kernel took 389 us with them for 363, the

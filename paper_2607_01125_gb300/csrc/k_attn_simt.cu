@@ -6,8 +6,9 @@
 // A block of 256 threads has a tile of M rows of (position, head of the group) pairs against M keys; a thread has M / 16 rows
 // and columns, spread 16 apart, so that its 16-byte reads of shared memory fall on different banks.  The gradient recomputes
 // P = exp(S - lse) in two passes, one over the keys for dq and one over the rows for dk and dv, so that no sum needs atomics.
-// Bound by the FMA pipes and by shared memory (12 of its cycles for 16 of FMAs): 8192 tokens of 32 heads on 8 of 128 22 ms
-// (25 TFLOP/s), two sequences of 64 in 4 heads of 64 13 us.
+// Bound by latencies: tiles of 128 columns leave room for one block of 8 warps on an SM, which issues in 45% of the cycles (37% of
+// the FMA rate) and reads shared memory in 45%.  8192 tokens of 32 heads on 8 of 128 22 ms (25 TFLOP/s), twice 2048 tokens 2.9 ms
+// (23.5), two sequences of 64 in 4 heads of 64 13 us.
 #include <type_traits>
 
 #include "attn.h"
@@ -252,7 +253,7 @@ __global__ void __launch_bounds__(THREADS) fwd_kernel(const Dev p) {
 // delta = the row sum of dO O for each (row, head) of the sequences, by a group of lanes that has V elements each of a pass over the
 // head; in fp16 also the largest finite |dO| and |v| of each sequence's group of heads (0 before).  It runs through the items of dq,
 // whose rows are those of the sequences, and for v through those of dk and dv.  EACH pairs of a group at a time; 4096 rows of 32
-// heads of 128 in bf16 20 us (3.4 TB/s).
+// heads of 128 in bf16 20 to 22 us (3.4 TB/s).
 constexpr int EACH = 4;
 
 // The largest of a warp's values goes to *to (above 0: ordered as integers).

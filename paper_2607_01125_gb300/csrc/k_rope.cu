@@ -11,7 +11,7 @@
 // thread's pieces in flight (four: 40 us for 35 at the first size below, the same at the second).
 //
 // Measured (GB300): 8192 rows of 40 heads of 128 in bf16 34.9 us (4.8 TB/s; a copy of as much takes 28.7), 3001 rows of 80 heads
-// of 80, 32 of them turned, in fp16 20.3 us (3.8 TB/s).
+// of 80, 32 of them turned, in fp16 20.3 to 21.2 us (3.7 TB/s).
 #include <cmath>
 
 #include "internal.h"
